@@ -354,6 +354,111 @@ int w2v_ns_objective(const w2v_model *m, const int32_t *noise_table, int32_t log
                      int64_t *n_terms_host, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Operators of a mini-batch step on hidden vectors: layer norm, the
+ * hierarchical softmax as a loss with gradients, AdamW. They write no host
+ * output and do not synchronise, so they can be captured into a HIP graph
+ * (w2v_adamw_build_plan excepted); overlapping calls need workspaces of their
+ * own. Rows are dim (cols) neighbouring elements, `stride` elements apart
+ * (stride >= dim where there is more than one row); columns between the rows
+ * are neither read nor written. Any element-aligned address is allowed.
+ * bf16 and fp16 elements are converted to fp32 exactly, all arithmetic and
+ * sums are fp32 and results are rounded once, to nearest. Sums over rows have
+ * a fixed order: equal inputs give equal bits.
+ * ---------------------------------------------------------------------- */
+typedef enum { W2V_F32 = 0, W2V_BF16 = 1, W2V_F16 = 2 } w2v_type;
+
+/* Layer norm: mean = sum x / dim, rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps),
+   y = (x - mean) rstd weight + bias.
+     x, y        rows x dim elements of type; y may be x
+     weight, bias  dim elements of w_type (W2V_F32 or type), each may be NULL (1, 0)
+     mean, rstd  float[rows] out, each may be NULL
+   Errors: W2V_E_ARG for rows < 0, dim not in 1..16384, a short stride, eps
+   that is negative or not finite, an unknown type or a NULL required pointer. */
+int w2v_layer_norm(const void *x, int32_t type, int64_t rows, int32_t dim, int64_t x_stride, const void *weight,
+                   const void *bias, int32_t w_type, float eps, void *y, int64_t y_stride, float *mean, float *rstd,
+                   void *hip_stream);
+
+/* Its gradients, from the upstream gradient dy and the forward pass's x, mean
+   and rstd: with h = (x - mean) rstd and a = dy weight,
+   dx = rstd (a - sum a / dim - h sum (a h) / dim) (elements of type; may be dy
+   or x), dweight = sum over rows of dy h and dbias = sum over rows of dy
+   (float[dim], each may be NULL; zeros for rows = 0). */
+size_t w2v_layer_norm_backward_workspace_bytes(int64_t rows, int32_t dim);
+int w2v_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int32_t type, int64_t rows, int32_t dim,
+                            int64_t x_stride, const void *weight, int32_t w_type, const float *mean,
+                            const float *rstd, void *dx, int64_t dx_stride, float *dweight, float *dbias,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The hierarchical softmax of rows hidden vectors x (rows x m->dim elements of
+   type) with target words targets int32[rows], as a loss with its gradients:
+     loss    float[rows] out, may be NULL: -log P(targets[i] | x_i), with
+             P(v|x) = prod_j sigmoid((1 - 2 t_j) x . syn1[n_j]) over v's path
+     dx      rows x dim elements of type out, may be NULL
+     dsyn1   float[V-1][dsyn1_stride] out, may be NULL: every row's first dim
+             columns are written
+   The gradients are those of sum_i weights[i] loss[i] (weights float[rows], or
+   NULL: ones). A negative target means none: loss 0, a dx of zeros, x not
+   read into any sum. A target outside the vocabulary, or one whose code is
+   longer than max_code_len (w2v_build_huffman's max_len_host, 1..64), has the
+   loss NaN and no gradient. Of m: V, dim, row_stride, syn1 and the Huffman
+   arrays; the others are not used. dsyn1 may not be m->syn1. Errors:
+   W2V_E_ARG, W2V_E_WORKSPACE (the workspace is needed with dsyn1 only). */
+size_t w2v_hs_loss_workspace_bytes(const w2v_model *m, int32_t max_code_len, int64_t rows);
+int w2v_hs_loss(const w2v_model *m, int32_t max_code_len, const void *x, int32_t type, int64_t rows, int64_t x_stride,
+                const int32_t *targets, const float *weights, float *loss, void *dx, int64_t dx_stride, float *dsyn1,
+                int64_t dsyn1_stride, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* AdamW with decoupled weight decay, over many tensors in one launch. At step
+   t (1, 2, ...), for every element, in fp32:
+     g = grad grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+   The moments of all tensors lie in two arrays of n_moments elements, tensor
+   i's (in row order, without gaps) from moment_offset on, a multiple of 256.
+   bits = 32: float arrays. bits = 8: uint8 arrays with a scale for each 256
+   elements, m_scale and v_scale float[n_moments / 256]: m = e4m3 code x scale,
+   sqrt(v) = u x scale with u(c) = c 2^-18 for c < 16, else
+   (1 + (c % 16) / 16) 2^(c / 16 - 15). m is rounded to nearest, sqrt(v) up or
+   down in proportion by a hash of (seed, t, place of the moment), a positive
+   one never to 0. A block with a moment that is not finite stays not finite.
+   All zeros is the state before the first step in either form. */
+typedef struct {
+    void *param;              /* rows x cols elements of param_type */
+    const void *grad;         /* rows x cols elements of grad_type */
+    int64_t rows, cols;
+    int64_t param_stride, grad_stride;
+    int64_t moment_offset;
+    int32_t param_type, grad_type;
+    float weight_decay;
+    int32_t reserved0;
+} w2v_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;               /* t, >= 1 */
+    const float *lr_device;     /* NULL, or the learning rate in device memory (instead of lr) */
+    const int64_t *step_device; /* NULL, or t in device memory (instead of step): for steps replayed from a graph */
+    float grad_scale;
+    uint32_t seed;
+} w2v_adamw_params;
+
+/* The plan of a list of tensors: which parts of which tensor a step's
+   workgroups update, laid out once in plan, device memory of
+   w2v_adamw_plan_bytes bytes that the caller keeps (0: an invalid list).
+   n_chunks_host is handed to every step. Synchronises the stream. A plan
+   belongs to one step at a time. Errors: W2V_E_ARG for sizes, strides, types
+   or NULL pointers out of range, moments that overlap or reach past n_moments
+   (a tensor's last block counts whole), or packed parameters that overlap. */
+size_t w2v_adamw_plan_bytes(const w2v_adamw_tensor *tensors_host, int32_t n_tensors);
+int w2v_adamw_build_plan(const w2v_adamw_tensor *tensors_host, int32_t n_tensors, int64_t n_moments, void *plan,
+                         size_t plan_bytes, int64_t *n_chunks_host, void *hip_stream);
+int w2v_adamw_step(void *plan, int64_t n_chunks, int32_t bits, void *m, void *v, float *m_scale, float *v_scale,
+                   const w2v_adamw_params *p, void *hip_stream);
+
+/* The values that 8-bit moments stand for: m_out, v_out float[n_moments]. */
+int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const float *v_scale, int64_t n_moments,
+                      float *m_out, float *v_out, void *hip_stream);
+
+/* ------------------------------------------------------------------------
  * Test hooks (not part of the training contract).
  *
  * w2v_sample_pairs: the (centre, context) pairs of the sampler in stream

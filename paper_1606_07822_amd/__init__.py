@@ -7,6 +7,7 @@ allocates device memory; workspaces are torch uint8 tensors made here.
 Entry points mirror the C ABI in include/w2v.h:
     build_vocab, build_huffman, train_hs_epoch, hs_loglik
     build_noise_table, train_ns_epoch, ns_objective (negative sampling)
+    layer_norm, layer_norm_backward, hs_loss, AdamW (a mini-batch step on hidden vectors)
 plus the test hooks sample_pairs, keep_thresholds and sample_negatives.
 """
 from __future__ import annotations
@@ -49,7 +50,20 @@ class CParams(ctypes.Structure):
                 ("span_refresh", I32), ("span_stash", I32), ("stash_from", I32)]
 
 
+class CAdamWTensor(ctypes.Structure):
+    _fields_ = [("param", P), ("grad", P), ("rows", I64), ("cols", I64), ("param_stride", I64), ("grad_stride", I64),
+                ("moment_offset", I64), ("param_type", I32), ("grad_type", I32), ("weight_decay", ctypes.c_float),
+                ("reserved0", I32)]
+
+
+class CAdamWParams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", I64), ("lr_device", P), ("step_device", P),
+                ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32)]
+
+
 assert ctypes.sizeof(CModel) == 80 and ctypes.sizeof(CParams) == 112
+assert ctypes.sizeof(CAdamWTensor) == 72 and ctypes.sizeof(CAdamWParams) == 64
 
 _LIB = None
 
@@ -118,6 +132,26 @@ def lib() -> ctypes.CDLL:
         L.w2v_sample_negatives.restype = ctypes.c_int
         L.w2v_sample_negatives.argtypes = [P, I64, I32, P, I64, ctypes.POINTER(CParams), P, I32, P, I64, P, P, P,
                                            ctypes.c_size_t, P]
+        L.w2v_layer_norm.restype = ctypes.c_int
+        L.w2v_layer_norm.argtypes = [P, I32, I64, I32, I64, P, P, I32, ctypes.c_float, P, I64, P, P, P]
+        L.w2v_layer_norm_backward_workspace_bytes.restype = ctypes.c_size_t
+        L.w2v_layer_norm_backward_workspace_bytes.argtypes = [I64, I32]
+        L.w2v_layer_norm_backward.restype = ctypes.c_int
+        L.w2v_layer_norm_backward.argtypes = [P, I64, P, I32, I64, I32, I64, P, I32, P, P, P, I64, P, P, P,
+                                              ctypes.c_size_t, P]
+        L.w2v_hs_loss_workspace_bytes.restype = ctypes.c_size_t
+        L.w2v_hs_loss_workspace_bytes.argtypes = [ctypes.POINTER(CModel), I32, I64]
+        L.w2v_hs_loss.restype = ctypes.c_int
+        L.w2v_hs_loss.argtypes = [ctypes.POINTER(CModel), I32, P, I32, I64, I64, P, P, P, P, I64, P, I64, P,
+                                  ctypes.c_size_t, P]
+        L.w2v_adamw_plan_bytes.restype = ctypes.c_size_t
+        L.w2v_adamw_plan_bytes.argtypes = [ctypes.POINTER(CAdamWTensor), I32]
+        L.w2v_adamw_build_plan.restype = ctypes.c_int
+        L.w2v_adamw_build_plan.argtypes = [ctypes.POINTER(CAdamWTensor), I32, I64, P, ctypes.c_size_t, P, P]
+        L.w2v_adamw_step.restype = ctypes.c_int
+        L.w2v_adamw_step.argtypes = [P, I64, I32, P, P, P, P, ctypes.POINTER(CAdamWParams), P]
+        L.w2v_adamw_moments.restype = ctypes.c_int
+        L.w2v_adamw_moments.argtypes = [P, P, P, P, I64, P, P, P]
         _LIB = L
     return _LIB
 
@@ -552,3 +586,260 @@ def sample_negatives(tokens: torch.Tensor, V: int, vocab_counts: torch.Tensor, t
                                       ctypes.byref(cs), ws.data_ptr(), ws.numel(), _stream(dev)))
     m = min(cap, nk.value)
     return Negatives(out[:m * p.negative].view(m, p.negative) if cap else None, nk.value, cs.value)
+
+
+# ---------------------------------------------------- a mini-batch step on hidden vectors
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _type_of(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _rows_ptr(t: torch.Tensor, name: str, like: torch.Tensor, dtype: torch.dtype | None = None) -> tuple[int, int]:
+    """(pointer, row stride) of a [rows, dim] tensor of like's shape, device and (or dtype's) type."""
+    if t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor on the rows' device")
+    if t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name} must be {dtype or like.dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return t.data_ptr(), t.stride(0)
+
+
+def _vector_ptr(t: torch.Tensor | None, dtype: torch.dtype, n: int, dev: torch.device, name: str):
+    if t is None:
+        return None
+    ptr = _dev_ptr(t, dtype, name)
+    if t.device != dev or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements on {dev}, got {tuple(t.shape)} on {t.device}")
+    return ptr
+
+
+def _affine_ptr(t: torch.Tensor | None, x: torch.Tensor, name: str):
+    if t is None:
+        return None
+    return _vector_ptr(t, torch.float32 if t.dtype == torch.float32 else x.dtype, x.shape[1], x.device, name)
+
+
+class _On:
+    """The current device for the time of a call (streams belong to a device, and launches go to the current one)."""
+
+    def __init__(self, dev: torch.device):
+        self.other = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.other:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other:
+            self.other.__exit__(*exc)
+
+
+def _kept(workspace: torch.Tensor | None, need: int, dev: torch.device) -> torch.Tensor | None:
+    """The caller's workspace, or a new one where there is none or it is too small."""
+    if need == 0:
+        return None
+    if workspace is not None:
+        _dev_ptr(workspace, torch.uint8, "workspace")
+        if workspace.device != dev:
+            raise ValueError(f"workspace must be on {dev}")
+        if workspace.numel() >= need:
+            return workspace
+    return _workspace(need, dev)
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               eps: float = 1e-5, out: torch.Tensor | None = None
+               ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Rows of x [rows, dim] normalised: (y, mean, rstd), y in x's type (in out, which may be x), mean and rstd float32.
+    weight and bias: float32 or x's type. Does not sync."""
+    xp, xs = _rows_ptr(x, "x", x)
+    kind = _type_of(x, "x")
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
+    yp, ys = _rows_ptr(y, "out", x)
+    wp, bp = _affine_ptr(weight, x, "weight"), _affine_ptr(bias, x, "bias")
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must have the same type")
+    w = weight if weight is not None else bias
+    n, dim = x.shape
+    stats = torch.empty(2, n, dtype=torch.float32, device=x.device)
+    with _On(x.device):
+        _check(lib().w2v_layer_norm(xp, kind, n, dim, xs, wp, bp, 0 if w is None else _TYPES[w.dtype], eps, yp, ys,
+                                    stats.data_ptr(), stats.data_ptr() + 4 * n, _stream(x.device)))
+    return y, stats[0], stats[1]
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
+                        rstd: torch.Tensor, dx: torch.Tensor | None = None, dweight: torch.Tensor | None = None,
+                        dbias: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+                        ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
+    """Gradients (dx, dweight, dbias) of layer_norm for the upstream gradient dy, from its x, mean and rstd. dx in x's
+    type (may be dy or x); dweight and dbias float32, None without a weight unless given. Does not sync."""
+    xp, xs = _rows_ptr(x, "x", x)
+    kind = _type_of(x, "x")
+    dyp, dys = _rows_ptr(dy, "dy", x)
+    n, dim = x.shape
+    dev = x.device
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+    dxp, dxs = _rows_ptr(dx, "dx", x)
+    if weight is not None and dweight is None and dbias is None:
+        both = torch.empty(2, dim, dtype=torch.float32, device=dev)
+        dweight, dbias = both[0], both[1]
+    dwp = _vector_ptr(dweight, torch.float32, dim, dev, "dweight")
+    dbp = _vector_ptr(dbias, torch.float32, dim, dev, "dbias")
+    wp = _affine_ptr(weight, x, "weight")
+    mp, rp = _vector_ptr(mean, torch.float32, n, dev, "mean"), _vector_ptr(rstd, torch.float32, n, dev, "rstd")
+    need = lib().w2v_layer_norm_backward_workspace_bytes(n, dim) if dwp or dbp else 0
+    with _On(dev):
+        ws = _kept(workspace, need, dev)
+        _check(lib().w2v_layer_norm_backward(dyp, dys, xp, kind, n, dim, xs, wp,
+                                             0 if weight is None else _TYPES[weight.dtype], mp, rp, dxp, dxs, dwp, dbp,
+                                             None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                             _stream(dev)))
+    return dx, dweight, dbias
+
+
+def hs_loss_workspace(model: Model, x: torch.Tensor, grads: bool = True) -> torch.Tensor | None:
+    """A workspace for hs_loss on x's rows, to be kept from call to call (calls that overlap need one each)."""
+    if not grads:
+        return None
+    cm = model.c()
+    return _workspace(lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), model.tree.max_len, x.shape[0]), x.device)
+
+
+def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor | None = None,
+            grads: bool = True, loss: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+            dsyn1: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+            ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
+    """(loss, dx, dsyn1): -log P(targets[i] | x[i]) under the model's hierarchical softmax (float32) and, with grads,
+    the gradients of sum(weights * loss) for x [rows, dim] and for model.syn1 (dsyn1 float32 of syn1's shape, all rows
+    written in their first dim columns). targets int32, negative: none. Does not sync."""
+    xp, xs = _rows_ptr(x, "x", x)
+    kind = _type_of(x, "x")
+    n, dev = x.shape[0], x.device
+    if x.shape[1] != model.dim:
+        raise ValueError(f"x must have {model.dim} columns, got {x.shape[1]}")
+    if model.syn1.device != dev:
+        raise ValueError(f"the model must be on {dev}")
+    tp = _vector_ptr(targets, torch.int32, n, dev, "targets")
+    wp = _vector_ptr(weights, torch.float32, n, dev, "weights")
+    if loss is None:
+        loss = torch.empty(n, dtype=torch.float32, device=dev)
+    dxp = dxs = dsp = None
+    if grads:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+        dxp, dxs = _rows_ptr(dx, "dx", x)
+        dsyn1 = torch.zeros_like(model.syn1) if dsyn1 is None else dsyn1
+        dsp, _ = _rows_ptr(dsyn1, "dsyn1", model.syn1)
+    else:
+        dx = dsyn1 = None
+    cm = model.c()
+    with _On(dev):
+        ws = None
+        if grads:
+            ws = _kept(workspace, lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), model.tree.max_len, n), dev)
+        _check(lib().w2v_hs_loss(ctypes.byref(cm), model.tree.max_len, xp, kind, n, xs, tp, wp,
+                                 _vector_ptr(loss, torch.float32, n, dev, "loss"), dxp, dxs or 0, dsp,
+                                 dsyn1.stride(0) if grads else 0, None if ws is None else ws.data_ptr(),
+                                 0 if ws is None else ws.numel(), _stream(dev)))
+    return loss, dx, dsyn1
+
+
+class AdamW:
+    """AdamW over a list of tensors and their gradient buffers, updated in place by one launch a step.
+
+    params, grads: float32, bfloat16 or float16 tensors of equal shapes, contiguous or 2-D with contiguous rows (views
+    such as Model.vectors()). The buffers are fixed: write each step's gradients into `grads`. bits: of the moments, 32
+    or 8. weight_decay: one number, or one for each tensor.
+
+    m and v hold all tensors' moments, tensor i's from offsets[i] on (multiples of 256): float32, or uint8 codes with the
+    scales m_scale and v_scale (see include/w2v.h). state: those arrays of an earlier optimizer, (m, v) or
+    (m, v, m_scale, v_scale), which are then used as they are; zeros otherwise."""
+
+    BLOCK = 256
+
+    def __init__(self, params, grads, bits: int = 32, betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+                 weight_decay=0.01, seed: int = 0, state=None):
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        if not params or len(params) != len(grads):
+            raise ValueError("params and grads must be lists of the same length, at least 1")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
+        if len(decay) != len(params):
+            raise ValueError("weight_decay must be a number or hold one for each tensor")
+        self.params, self.grads, self.bits, self.betas, self.eps, self.seed = (list(params), list(grads), bits, betas,
+                                                                              eps, seed)
+        self.device = dev = params[0].device
+        self.offsets, at = [], 0
+        table = (CAdamWTensor * len(params))()
+        for i, (p, g) in enumerate(zip(params, grads)):
+            for t, name in ((p, f"params[{i}]"), (g, f"grads[{i}]")):
+                if not t.is_cuda or t.device != dev:
+                    raise ValueError(f"{name} must be a GPU tensor on {dev}")
+                if t.shape != p.shape:
+                    raise ValueError(f"{name} must have the shape {tuple(p.shape)}, got {tuple(t.shape)}")
+                if not (t.is_contiguous() or (t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1))):
+                    raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows")
+            rows, cols = (1, p.numel()) if p.is_contiguous() and g.is_contiguous() else p.shape
+            table[i] = CAdamWTensor(p.data_ptr(), g.data_ptr(), rows, cols, p.stride(0) if rows > 1 else cols,
+                                    g.stride(0) if rows > 1 else cols, at, _type_of(p, f"params[{i}]"),
+                                    _type_of(g, f"grads[{i}]"), decay[i], 0)
+            self.offsets.append(at)
+            at += -(-p.numel() // self.BLOCK) * self.BLOCK
+        self.n_moments = at
+        kind = torch.float32 if bits == 32 else torch.uint8
+        shapes = [(at, kind), (at, kind)] + [(at // self.BLOCK, torch.float32)] * (2 if bits == 8 else 0)
+        if state is None:
+            state = [torch.zeros(n, dtype=d, device=dev) for n, d in shapes]
+        if len(state) != len(shapes):
+            raise ValueError(f"state must hold {len(shapes)} arrays")
+        for k, (t, (n, d)) in enumerate(zip(state, shapes)):
+            _vector_ptr(t, d, n, dev, f"state[{k}]")
+        self.m, self.v = state[0], state[1]
+        self.m_scale, self.v_scale = (state[2], state[3]) if bits == 8 else (None, None)
+        self._plan = _workspace(lib().w2v_adamw_plan_bytes(table, len(params)), dev)
+        chunks = ctypes.c_int64(0)
+        with _On(dev):
+            _check(lib().w2v_adamw_build_plan(table, len(params), at, self._plan.data_ptr(), self._plan.numel(),
+                                              ctypes.byref(chunks), _stream(dev)))
+        self._chunks = chunks.value
+
+    def step(self, step, lr, grad_scale: float = 1.0) -> None:
+        """Step number `step` (1, 2, ...) with the learning rate lr. Either may be a one-element tensor on the device
+        (int64, float32) that is read when the step runs, so that a captured step can be replayed with new values. Does
+        not sync."""
+        p = CAdamWParams(0.0, self.betas[0], self.betas[1], self.eps, 1, None, None, grad_scale, self.seed & 0xFFFFFFFF)
+        if isinstance(lr, torch.Tensor):
+            p.lr_device = _vector_ptr(lr, torch.float32, 1, self.device, "lr")
+        else:
+            p.lr = lr
+        if isinstance(step, torch.Tensor):
+            p.step_device = _vector_ptr(step, torch.int64, 1, self.device, "step")
+        else:
+            p.step = step
+        narrow = self.bits == 8
+        with _On(self.device):
+            _check(lib().w2v_adamw_step(self._plan.data_ptr(), self._chunks, self.bits, self.m.data_ptr(),
+                                        self.v.data_ptr(), self.m_scale.data_ptr() if narrow else None,
+                                        self.v_scale.data_ptr() if narrow else None, ctypes.byref(p),
+                                        _stream(self.device)))
+
+    def moments(self, m_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None
+                ) -> tuple[torch.Tensor, torch.Tensor]:
+        """The moments' values, float32[n_moments] each: m and v themselves, or what the 8-bit codes stand for (in m_out
+        and v_out). Does not sync."""
+        if self.bits == 32:
+            return self.m, self.v
+        outs = [torch.empty(self.n_moments, dtype=torch.float32, device=self.device) if t is None else t
+                for t in (m_out, v_out)]
+        mp, vp = (_vector_ptr(t, torch.float32, self.n_moments, self.device, "m_out or v_out") for t in outs)
+        with _On(self.device):
+            _check(lib().w2v_adamw_moments(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
+                                           self.v_scale.data_ptr(), self.n_moments, mp, vp, _stream(self.device)))
+        return outs[0], outs[1]
