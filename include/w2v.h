@@ -459,6 +459,57 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
                       float *m_out, float *v_out, void *hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Training in mini-batches with the operators above: CBOW whose hidden vector
+ * is the mean of the window's vectors, through a layer norm if gain and bias
+ * are given, scored against the centre word by the hierarchical softmax.
+ * Sampling, windows and the learning-rate schedule are w2v_train_hs_epoch's
+ * (p->arch 1); of p's other settings only sync_batch is used. Every
+ * sync_batch (1..2^20) consecutive kept centres make a batch; all gradients
+ * of its mean loss (the sum over the centres that have a window, divided by
+ * the batch's centres) are taken against the model at its start; then AdamW,
+ * with the learning rate of its first centre, updates syn0 and syn1 (decay
+ * weight_decay) and gain and bias (no decay): every row, whether or not the
+ * batch reached it. Deterministic.
+ *   m, v, m_scale, v_scale  moments as in w2v_adamw_step, of
+ *                    w2v_batch_n_moments elements: syn0 (V x dim), syn1
+ *                    (V-1 x dim), gain, bias, each from the next multiple of
+ *                    256 on
+ *   step0            steps taken before this call
+ * stats int64[W2V_N_STATS] may be NULL. steps_host: batches of this call.
+ * sum_ll_host, n_terms_host (may be NULL): sum of log P(centre | hidden) over
+ * the centres with a window, each scored before its batch's update, and their
+ * number. Synchronises the stream. Errors: as w2v_train_hs_epoch, and
+ * W2V_E_ARG for an arch other than 1, settings out of range or a NULL moment.
+ *
+ * w2v_batch_loglik: the same score without any update (the held-out
+ * objective; of bp gain, bias, norm_eps and max_code_len are used).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    float *gain, *bias;       /* float[dim] of the layer norm, both or neither */
+    void *m, *v;
+    float *m_scale, *v_scale; /* bits 8 only */
+    double beta1, beta2, eps;
+    int64_t step0;
+    float norm_eps, weight_decay;
+    int32_t bits;             /* of the moments: 32 or 8 */
+    int32_t max_code_len;     /* from w2v_build_huffman, 1..64 */
+    uint32_t seed;            /* of the 8-bit moments' rounding */
+    int32_t reserved0;
+} w2v_batch_params;
+
+int64_t w2v_batch_n_moments(const w2v_model *m, const w2v_batch_params *bp);
+size_t w2v_train_batch_workspace_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p,
+                                       const w2v_batch_params *bp);
+int w2v_train_batch_epoch(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p,
+                          const w2v_batch_params *bp, int64_t *stats, int64_t *steps_host, double *sum_ll_host,
+                          int64_t *n_terms_host, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t w2v_batch_loglik_workspace_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p,
+                                        const w2v_batch_params *bp);
+int w2v_batch_loglik(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p,
+                     const w2v_batch_params *bp, double *sum_ll_host, int64_t *n_terms_host, void *workspace,
+                     size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
  * Test hooks (not part of the training contract).
  *
  * w2v_sample_pairs: the (centre, context) pairs of the sampler in stream

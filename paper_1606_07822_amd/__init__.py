@@ -8,6 +8,7 @@ Entry points mirror the C ABI in include/w2v.h:
     build_vocab, build_huffman, train_hs_epoch, hs_loglik
     build_noise_table, train_ns_epoch, ns_objective (negative sampling)
     layer_norm, layer_norm_backward, hs_loss, AdamW (a mini-batch step on hidden vectors)
+    train_batch_epoch, batch_loglik (CBOW in mini-batches with them)
 plus the test hooks sample_pairs, keep_thresholds and sample_negatives.
 """
 from __future__ import annotations
@@ -62,6 +63,14 @@ class CAdamWParams(ctypes.Structure):
                 ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32)]
 
 
+class CBatchParams(ctypes.Structure):
+    _fields_ = [("gain", P), ("bias", P), ("m", P), ("v", P), ("m_scale", P), ("v_scale", P),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step0", I64),
+                ("norm_eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("bits", I32), ("max_code_len", I32),
+                ("seed", ctypes.c_uint32), ("reserved0", I32)]
+
+
+assert ctypes.sizeof(CBatchParams) == 104
 assert ctypes.sizeof(CModel) == 80 and ctypes.sizeof(CParams) == 112
 assert ctypes.sizeof(CAdamWTensor) == 72 and ctypes.sizeof(CAdamWParams) == 64
 
@@ -152,6 +161,19 @@ def lib() -> ctypes.CDLL:
         L.w2v_adamw_step.argtypes = [P, I64, I32, P, P, P, P, ctypes.POINTER(CAdamWParams), P]
         L.w2v_adamw_moments.restype = ctypes.c_int
         L.w2v_adamw_moments.argtypes = [P, P, P, P, I64, P, P, P]
+        batch = [ctypes.POINTER(CModel), I64, ctypes.POINTER(CParams), ctypes.POINTER(CBatchParams)]
+        L.w2v_batch_n_moments.restype = I64
+        L.w2v_batch_n_moments.argtypes = [ctypes.POINTER(CModel), ctypes.POINTER(CBatchParams)]
+        L.w2v_train_batch_workspace_bytes.restype = ctypes.c_size_t
+        L.w2v_train_batch_workspace_bytes.argtypes = batch
+        L.w2v_train_batch_epoch.restype = ctypes.c_int
+        L.w2v_train_batch_epoch.argtypes = [ctypes.POINTER(CModel), P, I64, ctypes.POINTER(CParams),
+                                            ctypes.POINTER(CBatchParams), P, P, P, P, P, ctypes.c_size_t, P]
+        L.w2v_batch_loglik_workspace_bytes.restype = ctypes.c_size_t
+        L.w2v_batch_loglik_workspace_bytes.argtypes = batch
+        L.w2v_batch_loglik.restype = ctypes.c_int
+        L.w2v_batch_loglik.argtypes = [ctypes.POINTER(CModel), P, I64, ctypes.POINTER(CParams),
+                                       ctypes.POINTER(CBatchParams), P, P, P, ctypes.c_size_t, P]
         _LIB = L
     return _LIB
 
@@ -843,3 +865,85 @@ class AdamW:
             _check(lib().w2v_adamw_moments(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
                                            self.v_scale.data_ptr(), self.n_moments, mp, vp, _stream(self.device)))
         return outs[0], outs[1]
+
+
+# ------------------------------------------------------------- training in mini-batches
+class BatchState:
+    """What train_batch_epoch keeps beside the model: the layer norm's gain and bias (norm=True; the hidden vector is the
+    window's mean itself otherwise), AdamW's moments (bits 32 or 8) and the number of steps taken."""
+
+    def __init__(self, model: Model, norm: bool = True, bits: int = 32, betas: tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay: float = 0.0, norm_eps: float = 1e-5, seed: int = 0):
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        dev = model.syn0.device
+        self.device, self.bits, self.betas, self.eps = dev, bits, betas, eps
+        self.weight_decay, self.norm_eps, self.seed, self.steps = weight_decay, norm_eps, seed, 0
+        self.gain = torch.ones(model.dim, dtype=torch.float32, device=dev) if norm else None
+        self.bias = torch.zeros(model.dim, dtype=torch.float32, device=dev) if norm else None
+        self.m = self.v = self.m_scale = self.v_scale = None
+        cm, cb = model.c(), self.c(model)
+        self.n_moments = n = lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb))
+        kind = torch.float32 if bits == 32 else torch.uint8
+        self.m, self.v = (torch.zeros(n, dtype=kind, device=dev) for _ in range(2))
+        if bits == 8:
+            self.m_scale, self.v_scale = (torch.zeros(n // AdamW.BLOCK, dtype=torch.float32, device=dev) for _ in range(2))
+
+    def c(self, model: Model) -> CBatchParams:
+        if model.syn0.device != self.device:
+            raise ValueError(f"the model must be on {self.device}")
+        for t, n in ((self.gain, model.dim), (self.bias, model.dim)):
+            _vector_ptr(t, torch.float32, n, self.device, "gain or bias")
+        ptr = [t.data_ptr() if t is not None else None
+               for t in (self.gain, self.bias, self.m, self.v, self.m_scale, self.v_scale)]
+        cb = CBatchParams(*ptr, self.betas[0], self.betas[1], self.eps, self.steps, self.norm_eps, self.weight_decay,
+                          self.bits, model.tree.max_len, self.seed & 0xFFFFFFFF, 0)
+        if self.m is not None:
+            cm = model.c()
+            if lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != self.n_moments:
+                raise ValueError("the state belongs to a model of other sizes")
+        return cb
+
+
+def train_batch_epoch(model: Model, tokens: torch.Tensor, p: Params, state: BatchState,
+                      stats: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+                      ) -> tuple[torch.Tensor, float, int]:
+    """One pass of CBOW (p.arch 1) over tokens (vocabulary indices) in batches of p.sync_batch kept centres, with AdamW.
+    (device stats int64[5], sum of log P over the centres as they were trained on, their number). Synchronises."""
+    dev = tokens.device
+    cm, cp, cb = model.c(), p.c(), state.c(model)
+    if cp.corpus_tokens <= 0:
+        cp.corpus_tokens = max(1, tokens.numel())
+    if stats is None:
+        stats = torch.zeros(N_STATS, dtype=torch.int64, device=dev)
+    sp, tp = _vector_ptr(stats, torch.int64, N_STATS, dev, "stats"), _dev_ptr(tokens, torch.int32, "tokens")
+    if dev != state.device:
+        raise ValueError(f"tokens must be on {state.device}")
+    steps, terms, s = ctypes.c_int64(0), ctypes.c_int64(0), ctypes.c_double(0)
+    with _On(dev):
+        ws = _kept(workspace, max(1, lib().w2v_train_batch_workspace_bytes(ctypes.byref(cm), tokens.numel(), ctypes.byref(cp),
+                                                                          ctypes.byref(cb))), dev)
+        _check(lib().w2v_train_batch_epoch(ctypes.byref(cm), tp, tokens.numel(), ctypes.byref(cp), ctypes.byref(cb), sp,
+                                           ctypes.byref(steps), ctypes.byref(s), ctypes.byref(terms), ws.data_ptr(),
+                                           ws.numel(), _stream(dev)))
+    state.steps += steps.value
+    return stats, s.value, terms.value
+
+
+def batch_loglik(model: Model, tokens: torch.Tensor, p: Params, state: BatchState) -> tuple[float, int]:
+    """Held-out score of a model trained by train_batch_epoch: (sum of log P(centre | hidden vector), number of centres
+    with a window) over the sampler's centres, through the state's layer norm. Synchronises."""
+    dev = tokens.device
+    cm, cp, cb = model.c(), p.c(), state.c(model)
+    if cp.corpus_tokens <= 0:
+        cp.corpus_tokens = max(1, tokens.numel())
+    if dev != state.device:
+        raise ValueError(f"tokens must be on {state.device}")
+    s, terms = ctypes.c_double(0), ctypes.c_int64(0)
+    with _On(dev):
+        ws = _workspace(lib().w2v_batch_loglik_workspace_bytes(ctypes.byref(cm), tokens.numel(), ctypes.byref(cp),
+                                                               ctypes.byref(cb)), dev)
+        _check(lib().w2v_batch_loglik(ctypes.byref(cm), _dev_ptr(tokens, torch.int32, "tokens"), tokens.numel(),
+                                      ctypes.byref(cp), ctypes.byref(cb), ctypes.byref(s), ctypes.byref(terms),
+                                      ws.data_ptr(), ws.numel(), _stream(dev)))
+    return s.value, terms.value

@@ -6,6 +6,7 @@
 #include <string>
 
 #include "w2v_internal.h"
+#include "w2v_ops.h"
 
 namespace w2v {
 
@@ -242,6 +243,11 @@ size_t train_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p) {
 }  // namespace
 
 namespace w2v {
+
+int check_training_args(const w2v_model *m, const w2v_params *p) {
+    if (int rc = check_model(m, true)) return rc;
+    return check_params(p, true);
+}
 
 int check_loglik_args(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p,
                       const double *sum_ll_host, const int64_t *n_pairs_host) {

@@ -10,7 +10,8 @@
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
 // j bits. A wavefront holds kRows sorted rows' x in registers, 64 columns a lane each, and goes down the levels: a
 // level's nodes are runs of rows, summed and written out where a run ends. Runs that reach over a block's border are
-// written as partial sums, which k_hs_join adds up in order, 64 blocks at a time.
+// written as partial sums, which k_hs_join adds up in order, 64 blocks at a time. The same sum with one level, every row
+// for its own word's row of the table, is the gradient of a table's looked-up rows (run_word_sums).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,6 +27,7 @@ constexpr int kRows = 64;         // sorted rows of a wavefront's sum
 constexpr int kFan = 64;          // blocks that one wavefront joins
 constexpr int kXcds = 8;
 
+// What a row's target stands for: a word's path, or (codelen null, longest 1) one row of the table, the word's own.
 struct Tree {
     int32_t V, longest;
     const uint8_t *codelen;
@@ -37,7 +39,7 @@ struct Tree {
 // a NaN, see k_hs_walk).
 __device__ __forceinline__ int path_len(const Tree &t, int32_t v) {
     if (v < 0 || v >= t.V) return 0;
-    const int len = t.codelen[v];
+    const int len = t.codelen ? t.codelen[v] : 1;
     return len <= t.longest ? len : 0;
 }
 
@@ -45,14 +47,19 @@ __device__ __forceinline__ int path_len(const Tree &t, int32_t v) {
 __device__ __forceinline__ uint64_t sort_key(const Tree &t, int32_t v) {
     const int len = path_len(t, v);
     if (len == 0) return ~0ull;
-    return __brevll(t.code[v]) & (~0ull << (64 - len));
+    return t.codelen ? __brevll(t.code[v]) & (~0ull << (64 - len)) : static_cast<uint64_t>(v);
 }
 
 // Levels that two neighbouring sorted rows share an inner node at.
-__device__ __forceinline__ int shared_levels(int32_t va, int la, uint64_t ka, int32_t vb, int lb, uint64_t kb) {
+__device__ __forceinline__ int shared_levels(const Tree &t, int32_t va, int la, uint64_t ka, int32_t vb, int lb,
+                                             uint64_t kb) {
     if (la == 0 || lb == 0) return 0;
     if (va == vb) return la;
-    return min(min(la, lb), static_cast<int>(__clzll(static_cast<long long>(ka ^ kb))) + 1);
+    return t.codelen ? min(min(la, lb), static_cast<int>(__clzll(static_cast<long long>(ka ^ kb))) + 1) : 0;
+}
+
+__device__ __forceinline__ int node_at(const Tree &t, int32_t v, int level) {   // of a path that long
+    return t.codelen ? t.points[t.point_off[v] + level] : v;
 }
 
 // ------------------------------------------------------------------ order
@@ -260,7 +267,7 @@ struct NodeArgs {
     int32_t n, dim;
     const void *x;
     int64_t x_stride;
-    const float *coef;
+    const float *coef;  // null: ones
     float *part;        // [block][2][level][dim]: sums of runs that come in from the left, and of those that go on right
     Borders borders;
     float *dsyn1;
@@ -270,7 +277,7 @@ struct NodeArgs {
 
 __device__ __forceinline__ void put(float *to, float v, bool add) { *to = add ? *to + v : v; }
 
-template <class T>
+template <class T, bool COEF>
 __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
     const int lane = lane_id();
     const int blk = static_cast<int>(blockIdx.x), longest = a.t.longest;
@@ -282,10 +289,9 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
     const int row = on ? a.order[pos] : 0;
     const int32_t v = on ? a.targets[row] : -1;
     const int len = path_len(a.t, v);
-    const int off = len > 0 ? a.t.point_off[v] : 0;
     auto neighbour = [&](int at) {   // levels that the row at place `at` shares with the one before it
         const int32_t va = a.targets[a.order[at - 1]], vb = a.targets[a.order[at]];
-        return shared_levels(va, path_len(a.t, va), a.keys[at - 1], vb, path_len(a.t, vb), a.keys[at]);
+        return shared_levels(a.t, va, path_len(a.t, va), a.keys[at - 1], vb, path_len(a.t, vb), a.keys[at]);
     };
     const int before = on && pos > 0 ? neighbour(pos) : 0;
     const int after = on && pos + 1 < a.n ? neighbour(pos + 1) : 0;
@@ -309,17 +315,17 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
         const int r = __builtin_amdgcn_readlane(row, q);
         if (q < rows && col < a.dim) x[q] = static_cast<float>((static_cast<const T *>(a.x) + r * a.x_stride)[col]);
     }
-    const float *coef = a.coef + static_cast<int64_t>(blk) * longest * kRows;
+    const float *coef = COEF ? a.coef + static_cast<int64_t>(blk) * longest * kRows : nullptr;
     for (int j = 0; j < deepest; ++j) {
         const uint64_t active = __ballot(len > j);
         const uint64_t ends = __ballot(len > j && (after <= j || lane == kWave - 1));
-        const int node = len > j ? a.t.points[off + j] : 0;
-        const float *c = coef + j * kRows;
+        const int node = len > j ? node_at(a.t, v, j) : 0;
+        const float *c = COEF ? coef + j * kRows : nullptr;
         float acc = 0.0f;
 #pragma unroll
         for (int q = 0; q < kRows; ++q) {
             if ((active >> q) & 1ull) {
-                acc = fmaf(c[q], x[q], acc);
+                acc = COEF ? fmaf(c[q], x[q], acc) : acc + x[q];
                 if ((ends >> q) & 1ull) {
                     const bool from_left = left > j && (ends & ((1ull << q) - 1)) == 0;
                     const bool to_right = q == kRows - 1 && right > j;
@@ -377,8 +383,7 @@ __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
     // the node that comes in from a block's left lies on its first row's path
     int node = 0;
     if (left > level) {
-        const int32_t v = a.targets[a.order[static_cast<int64_t>(blk) * a.rows]];
-        node = a.t.points[a.t.point_off[v] + level];
+        node = node_at(a.t, a.targets[a.order[static_cast<int64_t>(blk) * a.rows]], level);
     }
     const int bytes = a.dim * 4;
     const int64_t block_rows = static_cast<int64_t>(2) * longest;
@@ -480,6 +485,59 @@ void launch_walk(const WalkArgs &w, bool grads, unsigned grid, hipStream_t s) {
         k_hs_walk<T, NE, false><<<grid, kWalkThreads, 0, s>>>(w);
 }
 
+int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, hipStream_t s) {
+    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * dim, 1024), 64LL * device_cu_count()));
+    k_hs_zero<<<grid, 256, 0, s>>>(p, rows, dim, stride);
+    W2V_LAUNCH_CHECK("k_hs_zero");
+    return W2V_OK;
+}
+
+// Sorts n <= kSlab rows by their targets' keys.
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const int32_t **order,
+              const uint64_t **keys, hipStream_t s) {
+    const auto rank_grid = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / kWave));
+    k_hs_rank<<<rank_grid, kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
+    W2V_LAUNCH_CHECK("k_hs_rank");
+    *order = b.row0;
+    *keys = b.key0;
+    if (n > kSortBlock) {
+        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeThreads)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1,
+                                                                                             b.row1);
+        W2V_LAUNCH_CHECK("k_hs_merge");
+        *order = b.row1;
+        *keys = b.key1;
+    }
+    return W2V_OK;
+}
+
+// The sorted rows' sums, into rows of `out` that hold zeros or an earlier slab's sums.
+int sum_rows(const NodeArgs &m, int32_t type, const Buffers &b, hipStream_t s) {
+    const auto blocks = static_cast<int32_t>(blocks_of(m.n));
+    const auto tiles = static_cast<unsigned>(ceil_div(m.dim, kWave));
+    (void)with_type(type, [&](auto zero) {
+        using T = decltype(zero);
+        const dim3 grid(static_cast<unsigned>(blocks), tiles);
+        if (m.coef)
+            k_hs_nodes<T, true><<<grid, kWave, 0, s>>>(m);
+        else
+            k_hs_nodes<T, false><<<grid, kWave, 0, s>>>(m);
+        return 0;
+    });
+    W2V_LAUNCH_CHECK("k_hs_nodes");
+    // 1,024 blocks at most: two joins
+    int32_t left = blocks, rows = kRows;
+    for (int k = 0; k < 2 && left > 1; ++k) {
+        const auto fans = static_cast<int32_t>(ceil_div(left, kFan));
+        JoinArgs j{m.t, m.order, m.targets, m.n, m.dim, b.part[k], b.borders[k], left, rows, b.part[1], b.borders[k + 1],
+                   m.dsyn1, m.out_stride, m.add};
+        k_hs_join<<<dim3(static_cast<unsigned>(fans), tiles, static_cast<unsigned>(m.t.longest)), kWave, 0, s>>>(j);
+        W2V_LAUNCH_CHECK("k_hs_join");
+        left = fans;
+        rows *= kFan;
+    }
+    return W2V_OK;
+}
+
 }  // namespace
 
 size_t hs_loss_bytes(int64_t rows, int32_t dim, int32_t longest) {
@@ -491,16 +549,11 @@ size_t hs_loss_bytes(int64_t rows, int32_t dim, int32_t longest) {
 int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
     const Tree t{a.V, a.longest, a.codelen, a.code, a.point_off, a.points};
     const bool grads = a.dx || a.dsyn1;
-    if (a.dsyn1) {
-        const int64_t items = static_cast<int64_t>(a.V - 1) * a.dim;
-        const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(items, 1024), 64LL * device_cu_count()));
-        k_hs_zero<<<grid, 256, 0, s>>>(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride);
-        W2V_LAUNCH_CHECK("k_hs_zero");
-    }
     Buffers b{};
     if (a.dsyn1) {
         Carve c(workspace);
         b = carve(c, a.rows, a.dim, a.longest);
+        if (int rc = zero_rows(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, s)) return rc;
     }
     for (int64_t lo = 0; lo < a.rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, a.rows - lo));
@@ -508,20 +561,8 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         const char *x = static_cast<const char *>(a.x) + lo * a.x_stride * type_bytes(a.type);
         const int32_t *order = nullptr;
         const uint64_t *keys = nullptr;
-        if (a.dsyn1) {
-            const auto rank_grid = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / kWave));
-            k_hs_rank<<<rank_grid, kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
-            W2V_LAUNCH_CHECK("k_hs_rank");
-            order = b.row0;
-            keys = b.key0;
-            if (n > kSortBlock) {
-                k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeThreads)), kMergeThreads, 0, s>>>(b.key0, b.row0, n,
-                                                                                                     b.key1, b.row1);
-                W2V_LAUNCH_CHECK("k_hs_merge");
-                order = b.row1;
-                keys = b.key1;
-            }
-        }
+        if (a.dsyn1)
+            if (int rc = sort_rows(t, targets, n, b, &order, &keys, s)) return rc;
         WalkArgs w{};
         w.t = t;
         w.syn1 = a.syn1;
@@ -551,26 +592,33 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         });
         W2V_LAUNCH_CHECK("k_hs_walk");
         if (!a.dsyn1) continue;
-        const auto blocks = static_cast<int32_t>(blocks_of(n));
-        const auto tiles = static_cast<unsigned>(ceil_div(a.dim, kWave));
-        NodeArgs m{t, keys, order, targets, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.borders[0],
-                   a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0};
-        (void)with_type(a.type, [&](auto zero) {
-            k_hs_nodes<decltype(zero)><<<dim3(static_cast<unsigned>(blocks), tiles), kWave, 0, s>>>(m);
-            return 0;
-        });
-        W2V_LAUNCH_CHECK("k_hs_nodes");
-        // 1,024 blocks at most: two joins
-        int32_t left = blocks, rows = kRows;
-        for (int k = 0; k < 2 && left > 1; ++k) {
-            const auto fans = static_cast<int32_t>(ceil_div(left, kFan));
-            JoinArgs j{t, order, targets, n, a.dim, b.part[k], b.borders[k], left, rows, b.part[1], b.borders[k + 1],
-                       a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0};
-            k_hs_join<<<dim3(static_cast<unsigned>(fans), tiles, static_cast<unsigned>(a.longest)), kWave, 0, s>>>(j);
-            W2V_LAUNCH_CHECK("k_hs_join");
-            left = fans;
-            rows *= kFan;
-        }
+        const NodeArgs m{t, keys, order, targets, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.borders[0],
+                         a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0};
+        if (int rc = sum_rows(m, a.type, b, s)) return rc;
+    }
+    return W2V_OK;
+}
+
+size_t word_sums_bytes(int64_t rows, int32_t dim) {
+    Carve c;
+    carve(c, rows, dim, 1);
+    return c.used();
+}
+
+int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t dim, int64_t x_stride, int32_t V, float *out,
+                  int64_t out_stride, void *workspace, hipStream_t s) {
+    const Tree t{V, 1, nullptr, nullptr, nullptr, nullptr};
+    Carve c(workspace);
+    const Buffers b = carve(c, rows, dim, 1);
+    if (int rc = zero_rows(out, V, dim, out_stride, s)) return rc;
+    for (int64_t lo = 0; lo < rows; lo += kSlab) {
+        const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, rows - lo));
+        const int32_t *order = nullptr;
+        const uint64_t *keys = nullptr;
+        if (int rc = sort_rows(t, words + lo, n, b, &order, &keys, s)) return rc;
+        const NodeArgs m{t, keys, order, words + lo, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
+                         b.borders[0], out, out_stride, lo > 0 ? 1 : 0};
+        if (int rc = sum_rows(m, W2V_F32, b, s)) return rc;
     }
     return W2V_OK;
 }

@@ -102,6 +102,30 @@ int check_tensors(const w2v_adamw_tensor *t, int32_t n, int64_t n_moments) {
     return W2V_OK;
 }
 
+// What both calls on batches read of their arguments.
+int check_batch(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p, const w2v_batch_params *b) {
+    if (int rc = check_training_args(m, p)) return rc;
+    if (p->arch != 1) return fail(W2V_E_ARG, "training in batches is CBOW (arch 1) only");
+    if (p->sync_batch < 1 || p->sync_batch > (1 << 20)) return fail(W2V_E_ARG, "sync_batch must be in 1..2^20");
+    if (n_tokens < 0 || (n_tokens > 0 && !tokens)) return fail(W2V_E_ARG, "bad tokens / n_tokens");
+    if (ceil_div(n_tokens, p->doc_len) > (1 << 30))
+        return fail(W2V_E_ARG, "too many documents for one call: split the stream (first_raw_index)");
+    if (!b) return fail(W2V_E_ARG, "batch params is NULL");
+    if (b->max_code_len < 1 || b->max_code_len > 64) return fail(W2V_E_ARG, "max_code_len must be in 1..64");
+    if (!b->gain != !b->bias) return fail(W2V_E_ARG, "gain and bias come together");
+    if (int rc = check_floats(b->gain, "gain", false)) return rc;
+    if (int rc = check_floats(b->bias, "bias", false)) return rc;
+    if (b->gain && (!(b->norm_eps >= 0.0f) || !std::isfinite(b->norm_eps)))
+        return fail(W2V_E_ARG, "norm_eps must be >= 0 and finite");
+    return W2V_OK;
+}
+
+bool batch_sizes_ok(const w2v_model *m, int64_t n_tokens, const w2v_params *p, const w2v_batch_params *b) {
+    return m && p && b && m->V >= 2 && m->dim >= 1 && m->dim <= 1024 && n_tokens >= 0 && p->doc_len >= 1 && p->window >= 1 &&
+           p->window <= 10 && p->sync_batch >= 1 && p->sync_batch <= (1 << 20) && b->max_code_len >= 1 &&
+           b->max_code_len <= 64;
+}
+
 }  // namespace
 
 extern "C" {
@@ -284,6 +308,56 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
         return fail(W2V_E_ARG, "a required pointer is NULL");
     if (!aligned(m, 4) || !aligned(v, 4)) return fail(W2V_E_ARG, "m and v must be 4-byte aligned");
     return run_adamw_moments(m, v, m_scale, v_scale, n_moments, m_out, v_out, as_stream(hip_stream));
+}
+
+int64_t w2v_batch_n_moments(const w2v_model *m, const w2v_batch_params *bp) {
+    return !m || !bp || m->V < 2 || m->dim < 1 || m->dim > 1024 ? 0 : batch_moments(m, bp);
+}
+
+size_t w2v_train_batch_workspace_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p,
+                                       const w2v_batch_params *bp) {
+    return batch_sizes_ok(m, n_tokens, p, bp) ? batch_bytes(m, n_tokens, p, bp, true) : 0;
+}
+
+int w2v_train_batch_epoch(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p,
+                          const w2v_batch_params *bp, int64_t *stats, int64_t *steps_host, double *sum_ll_host,
+                          int64_t *n_terms_host, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    set_error("");
+    if (int rc = check_batch(m, tokens, n_tokens, p, bp)) return rc;
+    if (bp->bits != 8 && bp->bits != 32) return fail(W2V_E_ARG, "bits must be 8 or 32");
+    if (!bp->m || !bp->v || (bp->bits == 8 && (!bp->m_scale || !bp->v_scale))) return fail(W2V_E_ARG, "a moment is NULL");
+    if (!aligned(bp->m, 4) || !aligned(bp->v, 4) || !aligned(bp->m_scale, 4) || !aligned(bp->v_scale, 4))
+        return fail(W2V_E_ARG, "moments must be 4-byte aligned");
+    if (!(bp->beta1 >= 0.0 && bp->beta1 < 1.0) || !(bp->beta2 >= 0.0 && bp->beta2 < 1.0))
+        return fail(W2V_E_ARG, "beta1 and beta2 must be in [0, 1)");
+    if (!(bp->eps >= 0.0) || !std::isfinite(bp->eps)) return fail(W2V_E_ARG, "eps must be >= 0 and finite");
+    if (!std::isfinite(bp->weight_decay)) return fail(W2V_E_ARG, "weight_decay must be finite");
+    if (bp->step0 < 0) return fail(W2V_E_ARG, "step0 must be >= 0");
+    if (bp->gain && bp->gain == bp->bias) return fail(W2V_E_ARG, "gain and bias must differ");
+    if (!steps_host) return fail(W2V_E_ARG, "steps_host is NULL");
+    if (int rc = check_workspace(workspace, workspace_bytes, batch_bytes(m, n_tokens, p, bp, true))) return rc;
+    try {
+        return run_batches(m, tokens, n_tokens, p, bp, true, stats, steps_host, sum_ll_host, n_terms_host, workspace,
+                           as_stream(hip_stream));
+    } catch (const std::exception &e) {
+        return fail(W2V_E_ARG, std::string("the plan's tables: ") + e.what());
+    }
+}
+
+size_t w2v_batch_loglik_workspace_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p,
+                                        const w2v_batch_params *bp) {
+    return batch_sizes_ok(m, n_tokens, p, bp) ? batch_bytes(m, n_tokens, p, bp, false) : 0;
+}
+
+int w2v_batch_loglik(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p,
+                     const w2v_batch_params *bp, double *sum_ll_host, int64_t *n_terms_host, void *workspace,
+                     size_t workspace_bytes, void *hip_stream) {
+    set_error("");
+    if (int rc = check_batch(m, tokens, n_tokens, p, bp)) return rc;
+    if (!sum_ll_host || !n_terms_host) return fail(W2V_E_ARG, "a required pointer is NULL");
+    if (int rc = check_workspace(workspace, workspace_bytes, batch_bytes(m, n_tokens, p, bp, false))) return rc;
+    return run_batches(m, tokens, n_tokens, p, bp, false, nullptr, nullptr, sum_ll_host, n_terms_host, workspace,
+                       as_stream(hip_stream));
 }
 
 }  // extern "C"

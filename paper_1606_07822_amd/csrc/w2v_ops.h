@@ -120,6 +120,12 @@ struct HsLossArgs {
 size_t hs_loss_bytes(int64_t rows, int32_t dim, int32_t longest);
 int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s);
 
+// out[w] = sum of the rows x_i with words[i] = w, in the rows' order (rows of out without one: zeros; a word outside
+// [0, V): none).
+size_t word_sums_bytes(int64_t rows, int32_t dim);
+int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t dim, int64_t x_stride, int32_t V, float *out,
+                  int64_t out_stride, void *workspace, hipStream_t s);
+
 // ------------------------------------------------------------------ AdamW (adamw.hip)
 constexpr int kMomentBlock = 256;   // elements that share a scale, moments in 8 bits
 
@@ -130,5 +136,13 @@ int run_adamw_step(void *plan, int64_t n_chunks, int32_t bits, void *m, void *v,
                    const w2v_adamw_params &p, hipStream_t s);
 int run_adamw_moments(const void *m, const void *v, const float *m_scale, const float *v_scale, int64_t n, float *m_out,
                       float *v_out, hipStream_t s);
+
+// ------------------------------------------------------------------ training in mini-batches (batch.hip)
+int check_training_args(const w2v_model *m, const w2v_params *p);   // api.hip
+int64_t batch_moments(const w2v_model *m, const w2v_batch_params *b);
+size_t batch_bytes(const w2v_model *m, int64_t n_tokens, const w2v_params *p, const w2v_batch_params *b, bool train);
+int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p, const w2v_batch_params *b,
+                bool train, int64_t *stats, int64_t *steps_host, double *sum_ll_host, int64_t *n_terms_host,
+                void *workspace, hipStream_t s);
 
 }  // namespace w2v

@@ -150,3 +150,65 @@ def test_workspace_queries(w2v):
     q = L.w2v_hs_loss_workspace_bytes
     assert q(ctypes.byref(m), 65, 10) == 0 and q(ctypes.byref(m), 20, -1) == 0 and q(None, 20, 10) == 0
     assert q(ctypes.byref(m), 20, 65536) == q(ctypes.byref(m), 20, 10**7) > q(ctypes.byref(m), 20, 100) > 0
+
+
+def batch_call(w2v, train=True, model=None, params=None, **kw):
+    m = w2v.CModel(0x10000, 0x20000, 100, 50, 64, 0, 0x30000, 1000, 0x40000, 0x50000, 0x60000, 0x70000)
+    for k, v in (model or {}).items():
+        setattr(m, k, v)
+    p = w2v.Params(window=5, corpus_tokens=1000, arch=1, sync_batch=64).c()
+    for k, v in (params or {}).items():
+        setattr(p, k, v)
+    b = dict(gain=A, bias=B, m=C, v=D, m_scale=None, v_scale=None, beta1=0.9, beta2=0.999, eps=1e-8, step0=0, norm_eps=1e-5,
+             weight_decay=0.0, bits=32, max_code_len=20, seed=0, reserved0=0)
+    a = dict(tokens=0x80000, n=1000, steps=True, total=True, ws=0x900000, ws_bytes=1 << 40)
+    b.update({k: v for k, v in kw.items() if k in b})
+    a.update({k: v for k, v in kw.items() if k in a})
+    cb, steps, terms, total = w2v.CBatchParams(*b.values()), ctypes.c_int64(0), ctypes.c_int64(0), ctypes.c_double(0)
+    L = w2v.lib()
+    first = (ctypes.byref(m), a["tokens"], a["n"], ctypes.byref(p), ctypes.byref(cb))
+    if train:
+        return L.w2v_train_batch_epoch(*first, None, ctypes.byref(steps) if a["steps"] else None, None, None, a["ws"],
+                                       a["ws_bytes"], None)
+    return L.w2v_batch_loglik(*first, ctypes.byref(total) if a["total"] else None, ctypes.byref(terms), a["ws"],
+                              a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,code,msg", [
+    (dict(model=dict(V=1)), -1, "V must"), (dict(model=dict(dim=0)), -1, "dim"), (dict(model=dict(syn0=None)), -1, "syn0"),
+    (dict(model=dict(points=None)), -1, "Huffman"), (dict(params=dict(arch=0)), -1, "arch 1"),
+    (dict(params=dict(window=11)), -1, "window"), (dict(params=dict(sync_batch=0)), -1, "sync_batch"),
+    (dict(params=dict(sync_batch=(1 << 20) + 1)), -1, "sync_batch"), (dict(n=-1), -1, "tokens"), (dict(tokens=None), -1, "tokens"),
+    (dict(max_code_len=0), -1, "max_code_len"), (dict(max_code_len=65), -1, "max_code_len"), (dict(gain=None), -1, "together"),
+    (dict(bias=None), -1, "together"), (dict(gain=A + 2), -1, "aligned"), (dict(norm_eps=-1.0), -1, "norm_eps"),
+    (dict(ws=None), -1, "workspace"), (dict(ws=0x900010), -1, "workspace"), (dict(ws_bytes=100), -3, "workspace"),
+])
+@pytest.mark.parametrize("train", [True, False])
+def test_batch_argument_errors(w2v, train, kw, code, msg):
+    assert batch_call(w2v, train, **kw) == code
+    assert msg in w2v.last_error()
+
+
+@pytest.mark.parametrize("kw,msg", [
+    (dict(bits=16), "bits"), (dict(m=None), "moment"), (dict(v=None), "moment"), (dict(bits=8), "moment"), (dict(m=C + 2), "moments"),
+    (dict(beta1=1.0), "beta"), (dict(beta2=-1.0), "beta"), (dict(eps=-1.0), "eps"), (dict(weight_decay=float("inf")), "weight_decay"),
+    (dict(step0=-1), "step0"), (dict(bias=A), "differ"), (dict(steps=None), "steps_host"),
+])
+def test_batch_training_argument_errors(w2v, kw, msg):
+    assert batch_call(w2v, True, **kw) == w2v.W2V_E_ARG
+    assert msg in w2v.last_error()
+
+
+def test_batch_queries(w2v):
+    L = w2v.lib()
+    m = w2v.CModel(None, None, 100, 50, 64, 0, None, 0, None, None, None, None)
+    p = w2v.Params(window=5, arch=1, sync_batch=64).c()
+    b = w2v.CBatchParams()
+    b.max_code_len = 20
+    M, Q, B_ = ctypes.byref(m), ctypes.byref(p), ctypes.byref(b)
+    assert L.w2v_batch_n_moments(M, B_) == 5120 + 5120   # 5,000 and 4,950 in blocks of 256
+    b.gain = A
+    assert L.w2v_batch_n_moments(M, B_) == 5120 + 5120 + 2 * 256
+    assert 0 < L.w2v_batch_loglik_workspace_bytes(M, 1000, Q, B_) < L.w2v_train_batch_workspace_bytes(M, 1000, Q, B_)
+    p.sync_batch = 0
+    assert L.w2v_train_batch_workspace_bytes(M, 1000, Q, B_) == 0 and L.w2v_batch_loglik_workspace_bytes(None, 1, Q, B_) == 0
