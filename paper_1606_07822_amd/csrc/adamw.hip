@@ -155,6 +155,11 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
     uint32_t mc[kSteps], vc[kSteps];
     int64_t po[kSteps], go[kSteps];
     int in_row[kSteps];   // elements of the four that lie in the first one's row
+    uint32_t col[kSteps];
+    auto rows_on = [&](int i, int k) -> uint32_t {   // rows between the four's first element and its i-th
+        if (i < in_row[k]) return 0;
+        return t.cols >= kPer ? 1 : (col[k] + static_cast<uint32_t>(i)) / static_cast<uint32_t>(t.cols);
+    };
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
         const int local = (k * kAdamThreads + static_cast<int>(threadIdx.x)) * kPer;
@@ -165,7 +170,7 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
             load_pack<TG, kPer>(gp + e, g[k]);
         } else {
             in_row[k] = 0;
-            po[k] = go[k] = 0;
+            po[k] = go[k] = col[k] = 0;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) p[k][i] = g[k][i] = 0.0f;
             if (e < t.n) {
@@ -174,10 +179,11 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
                     in_row[k] = static_cast<int>(min<int64_t>(kPer, t.n - e));
                 } else {   // rem0 + local < cols + kChunk, below 2^32
                     const uint32_t c = static_cast<uint32_t>(t.cols), at_row = static_cast<uint32_t>(rem0) + local;
-                    const uint32_t q = at_row / c, col = at_row - q * c;
-                    po[k] = (row0 + q) * t.p_stride + col;
-                    go[k] = (row0 + q) * t.g_stride + col;
-                    in_row[k] = static_cast<int>(min<uint32_t>(kPer, c - col));
+                    const uint32_t q = at_row / c;
+                    col[k] = at_row - q * c;
+                    po[k] = (row0 + q) * t.p_stride + col[k];
+                    go[k] = (row0 + q) * t.g_stride + col[k];
+                    in_row[k] = static_cast<int>(min<uint32_t>(kPer, c - col[k]));
                 }
                 if (in_row[k] == kPer) {
                     load_pack<TP, kPer>(pp + po[k], p[k]);
@@ -186,7 +192,7 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
 #pragma unroll
                     for (int i = 0; i < kPer; ++i)
                         if (e + i < t.n) {
-                            const int64_t d = i < in_row[k] ? 0 : (e + i) / t.cols - e / t.cols;
+                            const uint32_t d = rows_on(i, k);
                             p[k][i] = static_cast<float>(pp[po[k] + i + d * (t.p_stride - t.cols)]);
                             g[k][i] = static_cast<float>(gp[go[k] + i + d * (t.g_stride - t.cols)]);
                         }
@@ -279,7 +285,7 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
                 if (e + i < t.n) {
-                    const int64_t d = i < in_row[k] ? 0 : (e + i) / t.cols - e / t.cols;
+                    const uint32_t d = rows_on(i, k);
                     pp[po[k] + i + d * (t.p_stride - t.cols)] = static_cast<TP>(p[k][i]);
                 }
         }

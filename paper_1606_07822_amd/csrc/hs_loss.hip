@@ -8,7 +8,7 @@
 //
 // dsyn1 is a sum over rows without atomics, in a fixed order. Rows are sorted by their word's code, left-aligned, so
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
-// j bits. A wavefront holds kRows sorted rows' x in registers, 64 columns a lane each, and goes down the levels: a
+// j bits. A wavefront holds up to 64 sorted rows' x in registers, one or two columns a lane, and goes down the levels: a
 // level's nodes are runs of rows, summed and written out where a run ends. Runs that reach over a block's border are
 // written as partial sums, which k_hs_join adds up in order, 64 blocks at a time. The same sum with one level, every row
 // for its own word's row of the table, is the gradient of a table's looked-up rows (run_word_sums).
@@ -23,7 +23,8 @@ namespace {
 
 constexpr int kSlab = 65536;      // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
 constexpr int kSortBlock = 2048;  // rows ranked against each other
-constexpr int kRows = 64;         // sorted rows of a wavefront's sum
+constexpr int kRows = 64;         // most sorted rows of a wavefront's sum
+constexpr int kFewRows = 16;      // of batches of at most kFan times as many, which have few wavefronts otherwise
 constexpr int kFan = 64;          // blocks that one wavefront joins
 constexpr int kXcds = 8;
 
@@ -64,77 +65,106 @@ __device__ __forceinline__ int node_at(const Tree &t, int32_t v, int level) {   
 
 // ------------------------------------------------------------------ order
 // Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order):
-// a workgroup places 64 rows, its wavefronts count in a sixteenth of the block each. Two instructions a comparison.
+// a workgroup places kRankRows rows, its wavefronts count in a sixteenth of the block each. A key read from LDS is
+// compared with kRankRows / 64 of a lane, two instructions each.
 constexpr int kRankThreads = 1024;
 constexpr int kRankWaves = kRankThreads / kWave;
+constexpr int kRankRows = 256;
+constexpr int kRankPer = kRankRows / kWave;
+constexpr int kRankKeys = kSortBlock / kRankWaves;   // keys that a wavefront compares with
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
                                                           uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
     __shared__ uint64_t keys[kSortBlock];
-    __shared__ int32_t counts[kRankWaves][kWave];
-    constexpr int kPerBlock = kSortBlock / kWave;
-    const int32_t lo = static_cast<int32_t>(blockIdx.x) / kPerBlock * kSortBlock;
-    const int own = static_cast<int>(blockIdx.x) % kPerBlock;   // this workgroup's 64 rows of the block
+    __shared__ int32_t counts[kRankWaves][kRankRows];
+    constexpr int kGroups = kSortBlock / kRankRows;
+    const int32_t lo = static_cast<int32_t>(blockIdx.x) / kGroups * kSortBlock;
+    const int own = static_cast<int>(blockIdx.x) % kGroups * kRankRows;   // this workgroup's rows of the block
     const int len = min(kSortBlock, n - lo);
-    if (own * kWave >= len) return;
+    if (own >= len) return;
     for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key(t, targets[lo + i]) : ~0ull;
     __syncthreads();
-    const int lane = lane_id(), wid = static_cast<int>(threadIdx.x) / kWave;
-    const uint64_t mine = keys[own * kWave + lane];
-    int32_t c = 0;
-    for (int seg = wid; seg * kWave < len; seg += kRankWaves) {
-        const uint64_t *k = keys + seg * kWave;
-        const int most = min(kWave, len - seg * kWave);
-        if (seg < own) {
-            for (int j = 0; j < most; ++j) c += k[j] <= mine ? 1 : 0;
-        } else if (seg > own) {
-            for (int j = 0; j < most; ++j) c += k[j] < mine ? 1 : 0;
-        } else {
-            for (int j = 0; j < most; ++j) c += k[j] < mine || (k[j] == mine && j < lane) ? 1 : 0;
-        }
+    const int lane = lane_id(), first = static_cast<int>(threadIdx.x) / kWave * kRankKeys;
+    uint64_t mine[kRankPer];
+    int32_t c[kRankPer];
+#pragma unroll
+    for (int r = 0; r < kRankPer; ++r) {
+        mine[r] = keys[own + r * kWave + lane];
+        c[r] = 0;
     }
-    counts[wid][lane] = c;
+    // keys past the block's end are the largest there are, and follow every row: they count for none
+    if (first + kRankKeys <= own) {
+#pragma unroll 8
+        for (int j = first; j < first + kRankKeys; ++j)
+#pragma unroll
+            for (int r = 0; r < kRankPer; ++r) c[r] += keys[j] <= mine[r] ? 1 : 0;
+    } else if (first >= own + kRankRows) {
+#pragma unroll 8
+        for (int j = first; j < first + kRankKeys; ++j)
+#pragma unroll
+            for (int r = 0; r < kRankPer; ++r) c[r] += keys[j] < mine[r] ? 1 : 0;
+    } else {
+#pragma unroll 4
+        for (int j = first; j < first + kRankKeys; ++j)
+#pragma unroll
+            for (int r = 0; r < kRankPer; ++r)
+                c[r] += keys[j] < mine[r] || (keys[j] == mine[r] && j < own + r * kWave + lane) ? 1 : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < kRankPer; ++r) counts[threadIdx.x / kWave][r * kWave + lane] = c[r];
     __syncthreads();
-    if (wid == 0 && own * kWave + lane < len) {
+    const int i = static_cast<int>(threadIdx.x);
+    if (i < kRankRows && own + i < len) {
         int32_t at = lo;
 #pragma unroll
-        for (int w = 0; w < kRankWaves; ++w) at += counts[w][lane];
-        key_out[at] = mine;
-        row_out[at] = lo + own * kWave + lane;
+        for (int w = 0; w < kRankWaves; ++w) at += counts[w][i];
+        key_out[at] = keys[own + i];
+        row_out[at] = lo + own + i;
     }
 }
 
 // Each key's place among all: its place in its own sorted block and, in every other, the keys before it (equal ones
 // count where their block comes first), found by bisection in LDS, four blocks at once.
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 512;
 constexpr int kMergeBlocks = 4;
 __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__restrict__ key_in,
                                                             const int32_t *__restrict__ row_in, int32_t n,
                                                             uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
-    __shared__ uint64_t keys[kMergeBlocks][kSortBlock];
+    __shared__ uint64_t keys[kMergeBlocks * kSortBlock];
     const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeThreads + static_cast<int32_t>(threadIdx.x);
     const int own = i / kSortBlock, blocks = static_cast<int>(ceil_div(n, kSortBlock));
     const uint64_t mine = i < n ? key_in[i] : 0;
+    constexpr int kLoads = kMergeBlocks * kSortBlock / kMergeThreads;
+    uint64_t next[kLoads];
+    auto load = [&](int b0) {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int32_t k = b0 * kSortBlock + u * kMergeThreads + static_cast<int32_t>(threadIdx.x);
+            next[u] = k < n ? key_in[k] : ~0ull;   // past the end: after every key
+        }
+    };
+    load(0);
     int32_t at = i % kSortBlock;
     for (int b0 = 0; b0 < blocks; b0 += kMergeBlocks) {
         __syncthreads();
-        for (int j = threadIdx.x; j < kMergeBlocks * kSortBlock; j += kMergeThreads) {
-            const int32_t k = b0 * kSortBlock + j;
-            (&keys[0][0])[j] = k < n ? key_in[k] : ~0ull;   // past the end: after every key
-        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) keys[u * kMergeThreads + static_cast<int>(threadIdx.x)] = next[u];
         __syncthreads();
+        if (b0 + kMergeBlocks < blocks) load(b0 + kMergeBlocks);
         int32_t lo[kMergeBlocks], len[kMergeBlocks];
 #pragma unroll
         for (int u = 0; u < kMergeBlocks; ++u) {
             lo[u] = 0;
             len[u] = max(0, min(kSortBlock, n - (b0 + u) * kSortBlock));
         }
+#pragma unroll
         for (int step = kSortBlock; step > 0; step >>= 1) {
+            uint64_t k[kMergeBlocks];
+#pragma unroll
+            for (int u = 0; u < kMergeBlocks; ++u) k[u] = keys[u * kSortBlock + min(lo[u] + step, kSortBlock) - 1];
 #pragma unroll
             for (int u = 0; u < kMergeBlocks; ++u) {
-                const int32_t p = lo[u] + step;
-                if (p > len[u]) continue;
-                const uint64_t k = keys[u][p - 1];
-                if (k < mine || (k == mine && b0 + u < own)) lo[u] = p;
+                const bool before = k[u] < mine || (k[u] == mine && b0 + u < own);
+                if (lo[u] + step <= len[u] && before) lo[u] += step;
             }
         }
 #pragma unroll
@@ -161,7 +191,8 @@ struct WalkArgs {
     float *loss;            // null: not written
     void *dx;               // null: not written
     int64_t dx_stride;
-    float *coef;            // [block of kRows][level][row of the block]; null: not written
+    float *coef;            // [block of block_rows][level][row of the block]; null: not written
+    int32_t block_rows;
 };
 
 constexpr int kWalkThreads = 256;
@@ -247,8 +278,8 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
             }
         }
         if (a.coef && lane < a.t.longest) {
-            float *c = a.coef + static_cast<int64_t>(pos / kRows) * a.t.longest * kRows;
-            c[lane * kRows + pos % kRows] = g_all;
+            float *c = a.coef + static_cast<int64_t>(pos / a.block_rows) * a.t.longest * a.block_rows;
+            c[lane * a.block_rows + pos % a.block_rows] = g_all;
         }
     }
 }
@@ -269,20 +300,63 @@ struct NodeArgs {
     int64_t x_stride;
     const float *coef;  // null: ones
     float *part;        // [block][2][level][dim]: sums of runs that come in from the left, and of those that go on right
+    int32_t *part_node; // [block][level]: the node of a run that comes in from the left
     Borders borders;
     float *dsyn1;
     int64_t out_stride;
     int32_t add;        // dsyn1 holds an earlier slab's sums
 };
 
-__device__ __forceinline__ void put(float *to, float v, bool add) { *to = add ? *to + v : v; }
+using f2 = float __attribute__((ext_vector_type(2)));
 
-template <class T, bool COEF>
+// C neighbouring columns of a row of dim floats, a multiple of C: zeros past the row, and no store there.
+template <int C>
+__device__ __forceinline__ void load_columns(const float *row, int col, int bytes, float (&v)[C]) {
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(row), 0, bytes, kRawBufferWord3);
+    if constexpr (C == 1) {
+        v[0] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4, 0, 0));
+    } else {
+        // the vector as a whole: a bit cast of one of its elements reads the first
+        const f2 u = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(rs, col * 4, 0, 0));
+        v[0] = u[0];
+        v[1] = u[1];
+    }
+}
+
+template <int C>
+__device__ __forceinline__ void store_columns(float *row, int col, int bytes, const float (&v)[C]) {
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(row, 0, bytes, kRawBufferWord3);
+    if constexpr (C == 1) {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[0]), rs, col * 4, 0, 0);
+    } else {
+        using u2 = uint32_t __attribute__((ext_vector_type(2)));
+        const f2 u = {v[0], v[1]};
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, u), rs, col * 4, 0, 0);
+    }
+}
+
+template <int C>
+__device__ __forceinline__ void put_columns(float *row, int col, int bytes, const float (&v)[C], bool add) {
+    if (add) {
+        float old[C];
+        load_columns<C>(row, col, bytes, old);
+#pragma unroll
+        for (int e = 0; e < C; ++e) old[e] += v[e];
+        store_columns<C>(row, col, bytes, old);
+    } else {
+        store_columns<C>(row, col, bytes, v);
+    }
+}
+
+// A lane holds C columns of RB sorted rows; what a level's rows need (coefficient, node, where a run that ends with the
+// row goes) is worked out by the row's lane and read from there. Eight rows inside one run take a multiply-add each;
+// elsewhere a row also takes a branch for whether it has the level and whether its run ends.
+template <class T, bool COEF, int RB, int C>
 __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
     const int lane = lane_id();
     const int blk = static_cast<int>(blockIdx.x), longest = a.t.longest;
-    const int col = static_cast<int>(blockIdx.y) * kWave + lane;
-    const int p0 = blk * kRows, rows = min(kRows, a.n - p0);
+    const int col = (static_cast<int>(blockIdx.y) * kWave + lane) * C;
+    const int p0 = blk * RB, rows = min(RB, a.n - p0);
     // lane q: row q of the block
     const int pos = p0 + lane;
     const bool on = lane < rows;
@@ -295,8 +369,21 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
     };
     const int before = on && pos > 0 ? neighbour(pos) : 0;
     const int after = on && pos + 1 < a.n ? neighbour(pos + 1) : 0;
+    float x[RB][C];
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+        const int64_t r = __builtin_amdgcn_readlane(row, q);
+        if constexpr (sizeof(T) == 4) {
+            load_columns<C>(static_cast<const float *>(a.x) + r * a.x_stride, col, q < rows ? a.dim * 4 : 0, x[q]);
+        } else {
+            const T *from = static_cast<const T *>(a.x) + r * a.x_stride;
+#pragma unroll
+            for (int e = 0; e < C; ++e) x[q][e] = 0.0f;
+            if (q < rows && col < a.dim) load_pack<T, C>(from + col, x[q]);
+        }
+    }
     const int left = __builtin_amdgcn_readlane(before, 0);
-    const int right = __builtin_amdgcn_readlane(after, kWave - 1);
+    const int right = __builtin_amdgcn_readlane(after, RB - 1);
     int deepest = len, inner = on && lane > 0 ? before : kWave;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) {
@@ -308,50 +395,71 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
         a.borders.left[blk] = left;
         a.borders.inner[blk] = inner;
     }
-    float x[kRows];
-#pragma unroll
-    for (int q = 0; q < kRows; ++q) {
-        x[q] = 0.0f;
-        const int r = __builtin_amdgcn_readlane(row, q);
-        if (q < rows && col < a.dim) x[q] = static_cast<float>((static_cast<const T *>(a.x) + r * a.x_stride)[col]);
-    }
-    const float *coef = COEF ? a.coef + static_cast<int64_t>(blk) * longest * kRows : nullptr;
+    const float *coef = COEF ? a.coef + static_cast<int64_t>(blk) * longest * RB : nullptr;
+    auto node_of = [&](int j) { return len > j ? node_at(a.t, v, j) : 0; };
+    auto coef_of = [&](int j) { return COEF && lane < RB && j < longest ? coef[j * RB + lane] : 0.0f; };
+    int next_node = node_of(0);
+    float next_coef = coef_of(0);
+    const int bytes = a.dim * 4;
+    const uint64_t lower = (1ull << lane) - 1;
     for (int j = 0; j < deepest; ++j) {
+        const int node = next_node;
+        const float coefs = next_coef;
+        next_node = node_of(j + 1);
+        next_coef = coef_of(j + 1);
         const uint64_t active = __ballot(len > j);
-        const uint64_t ends = __ballot(len > j && (after <= j || lane == kWave - 1));
-        const int node = len > j ? node_at(a.t, v, j) : 0;
-        const float *c = COEF ? coef + j * kRows : nullptr;
-        float acc = 0.0f;
+        const uint64_t ends = __ballot(len > j && (after <= j || lane == RB - 1));
+        // where the run that ends with this lane's row goes
+        const bool from_left = left > j && (ends & lower) == 0;
+        const bool to_right = lane == RB - 1 && right > j;
+        const int64_t slot = (static_cast<int64_t>(blk) * 2 + (from_left ? 0 : 1)) * longest + j;
+        const uint64_t to = reinterpret_cast<uint64_t>(from_left || to_right ? a.part + slot * a.dim
+                                                                             : a.dsyn1 + node * a.out_stride);
+        const int to_lo = static_cast<int>(to), to_hi = static_cast<int>(to >> 32);
+        const uint64_t direct = a.add ? ~__ballot(from_left || to_right) : 0;   // rows whose sum is added to dsyn1
+        if (left > j && lane == 0 && blockIdx.y == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
+        float acc[C];
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
-            if ((active >> q) & 1ull) {
-                acc = COEF ? fmaf(c[q], x[q], acc) : acc + x[q];
-                if ((ends >> q) & 1ull) {
-                    const bool from_left = left > j && (ends & ((1ull << q) - 1)) == 0;
-                    const bool to_right = q == kRows - 1 && right > j;
-                    if (col < a.dim) {
-                        if (from_left || to_right) {
-                            const int64_t slot = (static_cast<int64_t>(blk) * 2 + (from_left ? 0 : 1)) * longest + j;
-                            a.part[slot * a.dim + col] = acc;
-                        } else {
-                            put(a.dsyn1 + __builtin_amdgcn_readlane(node, q) * a.out_stride + col, acc, a.add);
-                        }
+        for (int e = 0; e < C; ++e) acc[e] = 0.0f;
+        auto add_row = [&](int q) {
+            const float c = COEF ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, coefs), q)) : 1.0f;
+#pragma unroll
+            for (int e = 0; e < C; ++e) acc[e] = COEF ? fmaf(c, x[q][e], acc[e]) : acc[e] + x[q][e];
+        };
+        auto end_run = [&](int q) {
+            const auto lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(to_lo, q));
+            const auto hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(to_hi, q));
+            put_columns<C>(reinterpret_cast<float *>(static_cast<uint64_t>(hi) << 32 | lo), col, bytes, acc, (direct >> q) & 1ull);
+#pragma unroll
+            for (int e = 0; e < C; ++e) acc[e] = 0.0f;
+        };
+#pragma unroll
+        for (int q0 = 0; q0 < RB; q0 += 8) {
+            const uint32_t act = static_cast<uint32_t>(active >> q0) & 255u, end = static_cast<uint32_t>(ends >> q0) & 255u;
+            if (act == 255u && (end & 127u) == 0) {
+#pragma unroll
+                for (int q = q0; q < q0 + 8; ++q) add_row(q);
+                if (end) end_run(q0 + 7);
+            } else if (act) {
+#pragma unroll
+                for (int q = q0; q < q0 + 8; ++q)
+                    if ((act >> (q - q0)) & 1u) {
+                        add_row(q);
+                        if ((end >> (q - q0)) & 1u) end_run(q);
                     }
-                    acc = 0.0f;
-                }
             }
         }
     }
 }
 
 struct JoinArgs {
-    Tree t;
-    const int32_t *order, *targets;
-    int32_t n, dim;
-    const float *in;    // [block][2][level][dim]
+    int32_t dim, longest;
+    const float *in;        // [block][2][level][dim]
+    const int32_t *in_node; // [block][level]
     Borders borders;
-    int32_t blocks, rows;   // rows of a block
-    float *out;         // the same of kFan blocks together
+    int32_t blocks;
+    float *out;             // the same of kFan blocks together
+    int32_t *out_node;
     Borders out_borders;
     float *dsyn1;
     int64_t out_stride;
@@ -361,7 +469,7 @@ struct JoinArgs {
 // Partial sums of kFan neighbouring blocks at one level, in order: a run's first part lies on a block's right, the
 // others on the left of the blocks that follow.
 __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
-    const int lane = lane_id(), level = static_cast<int>(blockIdx.z), longest = a.t.longest;
+    const int lane = lane_id(), level = static_cast<int>(blockIdx.z), longest = a.longest;
     const int first = static_cast<int>(blockIdx.x) * kFan, blk = first + lane;
     const int col = static_cast<int>(blockIdx.y) * kWave + lane;
     const bool on = blk < a.blocks;
@@ -380,86 +488,72 @@ __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
     const uint64_t through = __ballot(left > level && inner > level && right > level);
     const uint64_t has_right = __ballot(right > level) & ~through;
     if (!(has_left | has_right)) return;
-    // the node that comes in from a block's left lies on its first row's path
-    int node = 0;
-    if (left > level) {
-        node = node_at(a.t, a.targets[a.order[static_cast<int64_t>(blk) * a.rows]], level);
-    }
+    const int node = left > level ? a.in_node[static_cast<int64_t>(blk) * longest + level] : 0;
+    if (left > level && lane == 0 && blockIdx.y == 0)
+        a.out_node[static_cast<int64_t>(blockIdx.x) * longest + level] = node;
     const int bytes = a.dim * 4;
     const int64_t block_rows = static_cast<int64_t>(2) * longest;
-    float *in = const_cast<float *>(a.in);
     bool outside = has_left & 1ull;   // the run at hand began before these blocks
-    float acc = 0.0f;
-    constexpr int kAhead = 16;
+    float acc[1] = {0.0f};
+    float *out = a.out + (static_cast<int64_t>(blockIdx.x) * 2 * longest + level) * a.dim;
+    constexpr int kAhead = 32;
     for (int b0 = 0; b0 < kFan && first + b0 < a.blocks; b0 += kAhead) {
-        float l[kAhead], r[kAhead];
+        float l[kAhead][1], r[kAhead][1];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {   // an empty range where there is none: no branch around the loads
             const int b = b0 + u;
-            const int64_t at = (first + b) * block_rows + level;
-            const bool hl = (has_left >> b) & 1ull, hr = (has_right >> b) & 1ull;
-            l[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-                row_rsrc(in, hl ? at : 0, a.dim, hl ? bytes : 0), col * 4, 0, 0));
-            r[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-                row_rsrc(in, hr ? at + longest : 0, a.dim, hr ? bytes : 0), col * 4, 0, 0));
+            const float *at = a.in + ((first + b) * block_rows + level) * a.dim;
+            load_columns<1>(at, col, (has_left >> b) & 1ull ? bytes : 0, l[u]);
+            load_columns<1>(at + static_cast<int64_t>(longest) * a.dim, col, (has_right >> b) & 1ull ? bytes : 0, r[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int b = b0 + u;
             if ((has_left >> b) & 1ull) {
-                acc += l[u];
+                acc[0] += l[u][0];
                 if (!((through >> b) & 1ull)) {
-                    if (col < a.dim) {
-                        if (outside)
-                            a.out[(static_cast<int64_t>(blockIdx.x) * 2 * longest + level) * a.dim + col] = acc;
-                        else
-                            put(a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride + col, acc, a.add);
-                    }
+                    if (outside)
+                        store_columns<1>(out, col, bytes, acc);
+                    else
+                        put_columns<1>(a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride, col, bytes, acc, a.add);
                     outside = false;
-                    acc = 0.0f;
+                    acc[0] = 0.0f;
                 }
             }
             if ((has_right >> b) & 1ull) {
-                acc = r[u];
+                acc[0] = r[u][0];
                 outside = false;
             }
         }
     }
     // a run that goes on past the last block
-    if (((has_right | through) >> (kFan - 1)) & 1ull) {
-        if (col < a.dim)
-            a.out[((static_cast<int64_t>(blockIdx.x) * 2 + (outside ? 0 : 1)) * longest + level) * a.dim + col] = acc;
-    }
+    if (((has_right | through) >> (kFan - 1)) & 1ull)
+        store_columns<1>(out + (outside ? 0 : static_cast<int64_t>(longest) * a.dim), col, bytes, acc);
 }
 
-// The first dim columns of the rows set to zero: four at a time where dim is a multiple of 4.
+// The first dim columns of the rows set to zero, a wavefront a row.
 __global__ __launch_bounds__(256) void k_hs_zero(float *p, int64_t rows, int32_t dim, int64_t stride) {
-    const int per = dim % 4 == 0 ? 4 : 1, width = dim / per;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * blockDim.x;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < rows * width; i += step) {
-        const int64_t r = i / width;
-        float *to = p + r * stride + (i - r * width) * per;
-        if (per == 4) {
-            const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            store_pack<float, 4>(to, zero);
-        } else {
-            *to = 0.0f;
-        }
-    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (256 / kWave);
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (256 / kWave) + threadIdx.x / kWave; r < rows; r += step)
+        for (int c = lane_id() * 4; c < dim; c += kWave * 4) store_cols<float, 4>(p + r * stride, c, dim, zero);
 }
 
 struct Buffers {
     uint64_t *key0, *key1;
     int32_t *row0, *row1;
     float *coef, *part[2];
+    int32_t *node[2];
     Borders borders[3];
 };
 
-int64_t blocks_of(int64_t n) { return ceil_div(n, kRows); }
+// Rows of a wavefront's sum: few, so that there are more wavefronts, while one join takes all blocks.
+int block_rows(int64_t n) { return n <= kFewRows * kFan ? kFewRows : kRows; }
 
 Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     const auto n = static_cast<size_t>(std::min<int64_t>(std::max<int64_t>(rows, 1), kSlab));
-    const auto blocks = static_cast<size_t>(blocks_of(static_cast<int64_t>(n)));
+    // a last slab of few rows has blocks of kFewRows, at most kFan of them
+    const auto blocks = std::max<size_t>((n + kRows - 1) / kRows, std::min<size_t>((n + kFewRows - 1) / kFewRows, kFan));
     const size_t fans = (blocks + kFan - 1) / kFan, level = static_cast<size_t>(2) * longest * dim;
     Buffers b;
     b.key0 = c.take<uint64_t>(n);
@@ -469,6 +563,8 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     b.coef = c.take<float>(blocks * longest * kRows);
     b.part[0] = c.take<float>(blocks * level);
     b.part[1] = c.take<float>(fans * level);
+    b.node[0] = c.take<int32_t>(blocks * longest);
+    b.node[1] = c.take<int32_t>(fans * longest);
     const size_t counts[3] = {blocks, fans, 1};
     for (int k = 0; k < 3; ++k) {
         b.borders[k].left = c.take<int32_t>(counts[k]);
@@ -486,7 +582,7 @@ void launch_walk(const WalkArgs &w, bool grads, unsigned grid, hipStream_t s) {
 }
 
 int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, hipStream_t s) {
-    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * dim, 1024), 64LL * device_cu_count()));
+    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows, 256 / kWave), 64LL * device_cu_count()));
     k_hs_zero<<<grid, 256, 0, s>>>(p, rows, dim, stride);
     W2V_LAUNCH_CHECK("k_hs_zero");
     return W2V_OK;
@@ -495,7 +591,7 @@ int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, hipStream_t s
 // Sorts n <= kSlab rows by their targets' keys.
 int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const int32_t **order,
               const uint64_t **keys, hipStream_t s) {
-    const auto rank_grid = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / kWave));
+    const auto rank_grid = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / kRankRows));
     k_hs_rank<<<rank_grid, kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
     W2V_LAUNCH_CHECK("k_hs_rank");
     *order = b.row0;
@@ -510,30 +606,41 @@ int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b
     return W2V_OK;
 }
 
+template <int R, int C>
+struct SumShape {
+    static constexpr int rows = R, cols = C;
+};
+
 // The sorted rows' sums, into rows of `out` that hold zeros or an earlier slab's sums.
 int sum_rows(const NodeArgs &m, int32_t type, const Buffers &b, hipStream_t s) {
-    const auto blocks = static_cast<int32_t>(blocks_of(m.n));
-    const auto tiles = static_cast<unsigned>(ceil_div(m.dim, kWave));
+    const int rb = block_rows(m.n), cols = m.dim > kWave && m.dim % 2 == 0 ? 2 : 1;
+    const auto blocks = static_cast<int32_t>(ceil_div(m.n, rb));
     (void)with_type(type, [&](auto zero) {
         using T = decltype(zero);
-        const dim3 grid(static_cast<unsigned>(blocks), tiles);
-        if (m.coef)
-            k_hs_nodes<T, true><<<grid, kWave, 0, s>>>(m);
+        const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(ceil_div(m.dim, kWave * cols)));
+        auto launch = [&](auto shape) {
+            constexpr int RB = decltype(shape)::rows, C = decltype(shape)::cols;
+            if (m.coef)
+                k_hs_nodes<T, true, RB, C><<<grid, kWave, 0, s>>>(m);
+            else
+                k_hs_nodes<T, false, RB, C><<<grid, kWave, 0, s>>>(m);
+        };
+        if (rb == kRows)
+            cols == 2 ? launch(SumShape<kRows, 2>{}) : launch(SumShape<kRows, 1>{});
         else
-            k_hs_nodes<T, false><<<grid, kWave, 0, s>>>(m);
+            cols == 2 ? launch(SumShape<kFewRows, 2>{}) : launch(SumShape<kFewRows, 1>{});
         return 0;
     });
     W2V_LAUNCH_CHECK("k_hs_nodes");
-    // 1,024 blocks at most: two joins
-    int32_t left = blocks, rows = kRows;
+    const auto tiles = static_cast<unsigned>(ceil_div(m.dim, kWave));
+    int32_t left = blocks;   // 1,024 at most: two joins
     for (int k = 0; k < 2 && left > 1; ++k) {
         const auto fans = static_cast<int32_t>(ceil_div(left, kFan));
-        JoinArgs j{m.t, m.order, m.targets, m.n, m.dim, b.part[k], b.borders[k], left, rows, b.part[1], b.borders[k + 1],
+        JoinArgs j{m.dim, m.t.longest, b.part[k], b.node[k], b.borders[k], left, b.part[1], b.node[1], b.borders[k + 1],
                    m.dsyn1, m.out_stride, m.add};
         k_hs_join<<<dim3(static_cast<unsigned>(fans), tiles, static_cast<unsigned>(m.t.longest)), kWave, 0, s>>>(j);
         W2V_LAUNCH_CHECK("k_hs_join");
         left = fans;
-        rows *= kFan;
     }
     return W2V_OK;
 }
@@ -578,6 +685,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         w.dx = a.dx ? static_cast<char *>(a.dx) + lo * a.dx_stride * type_bytes(a.type) : nullptr;
         w.dx_stride = a.dx_stride;
         w.coef = a.dsyn1 ? b.coef : nullptr;
+        w.block_rows = block_rows(n);
         const auto grid = static_cast<unsigned>(ceil_div(n, kWalkThreads / kWave));
         const int ne = static_cast<int>(ceil_div(a.dim, kWave));
         (void)with_type(a.type, [&](auto zero) {
@@ -592,7 +700,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         });
         W2V_LAUNCH_CHECK("k_hs_walk");
         if (!a.dsyn1) continue;
-        const NodeArgs m{t, keys, order, targets, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.borders[0],
+        const NodeArgs m{t, keys, order, targets, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.node[0], b.borders[0],
                          a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0};
         if (int rc = sum_rows(m, a.type, b, s)) return rc;
     }
@@ -617,7 +725,7 @@ int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t di
         const uint64_t *keys = nullptr;
         if (int rc = sort_rows(t, words + lo, n, b, &order, &keys, s)) return rc;
         const NodeArgs m{t, keys, order, words + lo, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
-                         b.borders[0], out, out_stride, lo > 0 ? 1 : 0};
+                         b.node[0], b.borders[0], out, out_stride, lo > 0 ? 1 : 0};
         if (int rc = sum_rows(m, W2V_F32, b, s)) return rc;
     }
     return W2V_OK;
