@@ -360,7 +360,7 @@ int w2v_ns_objective(const w2v_model *m, const int32_t *noise_table, int32_t log
  * (w2v_adamw_build_plan excepted); overlapping calls need workspaces of their
  * own. Rows are dim (cols) neighbouring elements, `stride` elements apart
  * (stride >= dim where there is more than one row); columns between the rows
- * are neither read nor written. Any element-aligned address is allowed.
+ * are neither read nor written (but see dsyn1). Any element-aligned address is allowed.
  * bf16 and fp16 elements are converted to fp32 exactly, all arithmetic and
  * sums are fp32 and results are rounded once, to nearest. Sums over rows have
  * a fixed order: equal inputs give equal bits.
@@ -395,7 +395,8 @@ int w2v_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
              P(v|x) = prod_j sigmoid((1 - 2 t_j) x . syn1[n_j]) over v's path
      dx      rows x dim elements of type out, may be NULL
      dsyn1   float[V-1][dsyn1_stride] out, may be NULL: every row's first dim
-             columns are written
+             columns are written; where dsyn1_stride is m->row_stride, zeros may
+             be written into the rows' padding columns, too (as in training)
    The gradients are those of sum_i weights[i] loss[i] (weights float[rows], or
    NULL: ones). A negative target means none: loss 0, a dx of zeros, x not
    read into any sum. A target outside the vocabulary, or one whose code is

@@ -741,7 +741,7 @@ def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch
             ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
     """(loss, dx, dsyn1): -log P(targets[i] | x[i]) under the model's hierarchical softmax (float32) and, with grads,
     the gradients of sum(weights * loss) for x [rows, dim] and for model.syn1 (dsyn1 float32 of syn1's shape, all rows
-    written in their first dim columns). targets int32, negative: none. Does not sync."""
+    written: their first dim columns, and zeros perhaps in the padding). targets int32, negative: none. Does not sync."""
     xp, xs = _rows_ptr(x, "x", x)
     kind = _type_of(x, "x")
     n, dev = x.shape[0], x.device

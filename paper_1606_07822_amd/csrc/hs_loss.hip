@@ -26,6 +26,7 @@ constexpr int kSortBlock = 2048;  // rows ranked against each other
 constexpr int kRows = 64;         // most sorted rows of a wavefront's sum
 constexpr int kFewRows = 16;      // of batches of at most kFan times as many, which have few wavefronts otherwise
 constexpr int kFan = 64;          // blocks that one wavefront joins
+constexpr int kRankNarrow = 16384;   // rows up to which a workgroup ranks 64 of them, not 256
 constexpr int kXcds = 8;
 
 // What a row's target stands for: a word's path, or (codelen null, longest 1) one row of the table, the word's own.
@@ -64,56 +65,51 @@ __device__ __forceinline__ int node_at(const Tree &t, int32_t v, int level) {   
 }
 
 // ------------------------------------------------------------------ order
-// Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order):
-// a workgroup places kRankRows rows, its wavefronts count in a sixteenth of the block each. A key read from LDS is
-// compared with kRankRows / 64 of a lane, two instructions each.
+// Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order).
+// A workgroup places R rows; its wavefronts share the pairs of 64 of them and 64 keys of the block, two instructions a
+// comparison: keys that come first count where they are equal, too, later ones where they are smaller, and only a
+// pair of the same 64 compares the places as well.
 constexpr int kRankThreads = 1024;
 constexpr int kRankWaves = kRankThreads / kWave;
-constexpr int kRankRows = 256;
-constexpr int kRankPer = kRankRows / kWave;
-constexpr int kRankKeys = kSortBlock / kRankWaves;   // keys that a wavefront compares with
+template <int R>
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
                                                           uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
     __shared__ uint64_t keys[kSortBlock];
-    __shared__ int32_t counts[kRankWaves][kRankRows];
-    constexpr int kGroups = kSortBlock / kRankRows;
+    __shared__ int32_t counts[kRankWaves][R];
+    constexpr int kGroups = kSortBlock / R, kSets = R / kWave;
     const int32_t lo = static_cast<int32_t>(blockIdx.x) / kGroups * kSortBlock;
-    const int own = static_cast<int>(blockIdx.x) % kGroups * kRankRows;   // this workgroup's rows of the block
+    const int own = static_cast<int>(blockIdx.x) % kGroups * R;   // this workgroup's rows of the block
     const int len = min(kSortBlock, n - lo);
     if (own >= len) return;
     for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key(t, targets[lo + i]) : ~0ull;
     __syncthreads();
-    const int lane = lane_id(), first = static_cast<int>(threadIdx.x) / kWave * kRankKeys;
-    uint64_t mine[kRankPer];
-    int32_t c[kRankPer];
+    const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    int32_t c[kSets];
 #pragma unroll
-    for (int r = 0; r < kRankPer; ++r) {
-        mine[r] = keys[own + r * kWave + lane];
-        c[r] = 0;
-    }
-    // keys past the block's end are the largest there are, and follow every row: they count for none
-    if (first + kRankKeys <= own) {
-#pragma unroll 8
-        for (int j = first; j < first + kRankKeys; ++j)
+    for (int r = 0; r < kSets; ++r) c[r] = 0;
+    for (int seg = wid; seg * kWave < len; seg += kRankWaves) {   // keys past the end are the largest: they count for none
+        const uint64_t *k = keys + seg * kWave;
 #pragma unroll
-            for (int r = 0; r < kRankPer; ++r) c[r] += keys[j] <= mine[r] ? 1 : 0;
-    } else if (first >= own + kRankRows) {
-#pragma unroll 8
-        for (int j = first; j < first + kRankKeys; ++j)
-#pragma unroll
-            for (int r = 0; r < kRankPer; ++r) c[r] += keys[j] < mine[r] ? 1 : 0;
-    } else {
-#pragma unroll 4
-        for (int j = first; j < first + kRankKeys; ++j)
-#pragma unroll
-            for (int r = 0; r < kRankPer; ++r)
-                c[r] += keys[j] < mine[r] || (keys[j] == mine[r] && j < own + r * kWave + lane) ? 1 : 0;
+        for (int r = 0; r < kSets; ++r) {
+            const int mine_seg = own / kWave + r;
+            const uint64_t mine = keys[mine_seg * kWave + lane];
+            if (seg < mine_seg) {
+#pragma unroll 16
+                for (int j = 0; j < kWave; ++j) c[r] += k[j] <= mine ? 1 : 0;
+            } else if (seg > mine_seg) {
+#pragma unroll 16
+                for (int j = 0; j < kWave; ++j) c[r] += k[j] < mine ? 1 : 0;
+            } else {
+#pragma unroll 16
+                for (int j = 0; j < kWave; ++j) c[r] += k[j] < mine || (k[j] == mine && j < lane) ? 1 : 0;
+            }
+        }
     }
 #pragma unroll
-    for (int r = 0; r < kRankPer; ++r) counts[threadIdx.x / kWave][r * kWave + lane] = c[r];
+    for (int r = 0; r < kSets; ++r) counts[wid][r * kWave + lane] = c[r];
     __syncthreads();
     const int i = static_cast<int>(threadIdx.x);
-    if (i < kRankRows && own + i < len) {
+    if (i < R && own + i < len) {
         int32_t at = lo;
 #pragma unroll
         for (int w = 0; w < kRankWaves; ++w) at += counts[w][i];
@@ -123,14 +119,21 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
 }
 
 // Each key's place among all: its place in its own sorted block and, in every other, the keys before it (equal ones
-// count where their block comes first), found by bisection in LDS, four blocks at once.
-constexpr int kMergeThreads = 512;
-constexpr int kMergeBlocks = 4;
+// count where their block comes first), found by bisection in LDS. A workgroup places 256 keys; each of its four parts
+// takes two of the eight blocks that are in LDS at a time (a bisection is a chain of LDS reads, so several run at once),
+// and the next eight are on their way meanwhile.
+constexpr int kMergeKeys = 256;
+constexpr int kMergeParts = 4;
+constexpr int kMergeThreads = kMergeKeys * kMergeParts;
+constexpr int kMergePer = 2;
+constexpr int kMergeBlocks = kMergeParts * kMergePer;
 __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__restrict__ key_in,
                                                             const int32_t *__restrict__ row_in, int32_t n,
                                                             uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
     __shared__ uint64_t keys[kMergeBlocks * kSortBlock];
-    const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeThreads + static_cast<int32_t>(threadIdx.x);
+    __shared__ int32_t counts[kMergeParts][kMergeKeys];
+    const int slot = static_cast<int>(threadIdx.x) % kMergeKeys, part = static_cast<int>(threadIdx.x) / kMergeKeys;
+    const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeKeys + slot;
     const int own = i / kSortBlock, blocks = static_cast<int>(ceil_div(n, kSortBlock));
     const uint64_t mine = i < n ? key_in[i] : 0;
     constexpr int kLoads = kMergeBlocks * kSortBlock / kMergeThreads;
@@ -143,35 +146,42 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__re
         }
     };
     load(0);
-    int32_t at = i % kSortBlock;
+    int32_t at = 0;
     for (int b0 = 0; b0 < blocks; b0 += kMergeBlocks) {
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) keys[u * kMergeThreads + static_cast<int>(threadIdx.x)] = next[u];
         __syncthreads();
         if (b0 + kMergeBlocks < blocks) load(b0 + kMergeBlocks);
-        int32_t lo[kMergeBlocks], len[kMergeBlocks];
+        const int mine0 = part * kMergePer;
+        int32_t lo[kMergePer], len[kMergePer];
 #pragma unroll
-        for (int u = 0; u < kMergeBlocks; ++u) {
+        for (int u = 0; u < kMergePer; ++u) {
             lo[u] = 0;
-            len[u] = max(0, min(kSortBlock, n - (b0 + u) * kSortBlock));
+            len[u] = max(0, min(kSortBlock, n - (b0 + mine0 + u) * kSortBlock));
         }
 #pragma unroll
         for (int step = kSortBlock; step > 0; step >>= 1) {
-            uint64_t k[kMergeBlocks];
+            uint64_t k[kMergePer];
 #pragma unroll
-            for (int u = 0; u < kMergeBlocks; ++u) k[u] = keys[u * kSortBlock + min(lo[u] + step, kSortBlock) - 1];
+            for (int u = 0; u < kMergePer; ++u)
+                k[u] = keys[(mine0 + u) * kSortBlock + min(lo[u] + step, kSortBlock) - 1];
 #pragma unroll
-            for (int u = 0; u < kMergeBlocks; ++u) {
-                const bool before = k[u] < mine || (k[u] == mine && b0 + u < own);
+            for (int u = 0; u < kMergePer; ++u) {
+                const bool before = b0 + mine0 + u < own ? k[u] <= mine : k[u] < mine;
                 if (lo[u] + step <= len[u] && before) lo[u] += step;
             }
         }
 #pragma unroll
-        for (int u = 0; u < kMergeBlocks; ++u)
-            if (b0 + u != own) at += lo[u];
+        for (int u = 0; u < kMergePer; ++u)
+            if (b0 + mine0 + u != own) at += lo[u];
     }
-    if (i < n) {
+    counts[part][slot] = at;
+    __syncthreads();
+    if (part == 0 && i < n) {
+        at = i % kSortBlock;
+#pragma unroll
+        for (int k = 0; k < kMergeParts; ++k) at += counts[k][slot];
         key_out[at] = mine;
         row_out[at] = row_in[i];
     }
@@ -348,14 +358,17 @@ __device__ __forceinline__ void put_columns(float *row, int col, int bytes, cons
     }
 }
 
-// A lane holds C columns of RB sorted rows; what a level's rows need (coefficient, node, where a run that ends with the
-// row goes) is worked out by the row's lane and read from there. Eight rows inside one run take a multiply-add each;
-// elsewhere a row also takes a branch for whether it has the level and whether its run ends.
+// A lane holds C columns of RB sorted rows, a wavefront 64 C columns, a workgroup the whole row. What a level's rows need
+// (coefficient, node, where a run that ends with the row goes) is worked out by the row's lane and read from there; the
+// coefficients and nodes of all levels are fetched into LDS first, as a load waits for the stores that went before it.
+// Eight rows inside one run take a multiply-add each; elsewhere a row also takes a branch for whether it has the level
+// and whether its run ends.
 template <class T, bool COEF, int RB, int C>
-__global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
+__global__ __launch_bounds__(C == 1 ? 1024 : 512) void k_hs_nodes(NodeArgs a) {
+    extern __shared__ int32_t level_node[];   // [longest][RB], then the coefficients alike
     const int lane = lane_id();
     const int blk = static_cast<int>(blockIdx.x), longest = a.t.longest;
-    const int col = (static_cast<int>(blockIdx.y) * kWave + lane) * C;
+    const int col = static_cast<int>(threadIdx.x) * C;
     const int p0 = blk * RB, rows = min(RB, a.n - p0);
     // lane q: row q of the block
     const int pos = p0 + lane;
@@ -391,22 +404,27 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
         inner = min(inner, __shfl_xor(inner, m, kWave));
     }
     deepest = __builtin_amdgcn_readfirstlane(deepest);
-    if (blockIdx.y == 0 && lane == 0) {
+    if (threadIdx.x == 0) {
         a.borders.left[blk] = left;
         a.borders.inner[blk] = inner;
     }
-    const float *coef = COEF ? a.coef + static_cast<int64_t>(blk) * longest * RB : nullptr;
-    auto node_of = [&](int j) { return len > j ? node_at(a.t, v, j) : 0; };
-    auto coef_of = [&](int j) { return COEF && lane < RB && j < longest ? coef[j * RB + lane] : 0.0f; };
-    int next_node = node_of(0);
-    float next_coef = coef_of(0);
+    const int cells = longest * RB;
+    float *level_coef = reinterpret_cast<float *>(level_node + cells);
+    const int off = len > 0 && a.t.codelen ? a.t.point_off[v] : 0;
+    const int wid = static_cast<int>(threadIdx.x) / kWave, waves = static_cast<int>(blockDim.x) / kWave;
+    if (lane < RB) {
+        for (int j = wid; j < deepest; j += waves) level_node[j * RB + lane] = j < len ? (a.t.codelen ? a.t.points[off + j] : v) : 0;
+    }
+    if constexpr (COEF) {
+        const float *coef = a.coef + static_cast<int64_t>(blk) * cells;
+        for (int i = threadIdx.x; i < deepest * RB; i += blockDim.x) level_coef[i] = coef[i];
+    }
+    __syncthreads();
     const int bytes = a.dim * 4;
     const uint64_t lower = (1ull << lane) - 1;
     for (int j = 0; j < deepest; ++j) {
-        const int node = next_node;
-        const float coefs = next_coef;
-        next_node = node_of(j + 1);
-        next_coef = coef_of(j + 1);
+        const int node = level_node[j * RB + lane % RB];
+        const float coefs = COEF ? level_coef[j * RB + lane % RB] : 1.0f;
         const uint64_t active = __ballot(len > j);
         const uint64_t ends = __ballot(len > j && (after <= j || lane == RB - 1));
         // where the run that ends with this lane's row goes
@@ -417,7 +435,7 @@ __global__ __launch_bounds__(kWave) void k_hs_nodes(NodeArgs a) {
                                                                              : a.dsyn1 + node * a.out_stride);
         const int to_lo = static_cast<int>(to), to_hi = static_cast<int>(to >> 32);
         const uint64_t direct = a.add ? ~__ballot(from_left || to_right) : 0;   // rows whose sum is added to dsyn1
-        if (left > j && lane == 0 && blockIdx.y == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
+        if (left > j && threadIdx.x == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
         float acc[C];
 #pragma unroll
         for (int e = 0; e < C; ++e) acc[e] = 0.0f;
@@ -492,19 +510,20 @@ __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
     if (left > level && lane == 0 && blockIdx.y == 0)
         a.out_node[static_cast<int64_t>(blockIdx.x) * longest + level] = node;
     const int bytes = a.dim * 4;
-    const int64_t block_rows = static_cast<int64_t>(2) * longest;
+    const int64_t part = static_cast<int64_t>(longest) * a.dim;   // of a block's two
+    const float *in = a.in + first * 2 * part + static_cast<int64_t>(level) * a.dim;
     bool outside = has_left & 1ull;   // the run at hand began before these blocks
     float acc[1] = {0.0f};
     float *out = a.out + (static_cast<int64_t>(blockIdx.x) * 2 * longest + level) * a.dim;
-    constexpr int kAhead = 32;
-    for (int b0 = 0; b0 < kFan && first + b0 < a.blocks; b0 += kAhead) {
+    constexpr int kAhead = 16;
+    for (int b0 = 0; b0 < kFan; b0 += kAhead) {
+        if (!(((has_left | has_right) >> b0) & ((1ull << kAhead) - 1))) continue;
         float l[kAhead][1], r[kAhead][1];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {   // an empty range where there is none: no branch around the loads
             const int b = b0 + u;
-            const float *at = a.in + ((first + b) * block_rows + level) * a.dim;
-            load_columns<1>(at, col, (has_left >> b) & 1ull ? bytes : 0, l[u]);
-            load_columns<1>(at + static_cast<int64_t>(longest) * a.dim, col, (has_right >> b) & 1ull ? bytes : 0, r[u]);
+            load_columns<1>(in + b * 2 * part, col, (has_left >> b) & 1ull ? bytes : 0, l[u]);
+            load_columns<1>(in + b * 2 * part + part, col, (has_right >> b) & 1ull ? bytes : 0, r[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -528,15 +547,34 @@ __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
     }
     // a run that goes on past the last block
     if (((has_right | through) >> (kFan - 1)) & 1ull)
-        store_columns<1>(out + (outside ? 0 : static_cast<int64_t>(longest) * a.dim), col, bytes, acc);
+        store_columns<1>(out + (outside ? 0 : part), col, bytes, acc);
 }
 
 // The first dim columns of the rows set to zero, a wavefront a row.
-__global__ __launch_bounds__(256) void k_hs_zero(float *p, int64_t rows, int32_t dim, int64_t stride) {
-    const int64_t step = static_cast<int64_t>(gridDim.x) * (256 / kWave);
+constexpr int kZeroThreads = 256;
+__global__ __launch_bounds__(kZeroThreads) void k_hs_zero(float *p, int64_t rows, int32_t dim, int64_t stride) {
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (kZeroThreads / kWave);
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (256 / kWave) + threadIdx.x / kWave; r < rows; r += step)
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kZeroThreads / kWave) + threadIdx.x / kWave; r < rows; r += step)
         for (int c = lane_id() * 4; c < dim; c += kWave * 4) store_cols<float, 4>(p + r * stride, c, dim, zero);
+}
+
+// n floats set to zero, kZeroPer vectors a thread.
+constexpr int kZeroPer = 4;
+__global__ __launch_bounds__(kZeroThreads) void k_hs_zero_flat(float *p, int64_t n) {
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int64_t kGroup = kZeroThreads * kZeroPer * 4;
+    for (int64_t g = blockIdx.x * kGroup; g < n; g += gridDim.x * kGroup) {
+        const int64_t i = g + threadIdx.x * 4;
+        if (g + kGroup <= n) {
+#pragma unroll
+            for (int u = 0; u < kZeroPer; ++u) store_pack<float, 4>(p + i + u * kZeroThreads * 4, zero);
+        } else {
+            for (int u = 0; u < kZeroPer; ++u)
+                for (int e = 0; e < 4; ++e)
+                    if (i + u * kZeroThreads * 4 + e < n) p[i + u * kZeroThreads * 4 + e] = 0.0f;
+        }
+    }
 }
 
 struct Buffers {
@@ -581,9 +619,18 @@ void launch_walk(const WalkArgs &w, bool grads, unsigned grid, hipStream_t s) {
         k_hs_walk<T, NE, false><<<grid, kWalkThreads, 0, s>>>(w);
 }
 
-int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, hipStream_t s) {
-    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows, 256 / kWave), 64LL * device_cu_count()));
-    k_hs_zero<<<grid, 256, 0, s>>>(p, rows, dim, stride);
+// whole: the rows' padding may be written too. Rows that end inside a 128-byte line cost memory a read for the rest of
+// it (1M rows of 300 floats, 320 apart: 329 us, 193 with the padding), so short padding is then written with them.
+int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole, hipStream_t s) {
+    if (whole && stride - dim < 32) {
+        const int64_t n = rows * stride;
+        const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(n, kZeroThreads * kZeroPer * 4), kMaxGroups));
+        k_hs_zero_flat<<<grid, kZeroThreads, 0, s>>>(p, n);
+        W2V_LAUNCH_CHECK("k_hs_zero_flat");
+        return W2V_OK;
+    }
+    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows, kZeroThreads / kWave), 64LL * device_cu_count()));
+    k_hs_zero<<<grid, kZeroThreads, 0, s>>>(p, rows, dim, stride);
     W2V_LAUNCH_CHECK("k_hs_zero");
     return W2V_OK;
 }
@@ -591,14 +638,17 @@ int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, hipStream_t s
 // Sorts n <= kSlab rows by their targets' keys.
 int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const int32_t **order,
               const uint64_t **keys, hipStream_t s) {
-    const auto rank_grid = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / kRankRows));
-    k_hs_rank<<<rank_grid, kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
+    const auto sort_blocks = static_cast<unsigned>(ceil_div(n, kSortBlock));
+    if (n <= kRankNarrow)
+        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
+    else
+        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
     W2V_LAUNCH_CHECK("k_hs_rank");
     *order = b.row0;
     *keys = b.key0;
     if (n > kSortBlock) {
-        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeThreads)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1,
-                                                                                             b.row1);
+        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1,
+                                                                                         b.row1);
         W2V_LAUNCH_CHECK("k_hs_merge");
         *order = b.row1;
         *keys = b.key1;
@@ -617,13 +667,14 @@ int sum_rows(const NodeArgs &m, int32_t type, const Buffers &b, hipStream_t s) {
     const auto blocks = static_cast<int32_t>(ceil_div(m.n, rb));
     (void)with_type(type, [&](auto zero) {
         using T = decltype(zero);
-        const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(ceil_div(m.dim, kWave * cols)));
+        const auto threads = static_cast<unsigned>(ceil_div(m.dim, kWave * cols) * kWave);
+        const size_t lds = static_cast<size_t>(m.t.longest) * rb * (m.coef ? 8 : 4);
         auto launch = [&](auto shape) {
             constexpr int RB = decltype(shape)::rows, C = decltype(shape)::cols;
             if (m.coef)
-                k_hs_nodes<T, true, RB, C><<<grid, kWave, 0, s>>>(m);
+                k_hs_nodes<T, true, RB, C><<<static_cast<unsigned>(blocks), threads, lds, s>>>(m);
             else
-                k_hs_nodes<T, false, RB, C><<<grid, kWave, 0, s>>>(m);
+                k_hs_nodes<T, false, RB, C><<<static_cast<unsigned>(blocks), threads, lds, s>>>(m);
         };
         if (rb == kRows)
             cols == 2 ? launch(SumShape<kRows, 2>{}) : launch(SumShape<kRows, 1>{});
@@ -660,7 +711,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
     if (a.dsyn1) {
         Carve c(workspace);
         b = carve(c, a.rows, a.dim, a.longest);
-        if (int rc = zero_rows(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, s)) return rc;
+        if (int rc = zero_rows(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, a.dsyn1_stride == a.stride, s)) return rc;
     }
     for (int64_t lo = 0; lo < a.rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, a.rows - lo));
@@ -718,7 +769,7 @@ int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t di
     const Tree t{V, 1, nullptr, nullptr, nullptr, nullptr};
     Carve c(workspace);
     const Buffers b = carve(c, rows, dim, 1);
-    if (int rc = zero_rows(out, V, dim, out_stride, s)) return rc;
+    if (int rc = zero_rows(out, V, dim, out_stride, true, s)) return rc;
     for (int64_t lo = 0; lo < rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, rows - lo));
         const int32_t *order = nullptr;

@@ -121,7 +121,7 @@ size_t hs_loss_bytes(int64_t rows, int32_t dim, int32_t longest);
 int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s);
 
 // out[w] = sum of the rows x_i with words[i] = w, in the rows' order (rows of out without one: zeros; a word outside
-// [0, V): none).
+// [0, V): none; the padding of out's rows may be written with zeros).
 size_t word_sums_bytes(int64_t rows, int32_t dim);
 int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t dim, int64_t x_stride, int32_t V, float *out,
                   int64_t out_stride, void *workspace, hipStream_t s);
