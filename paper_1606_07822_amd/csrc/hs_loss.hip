@@ -8,13 +8,14 @@
 //
 // dsyn1 is a sum over rows without atomics, in a fixed order. Rows are sorted by their word's code, left-aligned, so
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
-// j bits. A wavefront holds up to 64 sorted rows' x in registers, one or two columns a lane, and goes down the levels: a
+// j bits. A wavefront holds up to 32 sorted rows' x in registers, up to five columns a lane, and goes down the levels: a
 // level's nodes are runs of rows, summed and written out where a run ends. Runs that reach over a block's border are
 // written as partial sums, which k_hs_join adds up in order, 64 blocks at a time. The same sum with one level, every row
 // for its own word's row of the table, is the gradient of a table's looked-up rows (run_word_sums).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "w2v_ops.h"
 
@@ -23,7 +24,7 @@ namespace {
 
 constexpr int kSlab = 65536;      // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
 constexpr int kSortBlock = 2048;  // rows ranked against each other
-constexpr int kRows = 64;         // most sorted rows of a wavefront's sum
+constexpr int kRows = 32;         // sorted rows of a wavefront's sum
 constexpr int kFewRows = 16;      // of batches of at most kFan times as many, which have few wavefronts otherwise
 constexpr int kFan = 64;          // blocks that one wavefront joins
 constexpr int kRankNarrow = 16384;   // rows up to which a workgroup ranks 64 of them, not 256
@@ -60,11 +61,21 @@ __device__ __forceinline__ int shared_levels(const Tree &t, int32_t va, int la, 
     return t.codelen ? min(min(la, lb), static_cast<int>(__clzll(static_cast<long long>(ka ^ kb))) + 1) : 0;
 }
 
-__device__ __forceinline__ int node_at(const Tree &t, int32_t v, int level) {   // of a path that long
-    return t.codelen ? t.points[t.point_off[v] + level] : v;
+// ------------------------------------------------------------------ order
+// A sorted row: its place in the batch, its target, and the length and the place of that word's path.
+struct Item {
+    int32_t row, word, off, len;
+};
+
+__device__ __forceinline__ Item item_of(const Tree &t, int32_t row, int32_t word) {
+    const int len = path_len(t, word);
+    return Item{row, word, len > 0 && t.codelen ? t.point_off[word] : 0, len};
 }
 
-// ------------------------------------------------------------------ order
+__device__ __forceinline__ int node_of(const Tree &t, const Item &i, int level) {   // of a path that long
+    return t.codelen ? t.points[i.off + level] : i.word;
+}
+
 // Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order).
 // A workgroup places R rows; its wavefronts share the pairs of 64 of them and 64 keys of the block, two instructions a
 // comparison: keys that come first count where they are equal, too, later ones where they are smaller, and only a
@@ -73,7 +84,7 @@ constexpr int kRankThreads = 1024;
 constexpr int kRankWaves = kRankThreads / kWave;
 template <int R>
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
-                                                          uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
+                                                          uint64_t *__restrict__ key_out, Item *__restrict__ item_out) {
     __shared__ uint64_t keys[kSortBlock];
     __shared__ int32_t counts[kRankWaves][R];
     constexpr int kGroups = kSortBlock / R, kSets = R / kWave;
@@ -81,6 +92,9 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
     const int own = static_cast<int>(blockIdx.x) % kGroups * R;   // this workgroup's rows of the block
     const int len = min(kSortBlock, n - lo);
     if (own >= len) return;
+    const int i = static_cast<int>(threadIdx.x);
+    Item item{};
+    if (i < R && own + i < len) item = item_of(t, lo + own + i, targets[lo + own + i]);
     for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key(t, targets[lo + i]) : ~0ull;
     __syncthreads();
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -108,13 +122,12 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
 #pragma unroll
     for (int r = 0; r < kSets; ++r) counts[wid][r * kWave + lane] = c[r];
     __syncthreads();
-    const int i = static_cast<int>(threadIdx.x);
     if (i < R && own + i < len) {
         int32_t at = lo;
 #pragma unroll
         for (int w = 0; w < kRankWaves; ++w) at += counts[w][i];
         key_out[at] = keys[own + i];
-        row_out[at] = lo + own + i;
+        item_out[at] = item;
     }
 }
 
@@ -128,14 +141,16 @@ constexpr int kMergeThreads = kMergeKeys * kMergeParts;
 constexpr int kMergePer = 2;
 constexpr int kMergeBlocks = kMergeParts * kMergePer;
 __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__restrict__ key_in,
-                                                            const int32_t *__restrict__ row_in, int32_t n,
-                                                            uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
+                                                            const Item *__restrict__ item_in, int32_t n,
+                                                            uint64_t *__restrict__ key_out, Item *__restrict__ item_out) {
     __shared__ uint64_t keys[kMergeBlocks * kSortBlock];
     __shared__ int32_t counts[kMergeParts][kMergeKeys];
     const int slot = static_cast<int>(threadIdx.x) % kMergeKeys, part = static_cast<int>(threadIdx.x) / kMergeKeys;
     const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeKeys + slot;
     const int own = i / kSortBlock, blocks = static_cast<int>(ceil_div(n, kSortBlock));
     const uint64_t mine = i < n ? key_in[i] : 0;
+    Item item{};
+    if (part == 0 && i < n) item = item_in[i];
     constexpr int kLoads = kMergeBlocks * kSortBlock / kMergeThreads;
     uint64_t next[kLoads];
     auto load = [&](int b0) {
@@ -183,7 +198,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__re
 #pragma unroll
         for (int k = 0; k < kMergeParts; ++k) at += counts[k][slot];
         key_out[at] = mine;
-        row_out[at] = row_in[i];
+        item_out[at] = item;
     }
 }
 
@@ -196,7 +211,8 @@ struct WalkArgs {
     int64_t x_stride;
     const int32_t *targets;
     const float *weights;   // null: ones
-    const int32_t *order;   // sorted place -> row; null: the rows' own order
+    const Item *items;      // the rows sorted; null: in their own order
+    const uint64_t *keys;
     int32_t n;
     float *loss;            // null: not written
     void *dx;               // null: not written
@@ -217,11 +233,10 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
                           : static_cast<int>(blockIdx.x);
     const int pos = group * (kWalkThreads / kWave) + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     if (pos >= a.n) return;
-    const int row = a.order ? a.order[pos] : pos;
-    const int32_t v = a.targets[row];
-    const int len = path_len(a.t, v);
-    const int pt = lane < len ? a.t.points[a.t.point_off[v] + lane] : 0;
-    const uint64_t code = len > 0 ? a.t.code[v] : 0;
+    const Item item = a.items ? a.items[pos] : item_of(a.t, pos, a.targets[pos]);
+    const int row = item.row, len = item.len;
+    const int pt = lane < len ? a.t.points[item.off + lane] : 0;
+    const uint64_t code = len == 0 ? 0 : a.items ? __brevll(a.keys[pos]) : a.t.code[item.word];
     const float weight = GRADS && a.weights ? a.weights[row] : 1.0f;
     const T *xr = static_cast<const T *>(a.x) + row * a.x_stride;
     float x[NE], dx[NE];
@@ -275,7 +290,7 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
         const float p0 = __shfl(prod, 0, kWave), p1 = __shfl(prod, 16, kWave), p2 = __shfl(prod, 32, kWave),
                     p3 = __shfl(prod, 48, kWave);
         const float s = rows_sum(wrong) + logf((p0 * p1) * (p2 * p3));
-        const bool missing = v >= 0 && len == 0;   // a target that the tree does not hold
+        const bool missing = item.word >= 0 && len == 0;   // a target that the tree does not hold
         if (lane == 0) a.loss[row] = missing ? __builtin_nanf("") : s;
     }
     if constexpr (GRADS) {
@@ -304,7 +319,7 @@ struct Borders {
 struct NodeArgs {
     Tree t;
     const uint64_t *keys;
-    const int32_t *order, *targets;
+    const Item *items;
     int32_t n, dim;
     const void *x;
     int64_t x_stride;
@@ -315,84 +330,82 @@ struct NodeArgs {
     float *dsyn1;
     int64_t out_stride;
     int32_t add;        // dsyn1 holds an earlier slab's sums
+    int32_t tiles;      // wavefronts for a row's columns
 };
 
-using f2 = float __attribute__((ext_vector_type(2)));
-
-// C neighbouring columns of a row of dim floats, a multiple of C: zeros past the row, and no store there.
+// A lane's C columns of a row of dim floats, 64 apart from `col` on: zeros past the row, and no store there.
 template <int C>
 __device__ __forceinline__ void load_columns(const float *row, int col, int bytes, float (&v)[C]) {
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(row), 0, bytes, kRawBufferWord3);
-    if constexpr (C == 1) {
-        v[0] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4, 0, 0));
-    } else {
-        // the vector as a whole: a bit cast of one of its elements reads the first
-        const f2 u = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(rs, col * 4, 0, 0));
-        v[0] = u[0];
-        v[1] = u[1];
-    }
-}
-
-template <int C>
-__device__ __forceinline__ void store_columns(float *row, int col, int bytes, const float (&v)[C]) {
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(row, 0, bytes, kRawBufferWord3);
-    if constexpr (C == 1) {
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[0]), rs, col * 4, 0, 0);
-    } else {
-        using u2 = uint32_t __attribute__((ext_vector_type(2)));
-        const f2 u = {v[0], v[1]};
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, u), rs, col * 4, 0, 0);
-    }
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+        v[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4 + e * kWave * 4, 0, 0));
 }
 
 template <int C>
 __device__ __forceinline__ void put_columns(float *row, int col, int bytes, const float (&v)[C], bool add) {
-    if (add) {
-        float old[C];
-        load_columns<C>(row, col, bytes, old);
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(row, 0, bytes, kRawBufferWord3);
+    float sum[C];
 #pragma unroll
-        for (int e = 0; e < C; ++e) old[e] += v[e];
-        store_columns<C>(row, col, bytes, old);
-    } else {
-        store_columns<C>(row, col, bytes, v);
+    for (int e = 0; e < C; ++e) sum[e] = v[e];
+    if (add) {
+#pragma unroll
+        for (int e = 0; e < C; ++e)
+            sum[e] += __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4 + e * kWave * 4, 0, 0));
     }
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, sum[e]), rs, col * 4 + e * kWave * 4, 0, 0);
 }
 
-// A lane holds C columns of RB sorted rows, a wavefront 64 C columns, a workgroup the whole row. What a level's rows need
-// (coefficient, node, where a run that ends with the row goes) is worked out by the row's lane and read from there; the
-// coefficients and nodes of all levels are fetched into LDS first, as a load waits for the stores that went before it.
-// Eight rows inside one run take a multiply-add each; elsewhere a row also takes a branch for whether it has the level
-// and whether its run ends.
+// A wavefront holds RB sorted rows, C columns a lane, and takes every so many of the levels; a workgroup has wavefronts
+// for all columns of the rows and, where there are few rows, for up to kLevelWaves parts of the levels. What bounds it is
+// the instructions around a row's multiply-adds, so a wavefront takes as many columns as its registers hold. What a
+// level's rows need (coefficient, node, where a run that ends with the row goes) is worked out by the row's lane and
+// read from there; the coefficients and nodes of all levels are fetched into LDS first, as a load waits for the stores
+// that went before it. Eight rows inside one run take a multiply-add a column each; elsewhere a row also takes a branch
+// for whether it has the level and whether its run ends.
+constexpr int kLevelWaves = 4;
+constexpr int kNodeWaves = 8;   // of a workgroup: 256 registers a lane
 template <class T, bool COEF, int RB, int C>
-__global__ __launch_bounds__(C == 1 ? 1024 : 512) void k_hs_nodes(NodeArgs a) {
+__global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
     extern __shared__ int32_t level_node[];   // [longest][RB], then the coefficients alike
-    const int lane = lane_id();
+    const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int waves = static_cast<int>(blockDim.x) / kWave, level_step = waves / a.tiles;
     const int blk = static_cast<int>(blockIdx.x), longest = a.t.longest;
-    const int col = static_cast<int>(threadIdx.x) * C;
+    const int col = wid % a.tiles * C * kWave + lane;
     const int p0 = blk * RB, rows = min(RB, a.n - p0);
-    // lane q: row q of the block
+    // lane q: row q of the block and the rows beside it
     const int pos = p0 + lane;
     const bool on = lane < rows;
-    const int row = on ? a.order[pos] : 0;
-    const int32_t v = on ? a.targets[row] : -1;
-    const int len = path_len(a.t, v);
-    auto neighbour = [&](int at) {   // levels that the row at place `at` shares with the one before it
-        const int32_t va = a.targets[a.order[at - 1]], vb = a.targets[a.order[at]];
-        return shared_levels(a.t, va, path_len(a.t, va), a.keys[at - 1], vb, path_len(a.t, vb), a.keys[at]);
-    };
-    const int before = on && pos > 0 ? neighbour(pos) : 0;
-    const int after = on && pos + 1 < a.n ? neighbour(pos + 1) : 0;
+    Item item{0, -1, 0, 0}, last{0, -1, 0, 0}, next{0, -1, 0, 0};
+    uint64_t key = 0, last_key = 0, next_key = 0;
+    if (on) {
+        item = a.items[pos];
+        key = a.keys[pos];
+        if (pos > 0) {
+            last = a.items[pos - 1];
+            last_key = a.keys[pos - 1];
+        }
+        if (pos + 1 < a.n) {
+            next = a.items[pos + 1];
+            next_key = a.keys[pos + 1];
+        }
+    }
+    const int len = item.len;
+    const int before = shared_levels(a.t, last.word, last.len, last_key, item.word, len, key);
+    const int after = shared_levels(a.t, item.word, len, key, next.word, next.len, next_key);
     float x[RB][C];
 #pragma unroll
     for (int q = 0; q < RB; ++q) {
-        const int64_t r = __builtin_amdgcn_readlane(row, q);
+        const int64_t r = __builtin_amdgcn_readlane(item.row, q);
         if constexpr (sizeof(T) == 4) {
             load_columns<C>(static_cast<const float *>(a.x) + r * a.x_stride, col, q < rows ? a.dim * 4 : 0, x[q]);
         } else {
             const T *from = static_cast<const T *>(a.x) + r * a.x_stride;
 #pragma unroll
-            for (int e = 0; e < C; ++e) x[q][e] = 0.0f;
-            if (q < rows && col < a.dim) load_pack<T, C>(from + col, x[q]);
+            for (int e = 0; e < C; ++e)
+                x[q][e] = q < rows && col + e * kWave < a.dim ? static_cast<float>(from[col + e * kWave]) : 0.0f;
         }
     }
     const int left = __builtin_amdgcn_readlane(before, 0);
@@ -410,10 +423,8 @@ __global__ __launch_bounds__(C == 1 ? 1024 : 512) void k_hs_nodes(NodeArgs a) {
     }
     const int cells = longest * RB;
     float *level_coef = reinterpret_cast<float *>(level_node + cells);
-    const int off = len > 0 && a.t.codelen ? a.t.point_off[v] : 0;
-    const int wid = static_cast<int>(threadIdx.x) / kWave, waves = static_cast<int>(blockDim.x) / kWave;
     if (lane < RB) {
-        for (int j = wid; j < deepest; j += waves) level_node[j * RB + lane] = j < len ? (a.t.codelen ? a.t.points[off + j] : v) : 0;
+        for (int j = wid; j < deepest; j += waves) level_node[j * RB + lane] = j < len ? node_of(a.t, item, j) : 0;
     }
     if constexpr (COEF) {
         const float *coef = a.coef + static_cast<int64_t>(blk) * cells;
@@ -422,7 +433,7 @@ __global__ __launch_bounds__(C == 1 ? 1024 : 512) void k_hs_nodes(NodeArgs a) {
     __syncthreads();
     const int bytes = a.dim * 4;
     const uint64_t lower = (1ull << lane) - 1;
-    for (int j = 0; j < deepest; ++j) {
+    for (int j = wid / a.tiles; j < deepest; j += level_step) {
         const int node = level_node[j * RB + lane % RB];
         const float coefs = COEF ? level_coef[j * RB + lane % RB] : 1.0f;
         const uint64_t active = __ballot(len > j);
@@ -435,7 +446,7 @@ __global__ __launch_bounds__(C == 1 ? 1024 : 512) void k_hs_nodes(NodeArgs a) {
                                                                              : a.dsyn1 + node * a.out_stride);
         const int to_lo = static_cast<int>(to), to_hi = static_cast<int>(to >> 32);
         const uint64_t direct = a.add ? ~__ballot(from_left || to_right) : 0;   // rows whose sum is added to dsyn1
-        if (left > j && threadIdx.x == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
+        if (left > j && lane == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
         float acc[C];
 #pragma unroll
         for (int e = 0; e < C; ++e) acc[e] = 0.0f;
@@ -515,39 +526,41 @@ __global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
     bool outside = has_left & 1ull;   // the run at hand began before these blocks
     float acc[1] = {0.0f};
     float *out = a.out + (static_cast<int64_t>(blockIdx.x) * 2 * longest + level) * a.dim;
-    constexpr int kAhead = 16;
-    for (int b0 = 0; b0 < kFan; b0 += kAhead) {
-        if (!(((has_left | has_right) >> b0) & ((1ull << kAhead) - 1))) continue;
-        float l[kAhead][1], r[kAhead][1];
+    // all of them on their way at once; an empty range where there is none, and no sixteen that have none
+    constexpr int kGroup = 16;
+    float l[kFan][1], r[kFan][1];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {   // an empty range where there is none: no branch around the loads
-            const int b = b0 + u;
-            load_columns<1>(in + b * 2 * part, col, (has_left >> b) & 1ull ? bytes : 0, l[u]);
-            load_columns<1>(in + b * 2 * part + part, col, (has_right >> b) & 1ull ? bytes : 0, r[u]);
+    for (int b0 = 0; b0 < kFan; b0 += kGroup) {
+        if (!(((has_left | has_right) >> b0) & ((1ull << kGroup) - 1))) continue;
+#pragma unroll
+        for (int b = b0; b < b0 + kGroup; ++b) {
+            load_columns<1>(in + b * 2 * part, col, (has_left >> b) & 1ull ? bytes : 0, l[b]);
+            load_columns<1>(in + b * 2 * part + part, col, (has_right >> b) & 1ull ? bytes : 0, r[b]);
         }
+    }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int b = b0 + u;
+    for (int b0 = 0; b0 < kFan; b0 += kGroup) {
+        if (!(((has_left | has_right) >> b0) & ((1ull << kGroup) - 1))) continue;
+#pragma unroll
+        for (int b = b0; b < b0 + kGroup; ++b) {
             if ((has_left >> b) & 1ull) {
-                acc[0] += l[u][0];
+                acc[0] += l[b][0];
                 if (!((through >> b) & 1ull)) {
-                    if (outside)
-                        store_columns<1>(out, col, bytes, acc);
-                    else
-                        put_columns<1>(a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride, col, bytes, acc, a.add);
+                    float *to = outside ? out : a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride;
+                    put_columns<1>(to, col, bytes, acc, a.add && !outside);
                     outside = false;
                     acc[0] = 0.0f;
                 }
             }
             if ((has_right >> b) & 1ull) {
-                acc[0] = r[u][0];
+                acc[0] = r[b][0];
                 outside = false;
             }
         }
     }
     // a run that goes on past the last block
     if (((has_right | through) >> (kFan - 1)) & 1ull)
-        store_columns<1>(out + (outside ? 0 : part), col, bytes, acc);
+        put_columns<1>(out + (outside ? 0 : part), col, bytes, acc, false);
 }
 
 // The first dim columns of the rows set to zero, a wavefront a row.
@@ -579,7 +592,7 @@ __global__ __launch_bounds__(kZeroThreads) void k_hs_zero_flat(float *p, int64_t
 
 struct Buffers {
     uint64_t *key0, *key1;
-    int32_t *row0, *row1;
+    Item *item0, *item1;
     float *coef, *part[2];
     int32_t *node[2];
     Borders borders[3];
@@ -596,8 +609,8 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     Buffers b;
     b.key0 = c.take<uint64_t>(n);
     b.key1 = c.take<uint64_t>(n);
-    b.row0 = c.take<int32_t>(n);
-    b.row1 = c.take<int32_t>(n);
+    b.item0 = c.take<Item>(n);
+    b.item1 = c.take<Item>(n);
     b.coef = c.take<float>(blocks * longest * kRows);
     b.part[0] = c.take<float>(blocks * level);
     b.part[1] = c.take<float>(fans * level);
@@ -636,21 +649,21 @@ int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole, h
 }
 
 // Sorts n <= kSlab rows by their targets' keys.
-int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const int32_t **order,
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const Item **items,
               const uint64_t **keys, hipStream_t s) {
     const auto sort_blocks = static_cast<unsigned>(ceil_div(n, kSortBlock));
     if (n <= kRankNarrow)
-        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
+        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.item0);
     else
-        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0);
+        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.item0);
     W2V_LAUNCH_CHECK("k_hs_rank");
-    *order = b.row0;
+    *items = b.item0;
     *keys = b.key0;
     if (n > kSortBlock) {
-        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1,
-                                                                                         b.row1);
+        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.item0, n, b.key1,
+                                                                                         b.item1);
         W2V_LAUNCH_CHECK("k_hs_merge");
-        *order = b.row1;
+        *items = b.item1;
         *keys = b.key1;
     }
     return W2V_OK;
@@ -662,29 +675,42 @@ struct SumShape {
 };
 
 // The sorted rows' sums, into rows of `out` that hold zeros or an earlier slab's sums.
-int sum_rows(const NodeArgs &m, int32_t type, const Buffers &b, hipStream_t s) {
-    const int rb = block_rows(m.n), cols = m.dim > kWave && m.dim % 2 == 0 ? 2 : 1;
+int sum_rows(NodeArgs m, int32_t type, const Buffers &b, hipStream_t s) {
+    const int rb = block_rows(m.n), columns = static_cast<int>(ceil_div(m.dim, kWave));
     const auto blocks = static_cast<int32_t>(ceil_div(m.n, rb));
+    const int per = columns <= 5 ? columns : 4;   // columns of a lane
+    m.tiles = static_cast<int32_t>(ceil_div(columns, per));
+    // the levels shared out while that gives a SIMD no more than four wavefronts
+    const int64_t waves = static_cast<int64_t>(blocks) * m.tiles;
+    const int most = std::min(kLevelWaves, kNodeWaves / m.tiles);
+    const int parts = waves * most <= 16LL * device_cu_count() ? most : 1;
+    const auto threads = static_cast<unsigned>(m.tiles * parts * kWave);
+    const size_t lds = static_cast<size_t>(m.t.longest) * rb * (m.coef ? 8 : 4);
     (void)with_type(type, [&](auto zero) {
         using T = decltype(zero);
-        const auto threads = static_cast<unsigned>(ceil_div(m.dim, kWave * cols) * kWave);
-        const size_t lds = static_cast<size_t>(m.t.longest) * rb * (m.coef ? 8 : 4);
         auto launch = [&](auto shape) {
             constexpr int RB = decltype(shape)::rows, C = decltype(shape)::cols;
             if (m.coef)
                 k_hs_nodes<T, true, RB, C><<<static_cast<unsigned>(blocks), threads, lds, s>>>(m);
-            else
+            else if constexpr (sizeof(T) == 4)
                 k_hs_nodes<T, false, RB, C><<<static_cast<unsigned>(blocks), threads, lds, s>>>(m);
         };
-        if (rb == kRows)
-            cols == 2 ? launch(SumShape<kRows, 2>{}) : launch(SumShape<kRows, 1>{});
-        else
-            cols == 2 ? launch(SumShape<kFewRows, 2>{}) : launch(SumShape<kFewRows, 1>{});
+        auto with_rows = [&](auto cols) {
+            constexpr int C = decltype(cols)::value;
+            rb == kRows ? launch(SumShape<kRows, C>{}) : launch(SumShape<kFewRows, C>{});
+        };
+        switch (per) {
+            case 1: with_rows(std::integral_constant<int, 1>{}); break;
+            case 2: with_rows(std::integral_constant<int, 2>{}); break;
+            case 3: with_rows(std::integral_constant<int, 3>{}); break;
+            case 4: with_rows(std::integral_constant<int, 4>{}); break;
+            default: with_rows(std::integral_constant<int, 5>{}); break;
+        }
         return 0;
     });
     W2V_LAUNCH_CHECK("k_hs_nodes");
     const auto tiles = static_cast<unsigned>(ceil_div(m.dim, kWave));
-    int32_t left = blocks;   // 1,024 at most: two joins
+    int32_t left = blocks;   // 2,048 at most: two joins
     for (int k = 0; k < 2 && left > 1; ++k) {
         const auto fans = static_cast<int32_t>(ceil_div(left, kFan));
         JoinArgs j{m.dim, m.t.longest, b.part[k], b.node[k], b.borders[k], left, b.part[1], b.node[1], b.borders[k + 1],
@@ -717,10 +743,10 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, a.rows - lo));
         const int32_t *targets = a.targets + lo;
         const char *x = static_cast<const char *>(a.x) + lo * a.x_stride * type_bytes(a.type);
-        const int32_t *order = nullptr;
+        const Item *items = nullptr;
         const uint64_t *keys = nullptr;
         if (a.dsyn1)
-            if (int rc = sort_rows(t, targets, n, b, &order, &keys, s)) return rc;
+            if (int rc = sort_rows(t, targets, n, b, &items, &keys, s)) return rc;
         WalkArgs w{};
         w.t = t;
         w.syn1 = a.syn1;
@@ -730,7 +756,8 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         w.x_stride = a.x_stride;
         w.targets = targets;
         w.weights = a.weights ? a.weights + lo : nullptr;
-        w.order = order;
+        w.items = items;
+        w.keys = keys;
         w.n = n;
         w.loss = a.loss ? a.loss + lo : nullptr;
         w.dx = a.dx ? static_cast<char *>(a.dx) + lo * a.dx_stride * type_bytes(a.type) : nullptr;
@@ -751,8 +778,8 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         });
         W2V_LAUNCH_CHECK("k_hs_walk");
         if (!a.dsyn1) continue;
-        const NodeArgs m{t, keys, order, targets, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.node[0], b.borders[0],
-                         a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0};
+        const NodeArgs m{t, keys, items, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.node[0], b.borders[0],
+                         a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0, 1};
         if (int rc = sum_rows(m, a.type, b, s)) return rc;
     }
     return W2V_OK;
@@ -772,11 +799,11 @@ int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t di
     if (int rc = zero_rows(out, V, dim, out_stride, true, s)) return rc;
     for (int64_t lo = 0; lo < rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, rows - lo));
-        const int32_t *order = nullptr;
+        const Item *items = nullptr;
         const uint64_t *keys = nullptr;
-        if (int rc = sort_rows(t, words + lo, n, b, &order, &keys, s)) return rc;
-        const NodeArgs m{t, keys, order, words + lo, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
-                         b.node[0], b.borders[0], out, out_stride, lo > 0 ? 1 : 0};
+        if (int rc = sort_rows(t, words + lo, n, b, &items, &keys, s)) return rc;
+        const NodeArgs m{t, keys, items, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
+                         b.node[0], b.borders[0], out, out_stride, lo > 0 ? 1 : 0, 1};
         if (int rc = sum_rows(m, W2V_F32, b, s)) return rc;
     }
     return W2V_OK;
