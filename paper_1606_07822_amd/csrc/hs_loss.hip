@@ -84,7 +84,8 @@ constexpr int kRankThreads = 1024;
 constexpr int kRankWaves = kRankThreads / kWave;
 template <int R>
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
-                                                          uint64_t *__restrict__ key_out, Item *__restrict__ item_out) {
+                                                          uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out,
+                                                          Item *__restrict__ item_out) {
     __shared__ uint64_t keys[kSortBlock];
     __shared__ int32_t counts[kRankWaves][R];
     constexpr int kGroups = kSortBlock / R, kSets = R / kWave;
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
     if (own >= len) return;
     const int i = static_cast<int>(threadIdx.x);
     Item item{};
-    if (i < R && own + i < len) item = item_of(t, lo + own + i, targets[lo + own + i]);
+    if (item_out && i < R && own + i < len) item = item_of(t, lo + own + i, targets[lo + own + i]);
     for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key(t, targets[lo + i]) : ~0ull;
     __syncthreads();
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -127,7 +128,10 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
 #pragma unroll
         for (int w = 0; w < kRankWaves; ++w) at += counts[w][i];
         key_out[at] = keys[own + i];
-        item_out[at] = item;
+        if (item_out)
+            item_out[at] = item;
+        else
+            row_out[at] = lo + own + i;
     }
 }
 
@@ -141,16 +145,15 @@ constexpr int kMergeThreads = kMergeKeys * kMergeParts;
 constexpr int kMergePer = 2;
 constexpr int kMergeBlocks = kMergeParts * kMergePer;
 __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__restrict__ key_in,
-                                                            const Item *__restrict__ item_in, int32_t n,
-                                                            uint64_t *__restrict__ key_out, Item *__restrict__ item_out) {
+                                                            const int32_t *__restrict__ row_in, int32_t n,
+                                                            uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
     __shared__ uint64_t keys[kMergeBlocks * kSortBlock];
     __shared__ int32_t counts[kMergeParts][kMergeKeys];
     const int slot = static_cast<int>(threadIdx.x) % kMergeKeys, part = static_cast<int>(threadIdx.x) / kMergeKeys;
     const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeKeys + slot;
     const int own = i / kSortBlock, blocks = static_cast<int>(ceil_div(n, kSortBlock));
     const uint64_t mine = i < n ? key_in[i] : 0;
-    Item item{};
-    if (part == 0 && i < n) item = item_in[i];
+    const int32_t row = part == 0 && i < n ? row_in[i] : 0;
     constexpr int kLoads = kMergeBlocks * kSortBlock / kMergeThreads;
     uint64_t next[kLoads];
     auto load = [&](int b0) {
@@ -198,7 +201,45 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__re
 #pragma unroll
         for (int k = 0; k < kMergeParts; ++k) at += counts[k][slot];
         key_out[at] = mine;
-        item_out[at] = item;
+        row_out[at] = row;
+    }
+}
+
+// The sorted rows' items. (Written by the merge itself, 16 bytes apart from each other, they cost it 14 us more at
+// 65,536 rows: the lines are then shared between the XCDs' caches.)
+__global__ __launch_bounds__(256) void k_hs_items(Tree t, const int32_t *__restrict__ targets,
+                                                  const int32_t *__restrict__ rows, int32_t n, Item *__restrict__ items) {
+    const int32_t i = static_cast<int32_t>(blockIdx.x) * 256 + static_cast<int32_t>(threadIdx.x);
+    if (i >= n) return;
+    const int32_t row = rows[i];
+    items[i] = item_of(t, row, targets[row]);
+}
+
+// A lane's C columns of a row of `bytes` bytes, 64 apart from `col` on: zeros past the row, and no store there.
+template <int C, class T>
+__device__ __forceinline__ void load_columns(const T *row, int col, int bytes, float (&v)[C]) {
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(row), 0, bytes, kRawBufferWord3);
+    const int at = col * static_cast<int>(sizeof(T));
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+        if constexpr (sizeof(T) == 4)
+            v[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, at + e * kWave * 4, 0, 0));
+        else
+            v[e] = static_cast<float>(__builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(rs, at + e * kWave * 2, 0, 0)));
+    }
+}
+
+template <int C, class T>
+__device__ __forceinline__ void store_columns(T *row, int col, int bytes, const float (&v)[C]) {
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(row, 0, bytes, kRawBufferWord3);
+    const int at = col * static_cast<int>(sizeof(T));
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+        if constexpr (sizeof(T) == 4)
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[e]), rs, at + e * kWave * 4, 0, 0);
+        else
+            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, static_cast<T>(v[e])), rs, at + e * kWave * 2,
+                                                  0, 0);
     }
 }
 
@@ -223,88 +264,179 @@ struct WalkArgs {
 
 constexpr int kWalkThreads = 256;
 
-template <class T, int NE, bool GRADS>
+// What a node adds for s z (sz) at the lane: e = exp(-|z|) into the product of 1 + e, whose logarithm is the path's sum
+// of log(1 + e) (at most 2^64), and the rest of the loss; the value is sigmoid(-s z).
+__device__ __forceinline__ float node_terms(float sz, bool in, float &prod, float &wrong) {
+    const float e = in ? __expf(-fabsf(sz)) : 0.0f;
+    const float one = 1.0f + e;
+    prod *= one;
+    wrong += in && sz < 0.0f ? -sz : 0.0f;
+    return (sz < 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(one);
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
+// Product over the four rows of 16 lanes, lane by lane.
+__device__ __forceinline__ float rows_product(float v) {
+    float a = v, b = v;
+    swap16(a, b);
+    v = a * b;
+    a = v;
+    b = v;
+    swap32(a, b);
+    return a * b;
+}
+
+// A wavefront's stretch of the sorted rows: neighbouring ones share most of their path, so each XCD, with an L2 of its
+// own, takes one stretch of workgroups.
+__device__ __forceinline__ int walk_wave() {
+    const int per = static_cast<int>(gridDim.x) / kXcds, b = static_cast<int>(blockIdx.x);
+    const int group = b < per * kXcds ? b % kXcds * per + b / kXcds : b;
+    return group * (kWalkThreads / kWave) + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+}
+
+// R rows a wavefront, 1 or 4 (sorted ones). The levels that all four share are walked once for the four: a node's row
+// is loaded once, its four products are reduced together, and row r's terms are worked out in the r-th sixteen lanes.
+// Then each row's own levels follow, four at a time. The next four nodes are on their way meanwhile.
+template <class T, int NE, bool GRADS, int R>
 __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
-    const int lane = lane_id();
-    // neighbouring sorted rows share most of their path: each XCD, with an L2 of its own, takes one stretch of them
-    const int per = static_cast<int>(gridDim.x) / kXcds;
-    const int group = static_cast<int>(blockIdx.x) < per * kXcds
-                          ? static_cast<int>(blockIdx.x) % kXcds * per + static_cast<int>(blockIdx.x) / kXcds
-                          : static_cast<int>(blockIdx.x);
-    const int pos = group * (kWalkThreads / kWave) + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
-    if (pos >= a.n) return;
-    const Item item = a.items ? a.items[pos] : item_of(a.t, pos, a.targets[pos]);
-    const int row = item.row, len = item.len;
-    const int pt = lane < len ? a.t.points[item.off + lane] : 0;
-    const uint64_t code = len == 0 ? 0 : a.items ? __brevll(a.keys[pos]) : a.t.code[item.word];
-    const float weight = GRADS && a.weights ? a.weights[row] : 1.0f;
-    const T *xr = static_cast<const T *>(a.x) + row * a.x_stride;
-    float x[NE], dx[NE];
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-        const int col = lane + i * kWave;
-        x[i] = len > 0 && col < a.dim ? static_cast<float>(xr[col]) : 0.0f;
-        dx[i] = 0.0f;
+    const int lane = lane_id(), quarter = lane >> 4;
+    const int pos0 = walk_wave() * R;
+    if (pos0 >= a.n) return;
+    const int pos = pos0 + (R == 4 ? quarter : 0);   // the row that a lane loads for
+    Item item{0, -1, 0, 0};
+    uint64_t key = 0;
+    if (pos < a.n) {
+        item = a.items ? a.items[pos] : item_of(a.t, pos, a.targets[pos]);
+        key = item.len == 0 ? 0 : a.items ? a.keys[pos] : __brevll(a.t.code[item.word]);
     }
-    float y[4][NE];
-    auto load = [&](int j) {
+    const uint64_t code = __brevll(key);
+    const float weight = GRADS && a.weights && pos < a.n ? a.weights[item.row] : 1.0f;
+    int len[R], row[R], pt[R];
+    float x[R][NE], dx[R][NE];
+    const int x_bytes = a.dim * static_cast<int>(sizeof(T));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {   // zeros past the path's end
-            const bool in = j + u < len;
-            const int node = __builtin_amdgcn_readlane(pt, min(j + u, kWave - 1));
-            buf_load_row<NE>(y[u], row_rsrc(const_cast<float *>(a.syn1), in ? node : 0, a.stride, in ? a.dim * 4 : 0), lane);
+    for (int r = 0; r < R; ++r) {
+        len[r] = __builtin_amdgcn_readlane(item.len, 16 * r);
+        row[r] = __builtin_amdgcn_readlane(item.row, 16 * r);
+        const int off = __builtin_amdgcn_readlane(item.off, 16 * r);
+        pt[r] = lane < len[r] ? a.t.points[off + lane] : 0;
+        load_columns<NE>(static_cast<const T *>(a.x) + row[r] * a.x_stride, lane, len[r] > 0 ? x_bytes : 0, x[r]);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) dx[r][i] = 0.0f;
+    }
+    int shared = 0;
+    if constexpr (R == 4) {
+        auto word64 = [&](int l) {
+            return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key >> 32), l))) << 32 |
+                   static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), l));
+        };
+        shared = shared_levels(a.t, __builtin_amdgcn_readlane(item.word, 0), len[0], word64(0),
+                               __builtin_amdgcn_readlane(item.word, 48), len[R - 1], word64(48));
+    }
+    float y[4][NE], now[4][NE];
+    const int bytes = a.dim * 4;
+    auto load = [&](int r, int j, int end) {   // zeros past the end
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool in = j + u < end;
+            const int node = __builtin_amdgcn_readlane(pt[r], min(j + u, kWave - 1));
+            load_columns<NE>(a.syn1 + static_cast<int64_t>(in ? node : 0) * a.stride, lane, in ? bytes : 0, y[u]);
         }
     };
-    load(0);
-    // log(1 + e) of a path's nodes as the logarithm of their product, at most 2^64
-    float wrong = 0.0f, prod = 1.0f, g_all = 0.0f;
-    for (int j = 0; j < len; j += 4) {
-        float now[4][NE];
+    auto take = [&] {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int i = 0; i < NE; ++i) now[u][i] = y[u][i];
-        load(j + 4);
-        const float z = reduce4(dot_partial<NE>(x, now[0]), dot_partial<NE>(x, now[1]), dot_partial<NE>(x, now[2]),
-                                dot_partial<NE>(x, now[3]));   // lanes 16u..16u+15: node j + u
-        const int level = j + (lane >> 4);
-        const bool in = level < len;
-        const float sz = (code >> min(level, 63)) & 1ull ? -z : z;
-        const float e = in ? __expf(-fabsf(z)) : 0.0f;
-        prod *= 1.0f + e;
-        wrong += in && sz < 0.0f ? -sz : 0.0f;
-        if constexpr (GRADS) {
-            const float f = (sz < 0.0f ? 1.0f : e) / (1.0f + e);   // sigmoid(-s z)
-            const float g = in ? (((code >> min(level, 63)) & 1ull) ? f : -f) * weight : 0.0f;
+    };
+    float wrong = 0.0f, prod = 1.0f;   // a lane's: of its row's shared levels, later of all its row's
+    float g_all[R];                    // lane j: a row's coefficient at level j
+#pragma unroll
+    for (int r = 0; r < R; ++r) g_all[r] = 0.0f;
+    if constexpr (R == 4) {
+        load(0, 0, shared > 0 ? shared : len[0]);
+        for (int j = 0; j < shared; j += 4) {
+            take();
+            if (j + 4 < shared)
+                load(0, j + 4, shared);
+            else
+                load(0, shared, len[0]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float gu = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, g), 16 * u));
+                if (j + u >= shared) break;
+                const float z = reduce4(dot_partial<NE>(x[0], now[u]), dot_partial<NE>(x[R / 4], now[u]),
+                                        dot_partial<NE>(x[R / 2], now[u]), dot_partial<NE>(x[R - 1], now[u]));
+                const bool turn = (code >> (j + u)) & 1ull;
+                const float f = node_terms(turn ? -z : z, true, prod, wrong);
+                if constexpr (GRADS) {
+                    const float g = (turn ? f : -f) * weight;
 #pragma unroll
-                for (int i = 0; i < NE; ++i) dx[i] = fmaf(gu, now[u][i], dx[i]);
-                if (lane == j + u) g_all = gu;
+                    for (int r = 0; r < R; ++r) {
+                        const float gr = lane_value(g, 16 * r);
+#pragma unroll
+                        for (int i = 0; i < NE; ++i) dx[r][i] = fmaf(gr, now[u][i], dx[r][i]);
+                        if (lane == j + u) g_all[r] = gr;
+                    }
+                }
             }
         }
+    } else {
+        load(0, 0, len[0]);
     }
-    if (a.loss) {
-        // a row of lanes holds every fourth node's sums
-        const float p0 = __shfl(prod, 0, kWave), p1 = __shfl(prod, 16, kWave), p2 = __shfl(prod, 32, kWave),
-                    p3 = __shfl(prod, 48, kWave);
-        const float s = rows_sum(wrong) + logf((p0 * p1) * (p2 * p3));
-        const bool missing = item.word >= 0 && len == 0;   // a target that the tree does not hold
-        if (lane == 0) a.loss[row] = missing ? __builtin_nanf("") : s;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint64_t turns = static_cast<uint64_t>(static_cast<uint32_t>(
+                                   __builtin_amdgcn_readlane(static_cast<int>(code >> 32), 16 * r))) << 32 |
+                               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(code), 16 * r));
+        const float w = lane_value(weight, 16 * r);
+        float row_wrong = 0.0f, row_prod = 1.0f;
+        if (r + 1 < R && len[r] <= shared) load(r + 1 < R ? r + 1 : r, shared, len[r + 1 < R ? r + 1 : r]);
+        for (int j = shared; j < len[r]; j += 4) {
+            take();
+            if (j + 4 < len[r])
+                load(r, j + 4, len[r]);
+            else if (r + 1 < R)
+                load(r + 1 < R ? r + 1 : r, shared, len[r + 1 < R ? r + 1 : r]);
+            const float z = reduce4(dot_partial<NE>(x[r], now[0]), dot_partial<NE>(x[r], now[1]),
+                                    dot_partial<NE>(x[r], now[2]), dot_partial<NE>(x[r], now[3]));   // lanes 16u..: node j + u
+            const int level = j + quarter;
+            const bool in = level < len[r], turn = (turns >> min(level, 63)) & 1ull;
+            const float f = node_terms(turn ? -z : z, in, row_prod, row_wrong);
+            if constexpr (GRADS) {
+                const float g = in ? (turn ? f : -f) * w : 0.0f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float gu = lane_value(g, 16 * u);
+#pragma unroll
+                    for (int i = 0; i < NE; ++i) dx[r][i] = fmaf(gu, now[u][i], dx[r][i]);
+                    if (lane == j + u) g_all[r] = gu;
+                }
+            }
+        }
+        row_wrong = rows_sum(row_wrong);
+        row_prod = rows_product(row_prod);
+        if (R == 1 || quarter == r) {
+            wrong += row_wrong;
+            prod *= row_prod;
+        }
+    }
+    if (a.loss && (lane & 15) == 0 && quarter < R && pos < a.n) {
+        const bool missing = item.word >= 0 && item.len == 0;   // a target that the tree does not hold
+        a.loss[item.row] = missing ? __builtin_nanf("") : wrong + logf(prod);
     }
     if constexpr (GRADS) {
         if (a.dx) {
-            T *out = static_cast<T *>(a.dx) + row * a.dx_stride;
 #pragma unroll
-            for (int i = 0; i < NE; ++i) {
-                const int col = lane + i * kWave;
-                if (col < a.dim) out[col] = static_cast<T>(dx[i]);
-            }
+            for (int r = 0; r < R; ++r)
+                if (pos0 + r < a.n) store_columns<NE>(static_cast<T *>(a.dx) + row[r] * a.dx_stride, lane, x_bytes, dx[r]);
         }
         if (a.coef && lane < a.t.longest) {
-            float *c = a.coef + static_cast<int64_t>(pos / a.block_rows) * a.t.longest * a.block_rows;
-            c[lane * a.block_rows + pos % a.block_rows] = g_all;
+            float *c = a.coef + (static_cast<int64_t>(pos0 / a.block_rows) * a.t.longest + lane) * a.block_rows +
+                       pos0 % a.block_rows;
+            store_pack<float, R>(c, g_all);   // a block's rows are a multiple of four
         }
     }
 }
@@ -333,29 +465,18 @@ struct NodeArgs {
     int32_t tiles;      // wavefronts for a row's columns
 };
 
-// A lane's C columns of a row of dim floats, 64 apart from `col` on: zeros past the row, and no store there.
-template <int C>
-__device__ __forceinline__ void load_columns(const float *row, int col, int bytes, float (&v)[C]) {
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(row), 0, bytes, kRawBufferWord3);
-#pragma unroll
-    for (int e = 0; e < C; ++e)
-        v[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4 + e * kWave * 4, 0, 0));
-}
-
+// Stores a sum, or adds it to what an earlier slab left.
 template <int C>
 __device__ __forceinline__ void put_columns(float *row, int col, int bytes, const float (&v)[C], bool add) {
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(row, 0, bytes, kRawBufferWord3);
-    float sum[C];
-#pragma unroll
-    for (int e = 0; e < C; ++e) sum[e] = v[e];
     if (add) {
+        float sum[C];
+        load_columns<C>(row, col, bytes, sum);
 #pragma unroll
-        for (int e = 0; e < C; ++e)
-            sum[e] += __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, col * 4 + e * kWave * 4, 0, 0));
+        for (int e = 0; e < C; ++e) sum[e] += v[e];
+        store_columns<C>(row, col, bytes, sum);
+    } else {
+        store_columns<C>(row, col, bytes, v);
     }
-#pragma unroll
-    for (int e = 0; e < C; ++e)
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, sum[e]), rs, col * 4 + e * kWave * 4, 0, 0);
 }
 
 // A wavefront holds RB sorted rows, C columns a lane, and takes every so many of the levels; a workgroup has wavefronts
@@ -399,14 +520,8 @@ __global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
 #pragma unroll
     for (int q = 0; q < RB; ++q) {
         const int64_t r = __builtin_amdgcn_readlane(item.row, q);
-        if constexpr (sizeof(T) == 4) {
-            load_columns<C>(static_cast<const float *>(a.x) + r * a.x_stride, col, q < rows ? a.dim * 4 : 0, x[q]);
-        } else {
-            const T *from = static_cast<const T *>(a.x) + r * a.x_stride;
-#pragma unroll
-            for (int e = 0; e < C; ++e)
-                x[q][e] = q < rows && col + e * kWave < a.dim ? static_cast<float>(from[col + e * kWave]) : 0.0f;
-        }
+        load_columns<C>(static_cast<const T *>(a.x) + r * a.x_stride, col, q < rows ? a.dim * static_cast<int>(sizeof(T)) : 0,
+                        x[q]);
     }
     const int left = __builtin_amdgcn_readlane(before, 0);
     const int right = __builtin_amdgcn_readlane(after, RB - 1);
@@ -592,7 +707,8 @@ __global__ __launch_bounds__(kZeroThreads) void k_hs_zero_flat(float *p, int64_t
 
 struct Buffers {
     uint64_t *key0, *key1;
-    Item *item0, *item1;
+    int32_t *row0, *row1;
+    Item *items;
     float *coef, *part[2];
     int32_t *node[2];
     Borders borders[3];
@@ -609,8 +725,9 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     Buffers b;
     b.key0 = c.take<uint64_t>(n);
     b.key1 = c.take<uint64_t>(n);
-    b.item0 = c.take<Item>(n);
-    b.item1 = c.take<Item>(n);
+    b.row0 = c.take<int32_t>(n);
+    b.row1 = c.take<int32_t>(n);
+    b.items = c.take<Item>(n);
     b.coef = c.take<float>(blocks * longest * kRows);
     b.part[0] = c.take<float>(blocks * level);
     b.part[1] = c.take<float>(fans * level);
@@ -624,12 +741,23 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     return b;
 }
 
+// Four rows a wavefront from here on: fewer take longer one after the other than the loads they share save.
+constexpr int kWalkFour = 8192;
+
 template <class T, int NE>
-void launch_walk(const WalkArgs &w, bool grads, unsigned grid, hipStream_t s) {
+void launch_walk(const WalkArgs &w, bool grads, hipStream_t s) {
+    constexpr int kWaves = kWalkThreads / kWave;
+    const auto grid = static_cast<unsigned>(ceil_div(w.n, kWaves));
+    if constexpr (NE <= 8) {   // registers for four rows
+        if (grads && w.items && w.n >= kWalkFour) {
+            k_hs_walk<T, NE, true, 4><<<static_cast<unsigned>(ceil_div(w.n, 4 * kWaves)), kWalkThreads, 0, s>>>(w);
+            return;
+        }
+    }
     if (grads)
-        k_hs_walk<T, NE, true><<<grid, kWalkThreads, 0, s>>>(w);
+        k_hs_walk<T, NE, true, 1><<<grid, kWalkThreads, 0, s>>>(w);
     else
-        k_hs_walk<T, NE, false><<<grid, kWalkThreads, 0, s>>>(w);
+        k_hs_walk<T, NE, false, 1><<<grid, kWalkThreads, 0, s>>>(w);
 }
 
 // whole: the rows' padding may be written too. Rows that end inside a 128-byte line cost memory a read for the rest of
@@ -652,20 +780,20 @@ int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole, h
 int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const Item **items,
               const uint64_t **keys, hipStream_t s) {
     const auto sort_blocks = static_cast<unsigned>(ceil_div(n, kSortBlock));
+    Item *now = n <= kSortBlock ? b.items : nullptr;
     if (n <= kRankNarrow)
-        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.item0);
+        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0, now);
     else
-        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.item0);
+        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0, now);
     W2V_LAUNCH_CHECK("k_hs_rank");
-    *items = b.item0;
+    *items = b.items;
     *keys = b.key0;
-    if (n > kSortBlock) {
-        k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.item0, n, b.key1,
-                                                                                         b.item1);
-        W2V_LAUNCH_CHECK("k_hs_merge");
-        *items = b.item1;
-        *keys = b.key1;
-    }
+    if (now) return W2V_OK;
+    k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1, b.row1);
+    W2V_LAUNCH_CHECK("k_hs_merge");
+    k_hs_items<<<static_cast<unsigned>(ceil_div(n, 256)), 256, 0, s>>>(t, targets, b.row1, n, b.items);
+    W2V_LAUNCH_CHECK("k_hs_items");
+    *keys = b.key1;
     return W2V_OK;
 }
 
@@ -764,16 +892,15 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         w.dx_stride = a.dx_stride;
         w.coef = a.dsyn1 ? b.coef : nullptr;
         w.block_rows = block_rows(n);
-        const auto grid = static_cast<unsigned>(ceil_div(n, kWalkThreads / kWave));
         const int ne = static_cast<int>(ceil_div(a.dim, kWave));
         (void)with_type(a.type, [&](auto zero) {
             using T = decltype(zero);
-            if (ne <= 1) launch_walk<T, 1>(w, grads, grid, s);
-            else if (ne <= 2) launch_walk<T, 2>(w, grads, grid, s);
-            else if (ne <= 4) launch_walk<T, 4>(w, grads, grid, s);
-            else if (ne <= 5) launch_walk<T, 5>(w, grads, grid, s);
-            else if (ne <= 8) launch_walk<T, 8>(w, grads, grid, s);
-            else launch_walk<T, 16>(w, grads, grid, s);
+            if (ne <= 1) launch_walk<T, 1>(w, grads, s);
+            else if (ne <= 2) launch_walk<T, 2>(w, grads, s);
+            else if (ne <= 4) launch_walk<T, 4>(w, grads, s);
+            else if (ne <= 5) launch_walk<T, 5>(w, grads, s);
+            else if (ne <= 8) launch_walk<T, 8>(w, grads, s);
+            else launch_walk<T, 16>(w, grads, s);
             return 0;
         });
         W2V_LAUNCH_CHECK("k_hs_walk");
