@@ -46,34 +46,42 @@ __device__ __forceinline__ int path_len(const Tree &t, int32_t v) {
     return len <= t.longest ? len : 0;
 }
 
-// The code with its first turn in the top bit; rows without a path come last.
-__device__ __forceinline__ uint64_t sort_key(const Tree &t, int32_t v) {
-    const int len = path_len(t, v);
-    if (len == 0) return ~0ull;
-    return t.codelen ? __brevll(t.code[v]) & (~0ull << (64 - len)) : static_cast<uint64_t>(v);
-}
-
-// Levels that two neighbouring sorted rows share an inner node at.
-__device__ __forceinline__ int shared_levels(const Tree &t, int32_t va, int la, uint64_t ka, int32_t vb, int lb,
-                                             uint64_t kb) {
-    if (la == 0 || lb == 0) return 0;
-    if (va == vb) return la;
-    return t.codelen ? min(min(la, lb), static_cast<int>(__clzll(static_cast<long long>(ka ^ kb))) + 1) : 0;
-}
-
 // ------------------------------------------------------------------ order
-// A sorted row: its place in the batch, its target, and the length and the place of that word's path.
+// A row of the batch, its target and what is needed of that word's path.
 struct Item {
     int32_t row, word, off, len;
+    uint64_t code;
 };
 
 __device__ __forceinline__ Item item_of(const Tree &t, int32_t row, int32_t word) {
     const int len = path_len(t, word);
-    return Item{row, word, len > 0 && t.codelen ? t.point_off[word] : 0, len};
+    Item i{row, word, 0, len, 0};
+    if (len > 0 && t.codelen) {
+        i.off = t.point_off[word];
+        i.code = t.code[word];
+    }
+    return i;
 }
 
 __device__ __forceinline__ int node_of(const Tree &t, const Item &i, int level) {   // of a path that long
     return t.codelen ? t.points[i.off + level] : i.word;
+}
+
+// Levels that two neighbouring sorted rows share an inner node at.
+__device__ __forceinline__ int shared_levels(const Tree &t, const Item &a, const Item &b) {
+    if (a.len == 0 || b.len == 0) return 0;
+    if (a.word == b.word) return a.len;
+    return t.codelen ? min(min(a.len, b.len), static_cast<int>(__ffsll(static_cast<long long>(a.code ^ b.code)))) : 0;
+}
+
+// What the rows are sorted by: the code with its first turn in the top bit, and after all of them the rows without a
+// path. 32 bits do where no code is longer than 31 (so that none is all ones), and cost half as much to compare.
+template <class K>
+__device__ __forceinline__ K sort_key(const Tree &t, int32_t v) {
+    const int len = path_len(t, v);
+    if (len == 0) return static_cast<K>(~0ull);
+    if (!t.codelen) return static_cast<K>(v);
+    return static_cast<K>((__brevll(t.code[v]) & (~0ull << (64 - len))) >> (64 - 8 * sizeof(K)));
 }
 
 // Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order).
@@ -82,11 +90,11 @@ __device__ __forceinline__ int node_of(const Tree &t, const Item &i, int level) 
 // pair of the same 64 compares the places as well.
 constexpr int kRankThreads = 1024;
 constexpr int kRankWaves = kRankThreads / kWave;
-template <int R>
+template <class K, int R>
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
-                                                          uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out,
+                                                          K *__restrict__ key_out, int32_t *__restrict__ row_out,
                                                           Item *__restrict__ item_out) {
-    __shared__ uint64_t keys[kSortBlock];
+    __shared__ __align__(16) K keys[kSortBlock];
     __shared__ int32_t counts[kRankWaves][R];
     constexpr int kGroups = kSortBlock / R, kSets = R / kWave;
     const int32_t lo = static_cast<int32_t>(blockIdx.x) / kGroups * kSortBlock;
@@ -96,18 +104,18 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
     const int i = static_cast<int>(threadIdx.x);
     Item item{};
     if (item_out && i < R && own + i < len) item = item_of(t, lo + own + i, targets[lo + own + i]);
-    for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key(t, targets[lo + i]) : ~0ull;
+    for (int i = threadIdx.x; i < kSortBlock; i += kRankThreads) keys[i] = i < len ? sort_key<K>(t, targets[lo + i]) : static_cast<K>(~0ull);
     __syncthreads();
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     int32_t c[kSets];
 #pragma unroll
     for (int r = 0; r < kSets; ++r) c[r] = 0;
     for (int seg = wid; seg * kWave < len; seg += kRankWaves) {   // keys past the end are the largest: they count for none
-        const uint64_t *k = keys + seg * kWave;
+        const K *k = keys + seg * kWave;
 #pragma unroll
         for (int r = 0; r < kSets; ++r) {
             const int mine_seg = own / kWave + r;
-            const uint64_t mine = keys[mine_seg * kWave + lane];
+            const K mine = keys[mine_seg * kWave + lane];
             if (seg < mine_seg) {
 #pragma unroll 16
                 for (int j = 0; j < kWave; ++j) c[r] += k[j] <= mine ? 1 : 0;
@@ -127,11 +135,12 @@ __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t 
         int32_t at = lo;
 #pragma unroll
         for (int w = 0; w < kRankWaves; ++w) at += counts[w][i];
-        key_out[at] = keys[own + i];
-        if (item_out)
+        if (item_out) {
             item_out[at] = item;
-        else
+        } else {
+            key_out[at] = keys[own + i];
             row_out[at] = lo + own + i;
+        }
     }
 }
 
@@ -144,23 +153,24 @@ constexpr int kMergeParts = 4;
 constexpr int kMergeThreads = kMergeKeys * kMergeParts;
 constexpr int kMergePer = 2;
 constexpr int kMergeBlocks = kMergeParts * kMergePer;
-__global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__restrict__ key_in,
+template <class K>
+__global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict__ key_in,
                                                             const int32_t *__restrict__ row_in, int32_t n,
-                                                            uint64_t *__restrict__ key_out, int32_t *__restrict__ row_out) {
-    __shared__ uint64_t keys[kMergeBlocks * kSortBlock];
+                                                            int32_t *__restrict__ row_out) {
+    __shared__ K keys[kMergeBlocks * kSortBlock];
     __shared__ int32_t counts[kMergeParts][kMergeKeys];
     const int slot = static_cast<int>(threadIdx.x) % kMergeKeys, part = static_cast<int>(threadIdx.x) / kMergeKeys;
     const int32_t i = static_cast<int32_t>(blockIdx.x) * kMergeKeys + slot;
     const int own = i / kSortBlock, blocks = static_cast<int>(ceil_div(n, kSortBlock));
-    const uint64_t mine = i < n ? key_in[i] : 0;
+    const K mine = i < n ? key_in[i] : 0;
     const int32_t row = part == 0 && i < n ? row_in[i] : 0;
     constexpr int kLoads = kMergeBlocks * kSortBlock / kMergeThreads;
-    uint64_t next[kLoads];
+    K next[kLoads];
     auto load = [&](int b0) {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int32_t k = b0 * kSortBlock + u * kMergeThreads + static_cast<int32_t>(threadIdx.x);
-            next[u] = k < n ? key_in[k] : ~0ull;   // past the end: after every key
+            next[u] = k < n ? key_in[k] : static_cast<K>(~0ull);   // past the end: after every key
         }
     };
     load(0);
@@ -180,7 +190,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__re
         }
 #pragma unroll
         for (int step = kSortBlock; step > 0; step >>= 1) {
-            uint64_t k[kMergePer];
+            K k[kMergePer];
 #pragma unroll
             for (int u = 0; u < kMergePer; ++u)
                 k[u] = keys[(mine0 + u) * kSortBlock + min(lo[u] + step, kSortBlock) - 1];
@@ -200,12 +210,11 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const uint64_t *__re
         at = i % kSortBlock;
 #pragma unroll
         for (int k = 0; k < kMergeParts; ++k) at += counts[k][slot];
-        key_out[at] = mine;
         row_out[at] = row;
     }
 }
 
-// The sorted rows' items. (Written by the merge itself, 16 bytes apart from each other, they cost it 14 us more at
+// The sorted rows' items. (Written by the merge itself, they cost it 14 us more at
 // 65,536 rows: the lines are then shared between the XCDs' caches.)
 __global__ __launch_bounds__(256) void k_hs_items(Tree t, const int32_t *__restrict__ targets,
                                                   const int32_t *__restrict__ rows, int32_t n, Item *__restrict__ items) {
@@ -253,7 +262,6 @@ struct WalkArgs {
     const int32_t *targets;
     const float *weights;   // null: ones
     const Item *items;      // the rows sorted; null: in their own order
-    const uint64_t *keys;
     int32_t n;
     float *loss;            // null: not written
     void *dx;               // null: not written
@@ -306,13 +314,9 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
     const int pos0 = walk_wave() * R;
     if (pos0 >= a.n) return;
     const int pos = pos0 + (R == 4 ? quarter : 0);   // the row that a lane loads for
-    Item item{0, -1, 0, 0};
-    uint64_t key = 0;
-    if (pos < a.n) {
-        item = a.items ? a.items[pos] : item_of(a.t, pos, a.targets[pos]);
-        key = item.len == 0 ? 0 : a.items ? a.keys[pos] : __brevll(a.t.code[item.word]);
-    }
-    const uint64_t code = __brevll(key);
+    Item item{0, -1, 0, 0, 0};
+    if (pos < a.n) item = a.items ? a.items[pos] : item_of(a.t, pos, a.targets[pos]);
+    const uint64_t code = item.code;
     const float weight = GRADS && a.weights && pos < a.n ? a.weights[item.row] : 1.0f;
     int len[R], row[R], pt[R];
     float x[R][NE], dx[R][NE];
@@ -329,12 +333,12 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
     }
     int shared = 0;
     if constexpr (R == 4) {
-        auto word64 = [&](int l) {
-            return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key >> 32), l))) << 32 |
-                   static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), l));
+        auto item_at = [&](int l) {
+            return Item{0, __builtin_amdgcn_readlane(item.word, l), 0, __builtin_amdgcn_readlane(item.len, l),
+                        static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(code >> 32), l)))
+                                << 32 | static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(code), l))};
         };
-        shared = shared_levels(a.t, __builtin_amdgcn_readlane(item.word, 0), len[0], word64(0),
-                               __builtin_amdgcn_readlane(item.word, 48), len[R - 1], word64(48));
+        shared = shared_levels(a.t, item_at(0), item_at(48));
     }
     float y[4][NE], now[4][NE];
     const int bytes = a.dim * 4;
@@ -450,7 +454,6 @@ struct Borders {
 
 struct NodeArgs {
     Tree t;
-    const uint64_t *keys;
     const Item *items;
     int32_t n, dim;
     const void *x;
@@ -499,23 +502,13 @@ __global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
     // lane q: row q of the block and the rows beside it
     const int pos = p0 + lane;
     const bool on = lane < rows;
-    Item item{0, -1, 0, 0}, last{0, -1, 0, 0}, next{0, -1, 0, 0};
-    uint64_t key = 0, last_key = 0, next_key = 0;
+    Item item{0, -1, 0, 0, 0}, last = item, next = item;
     if (on) {
         item = a.items[pos];
-        key = a.keys[pos];
-        if (pos > 0) {
-            last = a.items[pos - 1];
-            last_key = a.keys[pos - 1];
-        }
-        if (pos + 1 < a.n) {
-            next = a.items[pos + 1];
-            next_key = a.keys[pos + 1];
-        }
+        if (pos > 0) last = a.items[pos - 1];
+        if (pos + 1 < a.n) next = a.items[pos + 1];
     }
-    const int len = item.len;
-    const int before = shared_levels(a.t, last.word, last.len, last_key, item.word, len, key);
-    const int after = shared_levels(a.t, item.word, len, key, next.word, next.len, next_key);
+    const int len = item.len, before = shared_levels(a.t, last, item), after = shared_levels(a.t, item, next);
     float x[RB][C];
 #pragma unroll
     for (int q = 0; q < RB; ++q) {
@@ -706,7 +699,7 @@ __global__ __launch_bounds__(kZeroThreads) void k_hs_zero_flat(float *p, int64_t
 }
 
 struct Buffers {
-    uint64_t *key0, *key1;
+    void *keys;
     int32_t *row0, *row1;
     Item *items;
     float *coef, *part[2];
@@ -723,8 +716,7 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     const auto blocks = std::max<size_t>((n + kRows - 1) / kRows, std::min<size_t>((n + kFewRows - 1) / kFewRows, kFan));
     const size_t fans = (blocks + kFan - 1) / kFan, level = static_cast<size_t>(2) * longest * dim;
     Buffers b;
-    b.key0 = c.take<uint64_t>(n);
-    b.key1 = c.take<uint64_t>(n);
+    b.keys = c.take<uint64_t>(n);
     b.row0 = c.take<int32_t>(n);
     b.row1 = c.take<int32_t>(n);
     b.items = c.take<Item>(n);
@@ -777,24 +769,26 @@ int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole, h
 }
 
 // Sorts n <= kSlab rows by their targets' keys.
-int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, const Item **items,
-              const uint64_t **keys, hipStream_t s) {
+template <class K>
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, hipStream_t s) {
     const auto sort_blocks = static_cast<unsigned>(ceil_div(n, kSortBlock));
     Item *now = n <= kSortBlock ? b.items : nullptr;
+    K *keys = static_cast<K *>(b.keys);
     if (n <= kRankNarrow)
-        k_hs_rank<64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0, now);
+        k_hs_rank<K, 64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now);
     else
-        k_hs_rank<256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, b.key0, b.row0, now);
+        k_hs_rank<K, 256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now);
     W2V_LAUNCH_CHECK("k_hs_rank");
-    *items = b.items;
-    *keys = b.key0;
     if (now) return W2V_OK;
-    k_hs_merge<<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(b.key0, b.row0, n, b.key1, b.row1);
+    k_hs_merge<K><<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(keys, b.row0, n, b.row1);
     W2V_LAUNCH_CHECK("k_hs_merge");
     k_hs_items<<<static_cast<unsigned>(ceil_div(n, 256)), 256, 0, s>>>(t, targets, b.row1, n, b.items);
     W2V_LAUNCH_CHECK("k_hs_items");
-    *keys = b.key1;
     return W2V_OK;
+}
+
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, hipStream_t s) {
+    return t.longest <= 31 ? sort_rows<uint32_t>(t, targets, n, b, s) : sort_rows<uint64_t>(t, targets, n, b, s);
 }
 
 template <int R, int C>
@@ -871,10 +865,8 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, a.rows - lo));
         const int32_t *targets = a.targets + lo;
         const char *x = static_cast<const char *>(a.x) + lo * a.x_stride * type_bytes(a.type);
-        const Item *items = nullptr;
-        const uint64_t *keys = nullptr;
         if (a.dsyn1)
-            if (int rc = sort_rows(t, targets, n, b, &items, &keys, s)) return rc;
+            if (int rc = sort_rows(t, targets, n, b, s)) return rc;
         WalkArgs w{};
         w.t = t;
         w.syn1 = a.syn1;
@@ -884,8 +876,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         w.x_stride = a.x_stride;
         w.targets = targets;
         w.weights = a.weights ? a.weights + lo : nullptr;
-        w.items = items;
-        w.keys = keys;
+        w.items = a.dsyn1 ? b.items : nullptr;
         w.n = n;
         w.loss = a.loss ? a.loss + lo : nullptr;
         w.dx = a.dx ? static_cast<char *>(a.dx) + lo * a.dx_stride * type_bytes(a.type) : nullptr;
@@ -905,7 +896,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
         });
         W2V_LAUNCH_CHECK("k_hs_walk");
         if (!a.dsyn1) continue;
-        const NodeArgs m{t, keys, items, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.node[0], b.borders[0],
+        const NodeArgs m{t, b.items, n, a.dim, x, a.x_stride, b.coef, b.part[0], b.node[0], b.borders[0],
                          a.dsyn1, a.dsyn1_stride, lo > 0 ? 1 : 0, 1};
         if (int rc = sum_rows(m, a.type, b, s)) return rc;
     }
@@ -926,10 +917,8 @@ int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t di
     if (int rc = zero_rows(out, V, dim, out_stride, true, s)) return rc;
     for (int64_t lo = 0; lo < rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, rows - lo));
-        const Item *items = nullptr;
-        const uint64_t *keys = nullptr;
-        if (int rc = sort_rows(t, words + lo, n, b, &items, &keys, s)) return rc;
-        const NodeArgs m{t, keys, items, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
+        if (int rc = sort_rows(t, words + lo, n, b, s)) return rc;
+        const NodeArgs m{t, b.items, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
                          b.node[0], b.borders[0], out, out_stride, lo > 0 ? 1 : 0, 1};
         if (int rc = sum_rows(m, W2V_F32, b, s)) return rc;
     }
