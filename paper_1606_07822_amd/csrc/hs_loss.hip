@@ -10,7 +10,7 @@
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
 // j bits. A wavefront holds up to 32 sorted rows' x in registers, up to five columns a lane, and goes down the levels: a
 // level's nodes are runs of rows, summed and written out where a run ends. Runs that reach over a block's border are
-// written as partial sums, which k_hs_join adds up in order, 64 blocks at a time. The same sum with one level, every row
+// written as partial sums, which k_hs_join adds up in order. The same sum with one level, every row
 // for its own word's row of the table, is the gradient of a table's looked-up rows (run_word_sums).
 #include <hip/hip_runtime.h>
 
@@ -25,8 +25,9 @@ namespace {
 constexpr int kSlab = 65536;      // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
 constexpr int kSortBlock = 2048;  // rows ranked against each other
 constexpr int kRows = 32;         // sorted rows of a wavefront's sum
-constexpr int kFewRows = 16;      // of batches of at most kFan times as many, which have few wavefronts otherwise
-constexpr int kFan = 64;          // blocks that one wavefront joins
+constexpr int kFewRows = 16;      // of batches of at most kFewBlocks times as many, which have few wavefronts otherwise
+constexpr int kFewBlocks = 64;
+constexpr int kFan = 16;          // blocks whose sums one wavefront joins
 constexpr int kRankNarrow = 16384;   // rows up to which a workgroup ranks 64 of them, not 256
 constexpr int kXcds = 8;
 
@@ -459,8 +460,8 @@ struct NodeArgs {
     const void *x;
     int64_t x_stride;
     const float *coef;  // null: ones
-    float *part;        // [block][2][level][dim]: sums of runs that come in from the left, and of those that go on right
-    int32_t *part_node; // [block][level]: the node of a run that comes in from the left
+    float *part;        // [level][block][2][dim]: sums of runs that come in from the left, and of those that go on right
+    int32_t *part_node; // [level][block]: the node of a run that comes in from the left
     Borders borders;
     float *dsyn1;
     int64_t out_stride;
@@ -549,12 +550,12 @@ __global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
         // where the run that ends with this lane's row goes
         const bool from_left = left > j && (ends & lower) == 0;
         const bool to_right = lane == RB - 1 && right > j;
-        const int64_t slot = (static_cast<int64_t>(blk) * 2 + (from_left ? 0 : 1)) * longest + j;
+        const int64_t slot = (static_cast<int64_t>(j) * gridDim.x + blk) * 2 + (from_left ? 0 : 1);
         const uint64_t to = reinterpret_cast<uint64_t>(from_left || to_right ? a.part + slot * a.dim
                                                                              : a.dsyn1 + node * a.out_stride);
         const int to_lo = static_cast<int>(to), to_hi = static_cast<int>(to >> 32);
         const uint64_t direct = a.add ? ~__ballot(from_left || to_right) : 0;   // rows whose sum is added to dsyn1
-        if (left > j && lane == 0) a.part_node[static_cast<int64_t>(blk) * longest + j] = node;
+        if (left > j && lane == 0) a.part_node[static_cast<int64_t>(j) * gridDim.x + blk] = node;
         float acc[C];
 #pragma unroll
         for (int e = 0; e < C; ++e) acc[e] = 0.0f;
@@ -590,12 +591,12 @@ __global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
 }
 
 struct JoinArgs {
-    int32_t dim, longest;
-    const float *in;        // [block][2][level][dim]
-    const int32_t *in_node; // [block][level]
+    int32_t dim;
+    const float *in;        // [level][block][2][dim]
+    const int32_t *in_node; // [level][block]
     Borders borders;
     int32_t blocks;
-    float *out;             // the same of kFan blocks together
+    float *out;             // the same of a workgroup's blocks together
     int32_t *out_node;
     Borders out_borders;
     float *dsyn1;
@@ -603,72 +604,105 @@ struct JoinArgs {
     int32_t add;
 };
 
-// Partial sums of kFan neighbouring blocks at one level, in order: a run's first part lies on a block's right, the
-// others on the left of the blocks that follow.
-__global__ __launch_bounds__(kWave) void k_hs_join(JoinArgs a) {
-    const int lane = lane_id(), level = static_cast<int>(blockIdx.z), longest = a.longest;
-    const int first = static_cast<int>(blockIdx.x) * kFan, blk = first + lane;
-    const int col = static_cast<int>(blockIdx.y) * kWave + lane;
-    const bool on = blk < a.blocks;
+// The partial sums of one level added up in the blocks' order, 64 columns of up to kJoinWaves kFan blocks a workgroup: a
+// run's first part lies on a block's right, the others on the left of the blocks that follow. Each wavefront fetches the
+// parts of kFan blocks at once (another XCD wrote them: a fetch takes a microsecond, whatever it is of) and adds up the
+// runs among them; the first one then puts together what leaves one wavefront's blocks for the next one's.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinWaves *kWave) void k_hs_join(JoinArgs a) {
+    __shared__ float s_in[kJoinWaves][kWave], s_out[kJoinWaves][kWave];
+    __shared__ int32_t s_flags[kJoinWaves], s_node[kJoinWaves], s_least[kJoinWaves];
+    const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int level = static_cast<int>(blockIdx.z), super = static_cast<int>(blockIdx.x);
+    const int col = static_cast<int>(blockIdx.y) * kWave + lane, bytes = a.dim * 4;
+    const int first = (super * kJoinWaves + wid) * kFan, blk = first + lane;
+    const bool on = lane < kFan && blk < a.blocks;
     const int left = on ? a.borders.left[blk] : 0, inner = on ? a.borders.inner[blk] : kWave;
     const int right = on && blk + 1 < a.blocks ? a.borders.left[blk + 1] : 0;
+    int least = on ? min(inner, lane > 0 || wid > 0 ? left : kWave) : kWave;
     if (blockIdx.y == 0 && level == 0) {
-        int least = on ? min(inner, lane > 0 ? left : kWave) : kWave;
 #pragma unroll
         for (int m = 32; m >= 1; m >>= 1) least = min(least, __shfl_xor(least, m, kWave));
-        if (lane == 0) {
-            a.out_borders.left[blockIdx.x] = left;
-            a.out_borders.inner[blockIdx.x] = least;
-        }
     }
-    const uint64_t has_left = __ballot(left > level);
-    const uint64_t through = __ballot(left > level && inner > level && right > level);
-    const uint64_t has_right = __ballot(right > level) & ~through;
-    if (!(has_left | has_right)) return;
-    const int node = left > level ? a.in_node[static_cast<int64_t>(blk) * longest + level] : 0;
-    if (left > level && lane == 0 && blockIdx.y == 0)
-        a.out_node[static_cast<int64_t>(blockIdx.x) * longest + level] = node;
-    const int bytes = a.dim * 4;
-    const int64_t part = static_cast<int64_t>(longest) * a.dim;   // of a block's two
-    const float *in = a.in + first * 2 * part + static_cast<int64_t>(level) * a.dim;
-    bool outside = has_left & 1ull;   // the run at hand began before these blocks
+    const auto has_left = static_cast<uint32_t>(__ballot(left > level));
+    const auto through = static_cast<uint32_t>(__ballot(left > level && inner > level && right > level));
+    const auto has_right = static_cast<uint32_t>(__ballot(right > level)) & ~through;
     float acc[1] = {0.0f};
-    float *out = a.out + (static_cast<int64_t>(blockIdx.x) * 2 * longest + level) * a.dim;
-    // all of them on their way at once; an empty range where there is none, and no sixteen that have none
-    constexpr int kGroup = 16;
-    float l[kFan][1], r[kFan][1];
+    bool outside = has_left & 1u;   // the run at hand began before these blocks
+    int first_node = 0;
+    if (has_left | has_right) {
+        const int node = left > level ? a.in_node[static_cast<int64_t>(level) * a.blocks + blk] : 0;
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<float *>(a.in + (static_cast<int64_t>(level) * a.blocks + first) * 2 * a.dim), 0,
+            min(kFan, a.blocks - first) * 2 * bytes, kRawBufferWord3);
+        float l[kFan], r[kFan];
 #pragma unroll
-    for (int b0 = 0; b0 < kFan; b0 += kGroup) {
-        if (!(((has_left | has_right) >> b0) & ((1ull << kGroup) - 1))) continue;
-#pragma unroll
-        for (int b = b0; b < b0 + kGroup; ++b) {
-            load_columns<1>(in + b * 2 * part, col, (has_left >> b) & 1ull ? bytes : 0, l[b]);
-            load_columns<1>(in + b * 2 * part + part, col, (has_right >> b) & 1ull ? bytes : 0, r[b]);
+        for (int b = 0; b < kFan; ++b) {   // out of range where there is none: no branch around the loads
+            const int at = col * 4 + b * 2 * bytes;
+            l[b] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (has_left >> b) & 1u ? at : -4, 0, 0));
+            r[b] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (has_right >> b) & 1u ? at + bytes : -4, 0, 0));
         }
-    }
+        first_node = __builtin_amdgcn_readlane(node, 0);
 #pragma unroll
-    for (int b0 = 0; b0 < kFan; b0 += kGroup) {
-        if (!(((has_left | has_right) >> b0) & ((1ull << kGroup) - 1))) continue;
-#pragma unroll
-        for (int b = b0; b < b0 + kGroup; ++b) {
-            if ((has_left >> b) & 1ull) {
-                acc[0] += l[b][0];
-                if (!((through >> b) & 1ull)) {
-                    float *to = outside ? out : a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride;
-                    put_columns<1>(to, col, bytes, acc, a.add && !outside);
+        for (int b = 0; b < kFan; ++b) {
+            if ((has_left >> b) & 1u) {
+                acc[0] += l[b];
+                if (!((through >> b) & 1u)) {
+                    if (outside)
+                        s_in[wid][lane] = acc[0];
+                    else
+                        put_columns<1>(a.dsyn1 + __builtin_amdgcn_readlane(node, b) * a.out_stride, col, bytes, acc, a.add);
                     outside = false;
                     acc[0] = 0.0f;
                 }
             }
-            if ((has_right >> b) & 1ull) {
-                acc[0] = r[b][0];
+            if ((has_right >> b) & 1u) {
+                acc[0] = r[b];
                 outside = false;
             }
         }
     }
-    // a run that goes on past the last block
-    if (((has_right | through) >> (kFan - 1)) & 1ull)
-        put_columns<1>(out + (outside ? 0 : part), col, bytes, acc, false);
+    const bool leaves = ((has_right | through) >> (kFan - 1)) & 1u;
+    if (leaves) (outside ? s_in : s_out)[wid][lane] = acc[0];
+    if (lane == 0) {
+        s_flags[wid] = (has_left & 1u ? 1 : 0) | (leaves ? (outside ? 2 : 4) : 0);   // a run comes in, goes through, leaves
+        s_node[wid] = first_node;
+        s_least[wid] = least;
+    }
+    __syncthreads();
+    if (wid > 0) return;
+    float *out = a.out + (static_cast<int64_t>(level) * gridDim.x + super) * 2 * a.dim;
+    const int waves = static_cast<int>(blockDim.x) / kWave;
+    outside = has_left & 1u;
+    acc[0] = 0.0f;
+    int flags = 0;
+    for (int w = 0; w < waves; ++w) {
+        flags = __builtin_amdgcn_readfirstlane(s_flags[w]);
+        if (flags & 1) {
+            acc[0] += s_in[w][lane];
+            if (!(flags & 2)) {
+                if (outside)
+                    put_columns<1>(out, col, bytes, acc, false);
+                else
+                    put_columns<1>(a.dsyn1 + __builtin_amdgcn_readfirstlane(s_node[w]) * a.out_stride, col, bytes, acc, a.add);
+                outside = false;
+                acc[0] = 0.0f;
+            }
+        }
+        if (flags & 4) {
+            acc[0] = s_out[w][lane];
+            outside = false;
+        }
+    }
+    if (flags & 6) put_columns<1>(out + (outside ? 0 : a.dim), col, bytes, acc, false);
+    if (blockIdx.y == 0 && lane == 0) {
+        if (has_left & 1u) a.out_node[static_cast<int64_t>(level) * gridDim.x + super] = first_node;
+        if (level == 0) {
+            for (int w = 0; w < waves; ++w) least = min(least, s_least[w]);
+            a.out_borders.left[super] = left;
+            a.out_borders.inner[super] = least;
+        }
+    }
 }
 
 // The first dim columns of the rows set to zero, a wavefront a row.
@@ -707,14 +741,14 @@ struct Buffers {
     Borders borders[3];
 };
 
-// Rows of a wavefront's sum: few, so that there are more wavefronts, while one join takes all blocks.
-int block_rows(int64_t n) { return n <= kFewRows * kFan ? kFewRows : kRows; }
+// Rows of a wavefront's sum: few, so that there are more wavefronts, in a small batch.
+int block_rows(int64_t n) { return n <= kFewRows * kFewBlocks ? kFewRows : kRows; }
 
 Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     const auto n = static_cast<size_t>(std::min<int64_t>(std::max<int64_t>(rows, 1), kSlab));
-    // a last slab of few rows has blocks of kFewRows, at most kFan of them
-    const auto blocks = std::max<size_t>((n + kRows - 1) / kRows, std::min<size_t>((n + kFewRows - 1) / kFewRows, kFan));
-    const size_t fans = (blocks + kFan - 1) / kFan, level = static_cast<size_t>(2) * longest * dim;
+    // a last slab of few rows has blocks of kFewRows, at most kFewBlocks of them
+    const auto blocks = std::max<size_t>((n + kRows - 1) / kRows, std::min<size_t>((n + kFewRows - 1) / kFewRows, kFewBlocks));
+    const size_t fans = (blocks + kFan * kJoinWaves - 1) / (kFan * kJoinWaves), level = static_cast<size_t>(2) * longest * dim;
     Buffers b;
     b.keys = c.take<uint64_t>(n);
     b.row0 = c.take<int32_t>(n);
@@ -832,14 +866,17 @@ int sum_rows(NodeArgs m, int32_t type, const Buffers &b, hipStream_t s) {
     });
     W2V_LAUNCH_CHECK("k_hs_nodes");
     const auto tiles = static_cast<unsigned>(ceil_div(m.dim, kWave));
-    int32_t left = blocks;   // 2,048 at most: two joins
+    static_assert(kSlab / kRows <= kFan * kJoinWaves * kFan * kJoinWaves, "two joins are enough");
+    int32_t left = blocks;
     for (int k = 0; k < 2 && left > 1; ++k) {
-        const auto fans = static_cast<int32_t>(ceil_div(left, kFan));
-        JoinArgs j{m.dim, m.t.longest, b.part[k], b.node[k], b.borders[k], left, b.part[1], b.node[1], b.borders[k + 1],
+        const auto supers = static_cast<int32_t>(ceil_div(left, kFan * kJoinWaves));
+        const auto waves = std::min<int64_t>(kJoinWaves, ceil_div(left, kFan));
+        JoinArgs j{m.dim, b.part[k], b.node[k], b.borders[k], left, b.part[1], b.node[1], b.borders[k + 1],
                    m.dsyn1, m.out_stride, m.add};
-        k_hs_join<<<dim3(static_cast<unsigned>(fans), tiles, static_cast<unsigned>(m.t.longest)), kWave, 0, s>>>(j);
+        k_hs_join<<<dim3(static_cast<unsigned>(supers), tiles, static_cast<unsigned>(m.t.longest)),
+                    static_cast<unsigned>(waves * kWave), 0, s>>>(j);
         W2V_LAUNCH_CHECK("k_hs_join");
-        left = fans;
+        left = supers;
     }
     return W2V_OK;
 }

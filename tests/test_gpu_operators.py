@@ -324,6 +324,17 @@ def test_loss_many_rows(w2v, n):
     check_loss(w2v, model, otree, hidden(n, 6, torch.float32), draw_targets(rng, counts, n), None)
 
 
+@pytest.mark.parametrize("n", [65, 1023, 1025, 2049, 5000])
+def test_loss_many_rows_of_a_deep_tree(w2v, n):
+    """Codes of up to 45 turns, every word as likely as the next: keys of 64 bits, runs that are cut at every level."""
+    import torch
+    counts = COUNTS["deep"]()
+    rng = np.random.default_rng(n)
+    model, otree = make_model(w2v, counts, 10)
+    targets = rng.integers(-1, counts.size, n).astype(np.int32)
+    check_loss(w2v, model, otree, hidden(n, 10, torch.float32), targets, rng.random(n, dtype=np.float32))
+
+
 @pytest.mark.parametrize("tree", ["two", "zipf"])
 def test_loss_more_rows_than_a_slab(w2v, tree):
     """65,536 rows are summed together; what comes after them is added."""
