@@ -117,40 +117,75 @@ __device__ __forceinline__ uint32_t encode_m(const float (&m)[kPer], float inver
     return static_cast<uint32_t>(c);
 }
 
-__device__ __forceinline__ float decode_r(uint32_t c) {
-    return c < 16 ? static_cast<float>(c) * 0x1p-18f : __builtin_bit_cast(float, (c + 112 * 16) << 19);
-}
+// The root's codes are the exponent and fraction bits of an fp32 number 2^-112 as large, subnormal ones among them:
+// either way is a product with a power of two and a shift, and rounding one up or down is an addition below the code.
+__device__ __forceinline__ float decode_r(uint32_t c) { return __builtin_bit_cast(float, c << 19) * 0x1p112f; }
 
 // r / scale as a code, rounded by the 16 random bits h.
 __device__ __forceinline__ uint32_t encode_r(float r, float inverse, uint32_t h) {
 #pragma clang fp contract(off)
-    const float t = r * inverse;
-    const int32_t normal = ((__builtin_bit_cast(int32_t, t) + static_cast<int32_t>(h * 8 + 4)) >> 19) - 112 * 16;
-    const int32_t small = static_cast<int32_t>(floorf(t * 0x1p18f + (static_cast<float>(h) + 0.5f) * 0x1p-16f));
-    const int32_t c = min(t < 0x1p-14f ? small : normal, 255);
-    return r > 0.0f && c == 0 ? 1u : static_cast<uint32_t>(c) & 255u;
+    const float t = (r * inverse) * 0x1p-112f;
+    const uint32_t c = min((__builtin_bit_cast(uint32_t, t) + (h * 8 + 4)) >> 19, 255u);
+    return r > 0.0f ? max(c, 1u) : c;
 }
 
-// One element: new moments (m, v) and the new parameter.
-__device__ __forceinline__ void update(float &p, float g, float &m, float &v, float &r, float keep, const Scalars &s) {
+// One element: new moments (m, v) and v's root.
+__device__ __forceinline__ void update_moments(float g, float &m, float &v, float &r, const Scalars &s) {
 #pragma clang fp contract(off)
     g *= s.grad_scale;
     m = m * s.b1 + g * s.c1;
     v = v * s.b2 + (g * g) * s.c2;
     r = sqrtf(v);
-    p = p * keep - (m * s.size) / (r * s.root + s.eps);
 }
 
-// A chunk's elements, four neighbouring ones of a lane at a time. FULL: every element lies in the tensor and both arrays
-// are packed; otherwise four that lie in one row are still one access.
-template <class TP, class TG, int BITS, bool FULL>
+// The new parameter. The quotient's reciprocal is the hardware's, off by one unit in the last place.
+__device__ __forceinline__ float updated(float p, float m, float r, float keep, const Scalars &s) {
+    return fmaf(p, keep, -(m * s.size) * __builtin_amdgcn_rcpf(fmaf(r, s.root, s.eps)));
+}
+
+// The tensors' addresses come from the plan, where the compiler can't tell global memory from the rest.
+template <class T>
+using Global = __attribute__((address_space(1))) T;
+
+// N neighbouring elements as words, at any element-aligned address.
+template <class T, int N>
+struct Words {
+    static constexpr int count = N * sizeof(T) / 4;
+    typedef uint32_t type __attribute__((ext_vector_type(count), aligned(sizeof(T))));
+};
+
+template <class T, int N>
+__device__ __forceinline__ void load_global(const T *p, float (&f)[N]) {
+    using W = typename Words<T, N>::type;
+    const W w = *(const Global<W> *)(p);
+    const auto u = __builtin_bit_cast(Pack<T, N>, w);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = static_cast<float>(u.v[e]);
+}
+
+template <class T, int N>
+__device__ __forceinline__ void store_global(T *p, const float (&f)[N]) {
+    using W = typename Words<T, N>::type;
+    Pack<T, N> u;
+#pragma unroll
+    for (int e = 0; e < N; ++e) u.v[e] = static_cast<T>(f[e]);
+    *(Global<W> *)(p) = __builtin_bit_cast(W, u);
+}
+
+// A chunk's elements, four neighbouring ones of a lane at a time. kPacked: every element lies in the tensor and both
+// arrays are packed; kRows: every element lies in the tensor, whose rows have gaps and a multiple of four columns, so
+// that any four lie in one row; kAny: all else, where four that lie in one row are still one access. (A table of rows of
+// 300 floats, 320 apart, as kAny: 600 M parameters in 3.84 ms, with a branch around every load.)
+enum Layout { kPacked, kRows, kAny };
+template <class TP, class TG, int BITS, Layout LAYOUT>
 __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void *mv, void *vv, float *m_scale,
                                              float *v_scale, const Scalars &s) {
     TP *pp = static_cast<TP *>(t.p);
     const TG *gp = static_cast<const TG *>(t.g);
     const float keep = static_cast<float>(1.0 - s.lr * static_cast<double>(t.decay));
-    const int64_t row0 = FULL || t.flat ? 0 : first / t.cols;
-    const int64_t rem0 = FULL || t.flat ? first : first - row0 * t.cols;
+    constexpr bool FULL = LAYOUT != kAny;   // no element past the tensor's end
+    const int64_t row0 = LAYOUT == kPacked || t.flat ? 0 : first / t.cols;
+    const int64_t rem0 = LAYOUT == kPacked || t.flat ? first : first - row0 * t.cols;
     float p[kSteps][kPer], g[kSteps][kPer], m[kSteps][kPer], v[kSteps][kPer];
     uint32_t mc[kSteps], vc[kSteps];
     int64_t po[kSteps], go[kSteps];
@@ -166,8 +201,14 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
         const int64_t e = first + local, at = t.offset + e;
         if constexpr (FULL) {
             po[k] = go[k] = e;
-            load_pack<TP, kPer>(pp + e, p[k]);
-            load_pack<TG, kPer>(gp + e, g[k]);
+            if constexpr (LAYOUT == kRows) {
+                const uint32_t c = static_cast<uint32_t>(t.cols), at_row = static_cast<uint32_t>(rem0) + local;
+                const uint32_t q = at_row / c, at_col = at_row - q * c;
+                po[k] = (row0 + q) * t.p_stride + at_col;
+                go[k] = (row0 + q) * t.g_stride + at_col;
+            }
+            load_global<TP, kPer>(pp + po[k], p[k]);
+            load_global<TG, kPer>(gp + go[k], g[k]);
         } else {
             in_row[k] = 0;
             po[k] = go[k] = col[k] = 0;
@@ -186,15 +227,15 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
                     in_row[k] = static_cast<int>(min<uint32_t>(kPer, c - col[k]));
                 }
                 if (in_row[k] == kPer) {
-                    load_pack<TP, kPer>(pp + po[k], p[k]);
-                    load_pack<TG, kPer>(gp + go[k], g[k]);
+                    load_global<TP, kPer>(pp + po[k], p[k]);
+                    load_global<TG, kPer>(gp + go[k], g[k]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < kPer; ++i)
                         if (e + i < t.n) {
                             const uint32_t d = rows_on(i, k);
-                            p[k][i] = static_cast<float>(pp[po[k] + i + d * (t.p_stride - t.cols)]);
-                            g[k][i] = static_cast<float>(gp[go[k] + i + d * (t.g_stride - t.cols)]);
+                            p[k][i] = static_cast<float>(((const Global<TP> *)pp)[po[k] + i + d * (t.p_stride - t.cols)]);
+                            g[k][i] = static_cast<float>(((const Global<TG> *)gp)[go[k] + i + d * (t.g_stride - t.cols)]);
                         }
                 }
             }
@@ -235,7 +276,8 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (!FULL && e + i >= t.n) continue;
-            update(p[k][i], g[k][i], m[k][i], v[k][i], r[i], keep, s);
+            update_moments(g[k][i], m[k][i], v[k][i], r[i], s);
+            p[k][i] = updated(p[k][i], m[k][i], r[i], keep, s);
             m_max = larger(m_max, fabsf(m[k][i]));
             r_max = larger(r_max, r[i]);
         }
@@ -278,15 +320,15 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
             }
         }
         if constexpr (FULL) {
-            store_pack<TP, kPer>(pp + e, p[k]);
+            store_global<TP, kPer>(pp + po[k], p[k]);
         } else if (in_row[k] == kPer) {
-            store_pack<TP, kPer>(pp + po[k], p[k]);
+            store_global<TP, kPer>(pp + po[k], p[k]);
         } else if (in_row[k] > 0) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
                 if (e + i < t.n) {
                     const uint32_t d = rows_on(i, k);
-                    pp[po[k] + i + d * (t.p_stride - t.cols)] = static_cast<TP>(p[k][i]);
+                    ((Global<TP> *)pp)[po[k] + i + d * (t.p_stride - t.cols)] = static_cast<TP>(p[k][i]);
                 }
         }
     }
@@ -301,14 +343,16 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(const Header *__restrict
         const Place at = h->places[b];
         const Entry t = h->entries[at.tensor];
         const int64_t first = static_cast<int64_t>(at.chunk) * kChunk;
-        const bool full = t.flat && first + kChunk <= t.n;
+        const bool full = first + kChunk <= t.n;
         auto with = [&](auto p0, auto g0) {
             using TP = decltype(p0);
             using TG = decltype(g0);
-            if (full)
-                chunk_update<TP, TG, BITS, true>(t, first, mv, vv, m_scale, v_scale, s);
+            if (full && t.flat)
+                chunk_update<TP, TG, BITS, kPacked>(t, first, mv, vv, m_scale, v_scale, s);
+            else if (full && t.cols % kPer == 0)
+                chunk_update<TP, TG, BITS, kRows>(t, first, mv, vv, m_scale, v_scale, s);
             else
-                chunk_update<TP, TG, BITS, false>(t, first, mv, vv, m_scale, v_scale, s);
+                chunk_update<TP, TG, BITS, kAny>(t, first, mv, vv, m_scale, v_scale, s);
         };
         auto with_grad = [&](auto p0) {
             if (t.g_type == W2V_F32)

@@ -611,9 +611,8 @@ def narrow_reference(g, m, v, offset, step, seed):
     key = mix(np.array([(seed ^ (step * 0x9E3779B9)) & 0xFFFFFFFF], dtype=np.uint64))
     h = mix(((at >> np.uint64(1)) & np.uint64(0xFFFFFFFF)) ^ key)
     h = np.where(at & np.uint64(1), h >> np.uint64(16), h & np.uint64(0xFFFF)).astype(np.int64)
-    normal = ((t.view(np.int32).astype(np.int64) + h * 8 + 4) >> 19) - 112 * 16
-    small = np.floor(t * f(2.0**18) + (h.astype(f) + f(0.5)) * f(2.0**-16)).astype(np.int64)
-    c = np.minimum(np.where(t < f(2.0**-14), small, normal), 255)
+    # a code is the exponent and fraction bits of t 2^-112 in fp32, subnormal numbers among them
+    c = np.minimum(((t * f(2.0**-112)).view(np.int32).astype(np.int64) + h * 8 + 4) >> 19, 255)
     return mc, np.where((r > 0) & (c == 0), 1, c).astype(np.uint8), ms, rs
 
 
