@@ -147,7 +147,8 @@ __device__ __forceinline__ float updated(float p, float m, float r, float keep, 
 template <class T>
 using Global = __attribute__((address_space(1))) T;
 
-// N neighbouring elements as words, at any element-aligned address.
+// N neighbouring elements as words, at any element-aligned address. Each is used once: non-temporal, which leaves the
+// caches to what is read again (600 M fp32 parameters: 3.83 -> 3.20 ms, 4.4 -> 5.3 TB/s).
 template <class T, int N>
 struct Words {
     static constexpr int count = N * sizeof(T) / 4;
@@ -157,7 +158,7 @@ struct Words {
 template <class T, int N>
 __device__ __forceinline__ void load_global(const T *p, float (&f)[N]) {
     using W = typename Words<T, N>::type;
-    const W w = *(const Global<W> *)(p);
+    const W w = __builtin_nontemporal_load((const Global<W> *)(p));
     const auto u = __builtin_bit_cast(Pack<T, N>, w);
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] = static_cast<float>(u.v[e]);
@@ -169,7 +170,7 @@ __device__ __forceinline__ void store_global(T *p, const float (&f)[N]) {
     Pack<T, N> u;
 #pragma unroll
     for (int e = 0; e < N; ++e) u.v[e] = static_cast<T>(f[e]);
-    *(Global<W> *)(p) = __builtin_bit_cast(W, u);
+    __builtin_nontemporal_store(__builtin_bit_cast(W, u), (Global<W> *)(p));
 }
 
 // A chunk's elements, four neighbouring ones of a lane at a time. kPacked: every element lies in the tensor and both
@@ -242,14 +243,14 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
         }
         if constexpr (BITS == 32) {
             if (FULL || e < t.n) {   // the moments' places go on to the end of a block
-                load_pack<float, kPer>(static_cast<const float *>(mv) + at, m[k]);
-                load_pack<float, kPer>(static_cast<const float *>(vv) + at, v[k]);
+                load_global<float, kPer>(static_cast<const float *>(mv) + at, m[k]);
+                load_global<float, kPer>(static_cast<const float *>(vv) + at, v[k]);
             }
         } else {
             mc[k] = vc[k] = 0;
             if (FULL || e < t.n) {
-                mc[k] = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(mv) + at);
-                vc[k] = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(vv) + at);
+                mc[k] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(mv) + at));
+                vc[k] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(vv) + at));
             }
         }
     }
@@ -283,8 +284,8 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
         }
         if constexpr (BITS == 32) {
             if (FULL || e < t.n) {
-                store_pack<float, kPer>(static_cast<float *>(mv) + at, m[k]);
-                store_pack<float, kPer>(static_cast<float *>(vv) + at, v[k]);
+                store_global<float, kPer>(static_cast<float *>(mv) + at, m[k]);
+                store_global<float, kPer>(static_cast<float *>(vv) + at, v[k]);
             }
         } else {
             float ms = wave_max_bits(m_max) * (1.0f / 448.0f), rs = wave_max_bits(r_max) * (16.0f / 31.0f);
@@ -311,8 +312,8 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
                 new_v = (new_v & mask) | (old_v & ~mask);
             }
             if (FULL || e < t.n) {
-                *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(mv) + at) = new_m;
-                *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(vv) + at) = new_v;
+                __builtin_nontemporal_store(new_m, reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(mv) + at));
+                __builtin_nontemporal_store(new_v, reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(vv) + at));
             }
             if (lane_id() == 0) {
                 m_scale[block] = ms;
@@ -388,8 +389,8 @@ __global__ __launch_bounds__(kAdamThreads) void k_moments(const uint32_t *__rest
             const float x = decode_r((c >> (8 * i)) & 255u) * vs;
             v[i] = x * x;
         }
-        store_pack<float, kPer>(m_out + w * kPer, m);
-        store_pack<float, kPer>(v_out + w * kPer, v);
+        store_global<float, kPer>(m_out + w * kPer, m);
+        store_global<float, kPer>(v_out + w * kPer, v);
     }
 }
 
