@@ -6,7 +6,9 @@
 // Both passes read each row once into registers (the variance is taken from the centred values there, not from a
 // difference of sums), so what bounds them is memory: 2 row transfers forward, 3 backward. A row is held by LPR
 // lanes, each with NCH vectors of 16 bytes: 16 lanes for narrow rows, so that a wavefront's loads are full at 50 to
-// 300 columns, a wavefront or a workgroup for wide ones. All sums are fp32, in a fixed order.
+// 300 columns, a wavefront or a workgroup for wide ones: with few elements a lane there are enough wavefronts to keep
+// memory busy (the forward pass of 16,384 rows of 4,096 bf16 columns takes 62 us with 256 lanes a row, 4.3 TB/s, and 170
+// with 64; the backward pass of 65,536 rows of 300 floats 48 us, 4.9 TB/s). All sums are fp32, in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -51,15 +53,18 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int &turn) {
 }
 
 // Weight or bias columns: in fp32, or in the rows' type (w_type tells).
-template <class T, int N>
+template <class T, int N, bool WHOLE>
 __device__ __forceinline__ void load_affine(const void *w, int32_t w_type, int col, int dim, float (&f)[N]) {
     if (w_type == W2V_F32)
-        load_cols<float, N>(static_cast<const float *>(w), col, dim, f);
+        load_cols<float, N, WHOLE>(static_cast<const float *>(w), col, dim, f);
     else
-        load_cols<T, N>(static_cast<const T *>(w), col, dim, f);
+        load_cols<T, N, WHOLE>(static_cast<const T *>(w), col, dim, f);
 }
 
-template <class T, int LPR, int NCH>
+// WHOLE: dim is a multiple of a vector's elements. (Reading the elements of a last part of a vector one by one takes
+// registers that rows without one had better keep for more wavefronts: 16,384 rows of 4,096 bf16 columns with 103
+// registers a lane 81 us, with 62 62 us.)
+template <class T, int LPR, int NCH, bool WHOLE>
 __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_norm(NormArgs a) {
     constexpr int VEC = kVec<T>;
     const int lane = static_cast<int>(threadIdx.x) % LPR;
@@ -71,7 +76,7 @@ __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_nor
         const T *x = static_cast<const T *>(a.x) + r * a.x_stride;
         float v[NCH][VEC], sum[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) load_cols<T, VEC>(x, (i * LPR + lane) * VEC, a.dim, v[i]);
+        for (int i = 0; i < NCH; ++i) load_cols<T, VEC, WHOLE>(x, (i * LPR + lane) * VEC, a.dim, v[i]);
 #pragma unroll
         for (int i = 0; i < NCH; ++i)
 #pragma unroll
@@ -97,25 +102,26 @@ __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_nor
             for (int e = 0; e < VEC; ++e) v[i][e] *= rs;
             if (a.w) {
                 float w[VEC];
-                load_affine<T, VEC>(a.w, a.w_type, col, a.dim, w);
+                load_affine<T, VEC, WHOLE>(a.w, a.w_type, col, a.dim, w);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[i][e] *= w[e];
             }
             if (a.b) {
                 float b[VEC];
-                load_affine<T, VEC>(a.b, a.w_type, col, a.dim, b);
+                load_affine<T, VEC, WHOLE>(a.b, a.w_type, col, a.dim, b);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[i][e] += b[e];
             }
-            store_cols<T, VEC>(y, col, a.dim, v[i]);
+            store_cols<T, VEC, WHOLE>(y, col, a.dim, v[i]);
         }
         if (lane == 0 && a.mean) a.mean[r] = mu;
         if (lane == 0 && a.rstd) a.rstd[r] = rs;
     }
 }
 
-// The columns' sums of a workgroup's rows go to part[blockIdx.x][0..dim) (dw) and [dim..2 dim) (db).
-template <class T, int LPR, int NCH>
+// The columns' sums of a workgroup's rows go to part[blockIdx.x][0..dim) (dw) and [dim..2 dim) (db). A row's elements are
+// fetched while the row before it is worked on.
+template <class T, int LPR, int NCH, bool WHOLE>
 __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_norm_back(NormArgs a, float *part) {
     constexpr int VEC = kVec<T>;
     const int lane = static_cast<int>(threadIdx.x) % LPR;
@@ -127,17 +133,36 @@ __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_nor
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.0f;
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * groups + threadIdx.x / LPR; r < a.rows;
-         r += static_cast<int64_t>(gridDim.x) * groups) {
+    Pack<T, VEC> next_x[NCH], next_dy[NCH];
+    float next_mu = 0.0f, next_rs = 0.0f;
+    auto fetch = [&](int64_t r) {
+        if (r >= a.rows) return;
         const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
-        float h[NCH][VEC], g[NCH][VEC], sum[2] = {0.0f, 0.0f};   // g: dy, then dy w
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int col = (i * LPR + lane) * VEC;
-            load_cols<T, VEC>(x, col, a.dim, h[i]);
-            load_cols<T, VEC>(dy, col, a.dim, g[i]);
+            next_x[i] = raw_cols<T, VEC, WHOLE>(x, col, a.dim);
+            next_dy[i] = raw_cols<T, VEC, WHOLE>(dy, col, a.dim);
         }
-        const float mu = a.mean[r], rs = a.rstd[r];
+        next_mu = a.mean[r];
+        next_rs = a.rstd[r];
+    };
+    const int64_t step = static_cast<int64_t>(gridDim.x) * groups;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * groups + threadIdx.x / LPR;
+    constexpr bool kAhead = LPR <= 256;   // sixteen wavefronts a workgroup have registers for one row
+    if (kAhead) fetch(first);
+    for (int64_t r = first; r < a.rows; r += step) {
+        if (!kAhead) fetch(r);
+        float h[NCH][VEC], g[NCH][VEC], sum[2] = {0.0f, 0.0f};   // g: dy, then dy w
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                h[i][e] = static_cast<float>(next_x[i].v[e]);
+                g[i][e] = static_cast<float>(next_dy[i].v[e]);
+            }
+        const float mu = next_mu, rs = next_rs;
+        if (kAhead) fetch(r + step);
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int col = (i * LPR + lane) * VEC;
@@ -149,7 +174,7 @@ __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_nor
             }
             if (a.w && col < a.dim) {
                 float w[VEC];
-                load_affine<T, VEC>(a.w, a.w_type, col, a.dim, w);
+                load_affine<T, VEC, WHOLE>(a.w, a.w_type, col, a.dim, w);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) g[i][e] *= w[e];
             }
@@ -168,7 +193,7 @@ __global__ __launch_bounds__(LPR > kNormThreads ? LPR : kNormThreads) void k_nor
             if (col >= a.dim) continue;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) g[i][e] = rs * (g[i][e] - c0 - h[i][e] * c1);
-            store_cols<T, VEC>(dx, col, a.dim, g[i]);
+            store_cols<T, VEC, WHOLE>(dx, col, a.dim, g[i]);
         }
     }
     if (!part) return;
@@ -236,34 +261,41 @@ __global__ __launch_bounds__(kColThreads) void k_norm_columns(const float *__res
 }
 
 // Calls f(LPR, NCH) with the smallest shape that holds a row of dim elements of T.
-template <int A, int B>
+template <int A, int B, bool W = false>
 struct Shape {
     static constexpr int lpr = A, nch = B;
+    static constexpr bool whole = W;
+    using Whole = Shape<A, B, true>;
 };
 template <class T, class F>
-int with_shape(int32_t dim, F f) {
+int with_shape(int32_t dim, F call) {
     const int chunks = static_cast<int>(ceil_div(dim, kVec<T>));
+    auto f = [&](auto shape) { return dim % kVec<T> == 0 ? call(typename decltype(shape)::Whole{}) : call(shape); };
+    // at most 20 elements a lane: with 32 the backward pass keeps a wavefront or two a SIMD
     if (chunks <= 16) return f(Shape<16, 1>{});
     if (chunks <= 32) return f(Shape<16, 2>{});
-    if (chunks <= 48) return f(Shape<16, 3>{});
-    if (chunks <= 80) return f(Shape<16, 5>{});
-    if (chunks <= 128) return f(Shape<64, 2>{});
-    if (chunks <= 256) return f(Shape<64, 4>{});
     if constexpr (sizeof(T) == 4) {
-        if (chunks <= 512) return f(Shape<64, 8>{});
-        if (chunks <= 1024) return f(Shape<256, 4>{});
-        if (chunks <= 2048) return f(Shape<256, 8>{});
-        return f(Shape<1024, 4>{});
-    } else {
+        if (chunks <= 48) return f(Shape<16, 3>{});
+        if (chunks <= 80) return f(Shape<16, 5>{});
+        if (chunks <= 128) return f(Shape<64, 2>{});
+        if (chunks <= 256) return f(Shape<64, 4>{});
         if (chunks <= 512) return f(Shape<256, 2>{});
         if (chunks <= 1024) return f(Shape<256, 4>{});
+        if (chunks <= 2048) return f(Shape<1024, 2>{});
+        return f(Shape<1024, 4>{});
+    } else {
+        if (chunks <= 64) return f(Shape<64, 1>{});
+        if (chunks <= 128) return f(Shape<64, 2>{});
+        if (chunks <= 256) return f(Shape<256, 1>{});
+        if (chunks <= 512) return f(Shape<256, 2>{});
+        if (chunks <= 1024) return f(Shape<1024, 1>{});
         return f(Shape<1024, 2>{});
     }
 }
 
 // Workgroups of the backward pass, each with a row of partial sums.
-constexpr int64_t kBackGroups = 1024;
-int64_t back_groups(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(kBackGroups, rows / 16)); }
+constexpr int64_t kBackGroups = 512, kBackRows = 8;   // at most, and rows for each at least (1,024: 62 us, not 54)
+int64_t back_groups(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(kBackGroups, rows / kBackRows)); }
 
 }  // namespace
 
@@ -275,7 +307,7 @@ int run_layer_norm(const NormArgs &a, hipStream_t s) {
             constexpr int threads = shape.lpr > kNormThreads ? shape.lpr : kNormThreads;
             const int64_t want = ceil_div(a.rows, threads / shape.lpr);
             const auto grid = static_cast<unsigned>(std::min<int64_t>(want, kMaxGroups));
-            k_norm<T, shape.lpr, shape.nch><<<grid, threads, 0, s>>>(a);
+            k_norm<T, shape.lpr, shape.nch, shape.whole><<<grid, threads, 0, s>>>(a);
             W2V_LAUNCH_CHECK("k_norm");
             return static_cast<int>(W2V_OK);
         });
@@ -295,7 +327,7 @@ int run_layer_norm_backward(const NormArgs &a, void *workspace, hipStream_t s) {
             using T = decltype(zero);
             return with_shape<T>(a.dim, [&](auto shape) {
                 constexpr int threads = shape.lpr > kNormThreads ? shape.lpr : kNormThreads;
-                k_norm_back<T, shape.lpr, shape.nch><<<static_cast<unsigned>(groups), threads, 0, s>>>(a, part);
+                k_norm_back<T, shape.lpr, shape.nch, shape.whole><<<static_cast<unsigned>(groups), threads, 0, s>>>(a, part);
                 W2V_LAUNCH_CHECK("k_norm_back");
                 return static_cast<int>(W2V_OK);
             });

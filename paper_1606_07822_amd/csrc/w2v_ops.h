@@ -39,22 +39,33 @@ __device__ __forceinline__ void store_pack(T *p, const float (&f)[N]) {
     *reinterpret_cast<Pack<T, N> *>(p) = u;
 }
 
-// The same for the columns from `col` of a row of dim elements; columns past it read as zeros and are not written.
-template <class T, int N>
-__device__ __forceinline__ void load_cols(const T *row, int col, int dim, float (&f)[N]) {
-    if (col + N <= dim) {
-        load_pack<T, N>(row + col, f);
-    } else {
+// The same for the columns from `col` of a row of dim elements; columns past it read as zeros and are not written. WHOLE:
+// dim and col are multiples of N.
+template <class T, int N, bool WHOLE = false>
+__device__ __forceinline__ Pack<T, N> raw_cols(const T *row, int col, int dim) {
+    Pack<T, N> u{};
+    if (WHOLE ? col < dim : col + N <= dim) {
+        u = *reinterpret_cast<const Pack<T, N> *>(row + col);
+    } else if (!WHOLE) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = col + e < dim ? static_cast<float>(row[col + e]) : 0.0f;
+        for (int e = 0; e < N; ++e)
+            if (col + e < dim) u.v[e] = row[col + e];
     }
+    return u;
 }
 
-template <class T, int N>
+template <class T, int N, bool WHOLE = false>
+__device__ __forceinline__ void load_cols(const T *row, int col, int dim, float (&f)[N]) {
+    const Pack<T, N> u = raw_cols<T, N, WHOLE>(row, col, dim);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = static_cast<float>(u.v[e]);
+}
+
+template <class T, int N, bool WHOLE = false>
 __device__ __forceinline__ void store_cols(T *row, int col, int dim, const float (&f)[N]) {
-    if (col + N <= dim) {
+    if (WHOLE ? col < dim : col + N <= dim) {
         store_pack<T, N>(row + col, f);
-    } else {
+    } else if (!WHOLE) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if (col + e < dim) row[col + e] = static_cast<T>(f[e]);
