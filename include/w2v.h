@@ -369,9 +369,11 @@ typedef enum { W2V_F32 = 0, W2V_BF16 = 1, W2V_F16 = 2 } w2v_type;
 
 /* Layer norm: mean = sum x / dim, rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps),
    y = (x - mean) rstd weight + bias.
-     x, y        rows x dim elements of type; y may be x
+     x, y        rows x dim elements of type; y may be x (the same rows, with
+                 the same stride), and may not overlap it otherwise
      weight, bias  dim elements of w_type (W2V_F32 or type), each may be NULL (1, 0)
      mean, rstd  float[rows] out, each may be NULL
+   With eps 0 a row of equal values has no finite rstd, and its y is NaN.
    Errors: W2V_E_ARG for rows < 0, dim not in 1..16384, a short stride, eps
    that is negative or not finite, an unknown type or a NULL required pointer. */
 int w2v_layer_norm(const void *x, int32_t type, int64_t rows, int32_t dim, int64_t x_stride, const void *weight,
@@ -402,7 +404,7 @@ int w2v_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
    read into any sum. A target outside the vocabulary, or one whose code is
    longer than max_code_len (w2v_build_huffman's max_len_host, 1..64), has the
    loss NaN and no gradient. Of m: V, dim, row_stride, syn1 and the Huffman
-   arrays; the others are not used. dsyn1 may not be m->syn1. Errors:
+   arrays; the others are not used. dx may not overlap x, nor dsyn1 m->syn1. Errors:
    W2V_E_ARG, W2V_E_WORKSPACE (the workspace is needed with dsyn1 only). */
 size_t w2v_hs_loss_workspace_bytes(const w2v_model *m, int32_t max_code_len, int64_t rows);
 int w2v_hs_loss(const w2v_model *m, int32_t max_code_len, const void *x, int32_t type, int64_t rows, int64_t x_stride,
@@ -421,7 +423,8 @@ int w2v_hs_loss(const w2v_model *m, int32_t max_code_len, const void *x, int32_t
    (1 + (c % 16) / 16) 2^(c / 16 - 15). m is rounded to nearest, sqrt(v) up or
    down in proportion by a hash of (seed, t, place of the moment), a positive
    one never to 0. A block with a moment that is not finite stays not finite.
-   All zeros is the state before the first step in either form. */
+   All zeros is the state before the first step in either form. With eps 0 a
+   parameter whose gradients were all zero becomes NaN. */
 typedef struct {
     void *param;              /* rows x cols elements of param_type */
     const void *grad;         /* rows x cols elements of grad_type */

@@ -727,12 +727,18 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     return dx, dweight, dbias
 
 
+def _tree_of(model: Model) -> Tree:
+    if model.tree is None:
+        raise ValueError("the model has no Huffman tree")
+    return model.tree
+
+
 def hs_loss_workspace(model: Model, x: torch.Tensor, grads: bool = True) -> torch.Tensor | None:
     """A workspace for hs_loss on x's rows, to be kept from call to call (calls that overlap need one each)."""
     if not grads:
         return None
     cm = model.c()
-    return _workspace(lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), model.tree.max_len, x.shape[0]), x.device)
+    return _workspace(lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), _tree_of(model).max_len, x.shape[0]), x.device)
 
 
 def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor | None = None,
@@ -743,7 +749,7 @@ def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch
     the gradients of sum(weights * loss) for x [rows, dim] and for model.syn1 (dsyn1 float32 of syn1's shape, all rows
     written: their first dim columns, and zeros perhaps in the padding). targets int32, negative: none. Does not sync."""
     xp, xs = _rows_ptr(x, "x", x)
-    kind = _type_of(x, "x")
+    kind, longest = _type_of(x, "x"), _tree_of(model).max_len
     n, dev = x.shape[0], x.device
     if x.shape[1] != model.dim:
         raise ValueError(f"x must have {model.dim} columns, got {x.shape[1]}")
@@ -765,8 +771,8 @@ def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch
     with _On(dev):
         ws = None
         if grads:
-            ws = _kept(workspace, lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), model.tree.max_len, n), dev)
-        _check(lib().w2v_hs_loss(ctypes.byref(cm), model.tree.max_len, xp, kind, n, xs, tp, wp,
+            ws = _kept(workspace, lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), longest, n), dev)
+        _check(lib().w2v_hs_loss(ctypes.byref(cm), longest, xp, kind, n, xs, tp, wp,
                                  _vector_ptr(loss, torch.float32, n, dev, "loss"), dxp, dxs or 0, dsp,
                                  dsyn1.stride(0) if grads else 0, None if ws is None else ws.data_ptr(),
                                  0 if ws is None else ws.numel(), _stream(dev)))
@@ -897,7 +903,7 @@ class BatchState:
         ptr = [t.data_ptr() if t is not None else None
                for t in (self.gain, self.bias, self.m, self.v, self.m_scale, self.v_scale)]
         cb = CBatchParams(*ptr, self.betas[0], self.betas[1], self.eps, self.steps, self.norm_eps, self.weight_decay,
-                          self.bits, model.tree.max_len, self.seed & 0xFFFFFFFF, 0)
+                          self.bits, _tree_of(model).max_len, self.seed & 0xFFFFFFFF, 0)
         if self.m is not None:
             cm = model.c()
             if lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != self.n_moments:

@@ -47,6 +47,38 @@ __device__ __forceinline__ int path_len(const Tree &t, int32_t v) {
     return len <= t.longest ? len : 0;
 }
 
+// ------------------------------------------------------------------ zeros
+// Rows set to zero by workgroups of kFillThreads threads, a group each. Sorting leaves memory idle, so its launches have
+// such workgroups behind their own (65,536 rows, 1M rows of 300 floats: TODO).
+constexpr int kFillThreads = 1024;
+constexpr int kFillFloats = kFillThreads * 4 * 8;   // of a group, whole rows
+constexpr int kFillRows = kFillThreads / kWave * 4;   // of a group, rows without their padding
+struct Fill {
+    float *p;
+    int64_t rows, stride;
+    int32_t dim, whole;   // whole: with their padding, as one array
+    int64_t first;        // group of this launch's first filling workgroup
+};
+
+__device__ __forceinline__ void fill_group(const Fill &f, int64_t group) {
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (f.whole) {
+        const int64_t n = f.rows * f.stride, lo = group * kFillFloats, at = lo + threadIdx.x * 4;
+        if (lo + kFillFloats <= n) {
+#pragma unroll
+            for (int u = 0; u < kFillFloats / kFillThreads; u += 4) store_pack<float, 4>(f.p + at + u * kFillThreads, zero);
+        } else {
+            for (int64_t i = lo + threadIdx.x; i < n; i += kFillThreads) f.p[i] = 0.0f;
+        }
+        return;
+    }
+    const int64_t end = min(f.rows, (group + 1) * kFillRows);
+    for (int64_t r = group * kFillRows + threadIdx.x / kWave; r < end; r += kFillThreads / kWave)
+        for (int c = lane_id() * 4; c < f.dim; c += kWave * 4) store_cols<float, 4>(f.p + r * f.stride, c, f.dim, zero);
+}
+
+__global__ __launch_bounds__(kFillThreads) void k_hs_zero(Fill f) { fill_group(f, f.first + blockIdx.x); }
+
 // ------------------------------------------------------------------ order
 // A row of the batch, its target and what is needed of that word's path.
 struct Item {
@@ -94,7 +126,11 @@ constexpr int kRankWaves = kRankThreads / kWave;
 template <class K, int R>
 __global__ __launch_bounds__(kRankThreads) void k_hs_rank(Tree t, const int32_t *__restrict__ targets, int32_t n,
                                                           K *__restrict__ key_out, int32_t *__restrict__ row_out,
-                                                          Item *__restrict__ item_out) {
+                                                          Item *__restrict__ item_out, int32_t ranking, Fill fill) {
+    if (static_cast<int32_t>(blockIdx.x) >= ranking) {
+        fill_group(fill, fill.first + blockIdx.x - ranking);
+        return;
+    }
     __shared__ __align__(16) K keys[kSortBlock];
     __shared__ int32_t counts[kRankWaves][R];
     constexpr int kGroups = kSortBlock / R, kSets = R / kWave;
@@ -157,7 +193,11 @@ constexpr int kMergeBlocks = kMergeParts * kMergePer;
 template <class K>
 __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict__ key_in,
                                                             const int32_t *__restrict__ row_in, int32_t n,
-                                                            int32_t *__restrict__ row_out) {
+                                                            int32_t *__restrict__ row_out, int32_t merging, Fill fill) {
+    if (static_cast<int32_t>(blockIdx.x) >= merging) {
+        fill_group(fill, fill.first + blockIdx.x - merging);
+        return;
+    }
     __shared__ K keys[kMergeBlocks * kSortBlock];
     __shared__ int32_t counts[kMergeParts][kMergeKeys];
     const int slot = static_cast<int>(threadIdx.x) % kMergeKeys, part = static_cast<int>(threadIdx.x) / kMergeKeys;
@@ -705,33 +745,6 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void k_hs_join(JoinArgs a) {
     }
 }
 
-// The first dim columns of the rows set to zero, a wavefront a row.
-constexpr int kZeroThreads = 256;
-__global__ __launch_bounds__(kZeroThreads) void k_hs_zero(float *p, int64_t rows, int32_t dim, int64_t stride) {
-    const int64_t step = static_cast<int64_t>(gridDim.x) * (kZeroThreads / kWave);
-    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kZeroThreads / kWave) + threadIdx.x / kWave; r < rows; r += step)
-        for (int c = lane_id() * 4; c < dim; c += kWave * 4) store_cols<float, 4>(p + r * stride, c, dim, zero);
-}
-
-// n floats set to zero, kZeroPer vectors a thread.
-constexpr int kZeroPer = 4;
-__global__ __launch_bounds__(kZeroThreads) void k_hs_zero_flat(float *p, int64_t n) {
-    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int64_t kGroup = kZeroThreads * kZeroPer * 4;
-    for (int64_t g = blockIdx.x * kGroup; g < n; g += gridDim.x * kGroup) {
-        const int64_t i = g + threadIdx.x * 4;
-        if (g + kGroup <= n) {
-#pragma unroll
-            for (int u = 0; u < kZeroPer; ++u) store_pack<float, 4>(p + i + u * kZeroThreads * 4, zero);
-        } else {
-            for (int u = 0; u < kZeroPer; ++u)
-                for (int e = 0; e < 4; ++e)
-                    if (i + u * kZeroThreads * 4 + e < n) p[i + u * kZeroThreads * 4 + e] = 0.0f;
-        }
-    }
-}
-
 struct Buffers {
     void *keys;
     int32_t *row0, *row1;
@@ -786,43 +799,67 @@ void launch_walk(const WalkArgs &w, bool grads, hipStream_t s) {
         k_hs_walk<T, NE, false, 1><<<grid, kWalkThreads, 0, s>>>(w);
 }
 
-// whole: the rows' padding may be written too. Rows that end inside a 128-byte line cost memory a read for the rest of
-// it (1M rows of 300 floats, 320 apart: 329 us, 193 with the padding), so short padding is then written with them.
-int zero_rows(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole, hipStream_t s) {
-    if (whole && stride - dim < 32) {
-        const int64_t n = rows * stride;
-        const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(n, kZeroThreads * kZeroPer * 4), kMaxGroups));
-        k_hs_zero_flat<<<grid, kZeroThreads, 0, s>>>(p, n);
-        W2V_LAUNCH_CHECK("k_hs_zero_flat");
-        return W2V_OK;
+// The groups of a filling, none for rows that hold an earlier slab's sums. whole: the rows' padding may be written too.
+// Rows that end inside a 128-byte line cost memory a read for the rest of it (1M rows of 300 floats, 320 apart: 329 us,
+// 204 with the padding), so short padding is then written with them.
+struct Zeros {
+    Fill fill{};
+    int64_t groups = 0;
+    Zeros() = default;
+    Zeros(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole) {
+        fill = Fill{p, rows, stride, dim, whole && stride - dim < 32 ? 1 : 0, 0};
+        groups = fill.whole ? ceil_div(rows * stride, kFillFloats) : ceil_div(rows, kFillRows);
     }
-    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows, kZeroThreads / kWave), 64LL * device_cu_count()));
-    k_hs_zero<<<grid, kZeroThreads, 0, s>>>(p, rows, dim, stride);
-    W2V_LAUNCH_CHECK("k_hs_zero");
+    // The next of them, at most `most`.
+    unsigned take(int64_t most, Fill *part) {
+        *part = fill;
+        const int64_t n = std::min(groups, most);
+        fill.first += n;
+        groups -= n;
+        return static_cast<unsigned>(n);
+    }
+};
+constexpr int64_t kFillLaunch = int64_t(1) << 20;   // groups of one launch
+
+int zero_rows(Zeros z, hipStream_t s) {
+    while (z.groups > 0) {
+        Fill part;
+        const unsigned n = z.take(kFillLaunch, &part);
+        k_hs_zero<<<n, kFillThreads, 0, s>>>(part);
+        W2V_LAUNCH_CHECK("k_hs_zero");
+    }
     return W2V_OK;
 }
 
-// Sorts n <= kSlab rows by their targets' keys.
+// Sorts n <= kSlab rows by their targets' keys, and sets z's rows to zero.
 template <class K>
-int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, hipStream_t s) {
-    const auto sort_blocks = static_cast<unsigned>(ceil_div(n, kSortBlock));
-    Item *now = n <= kSortBlock ? b.items : nullptr;
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, Zeros z, const Buffers &b, hipStream_t s) {
+    static_assert(kFillThreads == kRankThreads && kFillThreads == kMergeThreads);
+    const bool one = n <= kSortBlock;   // the ranks are the order
+    Item *now = one ? b.items : nullptr;
     K *keys = static_cast<K *>(b.keys);
+    Fill part;
+    unsigned filling = z.take(std::min(kFillLaunch, one ? z.groups : z.groups / 2), &part);
+    const auto ranking = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / (n <= kRankNarrow ? 64 : 256)));
     if (n <= kRankNarrow)
-        k_hs_rank<K, 64><<<sort_blocks * (kSortBlock / 64), kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now);
+        k_hs_rank<K, 64><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now,
+                                                                  static_cast<int32_t>(ranking), part);
     else
-        k_hs_rank<K, 256><<<sort_blocks * (kSortBlock / 256), kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now);
+        k_hs_rank<K, 256><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now,
+                                                                   static_cast<int32_t>(ranking), part);
     W2V_LAUNCH_CHECK("k_hs_rank");
-    if (now) return W2V_OK;
-    k_hs_merge<K><<<static_cast<unsigned>(ceil_div(n, kMergeKeys)), kMergeThreads, 0, s>>>(keys, b.row0, n, b.row1);
+    if (one) return zero_rows(z, s);
+    filling = z.take(kFillLaunch, &part);
+    const auto merging = static_cast<unsigned>(ceil_div(n, kMergeKeys));
+    k_hs_merge<K><<<merging + filling, kMergeThreads, 0, s>>>(keys, b.row0, n, b.row1, static_cast<int32_t>(merging), part);
     W2V_LAUNCH_CHECK("k_hs_merge");
     k_hs_items<<<static_cast<unsigned>(ceil_div(n, 256)), 256, 0, s>>>(t, targets, b.row1, n, b.items);
     W2V_LAUNCH_CHECK("k_hs_items");
-    return W2V_OK;
+    return zero_rows(z, s);
 }
 
-int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Buffers &b, hipStream_t s) {
-    return t.longest <= 31 ? sort_rows<uint32_t>(t, targets, n, b, s) : sort_rows<uint64_t>(t, targets, n, b, s);
+int sort_rows(const Tree &t, const int32_t *targets, int32_t n, const Zeros &z, const Buffers &b, hipStream_t s) {
+    return t.longest <= 31 ? sort_rows<uint32_t>(t, targets, n, z, b, s) : sort_rows<uint64_t>(t, targets, n, z, b, s);
 }
 
 template <int R, int C>
@@ -893,17 +930,19 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
     const Tree t{a.V, a.longest, a.codelen, a.code, a.point_off, a.points};
     const bool grads = a.dx || a.dsyn1;
     Buffers b{};
+    Zeros zeros;
     if (a.dsyn1) {
         Carve c(workspace);
         b = carve(c, a.rows, a.dim, a.longest);
-        if (int rc = zero_rows(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, a.dsyn1_stride == a.stride, s)) return rc;
+        zeros = Zeros(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, a.dsyn1_stride == a.stride);
+        if (a.rows == 0) return zero_rows(zeros, s);
     }
     for (int64_t lo = 0; lo < a.rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, a.rows - lo));
         const int32_t *targets = a.targets + lo;
         const char *x = static_cast<const char *>(a.x) + lo * a.x_stride * type_bytes(a.type);
         if (a.dsyn1)
-            if (int rc = sort_rows(t, targets, n, b, s)) return rc;
+            if (int rc = sort_rows(t, targets, n, lo == 0 ? zeros : Zeros(), b, s)) return rc;
         WalkArgs w{};
         w.t = t;
         w.syn1 = a.syn1;
@@ -951,10 +990,11 @@ int run_word_sums(const int32_t *words, const float *x, int64_t rows, int32_t di
     const Tree t{V, 1, nullptr, nullptr, nullptr, nullptr};
     Carve c(workspace);
     const Buffers b = carve(c, rows, dim, 1);
-    if (int rc = zero_rows(out, V, dim, out_stride, true, s)) return rc;
+    const Zeros zeros(out, V, dim, out_stride, true);
+    if (rows == 0) return zero_rows(zeros, s);
     for (int64_t lo = 0; lo < rows; lo += kSlab) {
         const auto n = static_cast<int32_t>(std::min<int64_t>(kSlab, rows - lo));
-        if (int rc = sort_rows(t, words + lo, n, b, s)) return rc;
+        if (int rc = sort_rows(t, words + lo, n, lo == 0 ? zeros : Zeros(), b, s)) return rc;
         const NodeArgs m{t, b.items, n, dim, x + lo * x_stride, x_stride, nullptr, b.part[0],
                          b.node[0], b.borders[0], out, out_stride, lo > 0 ? 1 : 0, 1};
         if (int rc = sum_rows(m, W2V_F32, b, s)) return rc;

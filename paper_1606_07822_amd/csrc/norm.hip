@@ -306,7 +306,7 @@ int run_layer_norm(const NormArgs &a, hipStream_t s) {
         return with_shape<T>(a.dim, [&](auto shape) {
             constexpr int threads = shape.lpr > kNormThreads ? shape.lpr : kNormThreads;
             const int64_t want = ceil_div(a.rows, threads / shape.lpr);
-            const auto grid = static_cast<unsigned>(std::min<int64_t>(want, kMaxGroups));
+            const auto grid = static_cast<unsigned>(std::min<int64_t>(want, kMaxGroups * kNormThreads / threads));
             k_norm<T, shape.lpr, shape.nch, shape.whole><<<grid, threads, 0, s>>>(a);
             W2V_LAUNCH_CHECK("k_norm");
             return static_cast<int>(W2V_OK);
