@@ -49,7 +49,8 @@ __device__ __forceinline__ int path_len(const Tree &t, int32_t v) {
 
 // ------------------------------------------------------------------ zeros
 // Rows set to zero by workgroups of kFillThreads threads, a group each. Sorting leaves memory idle, so its launches have
-// such workgroups behind their own (65,536 rows, 1M rows of 300 floats: TODO).
+// such workgroups behind their own (65,536 rows, 1M rows of 300 floats: 458 -> 443 us in all; in the walk as well, which
+// needs memory itself, 456).
 constexpr int kFillThreads = 1024;
 constexpr int kFillFloats = kFillThreads * 4 * 8;   // of a group, whole rows
 constexpr int kFillRows = kFillThreads / kWave * 4;   // of a group, rows without their padding
@@ -311,7 +312,7 @@ struct WalkArgs {
     int32_t block_rows;
 };
 
-constexpr int kWalkThreads = 256;
+constexpr int kWalkThreads = 64;   // a wavefront a workgroup: 65,536 rows of 200, 184 -> 181 us in all against four
 
 // What a node adds for s z (sz) at the lane: e = exp(-|z|) into the product of 1 + e, whose logarithm is the path's sum
 // of log(1 + e) (at most 2^64), and the rest of the loss; the value is sigmoid(-s z).
@@ -873,10 +874,10 @@ int sum_rows(NodeArgs m, int32_t type, const Buffers &b, hipStream_t s) {
     const auto blocks = static_cast<int32_t>(ceil_div(m.n, rb));
     const int per = columns <= 5 ? columns : 4;   // columns of a lane
     m.tiles = static_cast<int32_t>(ceil_div(columns, per));
-    // the levels shared out while that gives a SIMD no more than four wavefronts
+    // the levels shared out while that gives a SIMD no more than ten wavefronts (65,536 rows of 200: 184 -> 173 us in all)
     const int64_t waves = static_cast<int64_t>(blocks) * m.tiles;
     const int most = std::min(kLevelWaves, kNodeWaves / m.tiles);
-    const int parts = waves * most <= 16LL * device_cu_count() ? most : 1;
+    const int parts = waves * most <= 40LL * device_cu_count() ? most : 1;
     const auto threads = static_cast<unsigned>(m.tiles * parts * kWave);
     const size_t lds = static_cast<size_t>(m.t.longest) * rb * (m.coef ? 8 : 4);
     (void)with_type(type, [&](auto zero) {
