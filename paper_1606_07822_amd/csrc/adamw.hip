@@ -51,12 +51,14 @@ struct Place {
 
 // The plan's memory: this header, the entries, the chunks' places.
 struct Header {
+    uint64_t mark;   // kMark in a plan that was built: a step on other memory does nothing
     int64_t n_chunks;
     const Entry *entries;
     const Place *places;
     Scalars scalars;   // of the last step whose learning rate or step count lay in device memory
 };
 constexpr size_t kHeaderBytes = 256;
+constexpr uint64_t kMark = 0x6e616c7077616461ull;
 static_assert(sizeof(Header) <= kHeaderBytes);
 
 __host__ __device__ inline uint32_t mix32(uint32_t h) {   // MurmurHash3's finaliser
@@ -82,7 +84,7 @@ __host__ __device__ inline Scalars make_scalars(const w2v_adamw_params &p, doubl
 }
 
 __global__ void k_adamw_scalars(Header *h, w2v_adamw_params p) {
-    h->scalars = make_scalars(p, p.lr_device ? static_cast<double>(*p.lr_device) : p.lr,
+    if (h->mark == kMark) h->scalars = make_scalars(p, p.lr_device ? static_cast<double>(*p.lr_device) : p.lr,
                               p.step_device ? *p.step_device : p.step);
 }
 
@@ -338,6 +340,7 @@ __device__ __forceinline__ void chunk_update(const Entry &t, int64_t first, void
 template <int BITS>
 __global__ __launch_bounds__(kAdamThreads) void k_adamw(const Header *__restrict__ h, int64_t n_chunks, void *mv, void *vv,
                                                         float *m_scale, float *v_scale, Scalars given, int32_t device_scalars) {
+    if (h->mark != kMark) return;
     const int64_t n = min(n_chunks, h->n_chunks);
     const Scalars s = device_scalars ? h->scalars : given;
     for (int64_t b = blockIdx.x; b < n; b += gridDim.x) {
@@ -417,6 +420,7 @@ int run_adamw_plan(const w2v_adamw_tensor *t, int32_t n, void *plan, hipStream_t
     Entry *entries = c.take<Entry>(static_cast<size_t>(n));
     Place *places = c.take<Place>(static_cast<size_t>(chunks));
     Header h{};
+    h.mark = kMark;
     h.n_chunks = chunks;
     h.entries = entries;
     h.places = places;

@@ -158,6 +158,48 @@ def test_documents_and_batches_that_cut_windows(w2v):  # noqa: F811
         within(model.syn0[:, :8], torch.from_numpy(want[0]), torch.full((counts.size, 8), off, dtype=torch.float64), "syn0")
 
 
+def test_a_batch_of_many_blocks(w2v):  # noqa: F811
+    """One batch of some 75,000 centres (more than one slab of the sums, by word and by node): m after one step is
+    (1 - b1) times the gradient."""
+    import torch
+    counts = zipf_counts(50)
+    n, dim = 80_000, 4
+    tok = text(counts, n, 7)
+    model, otree = make_model(w2v, counts, dim)
+    syn0, syn1 = model.syn0[:, :dim].double().cpu().numpy(), model.syn1[:, :dim].double().cpu().numpy()
+    p = w2v.Params(window=2, arch=1, doc_len=1000, corpus_tokens=n, sync_batch=1 << 17, alpha0=1e-3)
+    s = w2v.sample_pairs(torch.from_numpy(tok).cuda(), counts.size, torch.from_numpy(counts).cuda(), int(counts.sum()), p,
+                         cap=4 * n, want_mask=True)
+    centre, context = s.centre.cpu().numpy(), s.context.cpu().numpy()
+    rows, first, size = np.unique(centre, return_index=True, return_counts=True)
+    place = np.repeat(np.arange(rows.size), size)
+    h = np.zeros((rows.size, dim))
+    np.add.at(h, place, syn0[tok[context]])
+    h /= size[:, None]
+    g1, dh, mag1 = np.zeros_like(syn1), np.zeros_like(h), np.zeros_like(syn1)
+    word = tok[rows]
+    for t in np.unique(word):
+        at = np.nonzero(word == t)[0]
+        for j, node in enumerate(otree.points[otree.point_off[t]:otree.point_off[t + 1]]):
+            turn = (int(otree.code[t]) >> j) & 1
+            g = 1 / (1 + np.exp(-(h[at] @ syn1[node]))) - (1 - turn)
+            dh[at] += g[:, None] * syn1[node]
+            g1[node] += g @ h[at]
+            mag1[node] += np.abs(g) @ np.abs(h[at])
+    g0, mag0 = np.zeros_like(syn0), np.zeros_like(syn0)
+    np.add.at(g0, tok[context], (dh / size[:, None])[place])
+    np.add.at(mag0, tok[context], np.abs(dh / size[:, None])[place])
+    state = w2v.BatchState(model, norm=False, betas=(B1, B2))
+    _, total, terms = w2v.train_batch_epoch(model, torch.from_numpy(tok).cuda(), p, state)
+    kept = int(s.keep_mask.sum())
+    assert terms == rows.size > 65536 and state.steps == 1
+    # a term is off by 60 U or so, the sums (32 rows, 16 and 256 blocks, two slabs) by 400 U of their magnitude at most
+    as_t = torch.from_numpy
+    for lo, want, mag in ((0, g0, mag0), (-(-g0.size // 256) * 256, g1, mag1)):
+        got = state.m[lo:lo + want.size].view(want.shape).double().cpu() / (1 - B1) * kept
+        within(got, as_t(want), as_t(500 * U * mag), "gradient")
+
+
 def test_empty_and_all_dropped_texts(w2v):  # noqa: F811
     import torch
     counts = zipf_counts(40)

@@ -182,6 +182,49 @@ def test_norm_backward(w2v, n, d, name):
         assert torch.equal(again[1], dw) and torch.equal(again[2], db) and torch.equal(again[0], dx)
 
 
+def test_norm_of_more_than_2_to_32_elements(w2v):
+    """The last rows of an array whose elements need 33 bits to count."""
+    import torch
+    n, d = 2**32 // 16384 + 64, 16384
+    x = torch.empty(n, d, dtype=torch.bfloat16, device="cuda")
+    x[-80:].normal_(generator=torch.Generator(device="cuda").manual_seed(3))
+    x[:-80].fill_(1.0)
+    y, mean, rstd = w2v.layer_norm(x, out=x.clone())
+    want, m64, r64, h = norm_reference(x[-80:], None, None, 1e-5)
+    off = (45 * U * x[-80:].double().cpu().abs().mean(1) * r64)[:, None]
+    fp32 = off + h.abs() * (off**2 + 30 * U)
+    within(y[-80:], want, fp32 + (want.abs() + fp32) * 2.0**-8, "y")
+    dx, _, _ = w2v.layer_norm_backward(x, x, None, mean, rstd, dx=y)
+    a = x[-80:].double().cpu()
+    want = r64[:, None] * (a - a.mean(1, keepdim=True) - h * (a * h).mean(1, keepdim=True))
+    # the kernel's own mean and rstd, off by 45 U and 28 U, and the bounds of the backward pass's sums
+    fp32 = 200 * U * r64[:, None] * (1 + a.abs()) * (1 + h.abs())
+    within(dx[-80:], want, fp32 + (want.abs() + fp32) * 2.0**-8, "dx")
+
+
+def test_norm_outputs_one_by_one(w2v):
+    """The C calls without statistics, with one of the two weight gradients."""
+    import torch
+    x, dy, w, b = norm_inputs(50, 130, torch.float32, 130, 0)
+    y, mean, rstd = w2v.layer_norm(x, w, b)
+    dx, dw, db = w2v.layer_norm_backward(dy, x, w, mean, rstd)
+    s, L = torch.cuda.current_stream().cuda_stream, w2v.lib()
+    alone = torch.zeros_like(x)
+    assert L.w2v_layer_norm(x.data_ptr(), 0, 50, 130, 130, w.data_ptr(), b.data_ptr(), 0, 1e-5, alone.data_ptr(), 130, None,
+                            None, s) == w2v.W2V_OK
+    assert torch.equal(alone, y)
+    ws = torch.empty(L.w2v_layer_norm_backward_workspace_bytes(50, 130), dtype=torch.uint8, device="cuda")
+    for which in (0, 1, 2):
+        out, sums = torch.zeros_like(x), torch.zeros(2, 130, device="cuda")
+        rc = L.w2v_layer_norm_backward(
+            dy.data_ptr(), 130, x.data_ptr(), 0, 50, 130, 130, w.data_ptr(), 0, mean.data_ptr(), rstd.data_ptr(), out.data_ptr(),
+            130, sums[0].data_ptr() if which == 1 else None, sums[1].data_ptr() if which == 2 else None,
+            ws.data_ptr() if which else None, ws.numel() if which else 0, s)
+        assert rc == w2v.W2V_OK and torch.equal(out, dx)
+        assert torch.equal(sums[0], dw) if which == 1 else not sums[0].any()
+        assert torch.equal(sums[1], db) if which == 2 else not sums[1].any()
+
+
 def test_norm_backward_against_differences(w2v):
     """dx, dweight and dbias as slopes of sum(dy y): a central difference of the forward kernel, h = 2^-5."""
     import torch
@@ -322,6 +365,16 @@ def test_loss_many_rows(w2v, n):
     rng = np.random.default_rng(n)
     model, otree = make_model(w2v, counts, 6)
     check_loss(w2v, model, otree, hidden(n, 6, torch.float32), draw_targets(rng, counts, n), None)
+
+
+@pytest.mark.parametrize("n,dim,name", [(8192, 130, "bf16"), (8195, 300, "f32"), (8193, 65, "f16"), (8200, 700, "f16")])
+def test_loss_rows_that_share_a_walk(w2v, n, dim, name):
+    """Four sorted rows a wavefront: their common levels together, then each row's own; and rows too wide for that."""
+    counts = COUNTS["zipf"]()
+    rng = np.random.default_rng(n)
+    model, otree = make_model(w2v, counts, dim)
+    check_loss(w2v, model, otree, hidden(n, dim, kind(name), dim + 3, 1), draw_targets(rng, counts, n),
+               rng.random(n, dtype=np.float32) / n, name)
 
 
 @pytest.mark.parametrize("n", [65, 1023, 1025, 2049, 5000])
@@ -505,6 +558,60 @@ def test_loss_against_differences(w2v):
         assert abs(slope - quotient) <= rounding + h * h / 6 * 12**3 / 8 * nodes * 0.5
 
 
+def test_loss_of_a_table_past_4_gigabytes(w2v):
+    """Inner nodes whose rows lie more than 2^32 bytes into the tables (the root's is the last of all)."""
+    import torch
+    v, dim, n = 1_100_000, 1000, 150
+    counts = torch.full((v,), 7, dtype=torch.int64, device="cuda")
+    tree = w2v.build_huffman(counts)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    syn1 = torch.empty(v - 1, 1024, device="cuda").normal_(generator=g).mul_(0.05)
+    model = w2v.Model(torch.empty(v, 1024, device="cuda"), syn1, dim, counts, 7 * v, tree)
+    x = torch.randn(n, dim, generator=g, device="cuda")
+    targets = torch.randint(0, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+    loss, dx, dsyn1 = w2v.hs_loss(model, x, targets)
+    off, length = tree.point_off.cpu().numpy(), tree.codelen.cpu().numpy()
+    code, points = tree.code.cpu().numpy(), tree.points.cpu().numpy()
+    want = torch.zeros(v - 1, dtype=torch.bool, device="cuda")
+    total = torch.zeros(dim, dtype=torch.float64, device="cuda")
+    for i, t in enumerate(targets.tolist()):
+        nodes = torch.from_numpy(points[off[t]:off[t] + length[t]].astype(np.int64)).cuda()
+        s = torch.from_numpy(1.0 - 2.0 * ((code[t] >> np.arange(length[t])) & 1)).cuda()
+        rows, row = syn1[nodes, :dim].double(), x[i].double()
+        z = rows @ row
+        z_off = 24 * U * (rows.abs() @ row.abs())
+        value = torch.nn.functional.softplus(-s * z).sum()
+        within(loss[i], value, (z_off + 8 * U).sum() + 6 * U * value, "loss")
+        grad = -s * torch.sigmoid(-s * z)
+        within(dx[i], grad @ rows, (z_off / 4 + 30 * U) @ rows.abs(), "dx")
+        want[nodes] = True
+        root = int((nodes == v - 2).nonzero()[0])
+        total += grad[root] * row
+    within(dsyn1[v - 2, :dim], total, 400 * U * x.double().abs().sum(0), "the root's gradient")
+    assert bool((dsyn1[:, :dim].abs().amax(1) > 0).eq(want).all())
+
+
+def test_loss_outputs_one_by_one(w2v):
+    """Each of the C call's outputs may be left out; the others are the same bits."""
+    import ctypes
+    import torch
+    counts = COUNTS["zipf"]()
+    rng = np.random.default_rng(12)
+    model, _ = make_model(w2v, counts, 24)
+    x, t = hidden(300, 24, torch.float32), torch.from_numpy(draw_targets(rng, counts, 300)).cuda()
+    loss, dx, dsyn1 = w2v.hs_loss(model, x, t)
+    cm, ws = model.c(), w2v.hs_loss_workspace(model, x)
+    for keep in (0, 1, 2, 3, 4, 5, 6):
+        a, b, c = torch.zeros_like(loss), torch.zeros_like(dx), torch.zeros_like(dsyn1)
+        rc = w2v.lib().w2v_hs_loss(
+            ctypes.byref(cm), model.tree.max_len, x.data_ptr(), 0, 300, 24, t.data_ptr(), None, a.data_ptr() if keep & 1 else None,
+            b.data_ptr() if keep & 2 else None, 24, c.data_ptr() if keep & 4 else None, c.stride(0),
+            ws.data_ptr() if keep & 4 else None, ws.numel() if keep & 4 else 0, torch.cuda.current_stream().cuda_stream)
+        assert rc == w2v.W2V_OK, w2v.last_error()
+        for bit, got, full in ((1, a, loss), (2, b, dx), (4, c[:, :24], dsyn1[:, :24])):
+            assert torch.equal(got, full) if keep & bit else not got.any(), (keep, bit)
+
+
 # ------------------------------------------------------------------ AdamW
 B1, B2, EPS = 0.9, 0.999, 1e-8
 
@@ -669,6 +776,37 @@ def test_adamw_eight_bits_root_is_unbiased_and_never_lost(w2v):
     opt = w2v.AdamW([p], [g], bits=8)
     opt.step(1, 1e-3)
     assert bool((opt.v > 0).all()) and p.abs().max().item() <= 1.01e-3
+
+
+def test_adamw_of_more_than_2_to_32_elements(w2v):
+    """The last elements of a tensor that needs 33 bits to count them, moments in 8 bits."""
+    import torch
+    n = 2**32 + 5000
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    lo = n // 256 * 256 - 4096
+    g[lo:].normal_(generator=torch.Generator(device="cuda").manual_seed(9))
+    p[lo:].normal_(generator=torch.Generator(device="cuda").manual_seed(8))
+    old = p[lo:].clone()
+    opt = w2v.AdamW([p], [g], bits=8, betas=(B1, B2), eps=EPS, weight_decay=0.1, seed=4)
+    opt.step(1, 0.01)
+    zero = np.zeros(n - lo, dtype=np.float32)
+    mc, vc, ms, rs = narrow_reference(g[lo:].float().cpu().numpy(), zero, zero, lo, 1, 4)
+    assert np.array_equal(opt.m[lo:n].cpu().numpy(), mc) and np.array_equal(opt.v[lo:n].cpu().numpy(), vc)
+    assert np.array_equal(opt.m_scale[lo // 256:].cpu().numpy(), ms) and not opt.m[:1000].any()
+    p1, _, _, p_b, _, _ = adam_reference(old, g[lo:], torch.zeros(n - lo), torch.zeros(n - lo), 1, 0.01, 0.1)
+    within(p[lo:], p1, p_b + (p1.abs() + p_b) * half_step(torch.bfloat16), "p")
+
+
+def test_adamw_of_memory_that_is_no_plan_does_nothing(w2v):
+    import ctypes
+    import torch
+    p, g = torch.ones(512, device="cuda"), torch.ones(512, device="cuda")
+    opt = w2v.AdamW([p], [g])
+    opt._plan = torch.zeros_like(opt._plan)
+    opt.step(1, 0.1)
+    opt.step(torch.ones(1, dtype=torch.int64, device="cuda"), 0.1)
+    assert bool((p == 1).all()) and not opt.m.any() and not opt._plan.any()
 
 
 def test_adamw_not_finite_stays_in_its_block(w2v):
