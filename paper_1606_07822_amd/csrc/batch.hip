@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "w2v_ops.h"
 #include "w2v_scan.h"
@@ -48,6 +49,35 @@ __device__ __forceinline__ int32_t place_of(const BatchArgs &a, int64_t g, int32
     return d;
 }
 
+// The sum of the table's rows index / divisor of the lanes that `in` marks, in the lanes' order.
+// Two rows at a time are on their way, whatever the row's width (NE elements a lane, 64 columns apart).
+template <int NE>
+__device__ __forceinline__ void sum_rows(const float *table, int64_t row_floats, int32_t dim, uint64_t in, int32_t index,
+                                         float divisor, float (&sum)[NE]) {
+    const int lane = lane_id(), bytes = dim * 4;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) sum[i] = 0.0f;
+    while (in) {
+        float x[2][NE], d[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {   // an empty range for a row past the last
+            const bool on = in != 0;
+            const int l = on ? __builtin_ctzll(in) : 0;
+            in &= in - 1;
+            const float of = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, divisor), l));
+            d[u] = on ? of : 1.0f;
+            const int64_t r = __builtin_amdgcn_readlane(index, l);
+            buf_load_row<NE>(x[u], __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(table) + r * row_floats, 0,
+                                                                    on ? bytes : 0, kRawBufferWord3), lane);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < NE; ++i) sum[i] += x[u][i] / d[u];
+    }
+}
+
+template <int NE>
 __global__ __launch_bounds__(kBatchThreads) void k_batch_rows(BatchArgs a) {
     const int lane = lane_id();
     const int32_t i = static_cast<int32_t>(blockIdx.x) * kBatchWaves + static_cast<int32_t>(threadIdx.x) / kWave;
@@ -66,15 +96,14 @@ __global__ __launch_bounds__(kBatchThreads) void k_batch_rows(BatchArgs a) {
     if (lane == 0) a.targets[i] = P > 0 ? a.kept_vid[base + j] : -1;
     const int32_t at = from + lane + (from + lane >= j ? 1 : 0);   // lane q: the q-th window word
     const int32_t mine = lane < P ? a.kept_vid[base + at] : 0;
-    float *h = a.hidden + static_cast<int64_t>(i) * a.row;
-    for (int c = lane; c < a.dim; c += kWave) {
-        float sum = 0.0f;
-        for (int q = 0; q < P; ++q)
-            sum += a.syn0[static_cast<int64_t>(__builtin_amdgcn_readlane(mine, q)) * a.stride + c];
-        h[c] = P > 0 ? sum / static_cast<float>(P) : 0.0f;
-    }
+    float h[NE];
+    sum_rows<NE>(a.syn0, a.stride, a.dim, (1ull << P) - 1, mine, 1.0f, h);
+#pragma unroll
+    for (int e = 0; e < NE; ++e) h[e] = P > 0 ? h[e] / static_cast<float>(P) : 0.0f;
+    buf_store_row<NE>(h, row_rsrc(a.hidden, i, a.row, a.dim * 4), lane);
 }
 
+template <int NE>
 __global__ __launch_bounds__(kBatchThreads) void k_batch_words(BatchArgs a) {
     const int lane = lane_id();
     const int32_t k = static_cast<int32_t>(blockIdx.x) * kBatchWaves + static_cast<int32_t>(threadIdx.x) / kWave;
@@ -99,17 +128,9 @@ __global__ __launch_bounds__(kBatchThreads) void k_batch_words(BatchArgs a) {
     const uint64_t in = __ballot(share > 0.0f);
     if (lane == 0) a.words[k] = in ? a.kept_vid[base + j] : -1;
     if (!in) return;
-    float *e = a.dword + static_cast<int64_t>(k) * a.row;
-    const int64_t row0 = g - a.window - a.lo;
-    for (int col = lane; col < a.dim; col += kWave) {
-        float sum = 0.0f;
-        for (uint64_t m = in; m; m &= m - 1) {
-            const int l = __builtin_ctzll(m);
-            const float p = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, share), l));
-            sum += a.dhidden[(row0 + l) * a.row + col] / p;
-        }
-        e[col] = sum;
-    }
+    float e[NE];   // a centre's mean has a part of 1 / its window words in each of them
+    sum_rows<NE>(a.dhidden, a.row, a.dim, in, static_cast<int32_t>(of), share, e);
+    buf_store_row<NE>(e, row_rsrc(a.dword, k, a.row, a.dim * 4), lane);
 }
 
 struct Totals {
@@ -126,12 +147,26 @@ __global__ __launch_bounds__(kTotalThreads) void k_batch_totals(const float *__r
     __shared__ int64_t s_terms[kTotalThreads / kWave], s_nodes[kTotalThreads / kWave];
     double sum = 0.0;
     int64_t terms = 0, nodes = 0;
-    for (int32_t i = threadIdx.x; i < n; i += kTotalThreads) {
-        const int32_t v = targets[i];
-        if (v < 0) continue;
-        sum += static_cast<double>(loss[i]);
-        ++terms;
-        nodes += codelen[v];
+    constexpr int kAhead = 8;
+    for (int32_t i0 = threadIdx.x; i0 < n; i0 += kAhead * kTotalThreads) {
+        int32_t v[kAhead];
+        float l[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int32_t i = i0 + u * kTotalThreads;
+            v[u] = i < n ? targets[i] : -1;
+            l[u] = i < n ? loss[i] : 0.0f;
+        }
+        int32_t len[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) len[u] = codelen[max(v[u], 0)];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (v[u] >= 0) {
+                sum += static_cast<double>(l[u]);
+                ++terms;
+                nodes += len[u];
+            }
     }
     sum = wave_sum(sum);
     terms = wave_sum(terms);
@@ -164,6 +199,18 @@ __global__ __launch_bounds__(kScanThreads) void k_batch_scan(const int32_t *__re
 __global__ void k_batch_stats(const int64_t *sampled, const Totals *t, int64_t *stats) {
     if (threadIdx.x < 4) stats[threadIdx.x] = sampled[threadIdx.x];
     if (threadIdx.x == 4) stats[4] = t->nodes;
+}
+
+// Calls f with the elements that a lane holds of a row of dim floats.
+template <class F>
+void with_columns(int32_t dim, F f) {
+    const int64_t ne = ceil_div(dim, kWave);
+    if (ne <= 1) f(std::integral_constant<int, 1>{});
+    else if (ne <= 2) f(std::integral_constant<int, 2>{});
+    else if (ne <= 4) f(std::integral_constant<int, 4>{});
+    else if (ne <= 5) f(std::integral_constant<int, 5>{});
+    else if (ne <= 8) f(std::integral_constant<int, 8>{});
+    else f(std::integral_constant<int, 16>{});
 }
 
 struct Buffers {
@@ -295,7 +342,10 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
     int64_t step = b->step0;
     for (a.lo = 0; a.lo < a.kept; a.lo += p->sync_batch) {
         a.n = static_cast<int32_t>(std::min<int64_t>(p->sync_batch, a.kept - a.lo));
-        k_batch_rows<<<static_cast<unsigned>(ceil_div(a.n, kBatchWaves)), kBatchThreads, 0, s>>>(a);
+        with_columns(m->dim, [&](auto ne) {
+            k_batch_rows<decltype(ne)::value>
+                <<<static_cast<unsigned>(ceil_div(a.n, kBatchWaves)), kBatchThreads, 0, s>>>(a);
+        });
         W2V_LAUNCH_CHECK("k_batch_rows");
         NormArgs f{};
         if (b->gain) {
@@ -346,7 +396,10 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
             if (int rc = run_layer_norm_backward(f, w.norm_ws, s)) return rc;
         }
         const int64_t around = a.n + 2 * static_cast<int64_t>(p->window);
-        k_batch_words<<<static_cast<unsigned>(ceil_div(around, kBatchWaves)), kBatchThreads, 0, s>>>(a);
+        with_columns(m->dim, [&](auto ne) {
+            k_batch_words<decltype(ne)::value>
+                <<<static_cast<unsigned>(ceil_div(around, kBatchWaves)), kBatchThreads, 0, s>>>(a);
+        });
         W2V_LAUNCH_CHECK("k_batch_words");
         if (int rc = run_word_sums(w.words, w.dword, around, m->dim, w.row, m->V, w.dsyn0, w.row, w.sum_ws, s)) return rc;
         w2v_adamw_params o{};

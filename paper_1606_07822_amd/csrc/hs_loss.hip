@@ -22,7 +22,7 @@
 namespace w2v {
 namespace {
 
-constexpr int kSlab = 65536;      // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
+constexpr int kSlab = 33 * 2048;  // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
 constexpr int kSortBlock = 2048;  // rows ranked against each other
 constexpr int kRows = 32;         // sorted rows of a wavefront's sum
 constexpr int kFewRows = 16;      // of batches of at most kFewBlocks times as many, which have few wavefronts otherwise

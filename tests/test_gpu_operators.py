@@ -390,10 +390,10 @@ def test_loss_many_rows_of_a_deep_tree(w2v, n):
 
 @pytest.mark.parametrize("tree", ["two", "zipf"])
 def test_loss_more_rows_than_a_slab(w2v, tree):
-    """65,536 rows are summed together; what comes after them is added."""
+    """67,584 rows are summed together; what comes after them is added."""
     import torch
     counts = COUNTS[tree]()
-    n = 65536 + 77
+    n = 67584 + 77
     rng = np.random.default_rng(4)
     model, otree = make_model(w2v, counts, 4)
     x = hidden(n, 4, torch.float32)

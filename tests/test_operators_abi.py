@@ -149,7 +149,7 @@ def test_workspace_queries(w2v):
     m = w2v.CModel(None, None, 100, 50, 64, 0, None, 0, None, None, None, None)
     q = L.w2v_hs_loss_workspace_bytes
     assert q(ctypes.byref(m), 65, 10) == 0 and q(ctypes.byref(m), 20, -1) == 0 and q(None, 20, 10) == 0
-    assert q(ctypes.byref(m), 20, 65536) == q(ctypes.byref(m), 20, 10**7) > q(ctypes.byref(m), 20, 100) > 0
+    assert q(ctypes.byref(m), 20, 67584) == q(ctypes.byref(m), 20, 10**7) > q(ctypes.byref(m), 20, 100) > 0
 
 
 def batch_call(w2v, train=True, model=None, params=None, **kw):
