@@ -37,6 +37,8 @@ struct BatchArgs {
     float *hidden;             // [n][row]
     int32_t row;               // floats between the batch's rows
     int32_t *targets;          // [n]: the centre word, -1 where it has no window
+    const uint8_t *codelen;
+    int32_t *lengths;          // [n]: nodes on that word's path
     const float *dhidden;
     float *dword;              // [n + 2 window][row]: gradient of the word at each kept position around the batch
     int32_t *words;            // [n + 2 window], -1 where no centre of the batch has the position in its window
@@ -93,7 +95,11 @@ __global__ __launch_bounds__(kBatchThreads) void k_batch_rows(BatchArgs a) {
         const int64_t g = a.epoch_base + a.first_raw + base + static_cast<int64_t>(meta & 0xFFFFu);
         *a.lr = a.alpha_tab[g / 10000 - a.blk0];
     }
-    if (lane == 0) a.targets[i] = P > 0 ? a.kept_vid[base + j] : -1;
+    if (lane == 0) {
+        const int32_t v = P > 0 ? a.kept_vid[base + j] : -1;
+        a.targets[i] = v;
+        a.lengths[i] = v >= 0 ? a.codelen[v] : 0;
+    }
     const int32_t at = from + lane + (from + lane >= j ? 1 : 0);   // lane q: the q-th window word
     const int32_t mine = lane < P ? a.kept_vid[base + at] : 0;
     float h[NE];
@@ -138,35 +144,24 @@ struct Totals {
     int64_t terms, nodes;
 };
 
-// A batch's loss, terms and path nodes added to the call's, by one workgroup in a fixed order.
+// A batch's loss, terms and path nodes, summed by up to kTotalGroups workgroups (one alone fetches 65,536 rows' numbers in
+// 54 us), whose sums k_batch_totals adds to the call's. In a fixed order.
 constexpr int kTotalThreads = 1024;
-__global__ __launch_bounds__(kTotalThreads) void k_batch_totals(const float *__restrict__ loss,
-                                                                const int32_t *__restrict__ targets,
-                                                                const uint8_t *__restrict__ codelen, int32_t n, Totals *to) {
-    __shared__ double s_loss[kTotalThreads / kWave];
-    __shared__ int64_t s_terms[kTotalThreads / kWave], s_nodes[kTotalThreads / kWave];
+constexpr int kTotalGroups = 64;   // a wavefront adds them up
+__global__ __launch_bounds__(kTotalThreads) void k_batch_parts(const float *__restrict__ loss,
+                                                               const int32_t *__restrict__ targets,
+                                                               const int32_t *__restrict__ lengths, int32_t n, Totals *parts) {
+    constexpr int kWaves = kTotalThreads / kWave;
+    __shared__ double s_loss[kWaves];
+    __shared__ int64_t s_terms[kWaves], s_nodes[kWaves];
     double sum = 0.0;
     int64_t terms = 0, nodes = 0;
-    constexpr int kAhead = 8;
-    for (int32_t i0 = threadIdx.x; i0 < n; i0 += kAhead * kTotalThreads) {
-        int32_t v[kAhead];
-        float l[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int32_t i = i0 + u * kTotalThreads;
-            v[u] = i < n ? targets[i] : -1;
-            l[u] = i < n ? loss[i] : 0.0f;
-        }
-        int32_t len[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) len[u] = codelen[max(v[u], 0)];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (v[u] >= 0) {
-                sum += static_cast<double>(l[u]);
-                ++terms;
-                nodes += len[u];
-            }
+    const int32_t step = static_cast<int32_t>(gridDim.x) * kTotalThreads;
+    for (int32_t i = static_cast<int32_t>(blockIdx.x) * kTotalThreads + static_cast<int32_t>(threadIdx.x); i < n; i += step) {
+        if (targets[i] < 0) continue;
+        sum += static_cast<double>(loss[i]);
+        ++terms;
+        nodes += lengths[i];
     }
     sum = wave_sum(sum);
     terms = wave_sum(terms);
@@ -179,11 +174,21 @@ __global__ __launch_bounds__(kTotalThreads) void k_batch_totals(const float *__r
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kTotalThreads / kWave; ++w) {
+        for (int w = 1; w < kWaves; ++w) {
             sum += s_loss[w];
             terms += s_terms[w];
             nodes += s_nodes[w];
         }
+        parts[blockIdx.x] = Totals{sum, terms, nodes};
+    }
+}
+
+__global__ __launch_bounds__(kWave) void k_batch_totals(const Totals *parts, int n, Totals *to) {
+    const int lane = lane_id();
+    const Totals mine = lane < n ? parts[lane] : Totals{0.0, 0, 0};
+    const double sum = wave_sum(mine.loss);
+    const int64_t terms = wave_sum(mine.terms), nodes = wave_sum(mine.nodes);
+    if (lane == 0) {
         to->loss += sum;
         to->terms += terms;
         to->nodes += nodes;
@@ -217,8 +222,8 @@ struct Buffers {
     SampleBufs sample;
     float *alpha_tab, *lr, *hidden, *normed, *dnormed, *loss, *mean, *rstd, *dgain, *dsyn0, *dsyn1, *dword;
     int64_t *kept_off;
-    Totals *totals;
-    int32_t *targets, *words;
+    Totals *totals, *parts;
+    int32_t *targets, *lengths, *words;
     char *loss_ws, *norm_ws, *sum_ws, *plan;
     int32_t row;
 };
@@ -250,8 +255,10 @@ Buffers carve(Carve &c, const w2v_model *m, int64_t n_tokens, const w2v_params *
     w.alpha_tab = c.take<float>(static_cast<size_t>(std::max<int64_t>(1, n_tokens) / 10000 + 3));
     w.kept_off = c.take<int64_t>(static_cast<size_t>(n_docs));
     w.totals = c.take<Totals>(1);
+    w.parts = c.take<Totals>(kTotalGroups);
     w.lr = c.take<float>(1);
     w.targets = c.take<int32_t>(rows);
+    w.lengths = c.take<int32_t>(rows);
     w.loss = c.take<float>(rows);
     w.hidden = c.take<float>(wide);
     w.normed = w.hidden;
@@ -336,6 +343,8 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
     a.hidden = w.hidden;
     a.row = w.row;
     a.targets = w.targets;
+    a.codelen = m->codelen;
+    a.lengths = w.lengths;
     a.dhidden = w.dnormed;
     a.dword = w.dword;
     a.words = w.words;
@@ -385,7 +394,10 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
             h.dsyn1_stride = w.row;
         }
         if (int rc = run_hs_loss(h, w.loss_ws, s)) return rc;
-        k_batch_totals<<<1, kTotalThreads, 0, s>>>(w.loss, w.targets, m->codelen, a.n, w.totals);
+        const auto groups = static_cast<int>(std::min<int64_t>(kTotalGroups, ceil_div(a.n, kTotalThreads)));
+        k_batch_parts<<<static_cast<unsigned>(groups), kTotalThreads, 0, s>>>(w.loss, w.targets, w.lengths, a.n, w.parts);
+        W2V_LAUNCH_CHECK("k_batch_parts");
+        k_batch_totals<<<1, kWave, 0, s>>>(w.parts, groups, w.totals);
         W2V_LAUNCH_CHECK("k_batch_totals");
         if (!train) continue;
         if (b->gain) {
