@@ -392,6 +392,7 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
             h.dx_stride = w.row;
             h.dsyn1 = w.dsyn1;
             h.dsyn1_stride = w.row;
+            h.dsyn1_whole = true;
         }
         if (int rc = run_hs_loss(h, w.loss_ws, s)) return rc;
         const auto groups = static_cast<int>(std::min<int64_t>(kTotalGroups, ceil_div(a.n, kTotalThreads)));

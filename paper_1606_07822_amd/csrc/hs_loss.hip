@@ -10,8 +10,8 @@
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
 // j bits. A wavefront holds up to 32 sorted rows' x in registers, up to five columns a lane, and goes down the levels: a
 // level's nodes are runs of rows, summed and written out where a run ends. Runs that reach over a block's border are
-// written as partial sums, which k_hs_join adds up in order. The same sum with one level, every row
-// for its own word's row of the table, is the gradient of a table's looked-up rows (run_word_sums).
+// written as partial sums, which k_hs_join adds up in order. The same sum with one level, every row for its own word's
+// row of the table, is the gradient of a table's looked-up rows (run_word_sums).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -256,8 +256,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict_
     }
 }
 
-// The sorted rows' items. (Written by the merge itself, they cost it 14 us more at
-// 65,536 rows: the lines are then shared between the XCDs' caches.)
+// The sorted rows' items. (Written by the merge itself, they cost it 14 us more at 65,536 rows: the lines are then shared
+// between the XCDs' caches.)
 __global__ __launch_bounds__(256) void k_hs_items(Tree t, const int32_t *__restrict__ targets,
                                                   const int32_t *__restrict__ rows, int32_t n, Item *__restrict__ items) {
     const int32_t i = static_cast<int32_t>(blockIdx.x) * 256 + static_cast<int32_t>(threadIdx.x);
@@ -935,7 +935,7 @@ int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s) {
     if (a.dsyn1) {
         Carve c(workspace);
         b = carve(c, a.rows, a.dim, a.longest);
-        zeros = Zeros(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, a.dsyn1_stride == a.stride);
+        zeros = Zeros(a.dsyn1, a.V - 1, a.dim, a.dsyn1_stride, a.dsyn1_whole);
         if (a.rows == 0) return zero_rows(zeros, s);
     }
     for (int64_t lo = 0; lo < a.rows; lo += kSlab) {

@@ -247,6 +247,7 @@ int w2v_hs_loss(const w2v_model *m, int32_t max_code_len, const void *x, int32_t
     a.dx_stride = dx_stride;
     a.dsyn1 = dsyn1;
     a.dsyn1_stride = dsyn1_stride;
+    a.dsyn1_whole = dsyn1_stride == m->row_stride;
     return run_hs_loss(a, workspace, as_stream(hip_stream));
 }
 

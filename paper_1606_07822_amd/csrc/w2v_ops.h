@@ -127,6 +127,7 @@ struct HsLossArgs {
     int64_t dx_stride;
     float *dsyn1;                      // V-1 rows, or null
     int64_t dsyn1_stride;
+    bool dsyn1_whole;                  // zeros may go into the rows' padding
 };
 size_t hs_loss_bytes(int64_t rows, int32_t dim, int32_t longest);
 int run_hs_loss(const HsLossArgs &a, void *workspace, hipStream_t s);
