@@ -829,14 +829,16 @@ class AdamW:
             raise ValueError(f"state must hold {len(shapes)} arrays")
         for k, (t, (n, d)) in enumerate(zip(state, shapes)):
             _vector_ptr(t, d, n, dev, f"state[{k}]")
-        self.m, self.v = state[0], state[1]
-        self.m_scale, self.v_scale = (state[2], state[3]) if bits == 8 else (None, None)
+        self._state = (*state, None, None)[:4]
+        self._buffers = [t.detach() for t in (*params, *grads)]   # the plan's memory stays, whatever becomes of the tensors
         self._plan = _workspace(lib().w2v_adamw_plan_bytes(table, len(params)), dev)
         chunks = ctypes.c_int64(0)
         with _On(dev):
             _check(lib().w2v_adamw_build_plan(table, len(params), at, self._plan.data_ptr(), self._plan.numel(),
                                               ctypes.byref(chunks), _stream(dev)))
         self._chunks = chunks.value
+
+    m, v, m_scale, v_scale = (property(lambda self, k=k: self._state[k]) for k in range(4))
 
     def step(self, step, lr, grad_scale: float = 1.0) -> None:
         """Step number `step` (1, 2, ...) with the learning rate lr. Either may be a one-element tensor on the device
@@ -887,27 +889,30 @@ class BatchState:
         self.weight_decay, self.norm_eps, self.seed, self.steps = weight_decay, norm_eps, seed, 0
         self.gain = torch.ones(model.dim, dtype=torch.float32, device=dev) if norm else None
         self.bias = torch.zeros(model.dim, dtype=torch.float32, device=dev) if norm else None
-        self.m = self.v = self.m_scale = self.v_scale = None
-        cm, cb = model.c(), self.c(model)
+        cm, cb = model.c(), self._c(model)
         self.n_moments = n = lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb))
         kind = torch.float32 if bits == 32 else torch.uint8
         self.m, self.v = (torch.zeros(n, dtype=kind, device=dev) for _ in range(2))
-        if bits == 8:
-            self.m_scale, self.v_scale = (torch.zeros(n // AdamW.BLOCK, dtype=torch.float32, device=dev) for _ in range(2))
+        self.m_scale, self.v_scale = (torch.zeros(n // AdamW.BLOCK, dtype=torch.float32, device=dev) if bits == 8 else None
+                                      for _ in range(2))
 
-    def c(self, model: Model) -> CBatchParams:
+    def _c(self, model: Model, m=None, v=None, m_scale=None, v_scale=None) -> CBatchParams:
         if model.syn0.device != self.device:
             raise ValueError(f"the model must be on {self.device}")
-        for t, n in ((self.gain, model.dim), (self.bias, model.dim)):
-            _vector_ptr(t, torch.float32, n, self.device, "gain or bias")
-        ptr = [t.data_ptr() if t is not None else None
-               for t in (self.gain, self.bias, self.m, self.v, self.m_scale, self.v_scale)]
-        cb = CBatchParams(*ptr, self.betas[0], self.betas[1], self.eps, self.steps, self.norm_eps, self.weight_decay,
-                          self.bits, _tree_of(model).max_len, self.seed & 0xFFFFFFFF, 0)
-        if self.m is not None:
-            cm = model.c()
-            if lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != self.n_moments:
-                raise ValueError("the state belongs to a model of other sizes")
+        gain, bias = (_vector_ptr(t, torch.float32, model.dim, self.device, name)
+                      for t, name in ((self.gain, "gain"), (self.bias, "bias")))
+        return CBatchParams(gain, bias, m, v, m_scale, v_scale, self.betas[0], self.betas[1], self.eps, self.steps,
+                            self.norm_eps, self.weight_decay, self.bits, _tree_of(model).max_len, self.seed & 0xFFFFFFFF, 0)
+
+    def c(self, model: Model) -> CBatchParams:
+        n, kind = self.n_moments, torch.float32 if self.bits == 32 else torch.uint8
+        m, v = (_vector_ptr(t, kind, n, self.device, name) for t, name in ((self.m, "m"), (self.v, "v")))
+        scales = [None, None] if self.bits == 32 else [
+            _vector_ptr(t, torch.float32, n // AdamW.BLOCK, self.device, name)
+            for t, name in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale"))]
+        cm, cb = model.c(), self._c(model, m, v, *scales)
+        if lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != n:
+            raise ValueError("the state belongs to a model of other sizes")
         return cb
 
 

@@ -249,3 +249,26 @@ def test_binding_refuses(w2v):  # noqa: F811
         w2v.train_batch_epoch(model, tok.long(), w2v.Params(window=3, arch=1), state)
     with pytest.raises(ValueError):
         w2v.BatchState(model, bits=16)
+
+
+@pytest.mark.parametrize("bits", (8, 32))
+def test_state_of_other_sizes_is_refused(w2v, bits):  # noqa: F811
+    """Moments that were put in place of the state's own ones: of its sizes and types, or refused."""
+    import torch
+    counts = zipf_counts(40)
+    model, _ = make_model(w2v, counts, 8)
+    tok = torch.from_numpy(text(counts, 300, 1)).cuda()
+    p = w2v.Params(window=3, arch=1, sync_batch=64)
+    names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
+    for name in names:
+        for bad in (lambda t: t[:-1], lambda t: t.double(), lambda t: t.cpu()):
+            state = w2v.BatchState(model, bits=bits)
+            setattr(state, name, bad(getattr(state, name)))
+            for call in (w2v.train_batch_epoch, w2v.batch_loglik):
+                with pytest.raises(ValueError):
+                    call(model, tok, p, state)
+    a, b = w2v.BatchState(model, bits=bits), w2v.BatchState(model, bits=bits)
+    for name in names:
+        setattr(b, name, getattr(a, name).clone())
+    w2v.train_batch_epoch(model, tok, p, b)
+    assert b.steps > 0 and b.m.any()

@@ -844,6 +844,23 @@ def test_adamw_resumes_from_its_state(w2v):
         assert torch.equal(p, q) and torch.equal(a.m, c.m) and torch.equal(a.v, c.v)
 
 
+def test_adamw_keeps_its_buffers(w2v):
+    """A parameter or gradient that gets other storage later: a step goes to the memory that the plan was made for, not to
+    whatever has taken its place. The moments are the optimizer's own."""
+    import torch
+    n = 1 << 20
+    p, g = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    opt = w2v.AdamW([p], [g])
+    p.data, g.data = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    opt.params.clear()
+    opt.grads.clear()
+    taken = [torch.full((n,), 7.0, device="cuda") for _ in range(4)]
+    opt.step(1, 0.1)
+    assert not p.any() and all(bool((t == 7).all()) for t in taken) and bool((opt.m != 0).all())
+    with pytest.raises(AttributeError):
+        opt.m = torch.zeros(256, device="cuda")
+
+
 # ------------------------------------------------------------------ streams, graphs, a step of them together
 def small_step(w2v, bits=32, seed=0, n=300):
     """hidden -> layer norm -> loss -> gradients -> AdamW on syn1, weight and bias, buffers kept."""
