@@ -200,7 +200,9 @@ def _dev_ptr(t: torch.Tensor | None, dtype: torch.dtype, name: str):
 
 
 def _stream(device: torch.device | None = None) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    if device is None or device.index is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)   # the same without a Stream object: 0.1 us, not 1.7
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -694,7 +696,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     with _On(x.device):
         _check(lib().w2v_layer_norm(xp, kind, n, dim, xs, wp, bp, 0 if w is None else _TYPES[w.dtype], eps, yp, ys,
                                     stats.data_ptr(), stats.data_ptr() + 4 * n, _stream(x.device)))
-    return y, stats[0], stats[1]
+    return y, *stats.unbind()
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
@@ -712,7 +714,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     dxp, dxs = _rows_ptr(dx, "dx", x)
     if weight is not None and dweight is None and dbias is None:
         both = torch.empty(2, dim, dtype=torch.float32, device=dev)
-        dweight, dbias = both[0], both[1]
+        dweight, dbias = both.unbind()
     dwp = _vector_ptr(dweight, torch.float32, dim, dev, "dweight")
     dbp = _vector_ptr(dbias, torch.float32, dim, dev, "dbias")
     wp = _affine_ptr(weight, x, "weight")
