@@ -525,16 +525,16 @@ __device__ __forceinline__ void put_columns(float *row, int col, int bytes, cons
 }
 
 // A wavefront holds RB sorted rows, C columns a lane, and takes every so many of the levels; a workgroup has wavefronts
-// for all columns of the rows and, where there are few rows, for up to kLevelWaves parts of the levels. What bounds it is
+// for all columns of the rows and, where there are few rows, for several parts of the levels. What bounds it is
 // the instructions around a row's multiply-adds, so a wavefront takes as many columns as its registers hold. What a
 // level's rows need (coefficient, node, where a run that ends with the row goes) is worked out by the row's lane and
 // read from there; the coefficients and nodes of all levels are fetched into LDS first, as a load waits for the stores
 // that went before it. Eight rows inside one run take a multiply-add a column each; elsewhere a row also takes a branch
 // for whether it has the level and whether its run ends.
-constexpr int kLevelWaves = 4;
-constexpr int kNodeWaves = 8;   // of a workgroup: 256 registers a lane
+template <int RB>   // of a workgroup: 256 registers a lane, or 128
+constexpr int kNodeWaves = RB == kFewRows ? 16 : 8;
 template <class T, bool COEF, int RB, int C>
-__global__ __launch_bounds__(kNodeWaves *kWave) void k_hs_nodes(NodeArgs a) {
+__global__ __launch_bounds__(kNodeWaves<RB> *kWave) void k_hs_nodes(NodeArgs a) {
     extern __shared__ int32_t level_node[];   // [longest][RB], then the coefficients alike
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     const int waves = static_cast<int>(blockDim.x) / kWave, level_step = waves / a.tiles;
@@ -874,10 +874,12 @@ int sum_rows(NodeArgs m, int32_t type, const Buffers &b, hipStream_t s) {
     const auto blocks = static_cast<int32_t>(ceil_div(m.n, rb));
     const int per = columns <= 5 ? columns : 4;   // columns of a lane
     m.tiles = static_cast<int32_t>(ceil_div(columns, per));
-    // the levels shared out while that gives a SIMD no more than ten wavefronts (65,536 rows of 200: 184 -> 173 us in all)
-    const int64_t waves = static_cast<int64_t>(blocks) * m.tiles;
-    const int most = std::min(kLevelWaves, kNodeWaves / m.tiles);
-    const int parts = waves * most <= 40LL * device_cu_count() ? most : 1;
+    // The levels are shared out, to more than four parts while that gives a SIMD no more than two wavefronts (rows of
+    // 200, 4,096 of them: 54 us in all with four parts, 48 with eight; 16,384: 82, 85), to up to four while it gives ten
+    // (65,536: 184 us with one part, 173 with four). Batches of few rows: 257 of 100, 22 us with eight parts, 21 with 16.
+    const int64_t waves = static_cast<int64_t>(blocks) * m.tiles, cus = device_cu_count();
+    int parts = std::min(m.t.longest, (rb == kRows ? kNodeWaves<kRows> : kNodeWaves<kFewRows>) / m.tiles);
+    while (parts > 1 && waves * parts > (parts > 4 ? 8 : 40) * cus) parts /= 2;
     const auto threads = static_cast<unsigned>(m.tiles * parts * kWave);
     const size_t lds = static_cast<size_t>(m.t.longest) * rb * (m.coef ? 8 : 4);
     (void)with_type(type, [&](auto zero) {
