@@ -192,9 +192,10 @@ constexpr int kMergeThreads = kMergeKeys * kMergeParts;
 constexpr int kMergePer = 2;
 constexpr int kMergeBlocks = kMergeParts * kMergePer;
 template <class K>
-__global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict__ key_in,
+__global__ __launch_bounds__(kMergeThreads) void k_hs_merge(Tree t, const int32_t *__restrict__ targets,
+                                                            const K *__restrict__ key_in,
                                                             const int32_t *__restrict__ row_in, int32_t n,
-                                                            int32_t *__restrict__ row_out, int32_t merging, Fill fill) {
+                                                            Item *__restrict__ item_out, int32_t merging, Fill fill) {
     if (static_cast<int32_t>(blockIdx.x) >= merging) {
         fill_group(fill, fill.first + blockIdx.x - merging);
         return;
@@ -216,6 +217,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict_
         }
     };
     load(0);
+    Item item{};   // fetched while the places are counted
+    if (part == 0 && i < n) item = item_of(t, row, targets[row]);
     int32_t at = 0;
     for (int b0 = 0; b0 < blocks; b0 += kMergeBlocks) {
         __syncthreads();
@@ -252,18 +255,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_hs_merge(const K *__restrict_
         at = i % kSortBlock;
 #pragma unroll
         for (int k = 0; k < kMergeParts; ++k) at += counts[k][slot];
-        row_out[at] = row;
+        item_out[at] = item;
     }
-}
-
-// The sorted rows' items. (Written by the merge itself, they cost it 14 us more at 65,536 rows: the lines are then shared
-// between the XCDs' caches.)
-__global__ __launch_bounds__(256) void k_hs_items(Tree t, const int32_t *__restrict__ targets,
-                                                  const int32_t *__restrict__ rows, int32_t n, Item *__restrict__ items) {
-    const int32_t i = static_cast<int32_t>(blockIdx.x) * 256 + static_cast<int32_t>(threadIdx.x);
-    if (i >= n) return;
-    const int32_t row = rows[i];
-    items[i] = item_of(t, row, targets[row]);
 }
 
 // A lane's C columns of a row of `bytes` bytes, 64 apart from `col` on: zeros past the row, and no store there.
@@ -748,7 +741,7 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void k_hs_join(JoinArgs a) {
 
 struct Buffers {
     void *keys;
-    int32_t *row0, *row1;
+    int32_t *row;
     Item *items;
     float *coef, *part[2];
     int32_t *node[2];
@@ -765,8 +758,7 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     const size_t fans = (blocks + kFan * kJoinWaves - 1) / (kFan * kJoinWaves), level = static_cast<size_t>(2) * longest * dim;
     Buffers b;
     b.keys = c.take<uint64_t>(n);
-    b.row0 = c.take<int32_t>(n);
-    b.row1 = c.take<int32_t>(n);
+    b.row = c.take<int32_t>(n);
     b.items = c.take<Item>(n);
     b.coef = c.take<float>(blocks * longest * kRows);
     b.part[0] = c.take<float>(blocks * level);
@@ -843,19 +835,18 @@ int sort_rows(const Tree &t, const int32_t *targets, int32_t n, Zeros z, const B
     unsigned filling = z.take(std::min(kFillLaunch, one ? z.groups : z.groups / 2), &part);
     const auto ranking = static_cast<unsigned>(ceil_div(n, kSortBlock) * (kSortBlock / (n <= kRankNarrow ? 64 : 256)));
     if (n <= kRankNarrow)
-        k_hs_rank<K, 64><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now,
+        k_hs_rank<K, 64><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row, now,
                                                                   static_cast<int32_t>(ranking), part);
     else
-        k_hs_rank<K, 256><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row0, now,
+        k_hs_rank<K, 256><<<ranking + filling, kRankThreads, 0, s>>>(t, targets, n, keys, b.row, now,
                                                                    static_cast<int32_t>(ranking), part);
     W2V_LAUNCH_CHECK("k_hs_rank");
     if (one) return zero_rows(z, s);
     filling = z.take(kFillLaunch, &part);
     const auto merging = static_cast<unsigned>(ceil_div(n, kMergeKeys));
-    k_hs_merge<K><<<merging + filling, kMergeThreads, 0, s>>>(keys, b.row0, n, b.row1, static_cast<int32_t>(merging), part);
+    k_hs_merge<K><<<merging + filling, kMergeThreads, 0, s>>>(t, targets, keys, b.row, n, b.items,
+                                                             static_cast<int32_t>(merging), part);
     W2V_LAUNCH_CHECK("k_hs_merge");
-    k_hs_items<<<static_cast<unsigned>(ceil_div(n, 256)), 256, 0, s>>>(t, targets, b.row1, n, b.items);
-    W2V_LAUNCH_CHECK("k_hs_items");
     return zero_rows(z, s);
 }
 
