@@ -3,8 +3,9 @@
 //   z_j = x . syn1[n_j] along v's path, s_j = 1 - 2 t_j,  loss = sum_j log(1 + exp(-s_j z_j))
 //   g_j = -w s_j sigmoid(-s_j z_j),  dx = sum_j g_j syn1[n_j],  dsyn1[n] = sum over the rows through n of g x
 //
-// The walk (k_hs_walk) is a wavefront per row: four inner nodes at a time, the next four on their way, dot products
-// reduced together. It reads a path's rows once for z and dx, and leaves the row's coefficients g_j.
+// The walk (k_hs_walk) is a wavefront per row, in large batches per four rows: four inner nodes at a time, the next four
+// on their way, dot products reduced together. It reads a path's rows once for z and dx, and leaves the row's
+// coefficients g_j.
 //
 // dsyn1 is a sum over rows without atomics, in a fixed order. Rows are sorted by their word's code, left-aligned, so
 // that the rows through an inner node are neighbours: node (row, j) continues its neighbour's where their codes share
@@ -25,10 +26,14 @@ namespace {
 constexpr int kSlab = 33 * 2048;  // rows sorted and summed together; a longer batch takes several, each adding to dsyn1
 constexpr int kSortBlock = 2048;  // rows ranked against each other
 constexpr int kRows = 32;         // sorted rows of a wavefront's sum
-constexpr int kFewRows = 16;      // of batches of at most kFewBlocks times as many, which have few wavefronts otherwise
-constexpr int kFewBlocks = 64;
+// Fewer of them in batches of at most kFewBlocks times as many, which have few wavefronts otherwise (257 rows of 100: 21.7
+// us in all, not 23.6; 2,048: 27.5, not 29.5; 4,096: 36.1, not 37.5; but 8,192: 45.9, not 42.4).
+constexpr int kFewRows = 16;
+constexpr int kFewBlocks = 256;
 constexpr int kFan = 16;          // blocks whose sums one wavefront joins
-constexpr int kRankNarrow = 16384;   // rows up to which a workgroup ranks 64 of them, not 256
+// Rows up to which a workgroup ranks 64 of them, not 256, which reads each key four times as often (1,024 rows of 100:
+// 24 us in all, not 27; 16,384: 59, not 65; 32,768 of 200: 118, not 120; but 65,536: 180, not 170).
+constexpr int kRankNarrow = 32768;
 constexpr int kXcds = 8;
 
 // What a row's target stands for: a word's path, or (codelen null, longest 1) one row of the table, the word's own.
@@ -773,8 +778,10 @@ Buffers carve(Carve &c, int64_t rows, int32_t dim, int32_t longest) {
     return b;
 }
 
-// Four rows a wavefront from here on: fewer take longer one after the other than the loads they share save.
-constexpr int kWalkFour = 8192;
+// Four rows a wavefront from here on: fewer take longer one after the other than the loads they share save (in all,
+// four and one: 8,192 rows of 200 62 and 56 us; 16,384 83 and 83, of 100 59 and 57; 32,768 of 200 120 and 124; 65,536 170
+// and 186).
+constexpr int kWalkFour = 20480;
 
 template <class T, int NE>
 void launch_walk(const WalkArgs &w, bool grads, hipStream_t s) {

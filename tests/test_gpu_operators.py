@@ -368,9 +368,22 @@ def test_loss_many_rows(w2v, n):
 
 
 @pytest.mark.parametrize("n,dim,name", [(8192, 130, "bf16"), (8195, 300, "f32"), (8193, 65, "f16"), (8200, 700, "f16")])
-def test_loss_rows_that_share_a_walk(w2v, n, dim, name):
-    """Four sorted rows a wavefront: their common levels together, then each row's own; and rows too wide for that."""
+def test_loss_thousands_of_rows(w2v, n, dim, name):
+    """Rows in thousands, at the widths of a lane's columns."""
     counts = COUNTS["zipf"]()
+    rng = np.random.default_rng(n)
+    model, otree = make_model(w2v, counts, dim)
+    check_loss(w2v, model, otree, hidden(n, dim, kind(name), dim + 3, 1), draw_targets(rng, counts, n),
+               rng.random(n, dtype=np.float32) / n, name)
+
+
+@pytest.mark.parametrize("tree,n,dim,name", [("zipf", 20479, 70, "f32"), ("zipf", 20480, 130, "bf16"), ("wide", 20483, 300, "f32"),
+                                             ("zipf", 20481, 65, "f16"), ("zipf", 20490, 700, "f16"), ("wide", 32768, 6, "f32"),
+                                             ("wide", 32769, 50, "bf16"), ("deep", 20493, 10, "f32"), ("deep", 40001, 9, "f32")])
+def test_loss_large_batches(w2v, tree, n, dim, name):
+    """From 20,480 rows on four sorted ones a wavefront, their common levels together, then each row's own (not where they
+    are too wide for that); past 32,768 more rows a workgroup in the sort."""
+    counts = COUNTS[tree]()
     rng = np.random.default_rng(n)
     model, otree = make_model(w2v, counts, dim)
     check_loss(w2v, model, otree, hidden(n, dim, kind(name), dim + 3, 1), draw_targets(rng, counts, n),
