@@ -312,29 +312,32 @@ struct WalkArgs {
 
 constexpr int kWalkThreads = 64;   // a wavefront a workgroup: 65,536 rows of 200, 184 -> 181 us in all against four
 
-// What a node adds for s z (sz) at the lane: e = exp(-|z|) into the product of 1 + e, whose logarithm is the path's sum
-// of log(1 + e) (at most 2^64), and the rest of the loss; the value is sigmoid(-s z).
+// (1 + a) (1 + b) - 1, in two roundings that are relative to it: the products of a path are held less one, as a node
+// with e below 2^-24 would not enter 1 + e, nor the digits of a small e.
+__device__ __forceinline__ float product_less_one(float a, float b) { return fmaf(a, b, a + b); }
+
+// What a node adds for s z (sz) at the lane: e = exp(-|z|) into the product of 1 + e (prod: less one; at most 2^64), whose
+// logarithm is the path's sum of log(1 + e), and the rest of the loss; the value is sigmoid(-s z).
 __device__ __forceinline__ float node_terms(float sz, bool in, float &prod, float &wrong) {
     const float e = in ? __expf(-fabsf(sz)) : 0.0f;
-    const float one = 1.0f + e;
-    prod *= one;
+    prod = product_less_one(prod, e);
     wrong += in && sz < 0.0f ? -sz : 0.0f;
-    return (sz < 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(one);
+    return (sz < 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
 __device__ __forceinline__ float lane_value(float v, int lane) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
-// Product over the four rows of 16 lanes, lane by lane.
-__device__ __forceinline__ float rows_product(float v) {
+// product_less_one over the four rows of 16 lanes, lane by lane.
+__device__ __forceinline__ float rows_product_less_one(float v) {
     float a = v, b = v;
     swap16(a, b);
-    v = a * b;
+    v = product_less_one(a, b);
     a = v;
     b = v;
     swap32(a, b);
-    return a * b;
+    return product_less_one(a, b);
 }
 
 // A wavefront's stretch of the sorted rows: neighbouring ones share most of their path, so each XCD, with an L2 of its
@@ -396,7 +399,7 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
 #pragma unroll
             for (int i = 0; i < NE; ++i) now[u][i] = y[u][i];
     };
-    float wrong = 0.0f, prod = 1.0f;   // a lane's: of its row's shared levels, later of all its row's
+    float wrong = 0.0f, prod = 0.0f;   // a lane's (prod less one): of its row's shared levels, later of all its row's
     float g_all[R];                    // lane j: a row's coefficient at level j
 #pragma unroll
     for (int r = 0; r < R; ++r) g_all[r] = 0.0f;
@@ -436,7 +439,7 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
                                    __builtin_amdgcn_readlane(static_cast<int>(code >> 32), 16 * r))) << 32 |
                                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(code), 16 * r));
         const float w = lane_value(weight, 16 * r);
-        float row_wrong = 0.0f, row_prod = 1.0f;
+        float row_wrong = 0.0f, row_prod = 0.0f;
         if (r + 1 < R && len[r] <= shared) load(r + 1 < R ? r + 1 : r, shared, len[r + 1 < R ? r + 1 : r]);
         for (int j = shared; j < len[r]; j += 4) {
             take();
@@ -461,15 +464,15 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
             }
         }
         row_wrong = rows_sum(row_wrong);
-        row_prod = rows_product(row_prod);
+        row_prod = rows_product_less_one(row_prod);
         if (R == 1 || quarter == r) {
             wrong += row_wrong;
-            prod *= row_prod;
+            prod = product_less_one(prod, row_prod);
         }
     }
     if (a.loss && (lane & 15) == 0 && quarter < R && pos < a.n) {
         const bool missing = item.word >= 0 && item.len == 0;   // a target that the tree does not hold
-        a.loss[item.row] = missing ? __builtin_nanf("") : wrong + logf(prod);
+        a.loss[item.row] = missing ? __builtin_nanf("") : wrong + log1pf(prod);
     }
     if constexpr (GRADS) {
         if (a.dx) {
