@@ -114,13 +114,15 @@ __device__ __forceinline__ int shared_levels(const Tree &t, const Item &a, const
 }
 
 // What the rows are sorted by: the code with its first turn in the top bit, and after all of them the rows without a
-// path. 32 bits do where no code is longer than 31 (so that none is all ones), and cost half as much to compare.
+// path, whose key is all ones. A code's 64th turn is left out: it leads to one of two words and to no inner node, so rows
+// that agree in 63 turns share every node of theirs in any order, and no code is all ones. 32 bits do where no code is
+// longer than 31, and cost half as much to compare.
 template <class K>
 __device__ __forceinline__ K sort_key(const Tree &t, int32_t v) {
     const int len = path_len(t, v);
     if (len == 0) return static_cast<K>(~0ull);
     if (!t.codelen) return static_cast<K>(v);
-    return static_cast<K>((__brevll(t.code[v]) & (~0ull << (64 - len))) >> (64 - 8 * sizeof(K)));
+    return static_cast<K>((__brevll(t.code[v]) & (~0ull << (64 - min(len, 63)))) >> (64 - 8 * sizeof(K)));
 }
 
 // Each key's place among the kSortBlock keys of its block, by counting the smaller ones (equal keys keep their order).

@@ -5,9 +5,77 @@ counts, to first order, and 1.01 for the orders above."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import COUNTS, U, make_model, w2v, within  # noqa: F401
+from test_gpu_operators import COUNTS, U, half_step, hidden, kind, make_model, w2v, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+def fibonacci(v):
+    """Counts whose tree is a chain: the two rarest words have codes of v - 1 turns, one of them all ones."""
+    f = [1, 1]
+    while len(f) < v:
+        f.append(f[-1] + f[-2])
+    return np.array(f[::-1], dtype=np.int64)
+
+
+def tree_of(name):
+    return fibonacci(int(name[3:])) if name.startswith("fib") else COUNTS[name]()
+
+
+def softmax_reference(otree, syn1, x, targets, weights=None, x_off=None):
+    """loss, dx and dsyn1 in 64 bits, word by word, and how far fp32 kernels may be off (x_off: how far x itself is).
+
+    z: ceil(d / 64) products of a lane, added as they are formed, and 6 levels of lanes.
+    e = exp(-|z|): z log2(e) rounded twice (2 |z| U ln 2 log2(e) of e), its power within 2 ulp (4 U).
+    The loss: prod (1 + e) - 1 takes two roundings a node and two a join of lanes, log1p 2 ulp, the terms -s z one
+    rounding a node; all of them relative, q / (1 + q) <= log1p(q) and e / (1 + e) <= log1p(e).
+    sigmoid: e's error, 1 + e, its reciprocal (1 ulp) and two products.
+    dx: a multiply-add a node. dsyn1: 32 rows of a block, 16 blocks of a wavefront, 16 wavefronts, 9 of those in a slab of
+    67,584 rows and a slab: 75 additions at most in a row."""
+    v, d = otree.codelen.size, x.shape[1]
+    x, y = np.asarray(x, dtype=np.float64), np.asarray(syn1, dtype=np.float64)[:, :d]
+    x_off = np.zeros_like(x) if x_off is None else x_off
+    n = x.shape[0]
+    out = dict(loss=np.zeros(n), dx=np.zeros((n, d)), d1=np.zeros((v - 1, d)), loss_b=np.zeros(n), dx_b=np.zeros((n, d)),
+               d1_b=np.zeros((v - 1, d)))
+    targets = np.asarray(targets)
+    for t in np.unique(targets[targets >= 0]):
+        at = np.nonzero(targets == t)[0]
+        k, code = int(otree.codelen[t]), int(otree.code[t])
+        nodes = otree.points[otree.point_off[t]:otree.point_off[t] + k]
+        s = np.array([1.0 - 2.0 * ((code >> j) & 1) for j in range(k)])
+        rows, xs = y[nodes], x[at]
+        sz = (xs @ rows.T) * s
+        z_off = (-(-d // 64) + 7) * U * (np.abs(xs) @ np.abs(rows).T) + x_off[at] @ np.abs(rows).T
+        e = np.exp(-np.abs(sz))
+        f = np.where(sz < 0, 1.0, e) / (1 + e)
+        e_rel = (2 * np.abs(sz) + 4) * U
+        loss = np.logaddexp(0, -sz).sum(1)
+        out["loss"][at] = loss
+        out["loss_b"][at] = 1.01 * ((f * z_off + e_rel * e / (1 + e)).sum(1) + (2 * k + 16) * U * loss) + k * 2.0**-126
+        w = np.ones((at.size, 1)) if weights is None else np.asarray(weights, dtype=np.float64)[at, None]
+        g = -w * s * f
+        g_off = 1.01 * np.abs(w) * (f * (1 - f) * z_off + f * (e_rel * np.where(sz < 0, e, 1.0) + 6 * U))
+        out["dx"][at] = g @ rows
+        out["dx_b"][at] = 1.01 * (g_off + (k + 2) * U * np.abs(g)) @ np.abs(rows)
+        out["d1"][nodes] += g.T @ xs
+        out["d1_b"][nodes] += 1.01 * (g_off + 76 * U * np.abs(g)).T @ np.abs(xs) + np.abs(g).T @ x_off[at]
+    return out
+
+
+def check(w2v, model, otree, x, targets, weights=None, name="f32"):  # noqa: F811
+    import torch
+    t = torch.from_numpy(np.asarray(targets, dtype=np.int32)).cuda()
+    w = None if weights is None else torch.from_numpy(weights).cuda()
+    loss, dx, dsyn1 = w2v.hs_loss(model, x, t, w)
+    alone = w2v.hs_loss(model, x, t, grads=False)[0]
+    ref = softmax_reference(otree, model.syn1.double().cpu().numpy(), x.double().cpu().numpy(), targets, weights)
+    as_t = torch.from_numpy
+    within(loss, as_t(ref["loss"]), as_t(ref["loss_b"]), "loss")
+    within(alone, as_t(ref["loss"]), as_t(ref["loss_b"]), "loss without gradients")
+    want, b = as_t(ref["dx"]), as_t(ref["dx_b"])
+    within(dx, want, b + (want.abs() + b) * half_step(kind(name)) + 2.0**-25 * (name == "f16"), "dx")
+    within(dsyn1[:, :model.dim], as_t(ref["d1"]), as_t(ref["d1_b"]), "dsyn1")
 
 
 # ------------------------------------------------------------------ losses near zero
@@ -35,3 +103,25 @@ def test_loss_of_likely_words_keeps_its_digits(w2v, tree, n):  # noqa: F811
     for grads in (True, False):
         got = w2v.hs_loss(model, x, t, grads=grads)[0]
         within(got, torch.from_numpy(loss), torch.from_numpy(bound), f"loss, grads={grads}")
+
+
+# ------------------------------------------------------------------ codes of 64 turns
+@pytest.mark.parametrize("v", [64, 65])
+@pytest.mark.parametrize("n", [4, 300, 2500, 20481])
+def test_loss_of_the_deepest_codes(w2v, v, n):  # noqa: F811
+    """Codes of 63 and 64 turns, all ones among them, with rows without a target before, between and behind the deepest
+    words: such a row has no part in any run, nor in what four sorted rows share."""
+    import torch
+    counts = fibonacci(v)
+    model, otree = make_model(w2v, counts, 10)
+    assert int(otree.codelen.max()) == model.tree.max_len == v - 1
+    rng = np.random.default_rng(n)
+    targets = np.array([0, v - 2, -1, v - 2], dtype=np.int32) if n == 4 else rng.integers(-1, v, n).astype(np.int32)
+    if n > 4:
+        deep = rng.random(n) < 0.5
+        targets[deep] = rng.choice([-1, v - 2, v - 1, v - 3], size=int(deep.sum()))
+    x = hidden(n, 10, torch.float32)
+    check(w2v, model, otree, x, targets, rng.random(n, dtype=np.float32))
+    loss, dx, _ = w2v.hs_loss(model, x, torch.from_numpy(targets).cuda())
+    none = torch.from_numpy(targets < 0).cuda()
+    assert not loss[none].any() and not dx[none].any()
