@@ -473,7 +473,9 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
  * the batch's centres) are taken against the model at its start; then AdamW,
  * with the learning rate of its first centre, updates syn0 and syn1 (decay
  * weight_decay) and gain and bias (no decay): every row, whether or not the
- * batch reached it. Deterministic.
+ * batch reached it. Deterministic. A centre without a window has no part in
+ * any gradient. With norm_eps 0 a window whose mean has equal columns has no
+ * finite deviation and makes the model NaN.
  *   m, v, m_scale, v_scale  moments as in w2v_adamw_step, of
  *                    w2v_batch_n_moments elements: syn0 (V x dim), syn1
  *                    (V-1 x dim), gain, bias, each from the next multiple of

@@ -145,12 +145,15 @@ struct Totals {
 };
 
 // A batch's loss, terms and path nodes, summed by up to kTotalGroups workgroups (one alone fetches 65,536 rows' numbers in
-// 54 us), whose sums k_batch_totals adds to the call's. In a fixed order.
+// 54 us), whose sums k_batch_totals adds to the call's. In a fixed order. A centre without a window gets an rstd of
+// 0 for the norm's backward pass, so that its normalised row is zeros there whatever norm_eps is: with norm_eps 0 its rstd
+// was infinite and its row NaN, which the zeros of its gradient would not take out of the gain's sums.
 constexpr int kTotalThreads = 1024;
 constexpr int kTotalGroups = 64;   // a wavefront adds them up
 __global__ __launch_bounds__(kTotalThreads) void k_batch_parts(const float *__restrict__ loss,
                                                                const int32_t *__restrict__ targets,
-                                                               const int32_t *__restrict__ lengths, int32_t n, Totals *parts) {
+                                                               const int32_t *__restrict__ lengths, int32_t n,
+                                                               float *__restrict__ rstd, Totals *parts) {
     constexpr int kWaves = kTotalThreads / kWave;
     __shared__ double s_loss[kWaves];
     __shared__ int64_t s_terms[kWaves], s_nodes[kWaves];
@@ -158,7 +161,10 @@ __global__ __launch_bounds__(kTotalThreads) void k_batch_parts(const float *__re
     int64_t terms = 0, nodes = 0;
     const int32_t step = static_cast<int32_t>(gridDim.x) * kTotalThreads;
     for (int32_t i = static_cast<int32_t>(blockIdx.x) * kTotalThreads + static_cast<int32_t>(threadIdx.x); i < n; i += step) {
-        if (targets[i] < 0) continue;
+        if (targets[i] < 0) {
+            if (rstd) rstd[i] = 0.0f;
+            continue;
+        }
         sum += static_cast<double>(loss[i]);
         ++terms;
         nodes += lengths[i];
@@ -396,7 +402,7 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
         }
         if (int rc = run_hs_loss(h, w.loss_ws, s)) return rc;
         const auto groups = static_cast<int>(std::min<int64_t>(kTotalGroups, ceil_div(a.n, kTotalThreads)));
-        k_batch_parts<<<static_cast<unsigned>(groups), kTotalThreads, 0, s>>>(w.loss, w.targets, w.lengths, a.n, w.parts);
+        k_batch_parts<<<static_cast<unsigned>(groups), kTotalThreads, 0, s>>>(w.loss, w.targets, w.lengths, a.n, w.rstd, w.parts);
         W2V_LAUNCH_CHECK("k_batch_parts");
         k_batch_totals<<<1, kWave, 0, s>>>(w.parts, groups, w.totals);
         W2V_LAUNCH_CHECK("k_batch_totals");

@@ -1,0 +1,149 @@
+"""A batch's gradients at every width, with moments in 8 and 32 bits over several steps, and training's edges.
+
+U = 2^-24 is fp32's largest relative rounding error; bounds are carried through the step to first order (1.01 for the
+orders above)."""
+import copy
+
+import numpy as np
+import pytest
+
+from test_gpu_batch import text, windows
+from test_gpu_operators import U, adam_reference, make_model, narrow_reference, w2v, within, zipf_counts  # noqa: F401
+from test_gpu_operators_edges import softmax_reference
+
+pytestmark = pytest.mark.gpu
+
+ROWS = 76   # additions one after the other in a sum over sorted rows (see softmax_reference)
+
+
+def batch_gradients(otree, syn0, syn1, gain, bias, centres, window, norm_eps):
+    """Gradients of the batch's mean loss in 64 bits, [(gradient, bound)] of syn0, syn1, gain and bias, and the summed
+    loss with its bound.
+
+    The window's mean: a sum of at most 2 window rows and a division. The norm: 20 elements a lane and 10 levels (30 U)
+    for each mean, the variance's second sum and a division (34 U, halved by the root), 3 U for the root's reciprocal.
+    dgain and dbias: 8 rows of a lane, 2 levels and 4 wavefronts, then 32 rows and 16 wavefronts (62, and 3 for h)."""
+    n, d = len(centres), syn0.shape[1]
+    norm = gain is not None
+    live = np.array([len(w) > 0 for _, w in centres])
+    targets = np.array([c if len(w) else -1 for c, w in centres])
+    h, h_b = np.zeros((n, d)), np.zeros((n, d))
+    for i, (_, w) in enumerate(centres):
+        if len(w):
+            h[i], h_b[i] = syn0[w].mean(0), (len(w) + 1) * U * np.abs(syn0[w]).mean(0)
+    y, y_b = h, h_b
+    if norm:
+        mu, mu_b = h.mean(1, keepdims=True), (30 * U * np.abs(h) + h_b).mean(1, keepdims=True)
+        c = h - mu
+        c_b = h_b + mu_b + U * np.abs(c)
+        var = (c * c).mean(1, keepdims=True) + norm_eps
+        var[~live] = 1.0   # no part in anything
+        r = 1 / np.sqrt(var)
+        r_rel = ((np.abs(c) * c_b).mean(1, keepdims=True) * 2 / var + 34 * U) / 2 + 3 * U
+        hat = c * r
+        hat_b = c_b * r + np.abs(hat) * (r_rel + U)
+        y = hat * gain + bias
+        y_b = np.abs(gain) * (hat_b + U * np.abs(hat)) + U * np.abs(y)
+    ref = softmax_reference(otree, syn1, y, targets, None, y_b)
+    dy, dy_b = ref["dx"], ref["dx_b"]
+    out = [None, (ref["d1"], ref["d1_b"])]
+    dh, dh_b = dy, dy_b
+    if norm:
+        out.append(((dy * hat)[live].sum(0), (dy_b * np.abs(hat) + np.abs(dy) * hat_b + 65 * U * np.abs(dy * hat))[live].sum(0)))
+        out.append((dy.sum(0), (dy_b + 62 * U * np.abs(dy)).sum(0)))
+        a, a_b = dy * gain, dy_b * np.abs(gain) + U * np.abs(dy * gain)
+        c0, c0_b = a.mean(1, keepdims=True), (a_b + 32 * U * np.abs(a)).mean(1, keepdims=True)
+        c1 = (a * hat).mean(1, keepdims=True)
+        c1_b = (a_b * np.abs(hat) + np.abs(a) * hat_b + 33 * U * np.abs(a * hat)).mean(1, keepdims=True)
+        dh = r * (a - c0 - hat * c1)
+        dh_b = r_rel * np.abs(dh) + r * (a_b + c0_b + hat_b * np.abs(c1) + np.abs(hat) * c1_b
+                                         + 4 * U * (np.abs(a) + np.abs(c0) + np.abs(hat * c1)))
+    g0, g0_b = np.zeros_like(syn0), np.zeros_like(syn0)
+    for (_, w), row, off in zip(centres, dh, dh_b):
+        if len(w):
+            np.add.at(g0, w, row / len(w))
+            np.add.at(g0_b, w, (off + (2 * window + 2 + ROWS) * U * np.abs(row)) / len(w))
+    out[0] = (g0, g0_b)
+    return ([(g / n, (1.01 * b + 3 * U * np.abs(g)) / n) for g, b in out], ref["loss"].sum(),
+            1.01 * (ref["loss_b"].sum() + 2 * U * ref["loss"].sum()))
+
+
+def clone(model):
+    return type(model)(model.syn0.clone(), model.syn1.clone(), model.dim, model.vocab_counts, model.train_words, model.tree)
+
+
+def clone_state(state):
+    import torch
+    s = copy.copy(state)
+    for name, t in vars(state).items():
+        if isinstance(t, torch.Tensor):
+            setattr(s, name, t.clone())
+    return s
+
+
+def parameters(model, state):
+    return [model.syn0[:, :model.dim], model.syn1[:model.V - 1, :model.dim]] + (
+        [state.gain, state.bias] if state.gain is not None else [])
+
+
+def gradients_of(w2v, model, tok, p, state):  # noqa: F811
+    """A batch's gradients as the kernels take them: with beta1 = 0 the first moment after a step is the gradient.
+    The moments' array of it, and where each parameter's part begins."""
+    m, s = clone(model), w2v.BatchState(model, norm=state.gain is not None, betas=(0.0, 0.0), eps=1.0, norm_eps=state.norm_eps)
+    if state.gain is not None:
+        s.gain, s.bias = state.gain.clone(), state.bias.clone()
+    _, total, terms = w2v.train_batch_epoch(m, tok, p, s)
+    assert s.steps == 1
+    starts, at = [], 0
+    for q in parameters(model, state):
+        starts.append(at)
+        at += -(-q.numel() // 256) * 256
+    return s.m, starts, total, terms
+
+
+def check_gradients(w2v, model, otree, tok, counts, p, state):  # noqa: F811
+    import torch
+    centres = windows(w2v, tok, counts, p)
+    q = [t.double().cpu().numpy() for t in parameters(model, state)] + [None, None]
+    want, loss, loss_b = batch_gradients(otree, q[0], q[1], q[2], q[3], centres, p.window, state.norm_eps)
+    m, starts, total, terms = gradients_of(w2v, model, torch.from_numpy(tok).cuda(), p, state)
+    assert terms == sum(len(w) > 0 for _, w in centres) and abs(total + loss) <= loss_b
+    for k, ((g, b), lo) in enumerate(zip(want, starts)):
+        within(m[lo:lo + g.size].view(g.shape), torch.from_numpy(g), torch.from_numpy(b), f"gradient {k}")
+    return m, starts
+
+
+def with_norm(model, state, seed):
+    """A gain and a bias that are no ones and zeros."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    state.gain.copy_(1 + 0.3 * torch.randn(model.dim, generator=g))
+    state.bias.copy_(0.2 * torch.randn(model.dim, generator=g))
+    return state
+
+
+# ------------------------------------------------------------------ centres without a window, and no eps
+def test_an_empty_window_has_no_part_in_the_norm(w2v):  # noqa: F811
+    """Documents with one kept word have a centre without a window, whose hidden vector is zeros. With norm_eps = 0 that
+    row has no finite deviation; the batch's gradients and the model are those of the other centres."""
+    import torch
+    counts = zipf_counts(60)
+    rng = np.random.default_rng(4)
+    tok = text(counts, 600, 9)
+    tok[rng.random(600) < 0.5] = -1
+    for dim, norm_eps in ((20, 0.0), (300, 0.0), (20, 1e-5)):
+        model, otree = make_model(w2v, counts, dim)
+        p = w2v.Params(window=3, arch=1, doc_len=3, corpus_tokens=600, sync_batch=1 << 12, alpha0=0.01)
+        state = with_norm(model, w2v.BatchState(model, norm_eps=norm_eps, eps=1e-3), dim)
+        centres = windows(w2v, tok, counts, p)
+        alone = sum(len(w) == 0 for _, w in centres)
+        assert 50 < alone < len(centres) - 50
+        check_gradients(w2v, model, otree, tok, counts, p, state)
+        t = torch.from_numpy(tok).cuda()
+        before = w2v.batch_loglik(model, t, p, state)
+        _, total, terms = w2v.train_batch_epoch(model, t, p, state)
+        assert (total, terms) == before and np.isfinite(total)
+        for q in parameters(model, state):
+            assert bool(torch.isfinite(q).all())
+        after = w2v.batch_loglik(model, t, p, state)
+        assert np.isfinite(after[0]) and after[0] > before[0]
