@@ -397,8 +397,9 @@ int w2v_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
              P(v|x) = prod_j sigmoid((1 - 2 t_j) x . syn1[n_j]) over v's path
      dx      rows x dim elements of type out, may be NULL
      dsyn1   float[V-1][dsyn1_stride] out, may be NULL: every row's first dim
-             columns are written; where dsyn1_stride is m->row_stride, zeros may
-             be written into the rows' padding columns, too (as in training)
+             columns are written; where dsyn1_stride is m->row_stride and less
+             than dim + 32, zeros are written into the rows' padding columns,
+             too (as in training)
    The gradients are those of sum_i weights[i] loss[i] (weights float[rows], or
    NULL: ones). A negative target means none: loss 0, a dx of zeros, x not
    read into any sum. A target outside the vocabulary, or one whose code is

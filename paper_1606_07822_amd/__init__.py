@@ -743,13 +743,25 @@ def hs_loss_workspace(model: Model, x: torch.Tensor, grads: bool = True) -> torc
     return _workspace(lib().w2v_hs_loss_workspace_bytes(ctypes.byref(cm), _tree_of(model).max_len, x.shape[0]), x.device)
 
 
+def _own_gradient(model: Model) -> torch.Tensor:
+    """Memory of syn1's shape for hs_loss, zeros where that writes none: in padding of 32 floats or more (shorter padding
+    gets the kernels' zeros), and in rows that belong to no inner node."""
+    d = torch.empty_like(model.syn1)
+    if d.shape[1] != model.stride or model.stride - model.dim >= 32:
+        d[:, model.dim:].zero_()
+    if d.shape[0] != model.V - 1:
+        d[model.V - 1:].zero_()
+    return d
+
+
 def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor | None = None,
             grads: bool = True, loss: torch.Tensor | None = None, dx: torch.Tensor | None = None,
             dsyn1: torch.Tensor | None = None, workspace: torch.Tensor | None = None
             ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
     """(loss, dx, dsyn1): -log P(targets[i] | x[i]) under the model's hierarchical softmax (float32) and, with grads,
     the gradients of sum(weights * loss) for x [rows, dim] and for model.syn1 (dsyn1 float32 of syn1's shape, all rows
-    written: their first dim columns, and zeros perhaps in the padding). targets int32, negative: none. Does not sync."""
+    written: their first dim columns, and zeros in padding of less than 32; a new dsyn1 has zeros in all its padding).
+    targets int32, negative: none. Does not sync."""
     xp, xs = _rows_ptr(x, "x", x)
     kind, longest = _type_of(x, "x"), _tree_of(model).max_len
     n, dev = x.shape[0], x.device
@@ -765,7 +777,7 @@ def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch
     if grads:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
         dxp, dxs = _rows_ptr(dx, "dx", x)
-        dsyn1 = torch.zeros_like(model.syn1) if dsyn1 is None else dsyn1
+        dsyn1 = _own_gradient(model) if dsyn1 is None else dsyn1
         dsp, _ = _rows_ptr(dsyn1, "dsyn1", model.syn1)
     else:
         dx = dsyn1 = None

@@ -806,13 +806,14 @@ void launch_walk(const WalkArgs &w, bool grads, hipStream_t s) {
 
 // The groups of a filling, none for rows that hold an earlier slab's sums. whole: the rows' padding may be written too.
 // Rows that end inside a 128-byte line cost memory a read for the rest of it (1M rows of 300 floats, 320 apart: 329 us,
-// 204 with the padding), so short padding is then written with them.
+// 204 with the padding), so padding of less than kShortPadding floats is then written with them (callers may rely on it).
+constexpr int64_t kShortPadding = 32;
 struct Zeros {
     Fill fill{};
     int64_t groups = 0;
     Zeros() = default;
     Zeros(float *p, int64_t rows, int32_t dim, int64_t stride, bool whole) {
-        fill = Fill{p, rows, stride, dim, whole && stride - dim < 32 ? 1 : 0, 0};
+        fill = Fill{p, rows, stride, dim, whole && stride - dim < kShortPadding ? 1 : 0, 0};
         groups = fill.whole ? ceil_div(rows * stride, kFillFloats) : ceil_div(rows, kFillRows);
     }
     // The next of them, at most `most`.

@@ -5,7 +5,7 @@ counts, to first order, and 1.01 for the orders above."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import COUNTS, U, half_step, hidden, kind, make_model, w2v, within  # noqa: F401
+from test_gpu_operators import COUNTS, U, draw_targets, half_step, hidden, kind, make_model, w2v, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,28 @@ def test_loss_of_the_deepest_codes(w2v, v, n):  # noqa: F811
     loss, dx, _ = w2v.hs_loss(model, x, torch.from_numpy(targets).cuda())
     none = torch.from_numpy(targets < 0).cuda()
     assert not loss[none].any() and not dx[none].any()
+
+
+# ------------------------------------------------------------------ the gradient that hs_loss makes itself
+@pytest.mark.parametrize("dim,stride", [(64, 64), (50, 64), (33, 64), (32, 64), (20, 64), (300, 320), (4, 4)])
+@pytest.mark.parametrize("n", [0, 1, 3000])
+def test_loss_makes_its_own_gradient(w2v, monkeypatch, dim, stride, n):  # noqa: F811
+    """Without a dsyn1 of the caller's: its columns as in one that is given, zeros in the padding whatever lay in the
+    memory before, and the zeros written once, by the kernels (torch fills padding of 32 columns and more alone)."""
+    import torch
+    counts = COUNTS["zipf"]()
+    model, _ = make_model(w2v, counts, dim, stride=stride)
+    x = hidden(n, dim, torch.float32)
+    t = torch.from_numpy(draw_targets(np.random.default_rng(n), counts, n)).cuda()
+    want = w2v.hs_loss(model, x, t, dsyn1=torch.full_like(model.syn1, 3.0))[2][:, :dim].clone()
+    filled = []
+    zero_ = torch.Tensor.zero_
+    monkeypatch.setattr(torch, "zeros_like", lambda *a, **k: pytest.fail("the gradient's zeros, twice"))
+    monkeypatch.setattr(torch.Tensor, "zero_", lambda self: filled.append(tuple(self.shape)) or zero_(self))
+    for _ in range(3):
+        stale = torch.full_like(model.syn1, float("nan"))
+        del stale   # the next tensor of this size takes its memory
+        got = w2v.hs_loss(model, x, t)[2]
+        assert got.shape == model.syn1.shape and torch.equal(got[:, :dim], want) and not got[:, dim:].any()
+        del got
+    assert set(filled) <= ({(model.V - 1, stride - dim)} if stride - dim >= 32 else set())
