@@ -452,7 +452,8 @@ typedef struct {
    n_chunks_host is handed to every step. Synchronises the stream. A plan
    belongs to one step at a time. Errors: W2V_E_ARG for sizes, strides, types
    or NULL pointers out of range, moments that overlap or reach past n_moments
-   (a tensor's last block counts whole), or packed parameters that overlap. */
+   (a tensor's last block counts whole), or packed parameters that overlap.
+   Gradients may share memory with each other, not with a parameter. */
 size_t w2v_adamw_plan_bytes(const w2v_adamw_tensor *tensors_host, int32_t n_tensors);
 int w2v_adamw_build_plan(const w2v_adamw_tensor *tensors_host, int32_t n_tensors, int64_t n_moments, void *plan,
                          size_t plan_bytes, int64_t *n_chunks_host, void *hip_stream);

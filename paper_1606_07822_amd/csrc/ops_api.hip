@@ -89,7 +89,8 @@ int check_tensors(const w2v_adamw_tensor *t, int32_t n, int64_t n_moments) {
         moments.emplace_back(x.moment_offset, x.moment_offset + places);
         const int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(x.param));
         // rows with gaps may interleave with another tensor's; the first row may not lie in one all the same
-        params.emplace_back(at, at + (packed ? count : x.cols) * type_bytes(x.param_type));
+        const bool one_span = x.rows <= 1 || x.param_stride == x.cols;
+        params.emplace_back(at, at + (one_span ? count : x.cols) * type_bytes(x.param_type));
     }
     auto overlap = [](std::vector<Span> &s) {
         std::sort(s.begin(), s.end());

@@ -212,3 +212,17 @@ def test_batch_queries(w2v):
     assert 0 < L.w2v_batch_loglik_workspace_bytes(M, 1000, Q, B_) < L.w2v_train_batch_workspace_bytes(M, 1000, Q, B_)
     p.sync_batch = 0
     assert L.w2v_train_batch_workspace_bytes(M, 1000, Q, B_) == 0 and L.w2v_batch_loglik_workspace_bytes(None, 1, Q, B_) == 0
+
+
+def test_adamw_plan_finds_packed_parameters_that_overlap_whatever_their_gradients(w2v):
+    """A packed parameter whose gradient's rows have gaps is one span as well: a second tensor in its middle would be
+    updated twice."""
+    a = tensor(w2v, grad_stride=128)                                        # 4 rows of 100 floats, one after the other
+    b = tensor(w2v, param=A + 1200, rows=1, cols=10, param_stride=10, grad_stride=10, moment_offset=512)
+    for pair in ([a, b], [b, a]):
+        assert build(w2v, pair) == w2v.W2V_E_ARG and "parameters overlap" in w2v.last_error()
+    beside = tensor(w2v, param=A + 1600, rows=1, cols=10, param_stride=10, grad_stride=10, moment_offset=512)
+    assert build(w2v, [a, beside], plan=None) == w2v.W2V_E_ARG and "workspace" in w2v.last_error()
+    gaps = tensor(w2v, param_stride=128)                                    # rows with gaps, another's row in one of them
+    inside = tensor(w2v, param=A + 400, rows=1, cols=28, param_stride=28, grad_stride=28, moment_offset=512)
+    assert build(w2v, [gaps, inside], plan=None) == w2v.W2V_E_ARG and "workspace" in w2v.last_error()
