@@ -483,7 +483,8 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
  *                    (V-1 x dim), gain, bias, each from the next multiple of
  *                    256 on
  *   step0            steps taken before this call
- * stats int64[W2V_N_STATS] may be NULL. steps_host: batches of this call.
+ * stats int64[W2V_N_STATS] may be NULL. steps_host: batches of this call, after
+ * an error those whose update was launched before it.
  * sum_ll_host, n_terms_host (may be NULL): sum of log P(centre | hidden) over
  * the centres with a window, each scored before its batch's update, and their
  * number. Synchronises the stream. Errors: as w2v_train_hs_epoch, and

@@ -948,10 +948,11 @@ def train_batch_epoch(model: Model, tokens: torch.Tensor, p: Params, state: Batc
     with _On(dev):
         ws = _kept(workspace, max(1, lib().w2v_train_batch_workspace_bytes(ctypes.byref(cm), tokens.numel(), ctypes.byref(cp),
                                                                           ctypes.byref(cb))), dev)
-        _check(lib().w2v_train_batch_epoch(ctypes.byref(cm), tp, tokens.numel(), ctypes.byref(cp), ctypes.byref(cb), sp,
-                                           ctypes.byref(steps), ctypes.byref(s), ctypes.byref(terms), ws.data_ptr(),
-                                           ws.numel(), _stream(dev)))
-    state.steps += steps.value
+        rc = lib().w2v_train_batch_epoch(ctypes.byref(cm), tp, tokens.numel(), ctypes.byref(cp), ctypes.byref(cb), sp,
+                                         ctypes.byref(steps), ctypes.byref(s), ctypes.byref(terms), ws.data_ptr(),
+                                         ws.numel(), _stream(dev))
+    state.steps += steps.value   # after an error, too: the moments hold the steps before it
+    _check(rc)
     return stats, s.value, terms.value
 
 

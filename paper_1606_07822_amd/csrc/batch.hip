@@ -430,12 +430,12 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
         o.grad_scale = 1.0f / static_cast<float>(a.n);
         o.seed = b->seed;
         if (int rc = run_adamw_step(w.plan, chunks, b->bits, b->m, b->v, b->m_scale, b->v_scale, o, s)) return rc;
+        *steps_host = step - b->step0;   // kept up to date: a later error leaves the steps that were launched
     }
     if (stats) {
         k_batch_stats<<<1, kWave, 0, s>>>(w.sample.totals, w.totals, stats);
         W2V_LAUNCH_CHECK("k_batch_stats");
     }
-    if (steps_host) *steps_host = step - b->step0;
     Totals t{};
     W2V_HIP(hipMemcpyAsync(&t, w.totals, sizeof(t), hipMemcpyDeviceToHost, s));
     W2V_HIP(hipStreamSynchronize(s));

@@ -325,6 +325,7 @@ int w2v_train_batch_epoch(const w2v_model *m, const int32_t *tokens, int64_t n_t
                           const w2v_batch_params *bp, int64_t *stats, int64_t *steps_host, double *sum_ll_host,
                           int64_t *n_terms_host, void *workspace, size_t workspace_bytes, void *hip_stream) {
     set_error("");
+    if (steps_host) *steps_host = 0;
     if (int rc = check_batch(m, tokens, n_tokens, p, bp)) return rc;
     if (bp->bits != 8 && bp->bits != 32) return fail(W2V_E_ARG, "bits must be 8 or 32");
     if (!bp->m || !bp->v || (bp->bits == 8 && (!bp->m_scale || !bp->v_scale))) return fail(W2V_E_ARG, "a moment is NULL");

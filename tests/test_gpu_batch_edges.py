@@ -147,3 +147,31 @@ def test_an_empty_window_has_no_part_in_the_norm(w2v):  # noqa: F811
             assert bool(torch.isfinite(q).all())
         after = w2v.batch_loglik(model, t, p, state)
         assert np.isfinite(after[0]) and after[0] > before[0]
+
+
+# ------------------------------------------------------------------ steps that were taken
+def test_a_failed_epoch_keeps_its_steps(w2v, monkeypatch):  # noqa: F811
+    """An error after some updates: the state counts those, as its moments hold them."""
+    import torch
+    counts = zipf_counts(40)
+    model, _ = make_model(w2v, counts, 8)
+    tok = torch.from_numpy(text(counts, 300, 1)).cuda()
+    p = w2v.Params(window=3, arch=1, doc_len=50, corpus_tokens=300, sync_batch=64)
+    state = w2v.BatchState(model)
+    w2v.train_batch_epoch(model, tok, p, state)
+    once = state.steps
+    assert once > 1
+    real = w2v.lib()
+
+    class Failing:
+        def __getattr__(self, name):
+            return getattr(real, name)
+
+        def w2v_train_batch_epoch(self, *args):
+            assert real.w2v_train_batch_epoch(*args) == w2v.W2V_OK
+            return w2v.W2V_E_ARG
+
+    monkeypatch.setattr(w2v, "lib", Failing)
+    with pytest.raises(w2v.W2VError):
+        w2v.train_batch_epoch(model, tok, p, state)
+    assert state.steps == 2 * once

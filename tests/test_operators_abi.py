@@ -226,3 +226,16 @@ def test_adamw_plan_finds_packed_parameters_that_overlap_whatever_their_gradient
     gaps = tensor(w2v, param_stride=128)                                    # rows with gaps, another's row in one of them
     inside = tensor(w2v, param=A + 400, rows=1, cols=28, param_stride=28, grad_stride=28, moment_offset=512)
     assert build(w2v, [gaps, inside], plan=None) == w2v.W2V_E_ARG and "workspace" in w2v.last_error()
+
+
+def test_batch_training_refused_has_taken_no_step(w2v):
+    """steps_host is the call's own, whatever it held before and whichever check refuses."""
+    m = w2v.CModel(0x10000, 0x20000, 100, 50, 64, 0, 0x30000, 1000, 0x40000, 0x50000, 0x60000, 0x70000)
+    b = w2v.CBatchParams(A, B, C, D, None, None, 0.9, 0.999, 1e-8, 0, 1e-5, 0.0, 32, 20, 0, 0)
+    for arch, n, ws_bytes, code in ((0, 1000, 1 << 40, w2v.W2V_E_ARG), (1, -1, 1 << 40, w2v.W2V_E_ARG),
+                                    (1, 1000, 100, w2v.W2V_E_WORKSPACE)):
+        p = w2v.Params(window=5, corpus_tokens=1000, arch=arch, sync_batch=64).c()
+        steps = ctypes.c_int64(77)
+        assert w2v.lib().w2v_train_batch_epoch(ctypes.byref(m), 0x80000, n, ctypes.byref(p), ctypes.byref(b), None,
+                                               ctypes.byref(steps), None, None, 0x900000, ws_bytes, None) == code
+        assert steps.value == 0
