@@ -903,6 +903,7 @@ class BatchState:
         self.weight_decay, self.norm_eps, self.seed, self.steps = weight_decay, norm_eps, seed, 0
         self.gain = torch.ones(model.dim, dtype=torch.float32, device=dev) if norm else None
         self.bias = torch.zeros(model.dim, dtype=torch.float32, device=dev) if norm else None
+        self._sizes = (model.V, model.dim)
         cm, cb = model.c(), self._c(model)
         self.n_moments = n = lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb))
         kind = torch.float32 if bits == 32 else torch.uint8
@@ -925,8 +926,8 @@ class BatchState:
             _vector_ptr(t, torch.float32, n // AdamW.BLOCK, self.device, name)
             for t, name in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale"))]
         cm, cb = model.c(), self._c(model, m, v, *scales)
-        if lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != n:
-            raise ValueError("the state belongs to a model of other sizes")
+        if (model.V, model.dim) != self._sizes or lib().w2v_batch_n_moments(ctypes.byref(cm), ctypes.byref(cb)) != n:
+            raise ValueError(f"the state belongs to a model of other sizes, {self._sizes[0]} words of {self._sizes[1]} columns")
         return cb
 
 

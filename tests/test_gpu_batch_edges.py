@@ -175,3 +175,23 @@ def test_a_failed_epoch_keeps_its_steps(w2v, monkeypatch):  # noqa: F811
     with pytest.raises(w2v.W2VError):
         w2v.train_batch_epoch(model, tok, p, state)
     assert state.steps == 2 * once
+
+
+def test_a_state_belongs_to_its_models_sizes(w2v):  # noqa: F811
+    """Moments are laid out by the tables' rows and columns: a model of others is refused, though its number of moments
+    (whole blocks of 256) may be the same. A model of the same sizes is taken."""
+    import torch
+    tok = torch.zeros(20, dtype=torch.int32, device="cuda")
+    p = w2v.Params(window=2, arch=1, sync_batch=16)
+    for norm, (v, dim), (v2, dim2) in ((True, (16, 16), (15, 16)), (False, (16, 16), (31, 8)), (False, (16, 16), (16, 15))):
+        model, _ = make_model(w2v, zipf_counts(v), dim)
+        other, _ = make_model(w2v, zipf_counts(v2), dim2)
+        state = w2v.BatchState(model, norm=norm)
+        assert w2v.BatchState(other, norm=norm).n_moments == state.n_moments
+        kept = other.syn0.clone()
+        for call in (w2v.train_batch_epoch, w2v.batch_loglik):
+            with pytest.raises(ValueError, match="other sizes"):
+                call(other, tok, p, state)
+        assert torch.equal(other.syn0.nan_to_num(7.0), kept.nan_to_num(7.0)) and state.steps == 0
+        same, _ = make_model(w2v, zipf_counts(v), dim, seed=5)
+        w2v.train_batch_epoch(same, tok, p, state)
