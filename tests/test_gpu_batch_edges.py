@@ -7,8 +7,8 @@ import copy
 import numpy as np
 import pytest
 
-from test_gpu_batch import text, windows
-from test_gpu_operators import U, adam_reference, make_model, narrow_reference, w2v, within, zipf_counts  # noqa: F401
+from test_gpu_batch import text
+from test_gpu_operators import B1, B2, U, make_model, narrow_reference, w2v, within, zipf_counts  # noqa: F401
 from test_gpu_operators_edges import softmax_reference
 
 pytestmark = pytest.mark.gpu
@@ -68,6 +68,19 @@ def batch_gradients(otree, syn0, syn1, gain, bias, centres, window, norm_eps):
             1.01 * (ref["loss_b"].sum() + 2 * U * ref["loss"].sum()))
 
 
+def windows(w2v, tok, counts, p):  # noqa: F811
+    """Kept centres in order, (word, window words), from the sampler's listing of pairs (places in the whole text)."""
+    import torch
+    s = w2v.sample_pairs(torch.from_numpy(tok).cuda(), counts.size, torch.from_numpy(counts).cuda(), int(counts.sum()), p,
+                         cap=40 * tok.size, want_mask=True)
+    keep = np.nonzero(s.keep_mask.cpu().numpy())[0]
+    centre, context = s.centre.cpu().numpy() - p.first_raw_index, s.context.cpu().numpy() - p.first_raw_index
+    order = np.argsort(centre, kind="stable")
+    cut = np.searchsorted(centre[order], np.append(keep, tok.size))
+    words = tok[context[order]]
+    return [(int(tok[k]), words[a:b]) for k, a, b in zip(keep, cut[:-1], cut[1:])]
+
+
 def clone(model):
     return type(model)(model.syn0.clone(), model.syn1.clone(), model.dim, model.vocab_counts, model.train_words, model.tree)
 
@@ -99,6 +112,19 @@ def gradients_of(w2v, model, tok, p, state):  # noqa: F811
         starts.append(at)
         at += -(-q.numel() // 256) * 256
     return s.m, starts, total, terms
+
+
+def adam_step(p, g, m, v, step, lr, wd, eps):
+    """New p, m and v in 64 bits, and their bounds for fp32 steps: m two products and their sum (4 U of the terms), v three
+    and its terms positive (5 U), the update those, the root, three constants rounded once, three products and a hardware
+    reciprocal (1 ulp) (10 U), p a product and the update's subtraction."""
+    p, g, m, v = (t.double().cpu() for t in (p, g, m, v))
+    m1, v1 = B1 * m + (1 - B1) * g, B2 * v + (1 - B2) * g * g
+    m_b = 4 * U * (B1 * m.abs() + (1 - B1) * g.abs())
+    size, den = lr / (1 - B1**step), (v1 / (1 - B2**step)).sqrt() + eps
+    upd = size * m1 / den
+    p1 = p * (1 - lr * wd) - upd
+    return p1, m1, v1, 1.01 * (3 * U * (p.abs() + p1.abs()) + size * m_b / den + 10 * U * upd.abs()), m_b, 5 * U * v1
 
 
 def check_gradients(w2v, model, otree, tok, counts, p, state):  # noqa: F811
@@ -195,3 +221,94 @@ def test_a_state_belongs_to_its_models_sizes(w2v):  # noqa: F811
         assert torch.equal(other.syn0.nan_to_num(7.0), kept.nan_to_num(7.0)) and state.steps == 0
         same, _ = make_model(w2v, zipf_counts(v), dim, seed=5)
         w2v.train_batch_epoch(same, tok, p, state)
+
+
+# ------------------------------------------------------------------ widths and steps
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("dim", [1, 64, 130, 200, 256, 300, 320, 400, 512, 513, 700, 1000, 1024])
+def test_gradients_at_every_width(w2v, norm, dim):  # noqa: F811
+    """All widths of a lane's columns: window means, norm, loss, the gradients' way back to syn0 and syn1."""
+    counts = zipf_counts(60)
+    tok = text(counts, 700, dim)
+    model, otree = make_model(w2v, counts, dim)
+    p = w2v.Params(window=5, sample=1e-2, arch=1, doc_len=100, corpus_tokens=700, sync_batch=1 << 12)
+    state = w2v.BatchState(model, norm=norm)
+    check_gradients(w2v, model, otree, tok, counts, p, with_norm(model, state, dim) if norm else state)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dim,norm", [(300, True), (300, False), (50, True), (600, True)])
+def test_steps_one_by_one_and_together(w2v, bits, dim, norm):  # noqa: F811
+    """Four batches of whole documents. One call a batch: each step's gradients against 64 bits, the moments (8 bits: codes
+    and scales bit for bit) and parameters against AdamW of the gradients as the kernels took them. One call for all: the
+    same bits."""
+    import torch
+    counts = zipf_counts(60)
+    rng = np.random.default_rng(dim)
+    per, batches, rate = 150, 4, 0.01
+    tok = rng.choice(60, size=per * batches, p=counts / counts.sum()).astype(np.int32)
+    model, otree = make_model(w2v, counts, dim)
+    decay, seed, eps = 0.1, 11, 1e-3
+    state = w2v.BatchState(model, norm=norm, bits=bits, eps=eps, weight_decay=decay, seed=seed)
+    if norm:
+        with_norm(model, state, dim)
+    together, state_together = clone(model), clone_state(state)
+
+    def settings(k):   # no token is dropped: a batch is three documents
+        return w2v.Params(window=5, arch=1, doc_len=50, corpus_tokens=per * batches, sync_batch=per, alpha0=rate, first_raw_index=k * per)
+
+    for k in range(batches):
+        part = tok[k * per:(k + 1) * per]
+        p = settings(k)
+        grads, starts = check_gradients(w2v, model, otree, part, counts, p, state)
+        before = [q.clone().flatten() for q in parameters(model, state)]
+        if bits == 8:
+            opt_m = (state.m.view(torch.float8_e4m3fn).float().view(-1, 256) * state.m_scale[:, None]).flatten()
+            c = state.v.long()
+            root = torch.where(c < 16, c * 2.0**-18, (1 + (c % 16) / 16) * 2.0 ** (c // 16 - 15).double()).float()
+            opt_v = ((root.view(-1, 256) * state.v_scale[:, None]) ** 2).flatten()
+        else:
+            opt_m, opt_v = state.m.clone(), state.v.clone()
+        w2v.train_batch_epoch(model, torch.from_numpy(part).cuda(), p, state)
+        assert state.steps == k + 1
+        for i, (q, old, lo) in enumerate(zip(parameters(model, state), before, starts)):
+            n = old.numel()
+            g, m0, v0 = grads[lo:lo + n], opt_m[lo:lo + n], opt_v[lo:lo + n]
+            p1, m1, v1, p_b, m_b, v_b = adam_step(old, g, m0, v0, k + 1, rate, decay if i < 2 else 0.0, eps)
+            within(q.flatten(), p1, p_b, f"parameter {i} after step {k + 1}")
+            if bits == 8:
+                mc, vc, ms, rs = narrow_reference(g.cpu().numpy(), m0.cpu().numpy(), v0.cpu().numpy(), lo, k + 1, seed)
+                blocks = slice(lo // 256, lo // 256 + -(-n // 256))
+                assert np.array_equal(state.m_scale[blocks].cpu().numpy(), ms), (i, k)
+                assert np.array_equal(state.v_scale[blocks].cpu().numpy(), rs), (i, k)
+                assert np.array_equal(state.m[lo:lo + n].cpu().numpy(), mc), (i, k)
+                assert np.array_equal(state.v[lo:lo + n].cpu().numpy(), vc), (i, k)
+            else:
+                within(state.m[lo:lo + n], m1, m_b, "m")
+                within(state.v[lo:lo + n], v1, v_b, "v")
+    w2v.train_batch_epoch(together, torch.from_numpy(tok).cuda(), settings(0), state_together)
+    assert state_together.steps == batches
+    for a, b in zip(parameters(model, state), parameters(together, state_together)):
+        assert torch.equal(a, b)
+    assert torch.equal(state.m, state_together.m) and torch.equal(state.v, state_together.v)
+    if bits == 8:
+        assert torch.equal(state.m_scale, state_together.m_scale) and torch.equal(state.v_scale, state_together.v_scale)
+
+
+def test_a_large_batch_through_the_norm(w2v):  # noqa: F811
+    """Some 21,000 centres: each group of sixteen lanes of the norm's backward pass has several rows, four sorted rows a
+    wavefront share their path, the words' sums have many blocks."""
+    import torch
+    counts = zipf_counts(50)
+    n, dim = 22_500, 36
+    tok = text(counts, n, 7)
+    model, otree = make_model(w2v, counts, dim)
+    state = with_norm(model, w2v.BatchState(model), 3)
+    p = w2v.Params(window=2, arch=1, doc_len=1000, corpus_tokens=n, sync_batch=1 << 17)
+    centres = windows(w2v, tok, counts, p)
+    q = [t.double().cpu().numpy() for t in parameters(model, state)]
+    want, loss, loss_b = batch_gradients(otree, *q, centres, p.window, state.norm_eps)
+    m, starts, total, terms = gradients_of(w2v, model, torch.from_numpy(tok).cuda(), p, state)
+    assert terms == sum(len(w) > 0 for _, w in centres) and len(centres) > 20_480 and abs(total + loss) <= loss_b
+    for k, ((g, b), lo) in enumerate(zip(want, starts)):
+        within(m[lo:lo + g.size].view(g.shape), torch.from_numpy(g), torch.from_numpy(b), f"gradient {k}")
