@@ -5,7 +5,8 @@ counts, to first order, and 1.01 for the orders above."""
 import numpy as np
 import pytest
 
-from test_gpu_operators import COUNTS, U, draw_targets, half_step, hidden, kind, make_model, w2v, within  # noqa: F401
+from test_gpu_operators import (B1, B2, COUNTS, EPS, U, adam_reference, draw_targets, guarded, half_step, hidden,  # noqa: F401
+                                kind, make_model, narrow_reference, untouched, w2v, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -150,3 +151,137 @@ def test_loss_makes_its_own_gradient(w2v, monkeypatch, dim, stride, n):  # noqa:
         assert got.shape == model.syn1.shape and torch.equal(got[:, :dim], want) and not got[:, dim:].any()
         del got
     assert set(filled) <= ({(model.V - 1, stride - dim)} if stride - dim >= 32 else set())
+
+
+# ------------------------------------------------------------------ sums of many rows
+@pytest.mark.parametrize("tree,n,dim,name", [("zipf", 257, 100, "f32"), ("zipf", 4096, 200, "f32"), ("wide", 9000, 65, "f32"),
+                                             ("zipf", 8191, 520, "bf16"), ("wide", 33000, 300, "f16"), ("two", 67584, 5, "f32"),
+                                             ("zipf", 67584 + 4097, 20, "f32")])
+def test_loss_within_its_longest_chain(w2v, tree, n, dim, name):  # noqa: F811
+    """Every output against the roundings that the kernels' arrangement has (see softmax_reference), from one block of the
+    sums to two slabs of them."""
+    counts = COUNTS[tree]()
+    rng = np.random.default_rng(n)
+    model, otree = make_model(w2v, counts, dim)
+    check(w2v, model, otree, hidden(n, dim, kind(name), dim + 3, 1), draw_targets(rng, counts, n), rng.random(n, dtype=np.float32),
+          name)
+
+
+# ------------------------------------------------------------------ layer norm, several rows a group of lanes
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,d", [(15, 300), (17, 50), (8193, 50), (8195, 300), (20001, 100), (16400, 200), (9001, 255), (5003, 512),
+                                 (1100, 700), (1027, 4100)])
+def test_norm_backward_of_many_rows(w2v, n, d, name):  # noqa: F811
+    """From 8,192 narrow rows on a group of sixteen lanes takes several, the next one on its way; wide rows have the same
+    from 512 (of a workgroup each) on. dx of its own, in dy's place and in x's: equal bits."""
+    import torch
+    t = kind(name)
+    stride = d + 5
+    g = torch.Generator().manual_seed(n)
+    x, xbuf = guarded(n, d, t, stride, 3)
+    dy, dybuf = guarded(n, d, t, stride, 3)
+    x.copy_(torch.randn(n, d, generator=g) * 1.5 + 0.5)
+    dy.copy_(torch.randn(n, d, generator=g))
+    w = (1 + 0.3 * torch.randn(d, generator=g)).cuda()
+    _, mean, rstd = w2v.layer_norm(x, w)
+    out, buf = guarded(n, d, t, d + 1, 2)
+    dx, dw, db = w2v.layer_norm_backward(dy, x, w, mean, rstd, dx=out)
+    assert untouched(buf, out, n, d, d + 1, 2)
+    x64, dy64, w64 = x.double().cpu(), dy.double().cpu(), w.double().cpu()
+    r = rstd.double().cpu()[:, None]
+    h = (x64 - mean.double().cpu()[:, None]) * r
+    a = dy64 * w64
+    c0, c1 = a.mean(1, keepdim=True), (a * h).mean(1, keepdim=True)
+    want = r * (a - c0 - h * c1)
+    # h: two roundings, a: one. A row's sums: 20 elements a lane, 6 levels, 16 wavefronts (42), their terms' own, 1 / d and
+    # its product (2). dx: three products and two subtractions.
+    c0_b = 45 * U * a.abs().mean(1, keepdim=True)
+    c1_b = 48 * U * (a * h).abs().mean(1, keepdim=True)
+    bound = 1.01 * r * (4 * U * (a.abs() + c0.abs() + (h * c1).abs()) + c0_b + h.abs() * c1_b + 2 * U * (h * c1).abs())
+    within(dx, want, bound + (want.abs() + bound) * half_step(t) + 2.0**-25 * (name == "f16"), "dx")
+    # columns: a lane's rows, 2 levels and 4 wavefronts, 32 workgroups one after the other and 16 wavefronts
+    chain = -(-n // 512) + 2 + 4 + 32 + 16
+    within(dw, (dy64 * h).sum(0), 1.01 * (chain + 3) * U * (dy64 * h).abs().sum(0), "dweight")
+    within(db, dy64.sum(0), 1.01 * chain * U * dy64.abs().sum(0), "dbias")
+    first = [q.clone() for q in (dx, dw, db)]
+    for place, place_buf in ((dy, dybuf), (x, xbuf)):
+        kept = place.clone()
+        again = w2v.layer_norm_backward(dy, x, w, mean, rstd, dx=place)
+        assert all(torch.equal(p, q) for p, q in zip(first, again)) and untouched(place_buf, place, n, d, stride, 3)
+        place.copy_(kept)
+
+
+# ------------------------------------------------------------------ AdamW, rows with gaps over several chunks
+GAPPED = [(1000, 50), (301, 301), (3001, 3), (5000, 2), (9000, 1), (130, 64), (700, 7), (2, 5001)]
+
+
+def gapped_case(p_kind, g_kind, seed):
+    """Parameters and gradients whose rows lie differently far apart, and the parameters' buffers."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    ps, gs, bufs = [], [], []
+    for i, (rows, cols) in enumerate(GAPPED):
+        p, buf = guarded(rows, cols, p_kind, cols + 1 + 2 * i, i % 3)
+        q, _ = guarded(rows, cols, g_kind, cols + 5 - i % 5, i % 2)
+        p.copy_(torch.randn(rows, cols, generator=g) * 0.5)
+        q.copy_(torch.randn(rows, cols, generator=g) * 0.1)
+        ps.append(p)
+        gs.append(q)
+        bufs.append((buf, cols + 1 + 2 * i, i % 3))
+    return ps, gs, bufs
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("p_name,g_name", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f32", "f16")])
+def test_adamw_of_rows_with_gaps(w2v, bits, p_name, g_name):  # noqa: F811
+    """Tensors of more than one chunk of 4,096 elements whose rows have gaps, any number of columns: parameters and moments
+    against 64 bits, 8-bit codes and scales bit for bit, the gaps as they were."""
+    import torch
+    ps, gs, bufs = gapped_case(kind(p_name), kind(g_name), 5)
+    opt = w2v.AdamW(ps, gs, bits=bits, betas=(B1, B2), eps=EPS, weight_decay=0.02, seed=9)
+    for step in (1, 2, 3):
+        old = [p.clone() for p in ps]
+        m0, v0 = (a.clone() for a in opt.moments())
+        opt.step(step, 0.02, grad_scale=0.5)
+        for i, (p, g) in enumerate(zip(ps, gs)):
+            n, at = p.numel(), opt.offsets[i]
+            cut, blocks = slice(at, at + n), slice(at // 256, at // 256 + -(-n // 256))
+            p1, m1, v1, p_b, m_b, v_b = adam_reference(old[i].flatten(), g.flatten(), m0[cut], v0[cut], step, 0.02, 0.02, 0.5)
+            within(p.flatten(), p1, p_b + (p1.abs() + p_b) * half_step(kind(p_name)) + 2.0**-25 * (p_name == "f16"), f"p {i}")
+            assert untouched(bufs[i][0], p, *GAPPED[i], *bufs[i][1:]), i
+            if bits == 32:
+                within(opt.m[cut], m1, m_b, f"m {i}")
+                within(opt.v[cut], v1, v_b, f"v {i}")
+                continue
+            scaled = (g.float() * 0.5).flatten().cpu().numpy()
+            mc, vc, ms, rs = narrow_reference(scaled, m0[cut].cpu().numpy(), v0[cut].cpu().numpy(), at, step, 9)
+            assert np.array_equal(opt.m_scale[blocks].cpu().numpy(), ms) and np.array_equal(opt.v_scale[blocks].cpu().numpy(), rs), (i, step)
+            assert np.array_equal(opt.m[cut].cpu().numpy(), mc) and np.array_equal(opt.v[cut].cpu().numpy(), vc), (i, step)
+        for g in gs:
+            g.mul_(-0.7)
+
+
+@pytest.mark.parametrize("g_name", ["bf16", "f16"])
+def test_adamw_eight_bits_of_narrow_gradients(w2v, g_name):  # noqa: F811
+    """8-bit moments with 16-bit parameters and gradients, packed tensors whose last chunk is full, short and ragged."""
+    import torch
+    gen = torch.Generator().manual_seed(4)
+    t = kind(g_name)
+    sizes = [1, 255, 256, 4096, 4097, 8192, 12289, 20000]
+    ps = [(torch.randn(n, generator=gen) * 0.5).to(t).cuda() for n in sizes]
+    gs = [(torch.randn(n, generator=gen) * 0.1).to(t).cuda() for n in sizes]
+    opt = w2v.AdamW(ps, gs, bits=8, betas=(B1, B2), eps=EPS, weight_decay=0.1, seed=3)
+    for step in (1, 2, 3):
+        old = [p.clone() for p in ps]
+        m0, v0 = (a.clone() for a in opt.moments())
+        opt.step(step, 0.01)
+        for i, (p, g) in enumerate(zip(ps, gs)):
+            n, at = p.numel(), opt.offsets[i]
+            cut, blocks = slice(at, at + n), slice(at // 256, at // 256 + -(-n // 256))
+            p1, _, _, p_b, _, _ = adam_reference(old[i], g, m0[cut], v0[cut], step, 0.01, 0.1)
+            within(p, p1, p_b + (p1.abs() + p_b) * half_step(t) + 2.0**-25 * (g_name == "f16"), f"p {i}")
+            mc, vc, ms, rs = narrow_reference(g.float().cpu().numpy(), m0[cut].cpu().numpy(), v0[cut].cpu().numpy(), at, step, 3)
+            assert np.array_equal(opt.m_scale[blocks].cpu().numpy(), ms) and np.array_equal(opt.v_scale[blocks].cpu().numpy(), rs), (i, step)
+            assert np.array_equal(opt.m[cut].cpu().numpy(), mc) and np.array_equal(opt.v[cut].cpu().numpy(), vc), (i, step)
+        for g in gs:
+            g.mul_(-0.5)
