@@ -613,6 +613,9 @@ def sample_negatives(tokens: torch.Tensor, V: int, vocab_counts: torch.Tensor, t
 
 
 # ---------------------------------------------------- a mini-batch step on hidden vectors
+# These calls work on the tensors' memory and know nothing of autograd: a tensor that requires gradients is taken as its
+# values, results carry no graph, and what is written in place (out, dx, parameters, moments) does not move autograd's
+# version counters. A forward and its backward call are a user's autograd.Function's two halves.
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -682,7 +685,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
                eps: float = 1e-5, out: torch.Tensor | None = None
                ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Rows of x [rows, dim] normalised: (y, mean, rstd), y in x's type (in out, which may be x), mean and rstd float32.
-    weight and bias: float32 or x's type. Does not sync."""
+    weight and bias: float32 or x's type. y carries no autograd graph: layer_norm_backward takes the gradients. Does not
+    sync."""
     xp, xs = _rows_ptr(x, "x", x)
     kind = _type_of(x, "x")
     y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
@@ -761,7 +765,8 @@ def hs_loss(model: Model, x: torch.Tensor, targets: torch.Tensor, weights: torch
     """(loss, dx, dsyn1): -log P(targets[i] | x[i]) under the model's hierarchical softmax (float32) and, with grads,
     the gradients of sum(weights * loss) for x [rows, dim] and for model.syn1 (dsyn1 float32 of syn1's shape, all rows
     written: their first dim columns, and zeros in padding of less than 32; a new dsyn1 has zeros in all its padding).
-    targets int32, negative: none. Does not sync."""
+    targets int32, negative: none. The loss carries no autograd graph, whatever x requires: dx and dsyn1 are the gradients.
+    Does not sync."""
     xp, xs = _rows_ptr(x, "x", x)
     kind, longest = _type_of(x, "x"), _tree_of(model).max_len
     n, dev = x.shape[0], x.device
@@ -798,7 +803,8 @@ class AdamW:
 
     params, grads: float32, bfloat16 or float16 tensors of equal shapes, contiguous or 2-D with contiguous rows (views
     such as Model.vectors()). The buffers are fixed: write each step's gradients into `grads`. bits: of the moments, 32
-    or 8. weight_decay: one number, or one for each tensor.
+    or 8. weight_decay: one number, or one for each tensor. A tensor's .grad is not looked at, and autograd does not see a
+    step's writes.
 
     m and v hold all tensors' moments, tensor i's from offsets[i] on (multiples of 256): float32, or uint8 codes with the
     scales m_scale and v_scale (see include/w2v.h). state: those arrays of an earlier optimizer, (m, v) or
