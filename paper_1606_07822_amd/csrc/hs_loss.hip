@@ -331,6 +331,13 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
+// log(1 + q), q >= 0, to a few units in the last place: u = 1 + q is rounded, and log(u) / (u - 1) changes so little with u
+// that a factor q in its place takes the rounding out (Kahan; q itself where u is 1).
+__device__ __forceinline__ float log_one_more(float q) {
+    const float u = 1.0f + q, d = u - 1.0f;
+    return d == 0.0f ? q : logf(u) * (q * __builtin_amdgcn_rcpf(d));
+}
+
 // product_less_one over the four rows of 16 lanes, lane by lane.
 __device__ __forceinline__ float rows_product_less_one(float v) {
     float a = v, b = v;
@@ -474,7 +481,7 @@ __global__ __launch_bounds__(kWalkThreads) void k_hs_walk(WalkArgs a) {
     }
     if (a.loss && (lane & 15) == 0 && quarter < R && pos < a.n) {
         const bool missing = item.word >= 0 && item.len == 0;   // a target that the tree does not hold
-        a.loss[item.row] = missing ? __builtin_nanf("") : wrong + log1pf(prod);
+        a.loss[item.row] = missing ? __builtin_nanf("") : wrong + log_one_more(prod);
     }
     if constexpr (GRADS) {
         if (a.dx) {

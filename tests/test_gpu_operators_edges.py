@@ -28,8 +28,10 @@ def softmax_reference(otree, syn1, x, targets, weights=None, x_off=None):
 
     z: ceil(d / 64) products of a lane, added as they are formed, and 6 levels of lanes.
     e = exp(-|z|): z log2(e) rounded twice (2 |z| U ln 2 log2(e) of e), its power within 2 ulp (4 U).
-    The loss: prod (1 + e) - 1 takes two roundings a node and two a join of lanes, log1p 2 ulp, the terms -s z one
-    rounding a node; all of them relative, q / (1 + q) <= log1p(q) and e / (1 + e) <= log1p(e).
+    The loss: q = prod (1 + e) - 1 takes two roundings a node and at each of three joins (2 k + 6), log(1 + q) a logarithm and
+    a reciprocal of 1 ulp each (4 U), u - 1, two products and what the ratio log(u) / (u - 1) moves with u's rounding (4 U),
+    the terms -s z one rounding a node (fewer than q), their sum one; all of them relative, q / (1 + q) <= log(1 + q) and
+    e / (1 + e) <= log(1 + e).
     sigmoid: e's error, 1 + e, its reciprocal (1 ulp) and two products.
     dx: a multiply-add a node. dsyn1: 32 rows of a block, 16 blocks of a wavefront, 16 wavefronts, 9 of those in a slab of
     67,584 rows and a slab: 75 additions at most in a row."""
@@ -98,7 +100,8 @@ def test_loss_of_likely_words_keeps_its_digits(w2v, tree, n):  # noqa: F811
     x[:, 0] = 14 + (torch.arange(n, device="cuda") % 76) / 4
     z = x[:, :1].double().cpu().numpy() * (1 + (np.arange(k) % 5) / 8)
     loss = np.log1p(np.exp(-z)).sum(1)
-    # e: the exponent rounded twice and the power (2 |z| + 4); 2 roundings a node and at 4 joins; log1p 2 ulp
+    # e: the exponent rounded twice and the power (2 |z| + 4); 2 roundings a node, or at a quarter of the nodes and 2 joins
+    # (2 k + 4); log(1 + q) 8 U
     bound = 1.01 * ((2 * z + 4) * U * np.exp(-z)).sum(1) + (2 * k + 12) * U * loss
     t = torch.full((n,), word, dtype=torch.int32, device="cuda")
     for grads in (True, False):
