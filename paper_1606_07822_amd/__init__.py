@@ -708,7 +708,8 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
                         dbias: torch.Tensor | None = None, workspace: torch.Tensor | None = None
                         ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
     """Gradients (dx, dweight, dbias) of layer_norm for the upstream gradient dy, from its x, mean and rstd. dx in x's
-    type (may be dy or x); dweight and dbias float32, None without a weight unless given. Does not sync."""
+    type (may be dy or x); dweight and dbias float32: new ones with a weight where neither is given, otherwise those that
+    are given (None for the other). Does not sync."""
     xp, xs = _rows_ptr(x, "x", x)
     kind = _type_of(x, "x")
     dyp, dys = _rows_ptr(dy, "dy", x)

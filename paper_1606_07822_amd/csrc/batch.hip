@@ -146,8 +146,8 @@ struct Totals {
 
 // A batch's loss, terms and path nodes, summed by up to kTotalGroups workgroups (one alone fetches 65,536 rows' numbers in
 // 54 us), whose sums k_batch_totals adds to the call's. In a fixed order. A centre without a window gets an rstd of
-// 0 for the norm's backward pass, so that its normalised row is zeros there whatever norm_eps is: with norm_eps 0 its rstd
-// was infinite and its row NaN, which the zeros of its gradient would not take out of the gain's sums.
+// 0 for the norm's backward pass, so that its normalised row is zeros there: with norm_eps 0 the forward pass leaves an
+// infinite one and a row of NaN, which the zeros of the row's gradient would not take out of the gain's sums.
 constexpr int kTotalThreads = 1024;
 constexpr int kTotalGroups = 64;   // a wavefront adds them up
 __global__ __launch_bounds__(kTotalThreads) void k_batch_parts(const float *__restrict__ loss,
@@ -402,7 +402,8 @@ int run_batches(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, con
         }
         if (int rc = run_hs_loss(h, w.loss_ws, s)) return rc;
         const auto groups = static_cast<int>(std::min<int64_t>(kTotalGroups, ceil_div(a.n, kTotalThreads)));
-        k_batch_parts<<<static_cast<unsigned>(groups), kTotalThreads, 0, s>>>(w.loss, w.targets, w.lengths, a.n, w.rstd, w.parts);
+        k_batch_parts<<<static_cast<unsigned>(groups), kTotalThreads, 0, s>>>(w.loss, w.targets, w.lengths, a.n,
+                                                                                  w.rstd, w.parts);
         W2V_LAUNCH_CHECK("k_batch_parts");
         k_batch_totals<<<1, kWave, 0, s>>>(w.parts, groups, w.totals);
         W2V_LAUNCH_CHECK("k_batch_totals");
