@@ -156,6 +156,28 @@ def test_loss_makes_its_own_gradient(w2v, monkeypatch, dim, stride, n):  # noqa:
     assert set(filled) <= ({(model.V - 1, stride - dim)} if stride - dim >= 32 else set())
 
 
+@pytest.mark.parametrize("dim,stride", [(50, 64), (20, 64)])
+def test_a_captured_loss_makes_its_own_gradient(w2v, dim, stride):  # noqa: F811
+    """The same in a graph: every replay writes all of it again, whatever became of it in between."""
+    import torch
+    counts = COUNTS["zipf"]()
+    model, _ = make_model(w2v, counts, dim, stride=stride)
+    x = hidden(2500, dim, torch.float32)
+    t = torch.from_numpy(draw_targets(np.random.default_rng(1), counts, 2500)).cuda()
+    w2v.hs_loss(model, x, t)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        loss, dx, dsyn1 = w2v.hs_loss(model, x, t)
+    for k in range(4):
+        for out in (loss, dx, dsyn1):
+            out.fill_(float("nan"))
+        x.mul_(0.9)
+        g.replay()
+        want = w2v.hs_loss(model, x, t)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want[0]) and torch.equal(dx, want[1]) and torch.equal(dsyn1, want[2]), k
+
+
 # ------------------------------------------------------------------ sums of many rows
 @pytest.mark.parametrize("tree,n,dim,name", [("zipf", 257, 100, "f32"), ("zipf", 4096, 200, "f32"), ("wide", 9000, 65, "f32"),
                                              ("zipf", 8191, 520, "bf16"), ("wide", 33000, 300, "f16"), ("two", 67584, 5, "f32"),
