@@ -465,6 +465,105 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
                       float *m_out, float *v_out, void *hip_stream);
 
 /* ------------------------------------------------------------------------
+ * A gated feed-forward block of rows x (rows x dim elements of type), with the
+ * weights w_gate, w_up (hidden x dim) and w_down (dim x hidden) of the same
+ * type:
+ *     g = x w_gate',  u = x w_up',  h = act(g) u,  y = h w_down'
+ * act: W2V_SILU, g sigmoid(g), or W2V_GELU, g Phi(g) with the normal
+ * distribution's Phi. Strides count elements; dim and hidden are 1..2^20.
+ * gate and up (rows x hidden elements of type, may be NULL) receive g and u,
+ * which the backward pass takes. y may be x with the same stride; outputs may
+ * not overlap any other array. Sums are fp32. With type fp32 the products keep
+ * 24 bits of each factor; with 16-bit types h is rounded to type before the
+ * second product. An infinity among the factors of a fp32 product may make it
+ * NaN. Errors: W2V_E_ARG, W2V_E_WORKSPACE, W2V_E_RANGE (more rows than a
+ * launch takes).
+ *
+ * w2v_gated_ffn_backward: the gradients for an upstream gradient dy (rows x
+ * dim), from x, the weights and g and u as the forward pass left them:
+ *     dh = dy w_down,  du = dh act(g),  dg = dh u act'(g)
+ *     dx = dg w_gate + du w_up,  dw_gate = dg' x,  dw_up = du' x,
+ *     dw_down = dy' h
+ * Each may be NULL: not wanted. All are of type; the weights' are written, not
+ * added to (zeros for rows = 0). dx may be dy or x with the same stride; other
+ * outputs may not overlap any array. With 16-bit types dg, du and h are
+ * rounded to type between the products.
+ *
+ * Calls that overlap in time need a workspace each.
+ * ---------------------------------------------------------------------- */
+enum { W2V_SILU = 0, W2V_GELU = 1 };
+
+typedef struct {
+    const void *p;
+    int64_t stride;   /* elements from a row to the next */
+} w2v_rows;
+
+size_t w2v_gated_ffn_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type);
+int w2v_gated_ffn(w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, int64_t rows, int32_t dim, int32_t hidden,
+                  int32_t type, int32_t act, w2v_rows y, w2v_rows gate, w2v_rows up, void *workspace,
+                  size_t workspace_bytes, void *hip_stream);
+size_t w2v_gated_ffn_backward_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type);
+int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, w2v_rows gate,
+                           w2v_rows up, int64_t rows, int32_t dim, int32_t hidden, int32_t type, int32_t act, w2v_rows dx,
+                           w2v_rows dw_gate, w2v_rows dw_up, w2v_rows dw_down, void *workspace, size_t workspace_bytes,
+                           void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Nearly orthogonal matrices by Newton-Schulz products: X = g / (|g| + eps)
+ * with the Frobenius norm, then `steps` (1..20) times X = (a I + b A + c A A) X
+ * with A = X X' and a, b, c = 3.4445, -4.7750, 2.0315, which brings singular
+ * values between 0.7 and 1.2 in five steps. g and out: batch matrices of rows
+ * x cols elements of type (sides up to 2^20), a row `stride` and a matrix
+ * `step` elements behind the one before; out may be g with the same strides.
+ * The products keep 22 bits of each factor and sum in fp32; with type bf16
+ * they keep 11, whose error, 1.2e-3 of the result in norm, is below bf16's
+ * rounding. A matrix with an element that is not finite becomes NaN, the
+ * others do not; one of zeros stays zero. Errors: W2V_E_ARG, W2V_E_WORKSPACE,
+ * W2V_E_RANGE. */
+size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type);
+int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t batch, int32_t rows, int32_t cols,
+                      int32_t type, int32_t steps, double eps, void *out, int64_t out_stride, int64_t out_step,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Muon over many matrices: with G = grad grad_scale and a momentum M (fp32),
+ *     M = momentum M + G;  U = G + momentum M if nesterov, else M
+ *     param = param (1 - lr weight_decay) - lr scale orthogonalize(U)
+ * where bf16 parameters take the products of 11 bits. The momenta lie in one
+ * float array m, matrix i's (in row order, without gaps) from moment_offset
+ * on, a multiple of 256; zeros before the first step. The plan, device memory
+ * of w2v_muon_plan_bytes bytes that the caller keeps, is made once from a list
+ * (synchronises the stream), and a step is given the same list again.
+ * Matrices of the same sizes and types go through the products together. A
+ * plan, and a workspace, belong to one step at a time. Errors: W2V_E_ARG for
+ * sizes, strides, types or NULL pointers out of range, momenta that overlap or
+ * reach past n_moments (a matrix's last 256 count whole), or packed parameters
+ * that overlap; W2V_E_WORKSPACE; W2V_E_RANGE. */
+typedef struct {
+    void *param;              /* rows x cols elements of param_type */
+    const void *grad;         /* rows x cols elements of grad_type */
+    int64_t rows, cols;       /* 0..2^20 */
+    int64_t param_stride, grad_stride;
+    int64_t moment_offset;
+    int32_t param_type, grad_type;
+    float weight_decay, scale;
+} w2v_muon_matrix;
+
+typedef struct {
+    double lr, momentum, eps;
+    const float *lr_device;   /* NULL, or the learning rate in device memory (instead of lr) */
+    float grad_scale;
+    int32_t nesterov, steps;  /* steps 1..20 */
+    int32_t reserved0;
+} w2v_muon_params;
+
+size_t w2v_muon_plan_bytes(const w2v_muon_matrix *matrices_host, int32_t n);
+size_t w2v_muon_workspace_bytes(const w2v_muon_matrix *matrices_host, int32_t n);
+int w2v_muon_build_plan(const w2v_muon_matrix *matrices_host, int32_t n, int64_t n_moments, void *plan, size_t plan_bytes,
+                        void *hip_stream);
+int w2v_muon_step(const w2v_muon_matrix *matrices_host, int32_t n, const void *plan, float *m, const w2v_muon_params *p,
+                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
  * Training in mini-batches with the operators above: CBOW whose hidden vector
  * is the mean of the window's vectors, through a layer norm if gain and bias
  * are given, scored against the centre word by the hierarchical softmax.

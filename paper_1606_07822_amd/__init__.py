@@ -8,6 +8,7 @@ Entry points mirror the C ABI in include/w2v.h:
     build_vocab, build_huffman, train_hs_epoch, hs_loglik
     build_noise_table, train_ns_epoch, ns_objective (negative sampling)
     layer_norm, layer_norm_backward, hs_loss, AdamW (a mini-batch step on hidden vectors)
+    gated_ffn, gated_ffn_backward, orthogonalize, Muon (a learned block of such a step, and its matrices' optimizer)
     train_batch_epoch, batch_loglik (CBOW in mini-batches with them)
 plus the test hooks sample_pairs, keep_thresholds and sample_negatives.
 """
@@ -70,6 +71,22 @@ class CBatchParams(ctypes.Structure):
                 ("seed", ctypes.c_uint32), ("reserved0", I32)]
 
 
+class CRows(ctypes.Structure):
+    _fields_ = [("p", P), ("stride", I64)]
+
+
+class CMuonMatrix(ctypes.Structure):
+    _fields_ = [("param", P), ("grad", P), ("rows", I64), ("cols", I64), ("param_stride", I64), ("grad_stride", I64),
+                ("moment_offset", I64), ("param_type", I32), ("grad_type", I32), ("weight_decay", ctypes.c_float),
+                ("scale", ctypes.c_float)]
+
+
+class CMuonParams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("eps", ctypes.c_double), ("lr_device", P),
+                ("grad_scale", ctypes.c_float), ("nesterov", I32), ("steps", I32), ("reserved0", I32)]
+
+
+assert ctypes.sizeof(CRows) == 16 and ctypes.sizeof(CMuonMatrix) == 72 and ctypes.sizeof(CMuonParams) == 48
 assert ctypes.sizeof(CBatchParams) == 104
 assert ctypes.sizeof(CModel) == 80 and ctypes.sizeof(CParams) == 112
 assert ctypes.sizeof(CAdamWTensor) == 72 and ctypes.sizeof(CAdamWParams) == 64
@@ -174,6 +191,25 @@ def lib() -> ctypes.CDLL:
         L.w2v_batch_loglik.restype = ctypes.c_int
         L.w2v_batch_loglik.argtypes = [ctypes.POINTER(CModel), P, I64, ctypes.POINTER(CParams),
                                        ctypes.POINTER(CBatchParams), P, P, P, ctypes.c_size_t, P]
+        for name in ("w2v_gated_ffn", "w2v_gated_ffn_backward"):
+            size = getattr(L, name + "_workspace_bytes")
+            size.restype, size.argtypes = ctypes.c_size_t, [I64, I32, I32, I32]
+        L.w2v_gated_ffn.restype = ctypes.c_int
+        L.w2v_gated_ffn.argtypes = [CRows] * 4 + [I64, I32, I32, I32, I32] + [CRows] * 3 + [P, ctypes.c_size_t, P]
+        L.w2v_gated_ffn_backward.restype = ctypes.c_int
+        L.w2v_gated_ffn_backward.argtypes = [CRows] * 7 + [I64, I32, I32, I32, I32] + [CRows] * 4 + [P, ctypes.c_size_t, P]
+        L.w2v_orthogonalize_workspace_bytes.restype = ctypes.c_size_t
+        L.w2v_orthogonalize_workspace_bytes.argtypes = [I64, I32, I32, I32]
+        L.w2v_orthogonalize.restype = ctypes.c_int
+        L.w2v_orthogonalize.argtypes = [P, I64, I64, I64, I32, I32, I32, I32, ctypes.c_double, P, I64, I64, P,
+                                        ctypes.c_size_t, P]
+        for name in ("w2v_muon_plan_bytes", "w2v_muon_workspace_bytes"):
+            getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [ctypes.POINTER(CMuonMatrix), I32]
+        L.w2v_muon_build_plan.restype = ctypes.c_int
+        L.w2v_muon_build_plan.argtypes = [ctypes.POINTER(CMuonMatrix), I32, I64, P, ctypes.c_size_t, P]
+        L.w2v_muon_step.restype = ctypes.c_int
+        L.w2v_muon_step.argtypes = [ctypes.POINTER(CMuonMatrix), I32, P, P, ctypes.POINTER(CMuonParams), P,
+                                    ctypes.c_size_t, P]
         _LIB = L
     return _LIB
 
@@ -894,6 +930,190 @@ class AdamW:
             _check(lib().w2v_adamw_moments(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
                                            self.v_scale.data_ptr(), self.n_moments, mp, vp, _stream(self.device)))
         return outs[0], outs[1]
+
+
+# ------------------------------------------------- a learned block of such a step, and its matrices' optimizer
+_ACTS = {"silu": 0, "gelu": 1}
+
+
+def _matrix(t: torch.Tensor | None, shape: tuple[int, int], like: torch.Tensor, name: str) -> CRows:
+    """A [rows, columns] tensor of like's type and device with contiguous rows; None: no array."""
+    if t is None:
+        return CRows(None, 0)
+    if t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor on x's device")
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.dim() != 2 or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return CRows(t.data_ptr(), t.stride(0))
+
+
+def _block_of(x: torch.Tensor, w_gate, w_up, w_down, act: str):
+    """(rows, dim, hidden, type, act) and the arrays x and weights of a gated feed-forward block."""
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError("x and w_gate must have two dimensions")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {', '.join(_ACTS)}")
+    n, d, h = x.shape[0], x.shape[1], w_gate.shape[0]
+    kind = _type_of(x, "x")
+    return (n, d, h, kind, _ACTS[act]), (_matrix(x, (n, d), x, "x"), _matrix(w_gate, (h, d), x, "w_gate"),
+                                         _matrix(w_up, (h, d), x, "w_up"), _matrix(w_down, (d, h), x, "w_down"))
+
+
+def gated_ffn_workspace(x: torch.Tensor, hidden: int, grads: bool = False) -> torch.Tensor:
+    """A workspace for gated_ffn (with grads: for gated_ffn_backward) on x's rows, to be kept from call to call (calls that
+    overlap need one each)."""
+    size = lib().w2v_gated_ffn_backward_workspace_bytes if grads else lib().w2v_gated_ffn_workspace_bytes
+    return _workspace(size(x.shape[0], x.shape[1], hidden, _type_of(x, "x")), x.device)
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, act: str = "silu",
+              save: bool = False, out: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+              up: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+              ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
+    """(y, gate, up) of y = (act(x w_gate') * (x w_up')) w_down' for rows x [rows, dim], weights [hidden, dim] twice and
+    [dim, hidden], all of one type; act "silu" or "gelu". With save, gate and up [rows, hidden] hold the two products for
+    gated_ffn_backward (None otherwise). y goes into out, which may be x; gate and up into those that are given. y carries
+    no autograd graph. Does not sync."""
+    sizes, arrays = _block_of(x, w_gate, w_up, w_down, act)
+    n, d, h = sizes[:3]
+    y = torch.empty(n, d, dtype=x.dtype, device=x.device) if out is None else out
+    if save:
+        gate, up = (torch.empty(n, h, dtype=x.dtype, device=x.device) if t is None else t for t in (gate, up))
+    elif gate is not None or up is not None:
+        raise ValueError("gate and up are written with save only")
+    outs = _matrix(y, (n, d), x, "out"), _matrix(gate, (n, h), x, "gate"), _matrix(up, (n, h), x, "up")
+    with _On(x.device):
+        ws = _kept(workspace, lib().w2v_gated_ffn_workspace_bytes(*sizes[:4]), x.device)
+        _check(lib().w2v_gated_ffn(*arrays, *sizes, *outs, None if ws is None else ws.data_ptr(),
+                                   0 if ws is None else ws.numel(), _stream(x.device)))
+    return y, gate, up
+
+
+def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                       gate: torch.Tensor, up: torch.Tensor, act: str = "silu", dx: torch.Tensor | None = None,
+                       dw_gate: torch.Tensor | None = None, dw_up: torch.Tensor | None = None,
+                       dw_down: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+                       ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the upstream gradient dy, from its x, its weights, and gate
+    and up as it saved them; all of x's type. dx may be dy or x. Does not sync."""
+    sizes, arrays = _block_of(x, w_gate, w_up, w_down, act)
+    n, d, h = sizes[:3]
+    ins = _matrix(dy, (n, d), x, "dy"), *arrays, _matrix(gate, (n, h), x, "gate"), _matrix(up, (n, h), x, "up")
+    shapes = (n, d), (h, d), (h, d), (d, h)
+    grads = [torch.empty(s, dtype=x.dtype, device=x.device) if t is None else t
+             for t, s in zip((dx, dw_gate, dw_up, dw_down), shapes)]
+    outs = [_matrix(t, s, x, name) for t, s, name in zip(grads, shapes, ("dx", "dw_gate", "dw_up", "dw_down"))]
+    with _On(x.device):
+        ws = _kept(workspace, lib().w2v_gated_ffn_backward_workspace_bytes(*sizes[:4]), x.device)
+        _check(lib().w2v_gated_ffn_backward(*ins, *sizes, *outs, None if ws is None else ws.data_ptr(),
+                                            0 if ws is None else ws.numel(), _stream(x.device)))
+    return tuple(grads)
+
+
+def _stack_of(t: torch.Tensor, name: str, like: torch.Tensor) -> tuple[int, int, int]:
+    """(pointer, row stride, matrix stride) of a matrix, or a stack of them, of like's shape, type and device."""
+    if t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor on g's device")
+    if t.dtype != like.dtype or t.shape != like.shape or t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be {like.dtype} of the shape {tuple(like.shape)}, of two or three dimensions")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return t.data_ptr(), t.stride(-2), t.stride(0) if t.dim() == 3 else 0
+
+
+def orthogonalize_workspace(g: torch.Tensor) -> torch.Tensor:
+    """A workspace for orthogonalize on matrices of g's shape, to be kept from call to call (calls that overlap need one
+    each)."""
+    return _workspace(lib().w2v_orthogonalize_workspace_bytes(g.shape[0] if g.dim() == 3 else 1, *g.shape[-2:],
+                                                              _type_of(g, "g")), g.device)
+
+
+def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """The matrix g [rows, cols], or each of a stack [count, rows, cols], with its singular values brought near one by
+    `steps` Newton-Schulz steps from g over its Frobenius norm plus eps; in g's type, in out, which may be g. Does not
+    sync."""
+    gp = _stack_of(g, "g", g)
+    kind = _type_of(g, "g")
+    out = torch.empty_like(g, memory_format=torch.contiguous_format) if out is None else out
+    op = _stack_of(out, "out", g)
+    sizes = g.shape[0] if g.dim() == 3 else 1, *g.shape[-2:], kind
+    with _On(g.device):
+        ws = _kept(workspace, lib().w2v_orthogonalize_workspace_bytes(*sizes), g.device)
+        _check(lib().w2v_orthogonalize(*gp, *sizes, steps, eps, *op, None if ws is None else ws.data_ptr(),
+                                       0 if ws is None else ws.numel(), _stream(g.device)))
+    return out
+
+
+class Muon:
+    """Muon over a list of matrices and their gradient buffers, updated in place: momentum, then an update orthogonalised by
+    Newton-Schulz products. AdamW is for the other tensors.
+
+    params, grads: 2-D float32, bfloat16 or float16 tensors of equal shapes with contiguous rows. The buffers are fixed:
+    write each step's gradients into `grads`. weight_decay: one number, or one for each matrix. scale: what an
+    orthogonalised update is multiplied with beside the learning rate, one number or one for each matrix; None takes
+    sqrt(max(1, rows / cols)). A tensor's .grad is not looked at, and autograd does not see a step's writes. One step at a
+    time: the workspace belongs to the optimizer.
+
+    m holds all matrices' momenta, matrix i's from offsets[i] on (multiples of 256), float32. state: that array of an
+    earlier optimizer, which is then used as it is; zeros otherwise."""
+
+    BLOCK = 256
+
+    def __init__(self, params, grads, momentum: float = 0.95, nesterov: bool = True, steps: int = 5, eps: float = 1e-7,
+                 weight_decay=0.0, scale=None, state: torch.Tensor | None = None):
+        if not params or len(params) != len(grads):
+            raise ValueError("params and grads must be lists of the same length, at least 1")
+        lists = []
+        for name, v in (("weight_decay", weight_decay), ("scale", scale)):
+            lists.append(list(v) if isinstance(v, (list, tuple)) else [v] * len(params))
+            if len(lists[-1]) != len(params):
+                raise ValueError(f"{name} must be a number or hold one for each matrix")
+        self.params, self.grads, self.momentum, self.nesterov, self.steps, self.eps = (list(params), list(grads), momentum,
+                                                                                       nesterov, steps, eps)
+        self.device = dev = params[0].device
+        self.offsets, at = [], 0
+        self._table = table = (CMuonMatrix * len(params))()
+        for i, (p, g, decay, factor) in enumerate(zip(params, grads, *lists)):
+            for t, name in ((p, f"params[{i}]"), (g, f"grads[{i}]")):
+                if not t.is_cuda or t.device != dev:
+                    raise ValueError(f"{name} must be a GPU tensor on {dev}")
+                if t.dim() != 2 or t.shape != p.shape:
+                    raise ValueError(f"{name} must have two dimensions and the shape {tuple(p.shape)}, got {tuple(t.shape)}")
+                if t.shape[1] > 1 and t.stride(1) != 1:
+                    raise ValueError(f"{name}'s rows must be contiguous")
+            rows, cols = p.shape
+            if factor is None:
+                factor = max(1.0, rows / max(1, cols)) ** 0.5
+            table[i] = CMuonMatrix(p.data_ptr(), g.data_ptr(), rows, cols, p.stride(0), g.stride(0), at,
+                                   _type_of(p, f"params[{i}]"), _type_of(g, f"grads[{i}]"), decay, factor)
+            self.offsets.append(at)
+            at += -(-p.numel() // self.BLOCK) * self.BLOCK
+        self.n_moments = at
+        self.m = torch.zeros(at, dtype=torch.float32, device=dev) if state is None else state
+        self._m_ptr = _vector_ptr(self.m, torch.float32, at, dev, "state")
+        self._buffers = [t.detach() for t in (*params, *grads, self.m)]   # their memory stays, whatever becomes of the tensors
+        n = len(params)
+        self._plan = _workspace(lib().w2v_muon_plan_bytes(table, n), dev)
+        self._workspace = _workspace(lib().w2v_muon_workspace_bytes(table, n), dev)
+        with _On(dev):
+            _check(lib().w2v_muon_build_plan(table, n, at, self._plan.data_ptr(), self._plan.numel(), _stream(dev)))
+
+    def step(self, lr, grad_scale: float = 1.0) -> None:
+        """One step with the learning rate lr, which may be a one-element float32 tensor on the device that is read when the
+        step runs, so that a captured step can be replayed with new values. Does not sync."""
+        p = CMuonParams(0.0, self.momentum, self.eps, None, grad_scale, int(self.nesterov), self.steps, 0)
+        if isinstance(lr, torch.Tensor):
+            p.lr_device = _vector_ptr(lr, torch.float32, 1, self.device, "lr")
+        else:
+            p.lr = lr
+        with _On(self.device):
+            _check(lib().w2v_muon_step(self._table, len(self._table), self._plan.data_ptr(), self._m_ptr, ctypes.byref(p),
+                                       self._workspace.data_ptr(), self._workspace.numel(), _stream(self.device)))
 
 
 # ------------------------------------------------------------- training in mini-batches

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libw2v.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "vocab.hip", "huffman.hip", "sampling.hip", "train.hip", "sync_loglik.hip", "negative.hip", "noalloc.hip",
-           "norm.hip", "hs_loss.hip", "adamw.hip", "batch.hip", "ops_api.hip"]
+           "norm.hip", "hs_loss.hip", "adamw.hip", "ffn.hip", "muon.hip", "batch.hip", "ops_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

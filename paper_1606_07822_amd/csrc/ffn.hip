@@ -1,0 +1,517 @@
+// A gated feed-forward block of rows, forward and backward.
+//
+//   g = x Wg',  u = x Wu',  h = act(g) u,  y = h Wd'        act: g sigmoid(g), or g Phi(g) (the normal distribution's)
+//   dh = dy Wd,  du = dh act(g),  dg = dh u act'(g),  dx = dg Wg + du Wu,  dWg = dg' x,  dWu = du' x,  dWd = dy' h
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "w2v_ops.h"
+#include "w2v_product.h"
+
+namespace w2v {
+namespace {
+
+// ------------------------------------------------------------------ activations
+__device__ __forceinline__ float act_value(int act, float g) {
+    if (act == W2V_SILU) return g / (1.0f + expf(-g));
+    return 0.5f * g * erfcf(-0.70710678f * g);
+}
+
+__device__ __forceinline__ void act_both(int act, float g, float &value, float &slope) {
+    if (act == W2V_SILU) {
+        const float p = 1.0f / (1.0f + expf(-g));
+        value = g * p;
+        slope = p * (1.0f + g * (1.0f - p));
+    } else {
+        const float p = 0.5f * erfcf(-0.70710678f * g);
+        value = g * p;
+        slope = p + g * 0.39894228f * expf(-0.5f * g * g);
+    }
+}
+
+// ------------------------------------------------------------------ operands as parts
+// An array as the matrix products read it: P planes of 16-bit parts in rows of whole chunks, zeros behind the last column.
+struct Source {
+    const void *from;
+    int64_t from_stride;   // elements
+    void *to;
+    int64_t rows, cols, to_stride;   // to_stride in elements, a multiple of 8
+    int64_t first;         // number of its first chunk in the launch
+};
+struct Sources {
+    Source s[7];
+    int32_t count;
+    int64_t chunks;
+};
+
+template <class T, class E, int P>
+__global__ __launch_bounds__(256) void k_parts(const Sources all) {
+    for (int64_t c = blockIdx.x * int64_t(256) + threadIdx.x; c < all.chunks; c += int64_t(gridDim.x) * 256) {
+        int i = 0;
+        while (i + 1 < all.count && c >= all.s[i + 1].first) ++i;
+        const Source &s = all.s[i];
+        const int64_t per = s.to_stride / 8, row = (c - s.first) / per, chunk = (c - s.first) % per;
+        float v[8];
+        const int64_t left = s.cols - chunk * 8;
+        load_cols<T, 8>(static_cast<const T *>(s.from) + row * s.from_stride + chunk * 8, 0,
+                        static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(left, 8))), v);
+        Frag<E> part[P];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            E one[P];
+            to_parts<E, P>(v[e], one);
+#pragma unroll
+            for (int p = 0; p < P; ++p) part[p][e] = one[p];
+        }
+        E *to = static_cast<E *>(s.to) + row * s.to_stride + chunk * 8;
+#pragma unroll
+        for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * s.rows * s.to_stride) = part[p];
+    }
+}
+
+// ------------------------------------------------------------------ jobs
+struct Place {
+    int64_t m0, n0;
+    int32_t which;
+};
+
+// Four elements of a row whose first `valid` exist.
+template <class T>
+__device__ __forceinline__ void store4(T *to, int64_t valid, f4 v) {
+    const float f[4] = {v[0], v[1], v[2], v[3]};
+    if (valid >= 4) {
+        store_pack<T, 4>(to, f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < valid) to[e] = static_cast<T>(f[e]);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ f4 load4(const T *from, int64_t valid) {
+    float f[4];
+    load_cols<T, 4>(from, 0, static_cast<int>(std::min<int64_t>(valid, 4)), f);
+    return f4{f[0], f[1], f[2], f[3]};
+}
+
+// Parts of a row's four elements; zeros from `valid` on.
+template <class E, int P>
+__device__ __forceinline__ void store_parts(E *to, int64_t plane, int64_t valid, f4 v) {
+    using E4 = E __attribute__((ext_vector_type(4)));
+    E4 part[P];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        E one[P];
+        to_parts<E, P>(e < valid ? v[e] : 0.0f, one);
+#pragma unroll
+        for (int p = 0; p < P; ++p) part[p][e] = one[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<E4 *>(to + p * plane) = part[p];
+}
+
+// Up to three products of one kind and k, or two whose results are added.
+struct Product {
+    Side a, b;
+    int64_t m, n, gm, gn, first;   // sizes, tiles, number of its first tile
+    void *out;
+    int64_t out_stride;
+};
+template <class T>
+struct ProductJob {
+    Product p[3];
+    int32_t count, splits;
+    bool sum;        // p[0] + p[1], in p[0].out
+    int64_t k, tiles;
+    f4 *part;
+
+    template <class Q>
+    __device__ __forceinline__ Place at(int64_t tile) const {
+        Place w;
+        w.which = count > 2 && tile >= p[2].first ? 2 : count > 1 && tile >= p[1].first ? 1 : 0;
+        int64_t tm, tn;
+        tile_at(tile - p[w.which].first, p[w.which].gm, p[w.which].gn, tm, tn);
+        w.m0 = tm * Q::BM;
+        w.n0 = tn * Q::BN;
+        return w;
+    }
+    template <class Q>
+    __device__ __forceinline__ void multiply(const Place &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        const Product &x = p[w.which];
+        if (!sum) {
+            const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
+            if (k0 < k1) Q::run(x.a, x.b, 0, w.m0, x.m, w.n0, x.n, k0, k1, lds, acc);
+            return;
+        }
+        const int64_t whole = ceil_div(k, Q::BK) * Q::BK, step = split_steps(2 * whole, Q::BK, splits), k0 = split * step;
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            const int64_t lo = std::max<int64_t>(0, k0 - i * whole), hi = std::min(k, k0 + step - i * whole);
+            if (i == 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the first product's reads of LDS
+            if (lo < hi) Q::run(p[i].a, p[i].b, 0, w.m0, x.m, w.n0, x.n, lo, hi, lds, acc);
+        }
+    }
+    __device__ __forceinline__ void put(const Place &w, int row, int col, f4 v0, f4 v1) const {
+        const Product &x = p[w.which];
+        const int64_t m = w.m0 + row, n = w.n0 + col;
+        if (m >= x.m) return;
+        T *to = static_cast<T *>(x.out) + m * x.out_stride + n;
+        store4<T>(to, x.n - n, v0);
+        store4<T>(to + 16, x.n - n - 16, v1);
+    }
+};
+
+// g and u of 16 columns each side by side in a tile; h's parts, and g and u themselves where they are wanted.
+template <class T, class E, int P>
+struct UpJob {
+    Side x, w;
+    int64_t other;   // from Wg to Wu, bytes
+    int64_t m, n, gm, gn, k, tiles;
+    int32_t splits, act;
+    f4 *part;
+    E *h;
+    int64_t h_stride, h_plane;
+    T *gate, *up;
+    int64_t gate_stride, up_stride;
+
+    template <class Q>
+    __device__ __forceinline__ Place at(int64_t tile) const {
+        int64_t tm, tn;
+        tile_at(tile, gm, gn, tm, tn);
+        return Place{tm * Q::BM, tn * (Q::BN / 2), 0};
+    }
+    template <class Q>
+    __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
+        if (k0 < k1) Q::run(x, w, other, w0.m0, m, w0.n0, n, k0, k1, lds, acc);
+    }
+    __device__ __forceinline__ void put(const Place &w0, int row, int col, f4 g, f4 u) const {
+        const int64_t r = w0.m0 + row, c = w0.n0 + col / 32 * 16 + col % 16, valid = n - c;
+        if (r >= m) return;
+        if (gate) store4<T>(gate + r * gate_stride + c, valid, g);
+        if (up) store4<T>(up + r * up_stride + c, valid, u);
+        if (c >= h_stride) return;
+        f4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = act_value(act, g[e]) * u[e];
+        store_parts<E, P>(h + r * h_stride + c, h_plane, valid, v);
+    }
+};
+
+// dh, from which the parts of dg, du and h are made where it lies in registers.
+template <class T, class E, int P>
+struct BackJob {
+    Side dy, w;
+    int64_t m, n, gm, gn, k, tiles;
+    int32_t splits, act;
+    f4 *part;
+    E *dg, *du, *h;
+    int64_t h_stride, h_plane;
+    const T *gate, *up;
+    int64_t gate_stride, up_stride;
+
+    template <class Q>
+    __device__ __forceinline__ Place at(int64_t tile) const {
+        int64_t tm, tn;
+        tile_at(tile, gm, gn, tm, tn);
+        return Place{tm * Q::BM, tn * Q::BN, 0};
+    }
+    template <class Q>
+    __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
+        if (k0 < k1) Q::run(dy, w, 0, w0.m0, m, w0.n0, n, k0, k1, lds, acc);
+    }
+    __device__ __forceinline__ void put(const Place &w0, int row, int col, f4 v0, f4 v1) const {
+        const int64_t r = w0.m0 + row, c = w0.n0 + col;
+        if (r >= m) return;
+        one(r, c, v0);
+        one(r, c + 16, v1);
+    }
+    __device__ __forceinline__ void one(int64_t r, int64_t c, f4 dh) const {
+        if (c >= h_stride) return;
+        const int64_t valid = n - c;
+        const f4 g = load4(gate + r * gate_stride + c, valid), u = load4(up + r * up_stride + c, valid);
+        f4 vg, vu, vh;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float value, slope;
+            act_both(act, g[e], value, slope);
+            vh[e] = value * u[e];
+            vu[e] = dh[e] * value;
+            vg[e] = dh[e] * u[e] * slope;
+        }
+        const int64_t at = r * h_stride + c;
+        store_parts<E, P>(dg + at, h_plane, valid, vg);
+        store_parts<E, P>(du + at, h_plane, valid, vu);
+        store_parts<E, P>(h + at, h_plane, valid, vh);
+    }
+};
+
+// ------------------------------------------------------------------ tiles and how a product is cut into them
+template <class E, bool A, bool B, bool PAIR = false>
+struct Tiles1 {
+    using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B, PAIR>;
+    using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR>;
+};
+template <class E, bool A, bool B, bool PAIR = false>
+struct Tiles3 {
+    using Large = Tile<E, 3, 256, 128, 4, 2, 32, A, B, PAIR>;
+    using Small = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR>;
+};
+template <class T>
+struct Kind {   // 16-bit rows are multiplied as they are
+    using E = T;
+    static constexpr int P = 1;
+    template <bool A, bool B, bool PAIR = false>
+    using Tiles = Tiles1<E, A, B, PAIR>;
+};
+template <>
+struct Kind<float> {   // fp32 rows as three parts of 8 bits, 24 in all
+    using E = __bf16;
+    static constexpr int P = 3;
+    template <bool A, bool B, bool PAIR = false>
+    using Tiles = Tiles3<E, A, B, PAIR>;
+};
+
+template <class S>
+int64_t count_tiles(int64_t m, int64_t n) {
+    return ceil_div(m, S::BM) * ceil_div(n, S::BN);
+}
+
+template <class L, class S>
+Cut cut_of(int64_t m, int64_t n, int64_t k) {
+    return choose_cut(count_tiles<L>(m, n), count_tiles<S>(m, n), double(S::BM * S::BN) / (L::BM * L::BN), k, S::BK);
+}
+
+template <class L, class S>
+size_t part_bytes(const Cut &c) {
+    return cut_bytes(c, L::BM * L::BN, S::BM * S::BN);
+}
+
+// ------------------------------------------------------------------ operands
+// 16-bit rows of whole, aligned chunks are read where they are.
+bool in_place(int32_t type, const Rows &r, int64_t rows, int64_t cols) {
+    return type != W2V_F32 && cols % 8 == 0 && reinterpret_cast<uintptr_t>(r.p) % 16 == 0 &&
+           (rows <= 1 || (r.stride % 8 == 0 && r.stride < (1 << 23)));
+}
+
+struct Packing {
+    Sources all{};
+    int32_t type;
+    int parts;
+    Carve *carve;
+
+    Side operand(const Rows &r, int64_t rows, int64_t cols) {
+        if (in_place(type, r, rows, cols))
+            return Side{static_cast<const char *>(r.p), 0, (rows <= 1 ? cols : r.stride) * 2};
+        const int64_t stride = ceil_div(cols, 8) * 8;
+        char *to = carve->take<char>(static_cast<size_t>(parts * rows * stride * 2));
+        Source &s = all.s[all.count++];
+        s = Source{r.p, r.stride, to, rows, cols, stride, all.chunks};
+        all.chunks += rows * (stride / 8);
+        return Side{to, rows * stride * 2, stride * 2};
+    }
+};
+
+template <class T>
+int launch_parts(const Packing &p, hipStream_t s) {
+    if (p.all.chunks == 0) return W2V_OK;
+    const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(p.all.chunks, 256), kMaxGroups));
+    k_parts<T, typename Kind<T>::E, Kind<T>::P><<<grid, 256, 0, s>>>(p.all);
+    W2V_LAUNCH_CHECK("k_parts");
+    return W2V_OK;
+}
+
+template <class S>
+int64_t tile_m(const Cut &c) {
+    return c.large ? S::Large::BM : S::Small::BM;
+}
+template <class S>
+int64_t tile_n(const Cut &c) {
+    return c.large ? S::Large::BN : S::Small::BN;
+}
+
+// One plan of a pass: where its arrays lie, without a workspace only how many bytes they are.
+template <class T>
+int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
+    using K = Kind<T>;
+    using E = typename K::E;
+    using Up = typename K::template Tiles<true, true, true>;
+    using Down = typename K::template Tiles<true, true>;
+    const int64_t n = a.rows, d = a.dim, f = a.hidden, hs = ceil_div(f, 64) * 64;
+    Packing pack{{}, a.type, K::P, &c};
+    const Side x = pack.operand(a.x, n, d);
+    Side wg = pack.operand(a.w_gate, f, d), wu = pack.operand(a.w_up, f, d);
+    const Side wd = pack.operand(a.w_down, d, f);
+    E *h = c.take<E>(static_cast<size_t>(K::P * n * hs));
+    const Cut up = cut_of<typename Up::Large, typename Up::Small>(n, 2 * f, d),
+              down = cut_of<typename Down::Large, typename Down::Small>(n, d, f);
+    char *part = c.take<char>(std::max(part_bytes<typename Up::Large, typename Up::Small>(up),
+                                       part_bytes<typename Down::Large, typename Down::Small>(down)));
+    if (!launch) return W2V_OK;
+    if (up.tiles > kMaxTiles || down.tiles > kMaxTiles) return fail(W2V_E_RANGE, "too many rows for one call");
+    if (int rc = launch_parts<T>(pack, s)) return rc;
+    UpJob<T, E, K::P> u{};
+    u.x = x;
+    u.w = wg;
+    u.other = wu.p - wg.p;
+    u.m = n;
+    u.n = f;
+    u.gm = ceil_div(n, tile_m<Up>(up));
+    u.gn = ceil_div(2 * f, tile_n<Up>(up));
+    u.k = d;
+    u.act = a.act;
+    u.part = reinterpret_cast<f4 *>(part);
+    u.h = h;
+    u.h_stride = hs;
+    u.h_plane = n * hs;
+    u.gate = static_cast<T *>(const_cast<void *>(a.gate.p));
+    u.up = static_cast<T *>(const_cast<void *>(a.up.p));
+    u.gate_stride = a.gate.stride;
+    u.up_stride = a.up.stride;
+    if (int rc = launch_cut<Up>(up, u, s)) return rc;
+    ProductJob<T> y{};
+    y.p[0] = Product{Side{reinterpret_cast<char *>(h), n * hs * 2, hs * 2}, wd, n, d, ceil_div(n, tile_m<Down>(down)),
+                     ceil_div(d, tile_n<Down>(down)), 0, const_cast<void *>(a.y.p), a.y.stride};
+    y.count = 1;
+    y.k = f;
+    y.part = reinterpret_cast<f4 *>(part);
+    return launch_cut<Down>(down, y, s);
+}
+
+template <class T>
+int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
+    using K = Kind<T>;
+    using E = typename K::E;
+    using Hidden = typename K::template Tiles<true, false>;
+    using Weights = typename K::template Tiles<false, false>;
+    const int64_t n = a.rows, d = a.dim, f = a.hidden, hs = ceil_div(f, 64) * 64;
+    Packing pack{{}, a.type, K::P, &c};
+    const Side dy = pack.operand(a.dy, n, d), wd = pack.operand(a.w_down, d, f);
+    const Side x = pack.operand(a.x, n, d);
+    const Side wg = pack.operand(a.w_gate, f, d), wu = pack.operand(a.w_up, f, d);
+    E *h[3];
+    Side hid[3];
+    for (int i = 0; i < 3; ++i) {
+        h[i] = c.take<E>(static_cast<size_t>(K::P * n * hs));
+        hid[i] = Side{reinterpret_cast<char *>(h[i]), n * hs * 2, hs * 2};
+    }
+    using HL = typename Hidden::Large;
+    using HS = typename Hidden::Small;
+    using WL = typename Weights::Large;
+    using WS = typename Weights::Small;
+    const Cut back = cut_of<HL, HS>(n, f, d), in = cut_of<HL, HS>(n, d, 2 * f);
+    const Cut weights = choose_cut(2 * count_tiles<WL>(f, d) + count_tiles<WL>(d, f),
+                               2 * count_tiles<WS>(f, d) + count_tiles<WS>(d, f),
+                               double(WS::BM * WS::BN) / (WL::BM * WL::BN), n, WS::BK);
+    char *part = c.take<char>(std::max({part_bytes<HL, HS>(back), part_bytes<HL, HS>(in), part_bytes<WL, WS>(weights)}));
+    if (!launch) return W2V_OK;
+    if (back.tiles > kMaxTiles || in.tiles > kMaxTiles || weights.tiles > kMaxTiles)
+        return fail(W2V_E_RANGE, "too many rows for one call");
+    if (int rc = launch_parts<T>(pack, s)) return rc;
+    BackJob<T, E, K::P> b{};
+    b.dy = dy;
+    b.w = wd;
+    b.m = n;
+    b.n = f;
+    b.gm = ceil_div(n, tile_m<Hidden>(back));
+    b.gn = ceil_div(f, tile_n<Hidden>(back));
+    b.k = d;
+    b.act = a.act;
+    b.part = reinterpret_cast<f4 *>(part);
+    b.dg = h[0];
+    b.du = h[1];
+    b.h = h[2];
+    b.h_stride = hs;
+    b.h_plane = n * hs;
+    b.gate = static_cast<const T *>(a.gate.p);
+    b.up = static_cast<const T *>(a.up.p);
+    b.gate_stride = a.gate.stride;
+    b.up_stride = a.up.stride;
+    if (int rc = launch_cut<Hidden>(back, b, s)) return rc;
+    ProductJob<T> j{};
+    const Rows outs[3] = {a.dw_gate, a.dw_up, a.dw_down};
+    int64_t first = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (!outs[i].p) continue;
+        const int64_t m = i < 2 ? f : d, cols = i < 2 ? d : f;
+        const int64_t gm = ceil_div(m, tile_m<Weights>(weights)), gn = ceil_div(cols, tile_n<Weights>(weights));
+        j.p[j.count++] = Product{i < 2 ? hid[i] : dy, i < 2 ? x : hid[2], m, cols, gm, gn, first, const_cast<void *>(outs[i].p),
+                                 outs[i].stride};
+        first += gm * gn;
+    }
+    if (first > 0) {
+        j.k = n;
+        j.part = reinterpret_cast<f4 *>(part);
+        Cut w = weights;
+        w.tiles = first;   // of the gradients that are wanted
+        if (int rc = launch_cut<Weights>(w, j, s)) return rc;
+    }
+    // dx last: it may lie where dy or x did
+    if (!a.dx.p) return W2V_OK;
+    ProductJob<T> i{};
+    for (int q = 0; q < 2; ++q)
+        i.p[q] = Product{hid[q], q ? wu : wg, n, d, ceil_div(n, tile_m<Hidden>(in)), ceil_div(d, tile_n<Hidden>(in)), 0,
+                         const_cast<void *>(a.dx.p), a.dx.stride};
+    i.count = 1;
+    i.sum = true;
+    i.k = f;
+    i.part = reinterpret_cast<f4 *>(part);
+    return launch_cut<Hidden>(in, i, s);
+}
+
+// Gradients of no rows: zeros, by a kernel (a captured graph takes no memset).
+template <class T>
+__global__ __launch_bounds__(256) void k_zero_rows(T *p, int64_t rows, int64_t cols, int64_t stride) {
+    for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < rows * cols; i += int64_t(gridDim.x) * 256)
+        p[i / cols * stride + i % cols] = static_cast<T>(0.0f);
+}
+
+}  // namespace
+
+size_t ffn_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type, bool backward_pass) {
+    if (rows == 0) return 0;
+    // the sizes are those of arrays none of which can be read in place
+    FfnArgs a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.hidden = hidden;
+    a.type = type;
+    Rows odd{reinterpret_cast<const void *>(uintptr_t(2)), 1};
+    a.x = a.w_gate = a.w_up = a.w_down = a.dy = odd;
+    Carve c;
+    with_type(type, [&](auto zero) {
+        using T = decltype(zero);
+        return backward_pass ? backward<T>(a, c, false, nullptr) : forward<T>(a, c, false, nullptr);
+    });
+    return c.used();
+}
+
+int run_ffn(const FfnArgs &a, void *workspace, hipStream_t s) {
+    if (a.rows == 0) return W2V_OK;
+    Carve c(workspace);
+    return with_type(a.type, [&](auto zero) { return forward<decltype(zero)>(a, c, true, s); });
+}
+
+int run_ffn_backward(const FfnArgs &a, void *workspace, hipStream_t s) {
+    Carve c(workspace);
+    if (a.rows > 0) return with_type(a.type, [&](auto zero) { return backward<decltype(zero)>(a, c, true, s); });
+    const Rows outs[3] = {a.dw_gate, a.dw_up, a.dw_down};
+    for (int i = 0; i < 3; ++i) {
+        if (!outs[i].p) continue;
+        const int64_t rows = i < 2 ? a.hidden : a.dim, cols = i < 2 ? a.dim : a.hidden;
+        const auto grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * cols, 256), kMaxGroups));
+        const int rc = with_type(a.type, [&](auto zero) {
+            using T = decltype(zero);
+            k_zero_rows<T><<<grid, 256, 0, s>>>(static_cast<T *>(const_cast<void *>(outs[i].p)), rows, cols, outs[i].stride);
+            W2V_LAUNCH_CHECK("k_zero_rows");
+            return static_cast<int>(W2V_OK);
+        });
+        if (rc) return rc;
+    }
+    return W2V_OK;
+}
+
+}  // namespace w2v

@@ -1,0 +1,508 @@
+// Muon: momentum, and an update whose singular values five Newton-Schulz steps bring near one.
+//
+//   M = mu M + G,  U = G + mu M (Nesterov) or M,  X = U / (|U| + eps),  five times X = (a I + b A + c A A) X with A = X X',
+//   W = W (1 - lr decay) - lr scale X
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <tuple>
+#include <type_traits>
+#include <vector>
+
+#include "w2v_ops.h"
+#include "w2v_product.h"
+
+namespace w2v {
+namespace {
+
+using E = _Float16;
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+// Everything that the steps hold is kept times 2^12 in fp16: entries of X are at most 1.21 in size, of A 1.45 and of
+// aI + bA + cAA 3.45, and the second part's absolute error, 2^-25, is 2^-37 of one.
+constexpr float kUp = 4096.0f, kDown = 1.0f / 4096.0f;
+constexpr int kParts = 256;       // sums of squares of a matrix
+
+// Where a matrix of a launch lies.
+struct Entry {
+    void *out;             // the parameter, or the orthogonalised matrix
+    const void *grad;
+    int64_t out_stride, grad_stride, moment;
+    float decay, scale;
+};
+struct Batch {
+    const Entry *table;    // null: `first`, and each next one `out_step` and `grad_step` bytes on
+    Entry first;
+    int64_t out_step, grad_step;
+    int64_t rows, cols, count;
+    float *m;              // null: no momentum
+    float mu;
+    int32_t nesterov, muon;
+    float grad_scale;
+    float lr;
+    const float *lr_device;
+
+    __device__ __forceinline__ Entry entry(int64_t z) const {
+        if (table) return table[z];
+        Entry e = first;
+        e.out = static_cast<char *>(e.out) + z * out_step;
+        e.grad = static_cast<const char *>(e.grad) + z * grad_step;
+        return e;
+    }
+};
+
+// ------------------------------------------------------------------ momentum and norms
+// Block b of matrix z: its share of the rows' chunks of four elements, and their sum of squares.
+template <class T>
+__global__ __launch_bounds__(256) void k_muon_momentum(const Batch b, double *part) {
+    const int64_t z = blockIdx.x / kParts;
+    const int chunk0 = static_cast<int>(blockIdx.x % kParts);
+    const Entry e = b.entry(z);
+    const int64_t per = ceil_div(b.cols, 4), chunks = b.rows * per;
+    double sum = 0.0;
+    for (int64_t c = chunk0 * int64_t(256) + threadIdx.x; c < chunks; c += kParts * 256) {
+        const int64_t row = c / per, col = c % per * 4;
+        const int valid = static_cast<int>(std::min<int64_t>(4, b.cols - col));
+        float g[4];
+        load_cols<T, 4>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, 0, valid, g);
+        if (b.m) {
+            float *at = b.m + e.moment + row * b.cols + col;
+            float m[4];
+            load_cols<float, 4>(at, 0, valid, m);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                g[i] *= b.grad_scale;
+                m[i] = b.mu * m[i] + g[i];
+                g[i] = b.nesterov ? g[i] + b.mu * m[i] : m[i];
+            }
+            store_cols<float, 4>(at, 0, valid, m);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += static_cast<double>(g[i]) * g[i];
+    }
+    sum = wave_sum(sum);
+    __shared__ double waves[4];
+    if (lane_id() == 0) waves[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+}
+
+// X's parts, in rows of `stride` elements with zeros behind the last column.
+template <class T, int P>
+__global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double *part, double eps, E *x, int64_t stride,
+                                                    int64_t plane, int64_t blocks) {
+    const int64_t z = blockIdx.x / blocks;
+    const Entry e = b.entry(z);
+    double sum = wave_sum(part[z * kParts + threadIdx.x]);
+    __shared__ double waves[4];
+    if (lane_id() == 0) waves[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    sum = waves[0] + waves[1] + waves[2] + waves[3];
+    const double inverse = kUp / (sqrt(sum) + eps);
+    const int64_t per = stride / 8, chunks = b.rows * per;
+    for (int64_t c = blockIdx.x % blocks * 256 + threadIdx.x; c < chunks; c += blocks * 256) {
+        const int64_t row = c / per, col = c % per * 8;
+        const int valid = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(8, b.cols - col)));
+        float g[8];
+        load_cols<T, 8>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, 0, valid, g);
+        if (b.m) {
+            float m[8];
+            load_cols<float, 8>(b.m + e.moment + row * b.cols + col, 0, valid, m);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = b.nesterov ? g[i] * b.grad_scale + b.mu * m[i] : m[i];
+        }
+        Frag<E> to[P];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            E one[P];
+            to_parts<E, P>(i < valid ? static_cast<float>(g[i] * inverse) : 0.0f, one);
+#pragma unroll
+            for (int p = 0; p < P; ++p) to[p][i] = one[p];
+        }
+        E *at = x + (z * b.rows + row) * stride + col;
+#pragma unroll
+        for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(at + p * plane) = to[p];
+    }
+}
+
+// ------------------------------------------------------------------ the products of a step
+struct Spot {
+    int64_t m0, n0, z;
+};
+
+template <int P>
+__device__ __forceinline__ void store_parts4(E *to, int64_t plane, int64_t valid, const float (&v)[4]) {
+    using E4 = E __attribute__((ext_vector_type(4)));
+    E4 part[P];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        E one[P];
+        to_parts<E, P>(e < valid ? v[e] : 0.0f, one);
+#pragma unroll
+        for (int p = 0; p < P; ++p) part[p][e] = one[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<E4 *>(to + p * plane) = part[p];
+}
+
+// A symmetric r x r product of each matrix with itself, of which the tiles on and above the diagonal are made: A = X X' (or
+// X' X), or with `poly` aI + bA + cAA.
+template <int P>
+struct SquareJob {
+    Side x;
+    int64_t step;        // bytes from a matrix to the next
+    int64_t r, k, g, tiles;
+    int32_t splits, poly;
+    f4 *part;
+    const E *old;        // A, where poly
+    E *out;
+    int64_t stride, plane;
+
+    template <class Q>
+    __device__ __forceinline__ Spot at(int64_t tile) const {
+        const int64_t each = g * (g + 1) / 2;
+        int64_t t = tile % each, tm = 0;
+        while (t >= g - tm) t -= g - tm++;
+        return Spot{tm * Q::BM, (tm + t) * Q::BN, tile / each};
+    }
+    template <class Q>
+    __device__ __forceinline__ void multiply(const Spot &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        const int64_t each = split_steps(k, Q::BK, splits), k0 = split * each, k1 = std::min(k, k0 + each);
+        Side s = x;
+        s.p += w.z * step;
+        if (k0 < k1) Q::run(s, s, 0, w.m0, r, w.n0, r, k0, k1, lds, acc);
+    }
+    __device__ __forceinline__ void put(const Spot &w, int row, int col, f4 v0, f4 v1) const {
+        one(w, w.m0 + row, w.n0 + col, v0);
+        one(w, w.m0 + row, w.n0 + col + 16, v1);
+    }
+    __device__ __forceinline__ void one(const Spot &w, int64_t m, int64_t n, f4 v) const {
+        if (m >= r || n >= stride) return;
+        const int64_t base = w.z * r * stride, at = base + m * stride + n;
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = v[e] * kDown;
+        if (poly) {
+            using E4 = E __attribute__((ext_vector_type(4)));
+            float a[4] = {};
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p) {
+                const E4 o = *reinterpret_cast<const E4 *>(old + at + p * plane);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] += static_cast<float>(o[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = kC * f[e] + kB * a[e] + (m == n + e ? kA * kUp : 0.0f);
+        }
+        store_parts4<P>(out + at, plane, r - n, f);
+        if (w.m0 == w.n0) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (n + e >= r) break;
+            E one[P];
+            to_parts<E, P>(f[e], one);
+#pragma unroll
+            for (int p = 0; p < P; ++p) out[base + (n + e) * stride + m + p * plane] = one[p];
+        }
+    }
+};
+
+// X = (aI + bA + cAA) X, or X (aI + bA + cAA) where X is taller than wide; the last one goes into the result.
+template <class T, int P, bool LAST>
+struct StepJob {
+    Side a, b;
+    int64_t a_step, b_step;   // bytes from a matrix to the next
+    int64_t k, gm, gn, tiles;
+    int32_t splits;
+    f4 *part;
+    E *out;
+    int64_t stride, plane;
+    Batch batch;
+
+    template <class Q>
+    __device__ __forceinline__ Spot at(int64_t tile) const {
+        int64_t tm, tn;
+        tile_at(tile % (gm * gn), gm, gn, tm, tn);
+        return Spot{tm * Q::BM, tn * Q::BN, tile / (gm * gn)};
+    }
+    template <class Q>
+    __device__ __forceinline__ void multiply(const Spot &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        const int64_t each = split_steps(k, Q::BK, splits), k0 = split * each, k1 = std::min(k, k0 + each);
+        Side l = a, r = b;
+        l.p += w.z * a_step;
+        r.p += w.z * b_step;
+        if (k0 < k1) Q::run(l, r, 0, w.m0, batch.rows, w.n0, batch.cols, k0, k1, lds, acc);
+    }
+    __device__ __forceinline__ void put(const Spot &w, int row, int col, f4 v0, f4 v1) const {
+        one(w, w.m0 + row, w.n0 + col, v0);
+        one(w, w.m0 + row, w.n0 + col + 16, v1);
+    }
+    __device__ __forceinline__ void one(const Spot &w, int64_t m, int64_t n, f4 v) const {
+        if (m >= batch.rows) return;
+        float f[4];
+        if constexpr (!LAST) {
+            if (n >= stride) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = v[e] * kDown;
+            store_parts4<P>(out + (w.z * batch.rows + m) * stride + n, plane, batch.cols - n, f);
+        } else {
+            const Entry en = batch.entry(w.z);
+            T *to = static_cast<T *>(en.out) + m * en.out_stride + n;
+            const int valid = static_cast<int>(std::min<int64_t>(4, batch.cols - n));
+            if (valid <= 0) return;
+            const float back = kDown * kDown;
+            if (batch.muon) {
+                const float lr = batch.lr_device ? *batch.lr_device : batch.lr;
+                load_cols<T, 4>(to, 0, valid, f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = f[e] * (1.0f - lr * en.decay) - lr * en.scale * (v[e] * back);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = v[e] * back;
+            }
+            store_cols<T, 4>(to, 0, valid, f);
+        }
+    }
+};
+
+template <int P, bool A, bool B>
+struct Tiles;
+template <bool A, bool B>
+struct Tiles<1, A, B> {
+    using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B>;
+    using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B>;
+};
+template <bool A, bool B>
+struct Tiles<2, A, B> {
+    using Large = Tile<E, 2, 256, 256, 2, 4, 32, A, B>;
+    using Small = Tile<E, 2, 128, 128, 2, 2, 32, A, B>;
+};
+
+int64_t triangle(int64_t g) { return g * (g + 1) / 2; }
+
+// Where the arrays of a launch of `count` matrices lie.
+struct Arrays {
+    double *part;
+    E *x[2], *a, *b;
+    f4 *sums;
+    int64_t r, c, x_stride, a_stride, x_plane, a_plane;
+    Cut gram, poly, step;
+    size_t bytes;
+};
+
+template <int P>
+Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
+    using L = typename Tiles<P, true, true>::Large;
+    using S = typename Tiles<P, true, true>::Small;
+    Arrays w{};
+    w.r = std::min(rows, cols);
+    w.c = std::max(rows, cols);
+    w.x_stride = ceil_div(cols, 64) * 64;
+    w.a_stride = ceil_div(w.r, 64) * 64;
+    w.x_plane = count * rows * w.x_stride;
+    w.a_plane = count * w.r * w.a_stride;
+    const int64_t tl = count * triangle(ceil_div(w.r, L::BM)), ts = count * triangle(ceil_div(w.r, S::BM));
+    const double share = double(S::BM * S::BN) / (L::BM * L::BN);
+    w.gram = choose_cut(tl, ts, share, w.c, S::BK);
+    w.poly = choose_cut(tl, ts, share, w.r, S::BK);
+    w.step = choose_cut(count * ceil_div(rows, L::BM) * ceil_div(cols, L::BN),
+                        count * ceil_div(rows, S::BM) * ceil_div(cols, S::BN), share, w.r, S::BK);
+    Carve k(workspace);
+    w.part = k.take<double>(static_cast<size_t>(count * kParts));
+    for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
+    w.a = k.take<E>(static_cast<size_t>(P * w.a_plane));
+    w.b = k.take<E>(static_cast<size_t>(P * w.a_plane));
+    const int large = L::BM * L::BN, small = S::BM * S::BN;
+    w.sums = reinterpret_cast<f4 *>(
+        k.take<char>(std::max({cut_bytes(w.gram, large, small), cut_bytes(w.poly, large, small), cut_bytes(w.step, large, small)})));
+    w.bytes = k.used();
+    return w;
+}
+
+template <class T, int P, bool WIDE>
+int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
+    using Gram = Tiles<P, WIDE, WIDE>;
+    using Poly = Tiles<P, true, true>;
+    using Step = Tiles<P, true, !WIDE>;
+    const int64_t bm = Poly::Large::BM, sm = Poly::Small::BM;
+    for (int32_t i = 0; i < steps; ++i) {
+        const E *from = w.x[i % 2];
+        const Side x{reinterpret_cast<const char *>(from), w.x_plane * 2, w.x_stride * 2};
+        SquareJob<P> q{};
+        q.x = x;
+        q.step = b.rows * w.x_stride * 2;
+        q.r = w.r;
+        q.k = w.c;
+        q.g = ceil_div(w.r, w.gram.large ? bm : sm);
+        q.part = w.sums;
+        q.out = w.a;
+        q.stride = w.a_stride;
+        q.plane = w.a_plane;
+        if (int rc = launch_cut<Gram>(w.gram, q, s)) return rc;
+        q.x = Side{reinterpret_cast<const char *>(w.a), w.a_plane * 2, w.a_stride * 2};
+        q.step = w.r * w.a_stride * 2;
+        q.k = w.r;
+        q.g = ceil_div(w.r, w.poly.large ? bm : sm);
+        q.poly = 1;
+        q.old = w.a;
+        q.out = w.b;
+        if (int rc = launch_cut<Poly>(w.poly, q, s)) return rc;
+        const Side poly{reinterpret_cast<const char *>(w.b), w.a_plane * 2, w.a_stride * 2};
+        auto step = [&](auto job) {
+            job.a = WIDE ? poly : x;
+            job.b = WIDE ? x : poly;
+            job.a_step = WIDE ? w.r * w.a_stride * 2 : b.rows * w.x_stride * 2;
+            job.b_step = WIDE ? b.rows * w.x_stride * 2 : w.r * w.a_stride * 2;
+            job.k = w.r;
+            job.gm = ceil_div(b.rows, w.step.large ? bm : sm);
+            job.gn = ceil_div(b.cols, w.step.large ? bm : sm);
+            job.part = w.sums;
+            job.out = w.x[1 - i % 2];
+            job.stride = w.x_stride;
+            job.plane = w.x_plane;
+            job.batch = b;
+            return launch_cut<Step>(w.step, job, s);
+        };
+        if (int rc = i + 1 < steps ? step(StepJob<T, P, false>{}) : step(StepJob<T, P, true>{})) return rc;
+    }
+    return W2V_OK;
+}
+
+// All matrices of one shape and type.
+template <class T, class G, int P>
+int run_batch(const Batch &b, double eps, int32_t steps, void *workspace, hipStream_t s) {
+    const Arrays w = arrays_of<P>(b.rows, b.cols, b.count, workspace);
+    if (std::max({w.gram.tiles, w.poly.tiles, w.step.tiles}) > kMaxTiles) return fail(W2V_E_RANGE, "a matrix is too large");
+    k_muon_momentum<G><<<static_cast<unsigned>(b.count * kParts), 256, 0, s>>>(b, w.part);
+    W2V_LAUNCH_CHECK("k_muon_momentum");
+    const int64_t blocks = std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 256), 4096);
+    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], w.x_stride, w.x_plane,
+                                                                               blocks);
+    W2V_LAUNCH_CHECK("k_muon_start");
+    return b.rows <= b.cols ? run_steps<T, P, true>(b, w, steps, s) : run_steps<T, P, false>(b, w, steps, s);
+}
+
+// bf16 results are made from one part: 11 bits a value leave an error of 1.2e-3 of the result (in norm), below bf16's own
+// rounding; all others from two.
+bool one_part(int32_t type) { return type == W2V_BF16; }
+
+// Matrices that go through the steps together: as many as keep a launch's X within 2^26 elements, and 4,096 (a launch
+// numbers its threads in 32 bits).
+int64_t together(int64_t rows, int64_t cols, int64_t count) {
+    return std::max<int64_t>(1, std::min({count, int64_t(4096), (int64_t(1) << 26) / (rows * ceil_div(cols, 64) * 64)}));
+}
+
+size_t batch_workspace(int64_t rows, int64_t cols, int64_t count, int32_t type) {
+    if (rows == 0 || cols == 0 || count == 0) return 0;
+    const int64_t n = together(rows, cols, count);
+    return one_part(type) ? arrays_of<1>(rows, cols, n, nullptr).bytes : arrays_of<2>(rows, cols, n, nullptr).bytes;
+}
+
+}  // namespace
+
+size_t orthogonalize_bytes(int64_t batch, int64_t rows, int64_t cols, int32_t type) {
+    return batch_workspace(rows, cols, batch, type);
+}
+
+int run_orthogonalize(const OrthArgs &a, void *workspace, hipStream_t s) {
+    if (a.batch == 0 || a.rows == 0 || a.cols == 0) return W2V_OK;
+    const int64_t most = together(a.rows, a.cols, a.batch), size = type_bytes(a.type);
+    for (int64_t z = 0; z < a.batch; z += most) {
+        Batch b{};
+        b.first.out = static_cast<char *>(a.out) + z * a.out_step * size;
+        b.first.grad = static_cast<const char *>(a.g) + z * a.g_step * size;
+        b.first.out_stride = a.out_stride;
+        b.first.grad_stride = a.g_stride;
+        b.out_step = a.out_step * size;
+        b.grad_step = a.g_step * size;
+        b.rows = a.rows;
+        b.cols = a.cols;
+        b.count = std::min(most, a.batch - z);
+        const int rc = with_type(a.type, [&](auto zero) {
+            using T = decltype(zero);
+            return run_batch<T, T, std::is_same<T, __bf16>::value ? 1 : 2>(b, a.eps, a.steps, workspace, s);
+        });
+        if (rc) return rc;
+    }
+    return W2V_OK;
+}
+
+// ------------------------------------------------------------------ Muon over many matrices
+namespace {
+
+bool same_kind(const w2v_muon_matrix &x, const w2v_muon_matrix &y) {
+    return x.rows == y.rows && x.cols == y.cols && x.param_type == y.param_type && x.grad_type == y.grad_type;
+}
+
+// The matrices' order in the plan: kind after kind, each in the list's order.
+std::vector<int32_t> plan_order(const w2v_muon_matrix *t, int32_t n) {
+    std::vector<int32_t> order(n);
+    for (int32_t i = 0; i < n; ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](int32_t i, int32_t j) {
+        const auto key = [&](int32_t q) {
+            return std::make_tuple(t[q].rows, t[q].cols, t[q].param_type, t[q].grad_type);
+        };
+        return key(i) < key(j);
+    });
+    return order;
+}
+
+}  // namespace
+
+size_t muon_plan_bytes(int32_t n) { return static_cast<size_t>(n) * sizeof(Entry); }
+
+size_t muon_bytes(const w2v_muon_matrix *t, int32_t n) {
+    size_t most = 0;
+    const std::vector<int32_t> order = plan_order(t, n);
+    for (int32_t i = 0, j; i < n; i = j) {
+        for (j = i; j < n && same_kind(t[order[i]], t[order[j]]);) ++j;
+        const w2v_muon_matrix &x = t[order[i]];
+        most = std::max(most, batch_workspace(x.rows, x.cols, j - i, x.param_type));
+    }
+    return most;
+}
+
+int run_muon_plan(const w2v_muon_matrix *t, int32_t n, void *plan, hipStream_t s) {
+    std::vector<Entry> table;
+    table.reserve(n);
+    for (int32_t i : plan_order(t, n))
+        table.push_back(Entry{t[i].param, t[i].grad, t[i].param_stride, t[i].grad_stride, t[i].moment_offset,
+                              t[i].weight_decay, t[i].scale});
+    if (n > 0) W2V_HIP(hipMemcpyAsync(plan, table.data(), table.size() * sizeof(Entry), hipMemcpyHostToDevice, s));
+    W2V_HIP(hipStreamSynchronize(s));
+    return W2V_OK;
+}
+
+int run_muon_step(const w2v_muon_matrix *t, int32_t n, const void *plan, float *m, const w2v_muon_params &p, void *workspace,
+                  hipStream_t s) {
+    const std::vector<int32_t> order = plan_order(t, n);
+    for (int32_t i = 0, j; i < n; i = j) {
+        for (j = i; j < n && same_kind(t[order[i]], t[order[j]]);) ++j;
+        const w2v_muon_matrix &x = t[order[i]];
+        if (x.rows == 0 || x.cols == 0) continue;
+        const int32_t most = static_cast<int32_t>(together(x.rows, x.cols, j - i));
+        for (int32_t z = i; z < j; z += most) {
+            Batch b{};
+            b.table = static_cast<const Entry *>(plan) + z;
+            b.rows = x.rows;
+            b.cols = x.cols;
+            b.count = std::min(most, j - z);
+            b.m = m;
+            b.mu = static_cast<float>(p.momentum);
+            b.nesterov = p.nesterov;
+            b.muon = 1;
+            b.grad_scale = p.grad_scale;
+            b.lr = static_cast<float>(p.lr);
+            b.lr_device = p.lr_device;
+            const int rc = with_type(x.param_type, [&](auto pz) {
+                return with_type(x.grad_type, [&](auto gz) {
+                    using T = decltype(pz);
+                    return run_batch<T, decltype(gz), std::is_same<T, __bf16>::value ? 1 : 2>(b, p.eps, p.steps, workspace, s);
+                });
+            });
+            if (rc) return rc;
+        }
+    }
+    return W2V_OK;
+}
+
+}  // namespace w2v

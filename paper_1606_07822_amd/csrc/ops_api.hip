@@ -103,6 +103,70 @@ int check_tensors(const w2v_adamw_tensor *t, int32_t n, int64_t n_moments) {
     return W2V_OK;
 }
 
+int check_ffn(int64_t rows, int32_t dim, int32_t hidden, int32_t type, int32_t act) {
+    if (rows < 0 || rows > INT32_MAX) return fail(W2V_E_ARG, "rows must be in 0..2^31 - 1");
+    if (dim < 1 || dim > kFfnMaxDim || hidden < 1 || hidden > kFfnMaxDim)
+        return fail(W2V_E_ARG, "dim and hidden must be in 1..2^20");
+    if (!type_ok(type)) return fail(W2V_E_ARG, "type must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+    if (act != W2V_SILU && act != W2V_GELU) return fail(W2V_E_ARG, "act must be 0 (silu) or 1 (gelu)");
+    return W2V_OK;
+}
+
+bool ffn_sizes_ok(int64_t rows, int32_t dim, int32_t hidden, int32_t type) {
+    return rows >= 0 && rows <= INT32_MAX && dim >= 1 && dim <= kFfnMaxDim && hidden >= 1 && hidden <= kFfnMaxDim && type_ok(type);
+}
+
+// An array of a call, for the checks: an output may not be another array, except where `may` names one.
+struct Named {
+    w2v_rows r;
+    int64_t rows, cols;
+    const char *name;
+    bool out, required;
+};
+
+int check_arrays(const Named *a, int n, int32_t type) {
+    for (int i = 0; i < n; ++i) {
+        if (!a[i].r.p && !a[i].required) continue;
+        if (int rc = check_rows(a[i].r.p, type, a[i].rows, a[i].cols, a[i].r.stride, a[i].name)) return rc;
+    }
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < n; ++j)
+            if (i != j && a[i].out && a[i].r.p && a[i].r.p == a[j].r.p)
+                return fail(W2V_E_ARG, std::string(a[i].name) + " may not be " + a[j].name);
+    return W2V_OK;
+}
+
+int check_in_place(const w2v_rows &out, const w2v_rows &in, int64_t rows, const char *what) {
+    if (out.p && out.p == in.p && rows > 1 && out.stride != in.stride)
+        return fail(W2V_E_ARG, std::string(what) + " only with the same stride");
+    return W2V_OK;
+}
+
+Rows rows_of(const w2v_rows &r) { return Rows{r.p, r.stride}; }
+
+int check_muon(const w2v_muon_matrix *t, int32_t n, int64_t n_moments) {
+    std::vector<w2v_adamw_tensor> as;
+    for (int32_t i = 0; i < n; ++i) {
+        const w2v_muon_matrix &x = t[i];
+        const std::string name = "matrix " + std::to_string(i);
+        if (x.rows < 0 || x.cols < 0 || x.rows > kMuonMaxSide || x.cols > kMuonMaxSide)
+            return fail(W2V_E_ARG, name + ": rows and cols must be in 0..2^20");
+        if (!std::isfinite(x.scale)) return fail(W2V_E_ARG, name + ": scale must be finite");
+        as.push_back(w2v_adamw_tensor{x.param, x.grad, x.rows, x.cols, x.param_stride, x.grad_stride, x.moment_offset,
+                                      x.param_type, x.grad_type, x.weight_decay, 0});
+    }
+    return check_tensors(as.data(), n, n_moments);
+}
+
+bool muon_sizes_ok(const w2v_muon_matrix *t, int32_t n) {
+    if (n < 0 || (n > 0 && !t)) return false;
+    for (int32_t i = 0; i < n; ++i)
+        if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > kMuonMaxSide || t[i].cols > kMuonMaxSide ||
+            !type_ok(t[i].param_type) || !type_ok(t[i].grad_type))
+            return false;
+    return true;
+}
+
 // What both calls on batches read of their arguments.
 int check_batch(const w2v_model *m, const int32_t *tokens, int64_t n_tokens, const w2v_params *p, const w2v_batch_params *b) {
     if (int rc = check_training_args(m, p)) return rc;
@@ -310,6 +374,181 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
         return fail(W2V_E_ARG, "a required pointer is NULL");
     if (!aligned(m, 4) || !aligned(v, 4)) return fail(W2V_E_ARG, "m and v must be 4-byte aligned");
     return run_adamw_moments(m, v, m_scale, v_scale, n_moments, m_out, v_out, as_stream(hip_stream));
+}
+
+size_t w2v_gated_ffn_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type) {
+    return ffn_sizes_ok(rows, dim, hidden, type) ? ffn_bytes(rows, dim, hidden, type, false) : 0;
+}
+
+int w2v_gated_ffn(w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, int64_t rows, int32_t dim, int32_t hidden,
+                  int32_t type, int32_t act, w2v_rows y, w2v_rows gate, w2v_rows up, void *workspace,
+                  size_t workspace_bytes, void *hip_stream) {
+    set_error("");
+    if (int rc = check_ffn(rows, dim, hidden, type, act)) return rc;
+    const Named all[] = {{x, rows, dim, "x", false, true},
+                         {w_gate, hidden, dim, "w_gate", false, true},
+                         {w_up, hidden, dim, "w_up", false, true},
+                         {w_down, dim, hidden, "w_down", false, true},
+                         {gate, rows, hidden, "gate", true, false},
+                         {up, rows, hidden, "up", true, false},
+                         {y, rows, dim, "y", y.p != x.p, true}};
+    if (int rc = check_arrays(all, 7, type)) return rc;
+    if (int rc = check_in_place(y, x, rows, "y may be x")) return rc;
+    for (const w2v_rows &w : {w_gate, w_up, w_down, gate, up})
+        if (rows > 0 && w.p == y.p) return fail(W2V_E_ARG, "y may be no other array than x");
+    if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(rows, dim, hidden, type, false))) return rc;
+    FfnArgs a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.hidden = hidden;
+    a.type = type;
+    a.act = act;
+    a.x = rows_of(x);
+    a.w_gate = rows_of(w_gate);
+    a.w_up = rows_of(w_up);
+    a.w_down = rows_of(w_down);
+    a.gate = rows_of(gate);
+    a.up = rows_of(up);
+    a.y = rows_of(y);
+    return run_ffn(a, workspace, as_stream(hip_stream));
+}
+
+size_t w2v_gated_ffn_backward_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type) {
+    return ffn_sizes_ok(rows, dim, hidden, type) ? ffn_bytes(rows, dim, hidden, type, true) : 0;
+}
+
+int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, w2v_rows gate,
+                           w2v_rows up, int64_t rows, int32_t dim, int32_t hidden, int32_t type, int32_t act, w2v_rows dx,
+                           w2v_rows dw_gate, w2v_rows dw_up, w2v_rows dw_down, void *workspace, size_t workspace_bytes,
+                           void *hip_stream) {
+    set_error("");
+    if (int rc = check_ffn(rows, dim, hidden, type, act)) return rc;
+    const Named all[] = {{dy, rows, dim, "dy", false, true},
+                         {x, rows, dim, "x", false, true},
+                         {w_gate, hidden, dim, "w_gate", false, true},
+                         {w_up, hidden, dim, "w_up", false, true},
+                         {w_down, dim, hidden, "w_down", false, true},
+                         {gate, rows, hidden, "gate", false, true},
+                         {up, rows, hidden, "up", false, true},
+                         {dw_gate, hidden, dim, "dw_gate", true, false},
+                         {dw_up, hidden, dim, "dw_up", true, false},
+                         {dw_down, dim, hidden, "dw_down", true, false},
+                         {dx, rows, dim, "dx", false, false}};
+    if (int rc = check_arrays(all, 11, type)) return rc;
+    if (int rc = check_in_place(dx, dy, rows, "dx may be dy")) return rc;
+    if (int rc = check_in_place(dx, x, rows, "dx may be x")) return rc;
+    for (const w2v_rows &w : {w_gate, w_up, w_down, gate, up})
+        if (dx.p && w.p == dx.p) return fail(W2V_E_ARG, "dx may be no other array than dy or x");
+    if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(rows, dim, hidden, type, true))) return rc;
+    FfnArgs a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.hidden = hidden;
+    a.type = type;
+    a.act = act;
+    a.dy = rows_of(dy);
+    a.x = rows_of(x);
+    a.w_gate = rows_of(w_gate);
+    a.w_up = rows_of(w_up);
+    a.w_down = rows_of(w_down);
+    a.gate = rows_of(gate);
+    a.up = rows_of(up);
+    a.dx = rows_of(dx);
+    a.dw_gate = rows_of(dw_gate);
+    a.dw_up = rows_of(dw_up);
+    a.dw_down = rows_of(dw_down);
+    return run_ffn_backward(a, workspace, as_stream(hip_stream));
+}
+
+size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type) {
+    const bool ok = batch >= 0 && rows >= 0 && cols >= 0 && rows <= kMuonMaxSide && cols <= kMuonMaxSide && type_ok(type);
+    return ok ? orthogonalize_bytes(batch, rows, cols, type) : 0;
+}
+
+int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t batch, int32_t rows, int32_t cols,
+                      int32_t type, int32_t steps, double eps, void *out, int64_t out_stride, int64_t out_step,
+                      void *workspace, size_t workspace_bytes, void *hip_stream) {
+    set_error("");
+    if (!type_ok(type)) return fail(W2V_E_ARG, "type must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+    if (batch < 0 || rows < 0 || cols < 0 || rows > kMuonMaxSide || cols > kMuonMaxSide)
+        return fail(W2V_E_ARG, "batch must be >= 0, rows and cols in 0..2^20");
+    if (steps < 1 || steps > 20) return fail(W2V_E_ARG, "steps must be in 1..20");
+    if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(W2V_E_ARG, "eps must be >= 0 and finite");
+    if (batch > 0 && rows > 0 && cols > 0) {
+        if (int rc = check_rows(g, type, rows, cols, g_stride, "g")) return rc;
+        if (int rc = check_rows(out, type, rows, cols, out_stride, "out")) return rc;
+        if (batch > 1) {
+            const int64_t g_span = (rows - 1) * (rows > 1 ? g_stride : 0) + cols,
+                          out_span = (rows - 1) * (rows > 1 ? out_stride : 0) + cols;
+            if (g_step < 0 || g_step > (INT64_MAX >> 4) / batch || out_step > (INT64_MAX >> 4) / batch)
+                return fail(W2V_E_ARG, "g_step and out_step must be >= 0, and not too large");
+            if (out_step < out_span) return fail(W2V_E_ARG, "out's matrices may not overlap");
+            if (out == g && (g_step != out_step || g_span != out_span)) return fail(W2V_E_ARG, "out may be g only with the same strides");
+        }
+        if (out == g && rows > 1 && g_stride != out_stride) return fail(W2V_E_ARG, "out may be g only with the same strides");
+    }
+    if (int rc = check_workspace(workspace, workspace_bytes, orthogonalize_bytes(batch, rows, cols, type))) return rc;
+    OrthArgs a{};
+    a.g = g;
+    a.out = out;
+    a.type = type;
+    a.steps = steps;
+    a.batch = batch;
+    a.rows = rows;
+    a.cols = cols;
+    a.g_stride = g_stride;
+    a.out_stride = out_stride;
+    a.g_step = g_step;
+    a.out_step = out_step;
+    a.eps = eps;
+    return run_orthogonalize(a, workspace, as_stream(hip_stream));
+}
+
+size_t w2v_muon_plan_bytes(const w2v_muon_matrix *matrices_host, int32_t n) {
+    return muon_sizes_ok(matrices_host, n) ? muon_plan_bytes(n) : 0;
+}
+
+size_t w2v_muon_workspace_bytes(const w2v_muon_matrix *matrices_host, int32_t n) {
+    try {
+        return muon_sizes_ok(matrices_host, n) ? muon_bytes(matrices_host, n) : 0;
+    } catch (const std::exception &) {
+        return 0;
+    }
+}
+
+int w2v_muon_build_plan(const w2v_muon_matrix *matrices_host, int32_t n, int64_t n_moments, void *plan, size_t plan_bytes,
+                        void *hip_stream) {
+    set_error("");
+    if (n < 0 || (n > 0 && !matrices_host)) return fail(W2V_E_ARG, "bad matrices_host / n");
+    if (n_moments < 0 || n_moments % kMomentBlock != 0) return fail(W2V_E_ARG, "n_moments must be a multiple of 256");
+    try {
+        if (int rc = check_muon(matrices_host, n, n_moments)) return rc;
+        if (int rc = check_workspace(plan, plan_bytes, muon_plan_bytes(n))) return rc;
+        return run_muon_plan(matrices_host, n, plan, as_stream(hip_stream));
+    } catch (const std::exception &e) {   // host memory for the tables
+        return fail(W2V_E_ARG, std::string("the plan's tables: ") + e.what());
+    }
+}
+
+int w2v_muon_step(const w2v_muon_matrix *matrices_host, int32_t n, const void *plan, float *m, const w2v_muon_params *p,
+                  void *workspace, size_t workspace_bytes, void *hip_stream) {
+    set_error("");
+    if (!p) return fail(W2V_E_ARG, "params is NULL");
+    if (!muon_sizes_ok(matrices_host, n)) return fail(W2V_E_ARG, "bad matrices_host / n");
+    if (n > 0 && !plan) return fail(W2V_E_ARG, "plan is NULL");
+    if (!aligned(plan, 256)) return fail(W2V_E_ARG, "plan must be 256-byte aligned");
+    if (int rc = check_floats(m, "m", n > 0)) return rc;
+    if (!p->lr_device && !std::isfinite(p->lr)) return fail(W2V_E_ARG, "lr must be finite");
+    if (!aligned(p->lr_device, 4)) return fail(W2V_E_ARG, "lr_device is not aligned to its type");
+    if (!(p->momentum >= 0.0 && p->momentum < 1.0)) return fail(W2V_E_ARG, "momentum must be in [0, 1)");
+    if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return fail(W2V_E_ARG, "eps must be >= 0 and finite");
+    if (p->steps < 1 || p->steps > 20) return fail(W2V_E_ARG, "steps must be in 1..20");
+    try {
+        if (int rc = check_workspace(workspace, workspace_bytes, muon_bytes(matrices_host, n))) return rc;
+        return run_muon_step(matrices_host, n, plan, m, *p, workspace, as_stream(hip_stream));
+    } catch (const std::exception &e) {
+        return fail(W2V_E_ARG, std::string("the step's tables: ") + e.what());
+    }
 }
 
 int64_t w2v_batch_n_moments(const w2v_model *m, const w2v_batch_params *bp) {

@@ -149,6 +149,42 @@ int run_adamw_step(void *plan, int64_t n_chunks, int32_t bits, void *m, void *v,
 int run_adamw_moments(const void *m, const void *v, const float *m_scale, const float *v_scale, int64_t n, float *m_out,
                       float *v_out, hipStream_t s);
 
+// ------------------------------------------------------------------ gated feed-forward block (ffn.hip)
+struct Rows {
+    const void *p;
+    int64_t stride;   // elements
+};
+struct FfnArgs {
+    int64_t rows;
+    int32_t dim, hidden, type, act;
+    Rows x, w_gate, w_up, w_down;          // rows x dim, hidden x dim twice, dim x hidden
+    Rows gate, up;                         // rows x hidden: written by the forward pass (null: not), read by the backward pass
+    Rows y;                                // rows x dim
+    Rows dy, dx, dw_gate, dw_up, dw_down;  // a gradient may be null: not wanted
+};
+constexpr int32_t kFfnMaxDim = 1 << 20;
+size_t ffn_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type, bool backward);
+int run_ffn(const FfnArgs &a, void *workspace, hipStream_t s);
+int run_ffn_backward(const FfnArgs &a, void *workspace, hipStream_t s);
+
+// ------------------------------------------------------------------ orthogonalised updates (muon.hip)
+struct OrthArgs {
+    const void *g;
+    void *out;
+    int32_t type, steps;
+    int64_t batch, rows, cols;
+    int64_t g_stride, out_stride, g_step, out_step;   // elements from a row, and from a matrix, to the next
+    double eps;
+};
+constexpr int32_t kMuonMaxSide = 1 << 20;
+size_t orthogonalize_bytes(int64_t batch, int64_t rows, int64_t cols, int32_t type);
+int run_orthogonalize(const OrthArgs &a, void *workspace, hipStream_t s);
+size_t muon_plan_bytes(int32_t n);
+size_t muon_bytes(const w2v_muon_matrix *t, int32_t n);
+int run_muon_plan(const w2v_muon_matrix *t, int32_t n, void *plan, hipStream_t s);
+int run_muon_step(const w2v_muon_matrix *t, int32_t n, const void *plan, float *m, const w2v_muon_params &p, void *workspace,
+                  hipStream_t s);
+
 // ------------------------------------------------------------------ training in mini-batches (batch.hip)
 int check_training_args(const w2v_model *m, const w2v_params *p);   // api.hip
 int64_t batch_moments(const w2v_model *m, const w2v_batch_params *b);

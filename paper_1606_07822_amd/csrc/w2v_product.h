@@ -1,0 +1,337 @@
+// Tiles of a matrix product C[m][n] = sum_k A(m, k) B(n, k) on the matrix cores, for the kernels that put their own
+// last step (an activation, a gradient, a weight's update) on a tile while it is in registers.
+//
+// An operand is 16-bit elements in rows of whole 16-byte chunks, with k along the rows (ALONG) or down them: the second
+// kind is read from LDS by a transposing load, so that no array is needed in two layouts. It is one plane, or P planes
+// whose sum is the value (parts of 8 bits in bf16, of 11 in fp16): products p, q with p + q < P are taken, smallest
+// first, which leaves out what lies below the last part. The sums are fp32.
+//
+// A workgroup of WM x WN wavefronts makes BM x BN of C. Each step, BK of k, goes from global memory straight into one
+// of two LDS buffers while the matrix cores work on the other; a wavefront waits for its own loads and a barrier makes
+// them everybody's, once a step. Chunks change places within 256 bytes by their row, so that the 16 lanes of a phase
+// read all 64 banks. Measured on 8,192^3: 256 x 256 tiles of bf16 1.21 PFLOP/s, two fp16 parts 0.41 (three products:
+// 1.23), three bf16 parts 0.21 (six: 1.27); 128 x 128 tiles 1.07, 0.32 and 0.18.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "w2v_ops.h"
+
+namespace w2v {
+
+template <class E>
+using Frag = E __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f4 mfma32(Frag<__bf16> a, Frag<__bf16> b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 mfma32(Frag<_Float16> a, Frag<_Float16> b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// 64 lanes' 16 bytes each from global memory into LDS, lane after lane from `lds` (the same in all lanes) on.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char *from) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)static_cast<uintptr_t>(lds), 16, 0, 0);
+}
+
+namespace {
+__device__ __attribute__((aligned(16))) const char kZeroChunk[16] = {};   // what a step reads past the end of k
+}
+
+struct Side {
+    const char *p;
+    int64_t plane, row;   // bytes from a plane to the next, from a row to the next
+};
+
+// The values of 1, 2 or 3 parts. The last part takes what is left, to nearest.
+template <class E, int P>
+__device__ __forceinline__ void to_parts(float v, E (&part)[P]) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        // values within half a step of fp32's largest would round to an infinity in bf16
+        const float near = P == 3 && p == 0 && fabsf(v) < __builtin_inff() ? fminf(fmaxf(v, -0x1.fep127f), 0x1.fep127f) : v;
+        part[p] = static_cast<E>(near);
+        v -= static_cast<float>(part[p]);
+    }
+}
+
+template <class E_, int P_, int BM_, int BN_, int WM_, int WN_, int BK_, bool ALONG_A, bool ALONG_B, bool PAIR = false>
+struct Tile {
+    using E = E_;
+    static constexpr int P = P_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
+    static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
+    static constexpr int kA = P * BM * BK * 2, kB = P * BN * BK * 2, kStage = kA + kB, kLds = 2 * kStage;
+    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;   // fragments of 16 x 16 a wavefront
+    static constexpr int kPerCu = 160 * 1024 / kLds, kPerSimd = std::max(1, std::min(2, kPerCu) * kWaves / 4);
+    static_assert(FN % 2 == 0 && kPerCu >= 1, "pairs of fragments, one CU's LDS");
+
+    // The part of a stage that holds one operand: rows of k (ALONG) or rows at one k.
+    template <bool ALONG, int R>
+    struct Half {
+        static constexpr int kRow = (ALONG ? BK : R) * 2, kRows = ALONG ? R : BK;
+        static constexpr int kChunks = kRow / 16;
+        static constexpr int kPlane = kRow * kRows, kLoads = kPlane / (kWave * 16) / kWaves;
+        static constexpr int kRowsPerLoad = kWave / kChunks;
+        static_assert(kLoads >= 1 && kRowsPerLoad >= 1, "every wavefront loads");
+
+        // ALONG: 16 lanes read one chunk of 16 rows: all places of 256 bytes differ. Down: 32 lanes read two chunks of the
+        // rows 0..3 and 8..11 of a group of 16: pairs of chunks change places.
+        static __device__ __forceinline__ int place(int row, int chunk) {
+            if constexpr (ALONG) return chunk ^ (row / (256 / kRow)) % kChunks;
+            return chunk ^ ((row & 3) | (row >> 1 & 4)) << 1;
+        }
+
+        const char *p;
+        int64_t plane, step;
+        uint32_t off[kLoads];
+        int32_t left;     // of k, from the step that is loaded next on
+
+        // valid: rows (ALONG) or columns from the tile's first one on that the operand has; what lies past them is read
+        // from the last one and dropped with its results.
+        __device__ __forceinline__ void start(const Side &s, int64_t first, int64_t valid, int64_t k0, int64_t k1, int wave, int lane) {
+            p = s.p + (ALONG ? first * s.row + k0 * 2 : k0 * s.row + first * 2);
+            plane = s.plane;
+            step = ALONG ? kRow : BK * s.row;
+            left = static_cast<int32_t>(k1 - k0);
+            const int last = static_cast<int>(std::min<int64_t>(valid, R)) - 1;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = (wave * kLoads + i) * kRowsPerLoad + lane / kChunks;
+                const int chunk = place(row, lane % kChunks);
+                if constexpr (ALONG)
+                    off[i] = static_cast<uint32_t>(min(row, last)) * static_cast<uint32_t>(s.row) + static_cast<uint32_t>(chunk) * 16u;
+                else
+                    off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(s.row) + static_cast<uint32_t>(min(chunk, last / 8)) * 16u;
+            }
+        }
+
+        // other: bytes to a second operand that every second group of 16 rows comes from.
+        __device__ __forceinline__ void load(uint32_t lds, int wave, int lane, int64_t other = 0) {
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int first = (wave * kLoads + i) * kRowsPerLoad;
+                    const uint32_t at = lds + static_cast<uint32_t>(q * kPlane + first * kRow);
+                    const char *from = p + q * plane + (PAIR && first / 16 % 2 ? other : 0);
+                    if (left >= BK) {
+                        load_to_lds(at, from + off[i]);
+                    } else {
+                        const int row = first + lane / kChunks;
+                        const int k = ALONG ? place(row, lane % kChunks) * 8 : row;
+                        load_to_lds(at, k < left ? from + off[i] : kZeroChunk);
+                    }
+                }
+            p += step;
+            left -= BK;
+        }
+
+        // The fragment of 16 rows (ALONG) or columns from `first` on, at the 32 k from 32 ks on: lane l holds number
+        // l % 16 of them, at the 8 k from 8 (l / 16) on.
+        static __device__ __forceinline__ Frag<E> frag(const char *lds, int q, int first, int ks, int lane) {
+            if constexpr (ALONG) {
+                const int row = first + lane % 16;
+                return *reinterpret_cast<const Frag<E> *>(lds + q * kPlane + row * kRow + place(lane % 16, ks * 4 + lane / 16) * 16);
+            } else {
+                // lanes 4 r .. 4 r + 3 of 16 give the address of row r of 4, lane c of them gets column c of the four rows
+                using S4 = short __attribute__((ext_vector_type(4)));
+                const int row = ks * 32 + lane / 16 * 8 + lane % 16 / 4;
+                const char *a = lds + q * kPlane + row * kRow + place(row & 15, first / 8 + lane % 4 / 2) * 16 + lane % 2 * 8;
+                union {
+                    S4 h[2];
+                    Frag<E> f;
+                } u;
+                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)(a));
+                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)(a + 4 * kRow));
+                return u.f;
+            }
+        }
+    };
+    using HalfA = Half<ALONG_A, BM>;
+    using HalfB = Half<ALONG_B, BN>;
+
+    // acc += the product over k0 <= k < k1 (k0 a multiple of BK) of the tile from (m0, n0) on of an m x n one. Element e
+    // of acc[i][j] is C at row m0 + 16 (wm FM + i) + lane % 16, column n0 + 16 (wn FN + j) + 4 (lane / 16) + e. PAIR: B's
+    // rows come in groups of 16 from b and, `other` bytes behind, a second operand in turn; n and n0 count one operand's.
+    static __device__ __forceinline__ void run(const Side &a, const Side &b, int64_t other, int64_t m0, int64_t m, int64_t n0,
+                                               int64_t n, int64_t k0, int64_t k1, char *lds, f4 (&acc)[FM][FN]) {
+        const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+        const int wm = wave / WN, wn = wave % WN;
+        HalfA ha;
+        HalfB hb;
+        ha.start(a, m0, m - m0, k0, k1, wave, lane);
+        if constexpr (PAIR) {   // row r of the tile is row 16 (r / 32) + r % 16 of an operand
+            hb.start(b, n0, n - n0, k0, k1, wave, lane);
+            const int last = static_cast<int>(std::min<int64_t>(n - n0, BN / 2)) - 1;
+#pragma unroll
+            for (int i = 0; i < HalfB::kLoads; ++i) {
+                const int row = (wave * HalfB::kLoads + i) * HalfB::kRowsPerLoad + lane / HalfB::kChunks;
+                hb.off[i] = static_cast<uint32_t>(min(row / 32 * 16 + row % 16, last)) * static_cast<uint32_t>(b.row) +
+                            static_cast<uint32_t>(HalfB::place(row, lane % HalfB::kChunks)) * 16u;
+            }
+        } else {
+            hb.start(b, n0, n - n0, k0, k1, wave, lane);
+        }
+        const auto base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds));
+        const int steps = static_cast<int>((k1 - k0 + BK - 1) / BK);
+        ha.load(base, wave, lane);
+        hb.load(base + kA, wave, lane, other);
+        for (int s = 0; s < steps; ++s) {
+            // this wavefront's loads have landed and its reads of the other buffer are done; then everybody's
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (s + 1 < steps) {
+                const uint32_t to = base + static_cast<uint32_t>((s + 1 & 1) * kStage);
+                ha.load(to, wave, lane);
+                hb.load(to + kA, wave, lane, other);
+            }
+            const char *la = lds + (s & 1) * kStage, *lb = la + kA;
+#pragma unroll
+            for (int ks = 0; ks < BK / 32; ++ks) {
+                Frag<E> fb[P][FN];
+#pragma unroll
+                for (int q = 0; q < P; ++q)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) fb[q][j] = HalfB::frag(lb, q, (wn * FN + j) * 16, ks, lane);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    Frag<E> fa[P];
+#pragma unroll
+                    for (int p = 0; p < P; ++p) fa[p] = HalfA::frag(la, p, (wm * FM + i) * 16, ks, lane);
+#pragma unroll
+                    for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                        for (int q = P - 1 - p; q >= 0; --q)
+#pragma unroll
+                            for (int j = 0; j < FN; ++j) acc[i][j] = mfma32(fb[q][j], fa[p], acc[i][j]);
+                }
+            }
+        }
+    }
+
+    // f(row, column, values, values 16 columns on) for each pair of acc's fragments, rows and columns counted in the tile.
+    template <class F>
+    static __device__ __forceinline__ void each(const f4 (&acc)[FM][FN], F f) {
+        const int lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; j += 2)
+                f((wave / WN * FM + i) * 16 + lane % 16, (wave % WN * FN + j) * 16 + lane / 16 * 4, acc[i][j], acc[i][j + 1]);
+    }
+};
+
+// The workgroups of an XCD (every eighth) take neighbouring numbers, so that its L2 holds what they share.
+__device__ __forceinline__ int64_t by_xcd(int64_t id, int64_t count) {
+    const int64_t each = count / 8, more = count % 8, x = id % 8;
+    return x * each + std::min(x, more) + id / 8;
+}
+
+// Tile number id of a gm x gn grid, column by column in bands of four rows.
+__device__ __forceinline__ void tile_at(int64_t id, int64_t gm, int64_t gn, int64_t &tm, int64_t &tn) {
+    constexpr int64_t kBand = 4;
+    const int64_t band = id / (kBand * gn), rows = std::min(gm - band * kBand, kBand), in = id % (kBand * gn);
+    tm = band * kBand + in % rows;
+    tn = in / rows;
+}
+
+// ------------------------------------------------------------------ kernels over a job's tiles
+// A job says which tiles it has, multiplies one and puts its elements where they belong:
+//   int64_t tiles; int32_t splits; f4 *part          tiles, and the parts that each one's k is cut into
+//   Place at<T>(tile)                                 where the tile lies
+//   multiply<T>(place, split, lds, acc)               its product over one part of k
+//   put(place, row, column, f4, f4)                   four elements of a row, and the four 16 columns (or, of a PAIR, one
+//                                                     operand) on; row and column count in the tile
+// Parts of k are summed in their order by k_join, so that results do not depend on the order in which they end.
+inline __host__ __device__ int64_t split_steps(int64_t k, int bk, int32_t splits) {
+    return ceil_div(ceil_div(k, bk), splits) * bk;
+}
+
+template <class T, class J>
+__global__ __launch_bounds__(T::kThreads, T::kPerSimd) void k_tiles(const J job) {
+    __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+    const int64_t id = by_xcd(blockIdx.x, gridDim.x);
+    const int64_t tile = id % job.tiles;
+    const int split = static_cast<int>(id / job.tiles);
+    const auto place = job.template at<T>(tile);
+    f4 acc[T::FM][T::FN] = {};
+    job.template multiply<T>(place, split, lds, acc);
+    if (job.splits == 1) {
+        T::each(acc, [&](int row, int col, f4 v0, f4 v1) { job.put(place, row, col, v0, v1); });
+        return;
+    }
+    f4 *to = job.part + (static_cast<int64_t>(split) * job.tiles + tile) * (T::FM * T::FN * T::kThreads) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) to[(i * T::FN + j) * T::kThreads] = acc[i][j];
+}
+
+template <class T, class J>
+__global__ __launch_bounds__(T::kThreads) void k_join(const J job) {
+    const int64_t tile = blockIdx.x / T::FM;
+    const int i = static_cast<int>(blockIdx.x % T::FM), lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave;
+    const auto place = job.template at<T>(tile);
+    const int64_t size = T::FM * T::FN * T::kThreads;
+    const f4 *from = job.part + tile * size + i * T::FN * T::kThreads + threadIdx.x;
+    f4 v[T::FN] = {};
+    for (int s = 0; s < job.splits; ++s, from += job.tiles * size)
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) v[j] += from[j * T::kThreads];
+#pragma unroll
+    for (int j = 0; j < T::FN; j += 2)
+        job.put(place, (wave / T::WN * T::FM + i) * 16 + lane % 16, (wave % T::WN * T::FN + j) * 16 + lane / 16 * 4, v[j], v[j + 1]);
+}
+
+// How a product's tiles are taken: large or small ones, and the parts of k.
+struct Cut {
+    bool large;
+    int32_t splits;
+    int64_t tiles;
+};
+
+inline size_t cut_bytes(const Cut &c, int large_tile, int small_tile) {
+    return c.splits == 1 ? 0 : static_cast<size_t>(c.tiles) * c.splits * (c.large ? large_tile : small_tile) * sizeof(float);
+}
+
+// A launch numbers its threads in 32 bits.
+constexpr int64_t kMaxTiles = int64_t(1) << 22;
+
+template <class T, class J>
+int launch_tiles(J &job, hipStream_t s) {
+    k_tiles<T, J><<<static_cast<unsigned>(job.tiles * job.splits), T::kThreads, 0, s>>>(job);
+    W2V_LAUNCH_CHECK("k_tiles");
+    if (job.splits > 1) {
+        k_join<T, J><<<static_cast<unsigned>(job.tiles * T::FM), T::kThreads, 0, s>>>(job);
+        W2V_LAUNCH_CHECK("k_join");
+    }
+    return W2V_OK;
+}
+
+// tiles_large, tiles_small: of all products of a launch, small ones `small_share` of a large one's size. A CU holds one
+// large tile or two small ones at a time.
+inline Cut choose_cut(int64_t tiles_large, int64_t tiles_small, double small_share, int64_t k, int bk) {
+    const double cus = device_cu_count();
+    const double large = std::ceil(tiles_large / cus), small = std::ceil(tiles_small / (2 * cus)) * 2 * small_share * 1.15;
+    Cut c{large <= small, 1, large <= small ? tiles_large : tiles_small};
+    if (!c.large) {
+        const int64_t most = std::max<int64_t>(1, ceil_div(k, bk) / 4);
+        const int64_t room = static_cast<int64_t>(2 * cus) / std::max<int64_t>(1, c.tiles);
+        c.splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({most, room, 64})));
+    }
+    return c;
+}
+
+// S: a pair of tiles, Large and Small.
+template <class S, class J>
+int launch_cut(const Cut &c, J &job, hipStream_t s) {
+    job.splits = c.splits;
+    job.tiles = c.tiles;
+    return c.large ? launch_tiles<typename S::Large, J>(job, s) : launch_tiles<typename S::Small, J>(job, s);
+}
+
+}  // namespace w2v
