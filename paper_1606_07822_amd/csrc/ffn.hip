@@ -275,21 +275,6 @@ struct Kind<float> {   // fp32 rows as three parts of 8 bits, 24 in all
     using Tiles = Tiles3<E, A, B, PAIR>;
 };
 
-template <class S>
-int64_t count_tiles(int64_t m, int64_t n) {
-    return ceil_div(m, S::BM) * ceil_div(n, S::BN);
-}
-
-template <class L, class S>
-Cut cut_of(int64_t m, int64_t n, int64_t k) {
-    return choose_cut(count_tiles<L>(m, n), count_tiles<S>(m, n), double(S::BM * S::BN) / (L::BM * L::BN), k, S::BK);
-}
-
-template <class L, class S>
-size_t part_bytes(const Cut &c) {
-    return cut_bytes(c, L::BM * L::BN, S::BM * S::BN);
-}
-
 // ------------------------------------------------------------------ operands
 // 16-bit rows of whole, aligned chunks are read where they are.
 bool in_place(int32_t type, const Rows &r, int64_t rows, int64_t cols) {
@@ -346,10 +331,9 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     Side wg = pack.operand(a.w_gate, f, d), wu = pack.operand(a.w_up, f, d);
     const Side wd = pack.operand(a.w_down, d, f);
     E *h = c.take<E>(static_cast<size_t>(K::P * n * hs));
-    const Cut up = cut_of<typename Up::Large, typename Up::Small>(n, 2 * f, d),
-              down = cut_of<typename Down::Large, typename Down::Small>(n, d, f);
-    char *part = c.take<char>(std::max(part_bytes<typename Up::Large, typename Up::Small>(up),
-                                       part_bytes<typename Down::Large, typename Down::Small>(down)));
+    const Cut up = choose_cut_of<Up>(n, 2 * f, d),
+              down = choose_cut_of<Down>(n, d, f);
+    char *part = c.take<char>(std::max(up.bytes, down.bytes));
     if (!launch) return W2V_OK;
     if (up.tiles > kMaxTiles || down.tiles > kMaxTiles) return fail(W2V_E_RANGE, "too many rows for one call");
     if (int rc = launch_parts<T>(pack, s)) return rc;
@@ -398,15 +382,12 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
         h[i] = c.take<E>(static_cast<size_t>(K::P * n * hs));
         hid[i] = Side{reinterpret_cast<char *>(h[i]), n * hs * 2, hs * 2};
     }
-    using HL = typename Hidden::Large;
-    using HS = typename Hidden::Small;
-    using WL = typename Weights::Large;
-    using WS = typename Weights::Small;
-    const Cut back = cut_of<HL, HS>(n, f, d), in = cut_of<HL, HS>(n, d, 2 * f);
-    const Cut weights = choose_cut(2 * count_tiles<WL>(f, d) + count_tiles<WL>(d, f),
-                               2 * count_tiles<WS>(f, d) + count_tiles<WS>(d, f),
-                               double(WS::BM * WS::BN) / (WL::BM * WL::BN), n, WS::BK);
-    char *part = c.take<char>(std::max({part_bytes<HL, HS>(back), part_bytes<HL, HS>(in), part_bytes<WL, WS>(weights)}));
+    using L = typename Weights::Large;
+    using S = typename Weights::Small;
+    const Cut back = choose_cut_of<Hidden>(n, f, d), in = choose_cut_of<Hidden>(n, d, 2 * f);
+    const Cut weights = choose_cut<Weights>(2 * count_tiles<L>(f, d) + count_tiles<L>(d, f),
+                                            2 * count_tiles<S>(f, d) + count_tiles<S>(d, f), n);
+    char *part = c.take<char>(std::max({back.bytes, in.bytes, weights.bytes}));
     if (!launch) return W2V_OK;
     if (back.tiles > kMaxTiles || in.tiles > kMaxTiles || weights.tiles > kMaxTiles)
         return fail(W2V_E_RANGE, "too many rows for one call");

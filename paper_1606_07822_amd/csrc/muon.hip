@@ -301,19 +301,15 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.x_plane = count * rows * w.x_stride;
     w.a_plane = count * w.r * w.a_stride;
     const int64_t tl = count * triangle(ceil_div(w.r, L::BM)), ts = count * triangle(ceil_div(w.r, S::BM));
-    const double share = double(S::BM * S::BN) / (L::BM * L::BN);
-    w.gram = choose_cut(tl, ts, share, w.c, S::BK);
-    w.poly = choose_cut(tl, ts, share, w.r, S::BK);
-    w.step = choose_cut(count * ceil_div(rows, L::BM) * ceil_div(cols, L::BN),
-                        count * ceil_div(rows, S::BM) * ceil_div(cols, S::BN), share, w.r, S::BK);
+    w.gram = choose_cut<Tiles<P, true, true>>(tl, ts, w.c);
+    w.poly = choose_cut<Tiles<P, true, true>>(tl, ts, w.r);
+    w.step = choose_cut<Tiles<P, true, true>>(count * count_tiles<L>(rows, cols), count * count_tiles<S>(rows, cols), w.r);
     Carve k(workspace);
     w.part = k.take<double>(static_cast<size_t>(count * kParts));
     for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
     w.a = k.take<E>(static_cast<size_t>(P * w.a_plane));
     w.b = k.take<E>(static_cast<size_t>(P * w.a_plane));
-    const int large = L::BM * L::BN, small = S::BM * S::BN;
-    w.sums = reinterpret_cast<f4 *>(
-        k.take<char>(std::max({cut_bytes(w.gram, large, small), cut_bytes(w.poly, large, small), cut_bytes(w.step, large, small)})));
+    w.sums = reinterpret_cast<f4 *>(k.take<char>(std::max({w.gram.bytes, w.poly.bytes, w.step.bytes})));
     w.bytes = k.used();
     return w;
 }
