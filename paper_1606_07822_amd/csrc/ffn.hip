@@ -54,19 +54,8 @@ __global__ __launch_bounds__(256) void k_parts(const Sources all) {
         const int64_t per = s.to_stride / 8, row = (c - s.first) / per, chunk = (c - s.first) % per;
         float v[8];
         const int64_t left = s.cols - chunk * 8;
-        load_cols<T, 8>(static_cast<const T *>(s.from) + row * s.from_stride + chunk * 8, 0,
-                        static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(left, 8))), v);
-        Frag<E> part[P];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            E one[P];
-            to_parts<E, P>(v[e], one);
-#pragma unroll
-            for (int p = 0; p < P; ++p) part[p][e] = one[p];
-        }
-        E *to = static_cast<E *>(s.to) + row * s.to_stride + chunk * 8;
-#pragma unroll
-        for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * s.rows * s.to_stride) = part[p];
+        load8<T>(static_cast<const T *>(s.from) + row * s.from_stride + chunk * 8, left, v);
+        store_parts8<E, P>(static_cast<E *>(s.to) + row * s.to_stride + chunk * 8, s.rows * s.to_stride, left, v);
     }
 }
 
@@ -75,42 +64,6 @@ struct Place {
     int64_t m0, n0;
     int32_t which;
 };
-
-// Four elements of a row whose first `valid` exist.
-template <class T>
-__device__ __forceinline__ void store4(T *to, int64_t valid, f4 v) {
-    const float f[4] = {v[0], v[1], v[2], v[3]};
-    if (valid >= 4) {
-        store_pack<T, 4>(to, f);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < valid) to[e] = static_cast<T>(f[e]);
-    }
-}
-
-template <class T>
-__device__ __forceinline__ f4 load4(const T *from, int64_t valid) {
-    float f[4];
-    load_cols<T, 4>(from, 0, static_cast<int>(std::min<int64_t>(valid, 4)), f);
-    return f4{f[0], f[1], f[2], f[3]};
-}
-
-// Parts of a row's four elements; zeros from `valid` on.
-template <class E, int P>
-__device__ __forceinline__ void store_parts(E *to, int64_t plane, int64_t valid, f4 v) {
-    using E4 = E __attribute__((ext_vector_type(4)));
-    E4 part[P];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        E one[P];
-        to_parts<E, P>(e < valid ? v[e] : 0.0f, one);
-#pragma unroll
-        for (int p = 0; p < P; ++p) part[p][e] = one[p];
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<E4 *>(to + p * plane) = part[p];
-}
 
 // Up to three products of one kind and k, or two whose results are added.
 struct Product {
@@ -123,9 +76,9 @@ template <class T>
 struct ProductJob {
     Product p[3];
     int32_t count, splits;
-    bool sum;        // p[0] + p[1], in p[0].out
+    const char *a2, *b2;           // what p[0]'s k goes on with, or null
     int64_t k, tiles;
-    f4 *part;
+    float *part;
 
     template <class Q>
     __device__ __forceinline__ Place at(int64_t tile) const {
@@ -140,26 +93,17 @@ struct ProductJob {
     template <class Q>
     __device__ __forceinline__ void multiply(const Place &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         const Product &x = p[w.which];
-        if (!sum) {
-            const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
-            if (k0 < k1) Q::run(x.a, x.b, 0, w.m0, x.m, w.n0, x.n, k0, k1, lds, acc);
-            return;
-        }
-        const int64_t whole = ceil_div(k, Q::BK) * Q::BK, step = split_steps(2 * whole, Q::BK, splits), k0 = split * step;
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            const int64_t lo = std::max<int64_t>(0, k0 - i * whole), hi = std::min(k, k0 + step - i * whole);
-            if (i == 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the first product's reads of LDS
-            if (lo < hi) Q::run(p[i].a, p[i].b, 0, w.m0, x.m, w.n0, x.n, lo, hi, lds, acc);
-        }
+        const int64_t all = Q::TWO ? ceil_div(k, Q::BK) * Q::BK + k : k;
+        const int64_t step = split_steps(all, Q::BK, splits), k0 = split * step, k1 = std::min(all, k0 + step);
+        if (k0 < k1) Q::run(x.a, x.b, a2, b2, 0, w.m0, x.m, w.n0, x.n, k, k0, k1, lds, acc);
     }
-    __device__ __forceinline__ void put(const Place &w, int row, int col, f4 v0, f4 v1) const {
+    template <class Q>
+    __device__ __forceinline__ void take(const Place &w, int row, int col, char *region, Lanes lanes) const {
         const Product &x = p[w.which];
-        const int64_t m = w.m0 + row, n = w.n0 + col;
-        if (m >= x.m) return;
-        T *to = static_cast<T *>(x.out) + m * x.out_stride + n;
-        store4<T>(to, x.n - n, v0);
-        store4<T>(to + 16, x.n - n - 16, v1);
+        Q::rows8(region, lanes, [&](int r, int c, const float (&v)[8]) {
+            const int64_t m = w.m0 + row + r, n = w.n0 + col + c;
+            if (m < x.m) store8<T>(static_cast<T *>(x.out) + m * x.out_stride + n, x.n - n, v);
+        });
     }
 };
 
@@ -170,7 +114,7 @@ struct UpJob {
     int64_t other;   // from Wg to Wu, bytes
     int64_t m, n, gm, gn, k, tiles;
     int32_t splits, act;
-    f4 *part;
+    float *part;
     E *h;
     int64_t h_stride, h_plane;
     T *gate, *up;
@@ -185,18 +129,20 @@ struct UpJob {
     template <class Q>
     __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
-        if (k0 < k1) Q::run(x, w, other, w0.m0, m, w0.n0, n, k0, k1, lds, acc);
+        if (k0 < k1) Q::run(x, w, nullptr, nullptr, other, w0.m0, m, w0.n0, n, k, k0, k1, lds, acc);
     }
-    __device__ __forceinline__ void put(const Place &w0, int row, int col, f4 g, f4 u) const {
-        const int64_t r = w0.m0 + row, c = w0.n0 + col / 32 * 16 + col % 16, valid = n - c;
-        if (r >= m) return;
-        if (gate) store4<T>(gate + r * gate_stride + c, valid, g);
-        if (up) store4<T>(up + r * up_stride + c, valid, u);
-        if (c >= h_stride) return;
-        f4 v;
+    template <class Q>
+    __device__ __forceinline__ void take(const Place &w0, int row, int col, char *region, Lanes lanes) const {
+        Q::pairs8(region, lanes, [&](int i, int j, const float (&g)[8], const float (&u)[8]) {
+            const int64_t r = w0.m0 + row + i, c = w0.n0 + col / 2 + j, valid = n - c;
+            if (r >= m || c >= h_stride) return;
+            if (gate) store8<T>(gate + r * gate_stride + c, valid, g);
+            if (up) store8<T>(up + r * up_stride + c, valid, u);
+            float v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = act_value(act, g[e]) * u[e];
-        store_parts<E, P>(h + r * h_stride + c, h_plane, valid, v);
+            for (int e = 0; e < 8; ++e) v[e] = act_value(act, g[e]) * u[e];
+            store_parts8<E, P>(h + r * h_stride + c, h_plane, valid, v);
+        });
     }
 };
 
@@ -206,7 +152,7 @@ struct BackJob {
     Side dy, w;
     int64_t m, n, gm, gn, k, tiles;
     int32_t splits, act;
-    f4 *part;
+    float *part;
     E *dg, *du, *h;
     int64_t h_stride, h_plane;
     const T *gate, *up;
@@ -221,58 +167,58 @@ struct BackJob {
     template <class Q>
     __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
-        if (k0 < k1) Q::run(dy, w, 0, w0.m0, m, w0.n0, n, k0, k1, lds, acc);
+        if (k0 < k1) Q::run(dy, w, nullptr, nullptr, 0, w0.m0, m, w0.n0, n, k, k0, k1, lds, acc);
     }
-    __device__ __forceinline__ void put(const Place &w0, int row, int col, f4 v0, f4 v1) const {
-        const int64_t r = w0.m0 + row, c = w0.n0 + col;
-        if (r >= m) return;
-        one(r, c, v0);
-        one(r, c + 16, v1);
-    }
-    __device__ __forceinline__ void one(int64_t r, int64_t c, f4 dh) const {
-        if (c >= h_stride) return;
-        const int64_t valid = n - c;
-        const f4 g = load4(gate + r * gate_stride + c, valid), u = load4(up + r * up_stride + c, valid);
-        f4 vg, vu, vh;
+    template <class Q>
+    __device__ __forceinline__ void take(const Place &w0, int row, int col, char *region, Lanes lanes) const {
+        Q::rows8(region, lanes, [&](int i, int j, const float (&dh)[8]) {
+            const int64_t r = w0.m0 + row + i, c = w0.n0 + col + j, valid = n - c;
+            if (r >= m || c >= h_stride) return;
+            float g[8], u[8], vg[8], vu[8], vh[8];
+            load8<T>(gate + r * gate_stride + c, valid, g);
+            load8<T>(up + r * up_stride + c, valid, u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float value, slope;
-            act_both(act, g[e], value, slope);
-            vh[e] = value * u[e];
-            vu[e] = dh[e] * value;
-            vg[e] = dh[e] * u[e] * slope;
-        }
-        const int64_t at = r * h_stride + c;
-        store_parts<E, P>(dg + at, h_plane, valid, vg);
-        store_parts<E, P>(du + at, h_plane, valid, vu);
-        store_parts<E, P>(h + at, h_plane, valid, vh);
+            for (int e = 0; e < 8; ++e) {
+                float value, slope;
+                act_both(act, g[e], value, slope);
+                vh[e] = value * u[e];
+                vu[e] = dh[e] * value;
+                vg[e] = dh[e] * u[e] * slope;
+            }
+            const int64_t at = r * h_stride + c;
+            store_parts8<E, P>(dg + at, h_plane, valid, vg);
+            store_parts8<E, P>(du + at, h_plane, valid, vu);
+            store_parts8<E, P>(h + at, h_plane, valid, vh);
+        });
     }
 };
 
 // ------------------------------------------------------------------ tiles and how a product is cut into them
-template <class E, bool A, bool B, bool PAIR = false>
+template <class E, bool A, bool B, bool PAIR, bool TWO>
 struct Tiles1 {
-    using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B, PAIR>;
-    using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR>;
+    using Large = Tile<E, 1, 256, 256, PAIR ? 4 : 2, PAIR ? 2 : 4, 64, A, B, PAIR, TWO>;
+    using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR, TWO>;
+    using Deep = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR, TWO, 5>;
 };
-template <class E, bool A, bool B, bool PAIR = false>
+template <class E, bool A, bool B, bool PAIR, bool TWO>
 struct Tiles3 {
-    using Large = Tile<E, 3, 256, 128, 4, 2, 32, A, B, PAIR>;
-    using Small = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR>;
+    using Large = Tile<E, 3, 256, 128, 4, 2, 32, A, B, PAIR, TWO>;
+    using Small = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR, TWO>;
+    using Deep = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR, TWO, 3>;
 };
 template <class T>
 struct Kind {   // 16-bit rows are multiplied as they are
     using E = T;
     static constexpr int P = 1;
-    template <bool A, bool B, bool PAIR = false>
-    using Tiles = Tiles1<E, A, B, PAIR>;
+    template <bool A, bool B, bool PAIR = false, bool TWO = false>
+    using Tiles = Tiles1<E, A, B, PAIR, TWO>;
 };
 template <>
 struct Kind<float> {   // fp32 rows as three parts of 8 bits, 24 in all
     using E = __bf16;
     static constexpr int P = 3;
-    template <bool A, bool B, bool PAIR = false>
-    using Tiles = Tiles3<E, A, B, PAIR>;
+    template <bool A, bool B, bool PAIR = false, bool TWO = false>
+    using Tiles = Tiles3<E, A, B, PAIR, TWO>;
 };
 
 // ------------------------------------------------------------------ operands
@@ -282,6 +228,11 @@ bool in_place(int32_t type, const Rows &r, int64_t rows, int64_t cols) {
            (rows <= 1 || (r.stride % 8 == 0 && r.stride < (1 << 23)));
 }
 
+// Two arrays of the same sizes that a product reads with one stride.
+bool in_place(int32_t type, const Rows &r, const Rows &q, int64_t rows, int64_t cols) {
+    return in_place(type, r, rows, cols) && in_place(type, q, rows, cols) && (rows <= 1 || r.stride == q.stride);
+}
+
 struct Packing {
     Sources all{};
     int32_t type;
@@ -289,12 +240,20 @@ struct Packing {
     Carve *carve;
 
     Side operand(const Rows &r, int64_t rows, int64_t cols) {
-        if (in_place(type, r, rows, cols))
-            return Side{static_cast<const char *>(r.p), 0, (rows <= 1 ? cols : r.stride) * 2};
+        return in_place(type, r, rows, cols) ? as_is(r, rows, cols) : packed(r, rows, cols);
+    }
+    void operands(const Rows &r, const Rows &q, int64_t rows, int64_t cols, Side &a, Side &b) {
+        const bool both = in_place(type, r, q, rows, cols);
+        a = both ? as_is(r, rows, cols) : packed(r, rows, cols);
+        b = both ? as_is(q, rows, cols) : packed(q, rows, cols);
+    }
+    static Side as_is(const Rows &r, int64_t rows, int64_t cols) {
+        return Side{static_cast<const char *>(r.p), 0, (rows <= 1 ? cols : r.stride) * 2};
+    }
+    Side packed(const Rows &r, int64_t rows, int64_t cols) {
         const int64_t stride = ceil_div(cols, 8) * 8;
         char *to = carve->take<char>(static_cast<size_t>(parts * rows * stride * 2));
-        Source &s = all.s[all.count++];
-        s = Source{r.p, r.stride, to, rows, cols, stride, all.chunks};
+        all.s[all.count++] = Source{r.p, r.stride, to, rows, cols, stride, all.chunks};
         all.chunks += rows * (stride / 8);
         return Side{to, rows * stride * 2, stride * 2};
     }
@@ -311,11 +270,11 @@ int launch_parts(const Packing &p, hipStream_t s) {
 
 template <class S>
 int64_t tile_m(const Cut &c) {
-    return c.large ? S::Large::BM : S::Small::BM;
+    return c.kind == kLarge ? S::Large::BM : S::Small::BM;
 }
 template <class S>
 int64_t tile_n(const Cut &c) {
-    return c.large ? S::Large::BN : S::Small::BN;
+    return c.kind == kLarge ? S::Large::BN : S::Small::BN;
 }
 
 // One plan of a pass: where its arrays lie, without a workspace only how many bytes they are.
@@ -328,12 +287,13 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     const int64_t n = a.rows, d = a.dim, f = a.hidden, hs = ceil_div(f, 64) * 64;
     Packing pack{{}, a.type, K::P, &c};
     const Side x = pack.operand(a.x, n, d);
-    Side wg = pack.operand(a.w_gate, f, d), wu = pack.operand(a.w_up, f, d);
+    Side wg, wu;
+    pack.operands(a.w_gate, a.w_up, f, d, wg, wu);
     const Side wd = pack.operand(a.w_down, d, f);
     E *h = c.take<E>(static_cast<size_t>(K::P * n * hs));
     const Cut up = choose_cut_of<Up>(n, 2 * f, d),
               down = choose_cut_of<Down>(n, d, f);
-    char *part = c.take<char>(std::max(up.bytes, down.bytes));
+    float *part = c.take<float>(std::max(up.floats, down.floats));
     if (!launch) return W2V_OK;
     if (up.tiles > kMaxTiles || down.tiles > kMaxTiles) return fail(W2V_E_RANGE, "too many rows for one call");
     if (int rc = launch_parts<T>(pack, s)) return rc;
@@ -347,7 +307,7 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     u.gn = ceil_div(2 * f, tile_n<Up>(up));
     u.k = d;
     u.act = a.act;
-    u.part = reinterpret_cast<f4 *>(part);
+    u.part = part;
     u.h = h;
     u.h_stride = hs;
     u.h_plane = n * hs;
@@ -361,7 +321,7 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
                      ceil_div(d, tile_n<Down>(down)), 0, const_cast<void *>(a.y.p), a.y.stride};
     y.count = 1;
     y.k = f;
-    y.part = reinterpret_cast<f4 *>(part);
+    y.part = part;
     return launch_cut<Down>(down, y, s);
 }
 
@@ -370,12 +330,14 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     using K = Kind<T>;
     using E = typename K::E;
     using Hidden = typename K::template Tiles<true, false>;
+    using Input = typename K::template Tiles<true, false, false, true>;
     using Weights = typename K::template Tiles<false, false>;
     const int64_t n = a.rows, d = a.dim, f = a.hidden, hs = ceil_div(f, 64) * 64;
     Packing pack{{}, a.type, K::P, &c};
     const Side dy = pack.operand(a.dy, n, d), wd = pack.operand(a.w_down, d, f);
     const Side x = pack.operand(a.x, n, d);
-    const Side wg = pack.operand(a.w_gate, f, d), wu = pack.operand(a.w_up, f, d);
+    Side wg, wu;
+    pack.operands(a.w_gate, a.w_up, f, d, wg, wu);
     E *h[3];
     Side hid[3];
     for (int i = 0; i < 3; ++i) {
@@ -384,10 +346,10 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     }
     using L = typename Weights::Large;
     using S = typename Weights::Small;
-    const Cut back = choose_cut_of<Hidden>(n, f, d), in = choose_cut_of<Hidden>(n, d, 2 * f);
+    const Cut back = choose_cut_of<Hidden>(n, f, d), in = choose_cut_of<Input>(n, d, 2 * f);
     const Cut weights = choose_cut<Weights>(2 * count_tiles<L>(f, d) + count_tiles<L>(d, f),
                                             2 * count_tiles<S>(f, d) + count_tiles<S>(d, f), n);
-    char *part = c.take<char>(std::max({back.bytes, in.bytes, weights.bytes}));
+    float *part = c.take<float>(std::max({back.floats, in.floats, weights.floats}));
     if (!launch) return W2V_OK;
     if (back.tiles > kMaxTiles || in.tiles > kMaxTiles || weights.tiles > kMaxTiles)
         return fail(W2V_E_RANGE, "too many rows for one call");
@@ -401,7 +363,7 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     b.gn = ceil_div(f, tile_n<Hidden>(back));
     b.k = d;
     b.act = a.act;
-    b.part = reinterpret_cast<f4 *>(part);
+    b.part = part;
     b.dg = h[0];
     b.du = h[1];
     b.h = h[2];
@@ -425,7 +387,7 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     }
     if (first > 0) {
         j.k = n;
-        j.part = reinterpret_cast<f4 *>(part);
+        j.part = part;
         Cut w = weights;
         w.tiles = first;   // of the gradients that are wanted
         if (int rc = launch_cut<Weights>(w, j, s)) return rc;
@@ -433,14 +395,14 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     // dx last: it may lie where dy or x did
     if (!a.dx.p) return W2V_OK;
     ProductJob<T> i{};
-    for (int q = 0; q < 2; ++q)
-        i.p[q] = Product{hid[q], q ? wu : wg, n, d, ceil_div(n, tile_m<Hidden>(in)), ceil_div(d, tile_n<Hidden>(in)), 0,
-                         const_cast<void *>(a.dx.p), a.dx.stride};
+    i.p[0] = Product{hid[0], wg, n, d, ceil_div(n, tile_m<Input>(in)), ceil_div(d, tile_n<Input>(in)), 0,
+                     const_cast<void *>(a.dx.p), a.dx.stride};
+    i.a2 = hid[1].p;
+    i.b2 = wu.p;
     i.count = 1;
-    i.sum = true;
     i.k = f;
-    i.part = reinterpret_cast<f4 *>(part);
-    return launch_cut<Hidden>(in, i, s);
+    i.part = part;
+    return launch_cut<Input>(in, i, s);
 }
 
 // Gradients of no rows: zeros, by a kernel (a captured graph takes no memset).

@@ -110,17 +110,9 @@ __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double 
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = b.nesterov ? g[i] * b.grad_scale + b.mu * m[i] : m[i];
         }
-        Frag<E> to[P];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            E one[P];
-            to_parts<E, P>(i < valid ? static_cast<float>(g[i] * inverse) : 0.0f, one);
-#pragma unroll
-            for (int p = 0; p < P; ++p) to[p][i] = one[p];
-        }
-        E *at = x + (z * b.rows + row) * stride + col;
-#pragma unroll
-        for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(at + p * plane) = to[p];
+        for (int i = 0; i < 8; ++i) g[i] = static_cast<float>(g[i] * inverse);
+        store_parts8<E, P>(x + (z * b.rows + row) * stride + col, plane, valid, g);
     }
 }
 
@@ -128,21 +120,6 @@ __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double 
 struct Spot {
     int64_t m0, n0, z;
 };
-
-template <int P>
-__device__ __forceinline__ void store_parts4(E *to, int64_t plane, int64_t valid, const float (&v)[4]) {
-    using E4 = E __attribute__((ext_vector_type(4)));
-    E4 part[P];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        E one[P];
-        to_parts<E, P>(e < valid ? v[e] : 0.0f, one);
-#pragma unroll
-        for (int p = 0; p < P; ++p) part[p][e] = one[p];
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<E4 *>(to + p * plane) = part[p];
-}
 
 // A symmetric r x r product of each matrix with itself, of which the tiles on and above the diagonal are made: A = X X' (or
 // X' X), or with `poly` aI + bA + cAA.
@@ -152,7 +129,7 @@ struct SquareJob {
     int64_t step;        // bytes from a matrix to the next
     int64_t r, k, g, tiles;
     int32_t splits, poly;
-    f4 *part;
+    float *part;
     const E *old;        // A, where poly
     E *out;
     int64_t stride, plane;
@@ -169,39 +146,42 @@ struct SquareJob {
         const int64_t each = split_steps(k, Q::BK, splits), k0 = split * each, k1 = std::min(k, k0 + each);
         Side s = x;
         s.p += w.z * step;
-        if (k0 < k1) Q::run(s, s, 0, w.m0, r, w.n0, r, k0, k1, lds, acc);
+        if (k0 < k1) Q::run(s, s, nullptr, nullptr, 0, w.m0, r, w.n0, r, k, k0, k1, lds, acc);
     }
-    __device__ __forceinline__ void put(const Spot &w, int row, int col, f4 v0, f4 v1) const {
-        one(w, w.m0 + row, w.n0 + col, v0);
-        one(w, w.m0 + row, w.n0 + col + 16, v1);
+    template <class Q>
+    __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
+        E *to = out + w.z * r * stride;
+        const E *a = old + w.z * r * stride;
+        Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
+            const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
+            if (m >= r || n >= stride) return;
+            finish(a + m * stride + n, m, n, v);
+            store_parts8<E, P>(to + m * stride + n, plane, r - n, v);
+        });
+        if (w.m0 == w.n0) return;
+        // the tile below the diagonal: A is symmetric, so that row n has from column m on what column n had from row m on
+        Q::columns8(region, lanes, [&](int i, int j, float (&v)[8]) {
+            const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
+            if (n >= r || m >= r) return;
+            finish(a + n * stride + m, n, m, v);
+            store_parts8<E, P>(to + n * stride + m, plane, r - m, v);
+        });
     }
-    __device__ __forceinline__ void one(const Spot &w, int64_t m, int64_t n, f4 v) const {
-        if (m >= r || n >= stride) return;
-        const int64_t base = w.z * r * stride, at = base + m * stride + n;
-        float f[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = v[e] * kDown;
+    // `from`: A's 8 elements from (row, col) on.
+    __device__ __forceinline__ void finish(const E *from, int64_t row, int64_t col, float (&v)[8]) const {
+        float a[8] = {};
         if (poly) {
-            using E4 = E __attribute__((ext_vector_type(4)));
-            float a[4] = {};
 #pragma unroll
             for (int p = P - 1; p >= 0; --p) {
-                const E4 o = *reinterpret_cast<const E4 *>(old + at + p * plane);
+                const Frag<E> o = *reinterpret_cast<const Frag<E> *>(from + p * plane);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] += static_cast<float>(o[e]);
+                for (int e = 0; e < 8; ++e) a[e] += static_cast<float>(o[e]);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = kC * f[e] + kB * a[e] + (m == n + e ? kA * kUp : 0.0f);
         }
-        store_parts4<P>(out + at, plane, r - n, f);
-        if (w.m0 == w.n0) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (n + e >= r) break;
-            E one[P];
-            to_parts<E, P>(f[e], one);
-#pragma unroll
-            for (int p = 0; p < P; ++p) out[base + (n + e) * stride + m + p * plane] = one[p];
+        for (int e = 0; e < 8; ++e) {
+            v[e] *= kDown;
+            if (poly) v[e] = kC * v[e] + kB * a[e] + (row == col + e ? kA * kUp : 0.0f);
         }
     }
 };
@@ -213,7 +193,7 @@ struct StepJob {
     int64_t a_step, b_step;   // bytes from a matrix to the next
     int64_t k, gm, gn, tiles;
     int32_t splits;
-    f4 *part;
+    float *part;
     E *out;
     int64_t stride, plane;
     Batch batch;
@@ -230,36 +210,32 @@ struct StepJob {
         Side l = a, r = b;
         l.p += w.z * a_step;
         r.p += w.z * b_step;
-        if (k0 < k1) Q::run(l, r, 0, w.m0, batch.rows, w.n0, batch.cols, k0, k1, lds, acc);
+        if (k0 < k1) Q::run(l, r, nullptr, nullptr, 0, w.m0, batch.rows, w.n0, batch.cols, k, k0, k1, lds, acc);
     }
-    __device__ __forceinline__ void put(const Spot &w, int row, int col, f4 v0, f4 v1) const {
-        one(w, w.m0 + row, w.n0 + col, v0);
-        one(w, w.m0 + row, w.n0 + col + 16, v1);
-    }
-    __device__ __forceinline__ void one(const Spot &w, int64_t m, int64_t n, f4 v) const {
-        if (m >= batch.rows) return;
-        float f[4];
+    template <class Q>
+    __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
         if constexpr (!LAST) {
-            if (n >= stride) return;
+            Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
+                const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
+                if (m >= batch.rows || n >= stride) return;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = v[e] * kDown;
-            store_parts4<P>(out + (w.z * batch.rows + m) * stride + n, plane, batch.cols - n, f);
+                for (int e = 0; e < 8; ++e) v[e] *= kDown;
+                store_parts8<E, P>(out + (w.z * batch.rows + m) * stride + n, plane, batch.cols - n, v);
+            });
         } else {
             const Entry en = batch.entry(w.z);
-            T *to = static_cast<T *>(en.out) + m * en.out_stride + n;
-            const int valid = static_cast<int>(std::min<int64_t>(4, batch.cols - n));
-            if (valid <= 0) return;
-            const float back = kDown * kDown;
-            if (batch.muon) {
-                const float lr = batch.lr_device ? *batch.lr_device : batch.lr;
-                load_cols<T, 4>(to, 0, valid, f);
+            const float lr = batch.lr_device ? *batch.lr_device : batch.lr;
+            const float keep = 1.0f - lr * en.decay, by = batch.muon ? -lr * en.scale * (kDown * kDown) : kDown * kDown;
+            Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
+                const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
+                if (m >= batch.rows) return;
+                T *to = static_cast<T *>(en.out) + m * en.out_stride + n;
+                float old[8] = {};
+                if (batch.muon) load8<T>(to, batch.cols - n, old);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = f[e] * (1.0f - lr * en.decay) - lr * en.scale * (v[e] * back);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = v[e] * back;
-            }
-            store_cols<T, 4>(to, 0, valid, f);
+                for (int e = 0; e < 8; ++e) v[e] = batch.muon ? old[e] * keep + v[e] * by : v[e] * by;
+                store8<T>(to, batch.cols - n, v);
+            });
         }
     }
 };
@@ -270,11 +246,13 @@ template <bool A, bool B>
 struct Tiles<1, A, B> {
     using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B>;
     using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B>;
+    using Deep = Tile<E, 1, 128, 128, 2, 2, 64, A, B, false, false, 5>;
 };
 template <bool A, bool B>
 struct Tiles<2, A, B> {
     using Large = Tile<E, 2, 256, 256, 2, 4, 32, A, B>;
     using Small = Tile<E, 2, 128, 128, 2, 2, 32, A, B>;
+    using Deep = Tile<E, 2, 128, 128, 2, 2, 32, A, B, false, false, 5>;
 };
 
 int64_t triangle(int64_t g) { return g * (g + 1) / 2; }
@@ -283,7 +261,7 @@ int64_t triangle(int64_t g) { return g * (g + 1) / 2; }
 struct Arrays {
     double *part;
     E *x[2], *a, *b;
-    f4 *sums;
+    float *sums;
     int64_t r, c, x_stride, a_stride, x_plane, a_plane;
     Cut gram, poly, step;
     size_t bytes;
@@ -309,7 +287,7 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
     w.a = k.take<E>(static_cast<size_t>(P * w.a_plane));
     w.b = k.take<E>(static_cast<size_t>(P * w.a_plane));
-    w.sums = reinterpret_cast<f4 *>(k.take<char>(std::max({w.gram.bytes, w.poly.bytes, w.step.bytes})));
+    w.sums = k.take<float>(std::max({w.gram.floats, w.poly.floats, w.step.floats}));
     w.bytes = k.used();
     return w;
 }
@@ -328,7 +306,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.step = b.rows * w.x_stride * 2;
         q.r = w.r;
         q.k = w.c;
-        q.g = ceil_div(w.r, w.gram.large ? bm : sm);
+        q.g = ceil_div(w.r, w.gram.kind == kLarge ? bm : sm);
         q.part = w.sums;
         q.out = w.a;
         q.stride = w.a_stride;
@@ -337,7 +315,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.x = Side{reinterpret_cast<const char *>(w.a), w.a_plane * 2, w.a_stride * 2};
         q.step = w.r * w.a_stride * 2;
         q.k = w.r;
-        q.g = ceil_div(w.r, w.poly.large ? bm : sm);
+        q.g = ceil_div(w.r, w.poly.kind == kLarge ? bm : sm);
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;
@@ -349,8 +327,8 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
             job.a_step = WIDE ? w.r * w.a_stride * 2 : b.rows * w.x_stride * 2;
             job.b_step = WIDE ? b.rows * w.x_stride * 2 : w.r * w.a_stride * 2;
             job.k = w.r;
-            job.gm = ceil_div(b.rows, w.step.large ? bm : sm);
-            job.gn = ceil_div(b.cols, w.step.large ? bm : sm);
+            job.gm = ceil_div(b.rows, w.step.kind == kLarge ? bm : sm);
+            job.gn = ceil_div(b.cols, w.step.kind == kLarge ? bm : sm);
             job.part = w.sums;
             job.out = w.x[1 - i % 2];
             job.stride = w.x_stride;

@@ -33,15 +33,37 @@ __device__ __forceinline__ f4 mfma32(Frag<_Float16> a, Frag<_Float16> b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// 64 lanes' 16 bytes each from global memory into LDS, lane after lane from `lds` (the same in all lanes) on.
+// 64 lanes' 16 bytes each from global memory into LDS, lane after lane from `lds` (the same in all lanes) on. In assembly,
+// because the compiler lets a transposing read of LDS wait for every such load before it, also of the other buffer; the
+// kernels wait for them themselves. M0 holds nothing else here: no other instruction of these kernels reads it.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const char *from) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)static_cast<uintptr_t>(lds), 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 
 namespace {
 __device__ __attribute__((aligned(16))) const char kZeroChunk[16] = {};   // what a step reads past the end of k
 }
+
+// A wavefront's writes of LDS before it, for its other lanes' reads behind it (and the other way round).
+__device__ __forceinline__ void lds_order() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// The first `valid` of 8 neighbouring elements (any number: none below 1, all from 8 on).
+template <class T>
+__device__ __forceinline__ void store8(T *to, int64_t valid, const float (&v)[8]) {
+    store_cols<T, 8>(to, 0, static_cast<int>(std::min<int64_t>(valid, 8)), v);
+}
+template <class T>
+__device__ __forceinline__ void load8(const T *from, int64_t valid, float (&v)[8]) {
+    load_cols<T, 8>(from, 0, static_cast<int>(std::min<int64_t>(valid, 8)), v);
+}
+
+// The threads that share a region: number `at` of `step`.
+struct Lanes {
+    int at, step;
+};
 
 struct Side {
     const char *p;
@@ -60,12 +82,32 @@ __device__ __forceinline__ void to_parts(float v, E (&part)[P]) {
     }
 }
 
-template <class E_, int P_, int BM_, int BN_, int WM_, int WN_, int BK_, bool ALONG_A, bool ALONG_B, bool PAIR = false>
+// Parts of 8 neighbouring elements, zeros from number `valid` on, `plane` elements from a part to the next.
+template <class E, int P>
+__device__ __forceinline__ void store_parts8(E *to, int64_t plane, int64_t valid, const float (&v)[8]) {
+    Frag<E> part[P];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        E one[P];
+        to_parts<E, P>(e < valid ? v[e] : 0.0f, one);
+#pragma unroll
+        for (int p = 0; p < P; ++p) part[p][e] = one[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * plane) = part[p];
+}
+
+// PAIR: B's rows come in groups of 16 from two arrays in turn. TWO: k runs through a second pair of operands after the
+// first.
+template <class E_, int P_, int BM_, int BN_, int WM_, int WN_, int BK_, bool ALONG_A, bool ALONG_B, bool PAIR_ = false,
+          bool TWO_ = false, int STAGES_ = 2>
 struct Tile {
     using E = E_;
     static constexpr int P = P_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
+    static constexpr bool PAIR = PAIR_, TWO = TWO_;
+    static constexpr int STAGES = STAGES_;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
-    static constexpr int kA = P * BM * BK * 2, kB = P * BN * BK * 2, kStage = kA + kB, kLds = 2 * kStage;
+    static constexpr int kA = P * BM * BK * 2, kB = P * BN * BK * 2, kStage = kA + kB, kLds = STAGES * kStage;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;   // fragments of 16 x 16 a wavefront
     static constexpr int kPerCu = 160 * 1024 / kLds, kPerSimd = std::max(1, std::min(2, kPerCu) * kWaves / 4);
     static_assert(FN % 2 == 0 && kPerCu >= 1, "pairs of fragments, one CU's LDS");
@@ -87,14 +129,15 @@ struct Tile {
         }
 
         const char *p;
-        int64_t plane, step;
+        int64_t plane, step, corner;   // corner: bytes from an operand's start to the tile's first row or column
         uint32_t off[kLoads];
-        int32_t left;     // of k, from the step that is loaded next on
+        int32_t left;                  // of k, from the step that is loaded next on
 
         // valid: rows (ALONG) or columns from the tile's first one on that the operand has; what lies past them is read
         // from the last one and dropped with its results.
         __device__ __forceinline__ void start(const Side &s, int64_t first, int64_t valid, int64_t k0, int64_t k1, int wave, int lane) {
-            p = s.p + (ALONG ? first * s.row + k0 * 2 : k0 * s.row + first * 2);
+            corner = ALONG ? first * s.row : first * 2;
+            p = s.p + corner + k0 * (ALONG ? 2 : s.row);
             plane = s.plane;
             step = ALONG ? kRow : BK * s.row;
             left = static_cast<int32_t>(k1 - k0);
@@ -110,25 +153,35 @@ struct Tile {
             }
         }
 
+        __device__ __forceinline__ void turn(const char *second, int64_t k) {
+            p = second + corner;
+            left = static_cast<int32_t>(k);
+        }
+
         // other: bytes to a second operand that every second group of 16 rows comes from.
         __device__ __forceinline__ void load(uint32_t lds, int wave, int lane, int64_t other = 0) {
+            if (left >= BK) {
+                each_load(lds, wave, other, [&](uint32_t at, const char *from, int i, int) { load_to_lds(at, from, off[i]); });
+            } else {
+                each_load(lds, wave, other, [&](uint32_t at, const char *from, int i, int first) {
+                    const int row = first + lane / kChunks;
+                    const int k = ALONG ? place(row, lane % kChunks) * 8 : row;
+                    load_to_lds(at, k < left ? from + off[i] : kZeroChunk);
+                });
+            }
+            p += step;
+            left -= BK;
+        }
+        template <class F>
+        __device__ __forceinline__ void each_load(uint32_t lds, int wave, int64_t other, F f) {
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int first = (wave * kLoads + i) * kRowsPerLoad;
-                    const uint32_t at = lds + static_cast<uint32_t>(q * kPlane + first * kRow);
-                    const char *from = p + q * plane + (PAIR && first / 16 % 2 ? other : 0);
-                    if (left >= BK) {
-                        load_to_lds(at, from + off[i]);
-                    } else {
-                        const int row = first + lane / kChunks;
-                        const int k = ALONG ? place(row, lane % kChunks) * 8 : row;
-                        load_to_lds(at, k < left ? from + off[i] : kZeroChunk);
-                    }
+                    f(lds + static_cast<uint32_t>(q * kPlane + first * kRow),
+                      p + q * plane + (PAIR && first / 16 % 2 ? other : 0), i, first);
                 }
-            p += step;
-            left -= BK;
         }
 
         // The fragment of 16 rows (ALONG) or columns from `first` on, at the 32 k from 32 ks on: lane l holds number
@@ -154,19 +207,30 @@ struct Tile {
     };
     using HalfA = Half<ALONG_A, BM>;
     using HalfB = Half<ALONG_B, BN>;
+    static constexpr int kStepLoads = P * (HalfA::kLoads + HalfB::kLoads);
 
-    // acc += the product over k0 <= k < k1 (k0 a multiple of BK) of the tile from (m0, n0) on of an m x n one. Element e
-    // of acc[i][j] is C at row m0 + 16 (wm FM + i) + lane % 16, column n0 + 16 (wn FN + j) + 4 (lane / 16) + e. PAIR: B's
-    // rows come in groups of 16 from b and, `other` bytes behind, a second operand in turn; n and n0 count one operand's.
-    static __device__ __forceinline__ void run(const Side &a, const Side &b, int64_t other, int64_t m0, int64_t m, int64_t n0,
-                                               int64_t n, int64_t k0, int64_t k1, char *lds, f4 (&acc)[FM][FN]) {
+    // The product over k0 <= k < k1 (k0 a multiple of BK) of the tile from (m0, n0) on of an m x n one. Element e of
+    // acc[i][j] is C at row m0 + 16 (wm FM + i) + lane % 16, column n0 + 16 (wn FN + j) + 4 (lane / 16) + e. PAIR: the second
+    // array lies `other` bytes behind b; n and n0 count one array's rows. TWO: both pairs of operands have k elements of k,
+    // the second's count from k rounded up to BK on; they share the first's strides.
+    static __device__ __forceinline__ void run(const Side &a, const Side &b, const char *a2, const char *b2, int64_t other,
+                                               int64_t m0, int64_t m, int64_t n0, int64_t n, int64_t k, int64_t k0,
+                                               int64_t k1, char *lds, f4 (&acc)[FM][FN]) {
         const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
         const int wm = wave / WN, wn = wave % WN;
         HalfA ha;
         HalfB hb;
-        ha.start(a, m0, m - m0, k0, k1, wave, lane);
-        if constexpr (PAIR) {   // row r of the tile is row 16 (r / 32) + r % 16 of an operand
-            hb.start(b, n0, n - n0, k0, k1, wave, lane);
+        int turn_at = -1;   // the step with which the second operands begin
+        const int64_t whole = (k + BK - 1) / BK * BK;
+        if (TWO && k0 >= whole) {
+            ha.start(Side{a2, a.plane, a.row}, m0, m - m0, k0 - whole, k1 - whole, wave, lane);
+            hb.start(Side{b2, b.plane, b.row}, n0, n - n0, k0 - whole, k1 - whole, wave, lane);
+        } else {
+            if (TWO && k1 > whole) turn_at = static_cast<int>((whole - k0) / BK);
+            ha.start(a, m0, m - m0, k0, std::min(k1, k), wave, lane);
+            hb.start(b, n0, n - n0, k0, std::min(k1, k), wave, lane);
+        }
+        if constexpr (PAIR) {   // row r of the tile is row 16 (r / 32) + r % 16 of an array
             const int last = static_cast<int>(std::min<int64_t>(n - n0, BN / 2)) - 1;
 #pragma unroll
             for (int i = 0; i < HalfB::kLoads; ++i) {
@@ -174,22 +238,34 @@ struct Tile {
                 hb.off[i] = static_cast<uint32_t>(min(row / 32 * 16 + row % 16, last)) * static_cast<uint32_t>(b.row) +
                             static_cast<uint32_t>(HalfB::place(row, lane % HalfB::kChunks)) * 16u;
             }
-        } else {
-            hb.start(b, n0, n - n0, k0, k1, wave, lane);
         }
         const auto base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds));
         const int steps = static_cast<int>((k1 - k0 + BK - 1) / BK);
-        ha.load(base, wave, lane);
-        hb.load(base + kA, wave, lane, other);
-        for (int s = 0; s < steps; ++s) {
-            // this wavefront's loads have landed and its reads of the other buffer are done; then everybody's
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (s + 1 < steps) {
-                const uint32_t to = base + static_cast<uint32_t>((s + 1 & 1) * kStage);
-                ha.load(to, wave, lane);
-                hb.load(to + kA, wave, lane, other);
+        int next = 0;       // the step that is loaded next on, and its place
+        uint32_t to = base;
+        auto load = [&] {
+            if (TWO && next == turn_at) {
+                ha.turn(a2, k1 - whole);
+                hb.turn(b2, k1 - whole);
             }
-            const char *la = lds + (s & 1) * kStage, *lb = la + kA;
+            ha.load(to, wave, lane);
+            hb.load(to + kA, wave, lane, other);
+            ++next;
+            to = to + kStage == base + kLds ? base : to + kStage;
+        };
+        f4 low[P == 3 ? FM : 1][P == 3 ? FN : 1] = {};
+        for (int s = 0; s < STAGES - 1 && s < steps; ++s) load();
+        int stage = 0;
+        for (int s = 0; s < steps; ++s) {
+            // this wavefront's loads of the step have landed (of STAGES - 2 further steps they may be on their way) and its
+            // reads of the step before are done; then everybody's
+            if (STAGES > 2 && s + STAGES - 1 <= steps)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kStepLoads) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (next < steps) load();
+            const char *la = lds + stage, *lb = la + kA;
+            stage = stage + kStage == kLds ? 0 : stage + kStage;
 #pragma unroll
             for (int ks = 0; ks < BK / 32; ++ks) {
                 Frag<E> fb[P][FN];
@@ -207,21 +283,96 @@ struct Tile {
 #pragma unroll
                         for (int q = P - 1 - p; q >= 0; --q)
 #pragma unroll
-                            for (int j = 0; j < FN; ++j) acc[i][j] = mfma32(fb[q][j], fa[p], acc[i][j]);
+                            for (int j = 0; j < FN; ++j) {
+                                // three parts: what lies below the first parts' product is summed apart, so that the large
+                                // sum is rounded once for each 32 k and not six times
+                                f4 &to = P == 3 && p + q > 0 ? low[P == 3 ? i : 0][P == 3 ? j : 0] : acc[i][j];
+                                to = mfma32(fb[q][j], fa[p], to);
+                            }
                 }
             }
+            // reads of LDS two rows of fragments ahead of the products that need them
+            constexpr int kReadA = P * (ALONG_A ? 1 : 2), kReadB = P * FN * (ALONG_B ? 1 : 2), kGroups = FM * (BK / 32);
+            constexpr int kFirst = kReadB + 2 * kReadA, kRest = (BK / 32) * (kReadB + FM * kReadA) - kFirst;
+            constexpr int kEach = (kRest + kGroups - 3) / (kGroups - 2);
+            __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x008, FN * P * (P + 1) / 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+            }
+        }
+        if constexpr (P == 3) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] += low[i][j];
         }
     }
 
-    // f(row, column, values, values 16 columns on) for each pair of acc's fragments, rows and columns counted in the tile.
-    template <class F>
-    static __device__ __forceinline__ void each(const f4 (&acc)[FM][FN], F f) {
-        const int lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave;
+    // ---- what becomes of acc: it goes through LDS, a wavefront's rows (in kPhases parts) in a region of its own, so that
+    // the code behind it is a loop over whole 128-byte lines, not acc's fragments written out one by one.
+    static constexpr int kCols = FN * 16, kPhases = FM * FN * 1024 * kWaves <= kLds ? 1 : 2, kRows = FM * 16 / kPhases;
+    static constexpr int kRegion = kRows * kCols * 4;
+    static_assert(kRegion * kWaves <= kLds && kCols % 64 == 0, "regions fit");
+
+    // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks.
+    static __device__ __forceinline__ f4 &cell(char *region, int row, int chunk) {
+        return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + (chunk & ~15) * 16 +
+                                       ((chunk & 15) ^ (row & 15) ^ (chunk >> 4) * 4) * 16);
+    }
+    static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], int phase, char *region) {
+        const int lane = lane_id();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
+            if (i / (FM / kPhases) == phase)
 #pragma unroll
-            for (int j = 0; j < FN; j += 2)
-                f((wave / WN * FM + i) * 16 + lane % 16, (wave % WN * FN + j) * 16 + lane / 16 * 4, acc[i][j], acc[i][j + 1]);
+                for (int j = 0; j < FN; ++j) cell(region, i % (FM / kPhases) * 16 + lane % 16, j * 4 + lane / 16) = acc[i][j];
+    }
+    static __device__ __forceinline__ void get8(char *region, int row, int chunk, float (&v)[8]) {
+        const f4 x = cell(region, row, chunk), y = cell(region, row, chunk + 1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = x[e];
+            v[4 + e] = y[e];
+        }
+    }
+    // f(row, column, values of 8 columns) for a region.
+    template <class F>
+    static __device__ __forceinline__ void rows8(char *region, Lanes lanes, F f) {
+        constexpr int kPer = kCols / 8;
+#pragma unroll 2
+        for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
+            float v[8];
+            get8(region, c / kPer, c % kPer * 2, v);
+            f(c / kPer, c % kPer * 8, v);
+        }
+    }
+    // PAIR: f(row, column of an array, the first's 8 columns, the second's).
+    template <class F>
+    static __device__ __forceinline__ void pairs8(char *region, Lanes lanes, F f) {
+        constexpr int kPer = kCols / 16;
+#pragma unroll 2
+        for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
+            const int row = c / kPer, col = c % kPer * 8, chunk = col / 16 * 8 + col % 16 / 4;
+            float v[8], w[8];
+            get8(region, row, chunk, v);
+            get8(region, row, chunk + 4, w);
+            f(row, col, v, w);
+        }
+    }
+    // f(row, column, values of 8 rows).
+    template <class F>
+    static __device__ __forceinline__ void columns8(char *region, Lanes lanes, F f) {
+        constexpr int kPer = kRows / 8;
+#pragma unroll 2
+        for (int c = lanes.at; c < kCols * kPer; c += lanes.step) {
+            const int row = c % kPer * 8, col = c / kPer;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = cell(region, row + e, col / 4)[col % 4];
+            f(row, col, v);
+        }
     }
 };
 
@@ -241,14 +392,20 @@ __device__ __forceinline__ void tile_at(int64_t id, int64_t gm, int64_t gn, int6
 
 // ------------------------------------------------------------------ kernels over a job's tiles
 // A job says which tiles it has, multiplies one and puts its elements where they belong:
-//   int64_t tiles; int32_t splits; f4 *part          tiles, and the parts that each one's k is cut into
+//   int64_t tiles; int32_t splits; float *part       tiles, and the parts that each one's k is cut into
 //   Place at<T>(tile)                                 where the tile lies
 //   multiply<T>(place, split, lds, acc)               its product over one part of k
-//   put(place, row, column, f4, f4)                   four elements of a row, and the four 16 columns (or, of a PAIR, one
-//                                                     operand) on; row and column count in the tile
+//   take<T>(place, row, column, region, lanes)        what a region holds, from that row and column of the tile on
 // Parts of k are summed in their order by k_join, so that results do not depend on the order in which they end.
 inline __host__ __device__ int64_t split_steps(int64_t k, int bk, int32_t splits) {
     return ceil_div(ceil_div(k, bk), splits) * bk;
+}
+
+template <class T, class J>
+__device__ __forceinline__ void take_region(const J &job, const decltype(job.template at<T>(0)) &place, int wave, int phase,
+                                            char *region, Lanes lanes) {
+    const int row = wave / T::WN * T::FM * 16 + phase * T::kRows, col = wave % T::WN * T::kCols;
+    job.template take<T>(place, row, col, region, lanes);
 }
 
 template <class T, class J>
@@ -260,39 +417,56 @@ __global__ __launch_bounds__(T::kThreads, T::kPerSimd) void k_tiles(const J job)
     const auto place = job.template at<T>(tile);
     f4 acc[T::FM][T::FN] = {};
     job.template multiply<T>(place, split, lds, acc);
-    if (job.splits == 1) {
-        T::each(acc, [&](int row, int col, f4 v0, f4 v1) { job.put(place, row, col, v0, v1); });
-        return;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody's reads of the last step
+    const int wave = static_cast<int>(threadIdx.x) / kWave;
+    char *region = lds + wave * T::kRegion;
+#pragma unroll
+    for (int phase = 0; phase < T::kPhases; ++phase) {
+        if (phase > 0) lds_order();
+        T::fill(acc, phase, region);
+        lds_order();
+        if (job.splits == 1) {
+            take_region<T>(job, place, wave, phase, region, Lanes{lane_id(), kWave});
+            continue;
+        }
+        float *to = job.part + ((id * T::kWaves + wave) * T::kPhases + phase) * (T::kRegion / 4);
+        for (int c = lane_id(); c < T::kRegion / 16; c += kWave)
+            reinterpret_cast<f4 *>(to)[c] = T::cell(region, c / (T::kCols / 4), c % (T::kCols / 4));
     }
-    f4 *to = job.part + (static_cast<int64_t>(split) * job.tiles + tile) * (T::FM * T::FN * T::kThreads) + threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < T::FN; ++j) to[(i * T::FN + j) * T::kThreads] = acc[i][j];
 }
 
+constexpr int kJoinThreads = 256;   // of a region
+
 template <class T, class J>
-__global__ __launch_bounds__(T::kThreads) void k_join(const J job) {
-    const int64_t tile = blockIdx.x / T::FM;
-    const int i = static_cast<int>(blockIdx.x % T::FM), lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave;
+__global__ __launch_bounds__(kJoinThreads) void k_join(const J job) {
+    __shared__ __attribute__((aligned(1024))) char region[T::kRegion];
+    const int64_t size = T::kRegion / 16, per = T::kWaves * T::kPhases, tile = blockIdx.x / per;
     const auto place = job.template at<T>(tile);
-    const int64_t size = T::FM * T::FN * T::kThreads;
-    const f4 *from = job.part + tile * size + i * T::FN * T::kThreads + threadIdx.x;
-    f4 v[T::FN] = {};
-    for (int s = 0; s < job.splits; ++s, from += job.tiles * size)
+    const f4 *from = reinterpret_cast<const f4 *>(job.part) + blockIdx.x * size;
+    const int64_t next = job.tiles * per * size;
+    constexpr int kMine = T::kRegion / 16 / kJoinThreads;
+    f4 v[kMine] = {};
+#pragma unroll 2
+    for (int s = 0; s < job.splits; ++s)
 #pragma unroll
-        for (int j = 0; j < T::FN; ++j) v[j] += from[j * T::kThreads];
+        for (int i = 0; i < kMine; ++i) v[i] += from[s * next + i * kJoinThreads + threadIdx.x];
 #pragma unroll
-    for (int j = 0; j < T::FN; j += 2)
-        job.put(place, (wave / T::WN * T::FM + i) * 16 + lane % 16, (wave % T::WN * T::FN + j) * 16 + lane / 16 * 4, v[j], v[j + 1]);
+    for (int i = 0; i < kMine; ++i) {
+        const int c = i * kJoinThreads + static_cast<int>(threadIdx.x);
+        T::cell(region, c / (T::kCols / 4), c % (T::kCols / 4)) = v[i];
+    }
+    __syncthreads();
+    const int at = static_cast<int>(blockIdx.x % per);
+    take_region<T>(job, place, at / T::kPhases, at % T::kPhases, region, Lanes{static_cast<int>(threadIdx.x), kJoinThreads});
 }
 
 // How a product's tiles are taken: large or small ones, and the parts of k.
+enum { kLarge, kSmall, kDeep };
 struct Cut {
-    bool large;
+    int32_t kind;
     int32_t splits;
     int64_t tiles;
-    size_t bytes;    // of the parts' sums
+    size_t floats;   // of the parts' sums
 };
 
 // A launch numbers its threads in 32 bits.
@@ -303,7 +477,7 @@ int launch_tiles(J &job, hipStream_t s) {
     k_tiles<T, J><<<static_cast<unsigned>(job.tiles * job.splits), T::kThreads, 0, s>>>(job);
     W2V_LAUNCH_CHECK("k_tiles");
     if (job.splits > 1) {
-        k_join<T, J><<<static_cast<unsigned>(job.tiles * T::FM), T::kThreads, 0, s>>>(job);
+        k_join<T, J><<<static_cast<unsigned>(job.tiles * T::kWaves * T::kPhases), kJoinThreads, 0, s>>>(job);
         W2V_LAUNCH_CHECK("k_join");
     }
     return W2V_OK;
@@ -312,27 +486,30 @@ int launch_tiles(J &job, hipStream_t s) {
 // The cut with the least time by this model: each CU takes its share of the tiles one after the other, at the matrix
 // cores' measured rate (4.7 TFLOP/s a CU; 15 % less with small tiles), with two steps until the first product; sums of
 // parts go through memory at 4 TB/s, and joining them is another launch. tiles_large, tiles_small: of all products of a
-// launch that have k in common. S: a pair of tiles, Large and Small.
+// launch that have k in common. S: its tiles, Large, Small, and Deep, which are small ones with more
+// steps on their way where a CU has but one.
 template <class S>
 Cut choose_cut(int64_t tiles_large, int64_t tiles_small, int64_t k) {
     using L = typename S::Large;
     using M = typename S::Small;
-    Cut best{true, 1, tiles_large, 0};
+    Cut best{kLarge, 1, tiles_large, 0};
     double least = 1e300;
-    auto weigh = [&](bool large, int64_t tiles, int64_t area, int bk, int products, double slow) {
+    const int64_t cus = device_cu_count();
+    auto weigh = [&](int32_t kind, int64_t tiles, int64_t area, int bk, int products, double slow) {
         const int64_t steps = ceil_div(k, bk);
         const double step_us = 2.0 * area * bk * products / 4.7e6 * slow;
         for (int32_t n = 1; n <= 64 && (n == 1 || n * 2 <= steps); ++n) {
-            const double turns = static_cast<double>(ceil_div(tiles * n, device_cu_count()));
+            const double turns = static_cast<double>(ceil_div(tiles * n, cus));
             const double join = n == 1 ? 0.0 : 5.0 + 8.0 * tiles * n * area / 4e6;
             const double us = turns * (ceil_div(steps, n) + 2) * step_us + join;
             if (us >= least * 0.999) continue;
             least = us;
-            best = Cut{large, n, tiles, n == 1 ? 0 : static_cast<size_t>(tiles * n * area) * sizeof(float)};
+            best = Cut{kind, n, tiles, n == 1 ? 0 : static_cast<size_t>(tiles * n * area)};
         }
     };
-    weigh(true, tiles_large, L::BM * L::BN, L::BK, L::P * (L::P + 1) / 2, 1.0);
-    weigh(false, tiles_small, M::BM * M::BN, M::BK, M::P * (M::P + 1) / 2, 1.15);
+    weigh(kLarge, tiles_large, L::BM * L::BN, L::BK, L::P * (L::P + 1) / 2, 1.0);
+    weigh(kSmall, tiles_small, M::BM * M::BN, M::BK, M::P * (M::P + 1) / 2, 1.15);
+    if (best.kind == kSmall && best.tiles * best.splits <= cus) best.kind = kDeep;
     return best;
 }
 
@@ -350,7 +527,8 @@ template <class S, class J>
 int launch_cut(const Cut &c, J &job, hipStream_t s) {
     job.splits = c.splits;
     job.tiles = c.tiles;
-    return c.large ? launch_tiles<typename S::Large, J>(job, s) : launch_tiles<typename S::Small, J>(job, s);
+    if (c.kind == kLarge) return launch_tiles<typename S::Large, J>(job, s);
+    return c.kind == kSmall ? launch_tiles<typename S::Small, J>(job, s) : launch_tiles<typename S::Deep, J>(job, s);
 }
 
 }  // namespace w2v
