@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "w2v_ops.h"
 #include "w2v_product.h"
@@ -277,9 +278,169 @@ int64_t tile_n(const Cut &c) {
     return c.kind == kLarge ? S::Large::BN : S::Small::BN;
 }
 
+// ------------------------------------------------------------------ few rows
+// Where there are few rows every weight is read for them, and the weights' bytes are the time. A workgroup takes 16 columns
+// of the result, its wavefronts take turns along k, 128 bytes of each of the 16 weight rows at a time straight from memory
+// into the matrix cores' registers (rows need no alignment but their elements'); the wavefronts' sums are joined in LDS in
+// their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts.
+constexpr int kFewWaves = 8;   // wavefronts a workgroup
+
+// fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles 0.46), 16-bit ones up to 16 (0.063 and 0.067)
+// and small products up to 64 (64 rows, 300 x 800: 15 us and 28; 48 rows, 1,024 x 2,816: 30 and 30; 32 rows, 4,096 x 10,240:
+// 91 and 67): what they read of x again and again grows with the rows.
+template <class T>
+bool few_rows(const FfnArgs &a) {
+    return a.rows <= 16 || (a.rows <= 64 && (sizeof(T) == 4 || a.rows * a.dim * a.hidden <= int64_t(1) << 27));
+}
+
+struct FewArgs {
+    const void *x, *w, *w2;              // n rows of X, cols rows of T (gate's and up's, or w alone)
+    int64_t x_stride, w_stride, w2_stride;
+    int32_t n, cols, k, act;
+    void *out, *gate, *up;               // float (PAIR) or T, and T
+    int64_t out_stride, gate_stride, up_stride;
+};
+
+// Products of 16 weight rows' chunks (V elements of each lane's row) with 16 rows' of x.
+template <class T, class X, int V>
+__device__ __forceinline__ f4 few_product(const Pack<T, V> &w, const Pack<X, V> &x, f4 acc) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], acc, 0, 0, 0);
+    } else {
+        Frag<T> a, hi, lo;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            a[e] = w.v[e];
+            hi[e] = static_cast<T>(x.v[e]);
+            if constexpr (sizeof(X) == 4) lo[e] = static_cast<T>(x.v[e] - static_cast<float>(hi[e]));
+        }
+        if constexpr (sizeof(X) == 4) acc = mfma32(a, lo, acc);
+        acc = mfma32(a, hi, acc);
+    }
+    return acc;
+}
+
+template <class T, class X, int NT, bool PAIR>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_few(const FewArgs a) {
+    constexpr int V = 16 / sizeof(T), kGroup = 8 * V, kArrays = PAIR ? 2 : 1;
+    const int lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave, c0 = static_cast<int>(blockIdx.x) * 16;
+    const int64_t row = min(c0 + lane % 16, a.cols - 1);
+    const T *w[kArrays];
+    w[0] = static_cast<const T *>(a.w) + row * a.w_stride;
+    if constexpr (PAIR) w[1] = static_cast<const T *>(a.w2) + row * a.w2_stride;
+    const X *x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t] = static_cast<const X *>(a.x) + min(t * 16 + lane % 16, a.n - 1) * a.x_stride;
+    f4 acc[NT][kArrays] = {};
+    const int full = a.k / kGroup, lead = lane / 16 * V;
+    // a lane's chunks of a group: number lane / 16 and 4 further on
+    auto group = [&](int g, auto whole) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int at = g * kGroup + c * 4 * V + lead;
+            const int valid = decltype(whole)::value ? V : a.k - at;
+            Pack<T, V> pw[kArrays];
+#pragma unroll
+            for (int i = 0; i < kArrays; ++i)
+                pw[i] = decltype(whole)::value ? *reinterpret_cast<const Pack<T, V> *>(w[i] + at) : raw_cols<T, V>(w[i] + at, 0, valid);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const Pack<X, V> px = decltype(whole)::value ? *reinterpret_cast<const Pack<X, V> *>(x[t] + at)
+                                                             : raw_cols<X, V>(x[t] + at, 0, valid);
+#pragma unroll
+                for (int i = 0; i < kArrays; ++i) acc[t][i] = few_product<T, X, V>(pw[i], px, acc[t][i]);
+            }
+        }
+    };
+    for (int g = wave; g < full; g += kFewWaves) group(g, std::true_type{});
+    if (a.k % kGroup != 0 && full % kFewWaves == wave) group(full, std::false_type{});
+    __shared__ f4 part[kFewWaves][NT][kArrays][kWave];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < kArrays; ++i) part[wave][t][i][lane] = acc[t][i];
+    __syncthreads();
+    if (wave >= NT) return;
+    f4 v[kArrays] = {};
+#pragma unroll
+    for (int q = 0; q < kFewWaves; ++q)
+#pragma unroll
+        for (int i = 0; i < kArrays; ++i) v[i] += part[q][wave][i][lane];
+    // the lane has four columns of one row
+    const int64_t r = wave * 16 + lane % 16;
+    const int c = c0 + lane / 16 * 4;
+    if (r >= a.n) return;
+    auto store = [&](auto *to, int64_t stride, const f4 &f) {
+        const float e[4] = {f[0], f[1], f[2], f[3]};
+        store_cols<std::remove_pointer_t<decltype(to)>, 4>(to + r * stride, c, a.cols, e);
+    };
+    if constexpr (PAIR) {
+        if (a.gate) store(static_cast<T *>(a.gate), a.gate_stride, v[0]);
+        if (a.up) store(static_cast<T *>(a.up), a.up_stride, v[1]);
+        f4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = act_value(a.act, v[0][e]) * v[1][e];
+        store(static_cast<float *>(a.out), a.out_stride, h);
+    } else {
+        store(static_cast<T *>(a.out), a.out_stride, v[0]);
+    }
+}
+
+template <class T, class X, bool PAIR>
+int launch_few(const FewArgs &a, hipStream_t s) {
+    const auto grid = static_cast<unsigned>(ceil_div(a.cols, 16));
+    const int threads = kFewWaves * kWave;
+    if (a.n <= 16)
+        k_few<T, X, 1, PAIR><<<grid, threads, 0, s>>>(a);
+    else if (a.n <= 32)
+        k_few<T, X, 2, PAIR><<<grid, threads, 0, s>>>(a);
+    else
+        k_few<T, X, 4, PAIR><<<grid, threads, 0, s>>>(a);
+    W2V_LAUNCH_CHECK("k_few");
+    return W2V_OK;
+}
+
+template <class T>
+int forward_few(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
+    const int64_t hs = ceil_div(a.hidden, 64) * 64;
+    float *h = c.take<float>(static_cast<size_t>(a.rows * hs));
+    if (!launch) return W2V_OK;
+    FewArgs u{};
+    u.x = a.x.p;
+    u.w = a.w_gate.p;
+    u.w2 = a.w_up.p;
+    u.x_stride = a.x.stride;
+    u.w_stride = a.w_gate.stride;
+    u.w2_stride = a.w_up.stride;
+    u.n = static_cast<int32_t>(a.rows);
+    u.cols = a.hidden;
+    u.k = a.dim;
+    u.act = a.act;
+    u.out = h;
+    u.out_stride = hs;
+    u.gate = const_cast<void *>(a.gate.p);
+    u.up = const_cast<void *>(a.up.p);
+    u.gate_stride = a.gate.stride;
+    u.up_stride = a.up.stride;
+    if (int rc = launch_few<T, T, true>(u, s)) return rc;
+    FewArgs d{};
+    d.x = h;
+    d.w = a.w_down.p;
+    d.x_stride = hs;
+    d.w_stride = a.w_down.stride;
+    d.n = u.n;
+    d.cols = a.dim;
+    d.k = a.hidden;
+    d.out = const_cast<void *>(a.y.p);
+    d.out_stride = a.y.stride;
+    return launch_few<T, float, false>(d, s);
+}
+
 // One plan of a pass: where its arrays lie, without a workspace only how many bytes they are.
 template <class T>
 int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
+    if (few_rows<T>(a)) return forward_few<T>(a, c, launch, s);
     using K = Kind<T>;
     using E = typename K::E;
     using Up = typename K::template Tiles<true, true, true>;
