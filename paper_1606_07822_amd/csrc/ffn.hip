@@ -14,20 +14,26 @@ namespace w2v {
 namespace {
 
 // ------------------------------------------------------------------ activations
+// 1 / (1 + exp(-g)): exp's argument is rounded once (|g| 2^-24 of its value), the power and the reciprocal are the
+// hardware's, 1 ulp each.
+__device__ __forceinline__ float sigmoid(float g) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
+}
+__device__ __forceinline__ float normal_share(float g) { return 0.5f + 0.5f * erff(0.70710678f * g); }
+
 __device__ __forceinline__ float act_value(int act, float g) {
-    if (act == W2V_SILU) return g / (1.0f + expf(-g));
-    return 0.5f * g * erfcf(-0.70710678f * g);
+    return g * (act == W2V_SILU ? sigmoid(g) : normal_share(g));
 }
 
 __device__ __forceinline__ void act_both(int act, float g, float &value, float &slope) {
     if (act == W2V_SILU) {
-        const float p = 1.0f / (1.0f + expf(-g));
+        const float p = sigmoid(g);
         value = g * p;
-        slope = p * (1.0f + g * (1.0f - p));
+        slope = p + value * (1.0f - p);
     } else {
-        const float p = 0.5f * erfcf(-0.70710678f * g);
+        const float p = normal_share(g);
         value = g * p;
-        slope = p + g * 0.39894228f * expf(-0.5f * g * g);
+        slope = p + g * 0.39894228f * __builtin_amdgcn_exp2f(-0.72134752f * g * g);
     }
 }
 
@@ -200,12 +206,14 @@ struct Tiles1 {
     using Large = Tile<E, 1, 256, 256, PAIR ? 4 : 2, PAIR ? 2 : 4, 64, A, B, PAIR, TWO>;
     using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR, TWO>;
     using Deep = Tile<E, 1, 128, 128, 2, 2, 64, A, B, PAIR, TWO, 5>;
+    using Tiny = Tile<E, 1, 64, 64, 2, 2, 64, A, B, PAIR, TWO, 4>;
 };
 template <class E, bool A, bool B, bool PAIR, bool TWO>
 struct Tiles3 {
     using Large = Tile<E, 3, 256, 128, 4, 2, 32, A, B, PAIR, TWO>;
-    using Small = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR, TWO>;
+    using Small = Tile<E, 3, 128, 64, 2, 2, 32, A, B, PAIR, TWO>;
     using Deep = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR, TWO, 3>;
+    using Tiny = Tile<E, 3, 64, 64, 2, 2, 32, A, B, PAIR, TWO, 3>;
 };
 template <class T>
 struct Kind {   // 16-bit rows are multiplied as they are
@@ -267,15 +275,6 @@ int launch_parts(const Packing &p, hipStream_t s) {
     k_parts<T, typename Kind<T>::E, Kind<T>::P><<<grid, 256, 0, s>>>(p.all);
     W2V_LAUNCH_CHECK("k_parts");
     return W2V_OK;
-}
-
-template <class S>
-int64_t tile_m(const Cut &c) {
-    return c.kind == kLarge ? S::Large::BM : S::Small::BM;
-}
-template <class S>
-int64_t tile_n(const Cut &c) {
-    return c.kind == kLarge ? S::Large::BN : S::Small::BN;
 }
 
 // ------------------------------------------------------------------ few rows
@@ -505,11 +504,11 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
         h[i] = c.take<E>(static_cast<size_t>(K::P * n * hs));
         hid[i] = Side{reinterpret_cast<char *>(h[i]), n * hs * 2, hs * 2};
     }
-    using L = typename Weights::Large;
-    using S = typename Weights::Small;
     const Cut back = choose_cut_of<Hidden>(n, f, d), in = choose_cut_of<Input>(n, d, 2 * f);
-    const Cut weights = choose_cut<Weights>(2 * count_tiles<L>(f, d) + count_tiles<L>(d, f),
-                                            2 * count_tiles<S>(f, d) + count_tiles<S>(d, f), n);
+    const Cut weights = choose_cut<Weights>(n, [&](auto tile) {
+        using Q = typename decltype(tile)::type;
+        return 2 * count_tiles<Q>(f, d) + count_tiles<Q>(d, f);
+    });
     float *part = c.take<float>(std::max({back.floats, in.floats, weights.floats}));
     if (!launch) return W2V_OK;
     if (back.tiles > kMaxTiles || in.tiles > kMaxTiles || weights.tiles > kMaxTiles)

@@ -247,12 +247,14 @@ struct Tiles<1, A, B> {
     using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B>;
     using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B>;
     using Deep = Tile<E, 1, 128, 128, 2, 2, 64, A, B, false, false, 5>;
+    using Tiny = Tile<E, 1, 64, 64, 2, 2, 64, A, B, false, false, 4>;
 };
 template <bool A, bool B>
 struct Tiles<2, A, B> {
     using Large = Tile<E, 2, 256, 256, 2, 4, 32, A, B>;
     using Small = Tile<E, 2, 128, 128, 2, 2, 32, A, B>;
     using Deep = Tile<E, 2, 128, 128, 2, 2, 32, A, B, false, false, 5>;
+    using Tiny = Tile<E, 2, 64, 64, 2, 2, 32, A, B, false, false, 4>;
 };
 
 int64_t triangle(int64_t g) { return g * (g + 1) / 2; }
@@ -269,8 +271,6 @@ struct Arrays {
 
 template <int P>
 Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
-    using L = typename Tiles<P, true, true>::Large;
-    using S = typename Tiles<P, true, true>::Small;
     Arrays w{};
     w.r = std::min(rows, cols);
     w.c = std::max(rows, cols);
@@ -278,10 +278,11 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.a_stride = ceil_div(w.r, 64) * 64;
     w.x_plane = count * rows * w.x_stride;
     w.a_plane = count * w.r * w.a_stride;
-    const int64_t tl = count * triangle(ceil_div(w.r, L::BM)), ts = count * triangle(ceil_div(w.r, S::BM));
-    w.gram = choose_cut<Tiles<P, true, true>>(tl, ts, w.c);
-    w.poly = choose_cut<Tiles<P, true, true>>(tl, ts, w.r);
-    w.step = choose_cut<Tiles<P, true, true>>(count * count_tiles<L>(rows, cols), count * count_tiles<S>(rows, cols), w.r);
+    const auto square = [&](auto tile) { return count * triangle(ceil_div(w.r, decltype(tile)::type::BM)); };
+    w.gram = choose_cut<Tiles<P, true, true>>(w.c, square);
+    w.poly = choose_cut<Tiles<P, true, true>>(w.r, square);
+    w.step = choose_cut<Tiles<P, true, true>>(
+        w.r, [&](auto tile) { return count * count_tiles<typename decltype(tile)::type>(rows, cols); });
     Carve k(workspace);
     w.part = k.take<double>(static_cast<size_t>(count * kParts));
     for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
@@ -297,7 +298,6 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
     using Gram = Tiles<P, WIDE, WIDE>;
     using Poly = Tiles<P, true, true>;
     using Step = Tiles<P, true, !WIDE>;
-    const int64_t bm = Poly::Large::BM, sm = Poly::Small::BM;
     for (int32_t i = 0; i < steps; ++i) {
         const E *from = w.x[i % 2];
         const Side x{reinterpret_cast<const char *>(from), w.x_plane * 2, w.x_stride * 2};
@@ -306,7 +306,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.step = b.rows * w.x_stride * 2;
         q.r = w.r;
         q.k = w.c;
-        q.g = ceil_div(w.r, w.gram.kind == kLarge ? bm : sm);
+        q.g = ceil_div(w.r, tile_m<Gram>(w.gram));
         q.part = w.sums;
         q.out = w.a;
         q.stride = w.a_stride;
@@ -315,7 +315,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.x = Side{reinterpret_cast<const char *>(w.a), w.a_plane * 2, w.a_stride * 2};
         q.step = w.r * w.a_stride * 2;
         q.k = w.r;
-        q.g = ceil_div(w.r, w.poly.kind == kLarge ? bm : sm);
+        q.g = ceil_div(w.r, tile_m<Poly>(w.poly));
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;
@@ -327,8 +327,8 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
             job.a_step = WIDE ? w.r * w.a_stride * 2 : b.rows * w.x_stride * 2;
             job.b_step = WIDE ? b.rows * w.x_stride * 2 : w.r * w.a_stride * 2;
             job.k = w.r;
-            job.gm = ceil_div(b.rows, w.step.kind == kLarge ? bm : sm);
-            job.gn = ceil_div(b.cols, w.step.kind == kLarge ? bm : sm);
+            job.gm = ceil_div(b.rows, tile_m<Step>(w.step));
+            job.gn = ceil_div(b.cols, tile_n<Step>(w.step));
             job.part = w.sums;
             job.out = w.x[1 - i % 2];
             job.stride = w.x_stride;

@@ -125,6 +125,7 @@ struct Tile {
         // rows 0..3 and 8..11 of a group of 16: pairs of chunks change places.
         static __device__ __forceinline__ int place(int row, int chunk) {
             if constexpr (ALONG) return chunk ^ (row / (256 / kRow)) % kChunks;
+            if constexpr (kRow == 128) return chunk ^ ((row >> 1 & 1) | (row >> 2 & 2)) << 1;
             return chunk ^ ((row & 3) | (row >> 1 & 4)) << 1;
         }
 
@@ -294,7 +295,7 @@ struct Tile {
             // reads of LDS two rows of fragments ahead of the products that need them
             constexpr int kReadA = P * (ALONG_A ? 1 : 2), kReadB = P * FN * (ALONG_B ? 1 : 2), kGroups = FM * (BK / 32);
             constexpr int kFirst = kReadB + 2 * kReadA, kRest = (BK / 32) * (kReadB + FM * kReadA) - kFirst;
-            constexpr int kEach = (kRest + kGroups - 3) / (kGroups - 2);
+            constexpr int kEach = kGroups > 2 ? (kRest + kGroups - 3) / (kGroups - 2) : 1;
             __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -314,12 +315,12 @@ struct Tile {
     // the code behind it is a loop over whole 128-byte lines, not acc's fragments written out one by one.
     static constexpr int kCols = FN * 16, kPhases = FM * FN * 1024 * kWaves <= kLds ? 1 : 2, kRows = FM * 16 / kPhases;
     static constexpr int kRegion = kRows * kCols * 4;
-    static_assert(kRegion * kWaves <= kLds && kCols % 64 == 0, "regions fit");
+    static_assert(kRegion * kWaves <= kLds && (kCols == 32 || kCols % 64 == 0), "regions fit");
 
     // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks.
     static __device__ __forceinline__ f4 &cell(char *region, int row, int chunk) {
-        return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + (chunk & ~15) * 16 +
-                                       ((chunk & 15) ^ (row & 15) ^ (chunk >> 4) * 4) * 16);
+        const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ (row & 15) ^ (chunk >> 4) * 4);
+        return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + to * 16);
     }
     static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], int phase, char *region) {
         const int lane = lane_id();
@@ -461,7 +462,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_join(const J job) {
 }
 
 // How a product's tiles are taken: large or small ones, and the parts of k.
-enum { kLarge, kSmall, kDeep };
+template <class T>
+struct Which {
+    using type = T;
+};
+enum { kLarge, kSmall, kDeep, kTiny };
 struct Cut {
     int32_t kind;
     int32_t splits;
@@ -484,20 +489,19 @@ int launch_tiles(J &job, hipStream_t s) {
 }
 
 // The cut with the least time by this model: each CU takes its share of the tiles one after the other, at the matrix
-// cores' measured rate (4.7 TFLOP/s a CU; 15 % less with small tiles), with two steps until the first product; sums of
-// parts go through memory at 4 TB/s, and joining them is another launch. tiles_large, tiles_small: of all products of a
-// launch that have k in common. S: its tiles, Large, Small, and Deep, which are small ones with more
-// steps on their way where a CU has but one.
-template <class S>
-Cut choose_cut(int64_t tiles_large, int64_t tiles_small, int64_t k) {
-    using L = typename S::Large;
-    using M = typename S::Small;
-    Cut best{kLarge, 1, tiles_large, 0};
+// cores' measured rate (4.7 TFLOP/s a CU, less with smaller tiles, which read LDS more often) but a step in no less than
+// 0.2 us, with two steps until the first product; sums of parts go through memory at 4 TB/s, and joining them is another
+// launch. count(tile): the tiles of all products of a launch that have k in common. S: the tiles, Large, Small, Tiny, and
+// Deep, which are small ones with more steps on their way where a CU has but one.
+template <class S, class F>
+Cut choose_cut(int64_t k, F count) {
+    Cut best{kLarge, 1, 0, 0};
     double least = 1e300;
     const int64_t cus = device_cu_count();
-    auto weigh = [&](int32_t kind, int64_t tiles, int64_t area, int bk, int products, double slow) {
-        const int64_t steps = ceil_div(k, bk);
-        const double step_us = 2.0 * area * bk * products / 4.7e6 * slow;
+    auto weigh = [&](int32_t kind, auto tile, double slow) {
+        using T = typename decltype(tile)::type;
+        const int64_t tiles = count(tile), steps = ceil_div(k, T::BK), area = T::BM * T::BN;
+        const double step_us = std::max(0.2, area * T::BK * (T::P * (T::P + 1)) / 4.7e6 * slow);
         for (int32_t n = 1; n <= 64 && (n == 1 || n * 2 <= steps); ++n) {
             const double turns = static_cast<double>(ceil_div(tiles * n, cus));
             const double join = n == 1 ? 0.0 : 5.0 + 8.0 * tiles * n * area / 4e6;
@@ -507,9 +511,11 @@ Cut choose_cut(int64_t tiles_large, int64_t tiles_small, int64_t k) {
             best = Cut{kind, n, tiles, n == 1 ? 0 : static_cast<size_t>(tiles * n * area)};
         }
     };
-    weigh(kLarge, tiles_large, L::BM * L::BN, L::BK, L::P * (L::P + 1) / 2, 1.0);
-    weigh(kSmall, tiles_small, M::BM * M::BN, M::BK, M::P * (M::P + 1) / 2, 1.15);
-    if (best.kind == kSmall && best.tiles * best.splits <= cus) best.kind = kDeep;
+    constexpr int P = S::Large::P;
+    weigh(kLarge, Which<typename S::Large>{}, 1.0);
+    weigh(kSmall, Which<typename S::Small>{}, 1.15);
+    weigh(kDeep, Which<typename S::Deep>{}, 1.15);
+    weigh(kTiny, Which<typename S::Tiny>{}, P == 1 ? 2.2 : P == 2 ? 1.6 : 1.3);
     return best;
 }
 
@@ -520,15 +526,29 @@ int64_t count_tiles(int64_t m, int64_t n) {
 }
 template <class S>
 Cut choose_cut_of(int64_t m, int64_t n, int64_t k) {
-    return choose_cut<S>(count_tiles<typename S::Large>(m, n), count_tiles<typename S::Small>(m, n), k);
+    return choose_cut<S>(k, [&](auto tile) { return count_tiles<typename decltype(tile)::type>(m, n); });
+}
+
+// A cut's tile sizes.
+template <class S>
+int64_t tile_m(const Cut &c) {
+    return c.kind == kLarge ? S::Large::BM : c.kind == kSmall ? S::Small::BM : c.kind == kDeep ? S::Deep::BM : S::Tiny::BM;
+}
+template <class S>
+int64_t tile_n(const Cut &c) {
+    return c.kind == kLarge ? S::Large::BN : c.kind == kSmall ? S::Small::BN : c.kind == kDeep ? S::Deep::BN : S::Tiny::BN;
 }
 
 template <class S, class J>
 int launch_cut(const Cut &c, J &job, hipStream_t s) {
     job.splits = c.splits;
     job.tiles = c.tiles;
-    if (c.kind == kLarge) return launch_tiles<typename S::Large, J>(job, s);
-    return c.kind == kSmall ? launch_tiles<typename S::Small, J>(job, s) : launch_tiles<typename S::Deep, J>(job, s);
+    switch (c.kind) {
+        case kLarge: return launch_tiles<typename S::Large, J>(job, s);
+        case kSmall: return launch_tiles<typename S::Small, J>(job, s);
+        case kDeep: return launch_tiles<typename S::Deep, J>(job, s);
+        default: return launch_tiles<typename S::Tiny, J>(job, s);
+    }
 }
 
 }  // namespace w2v
