@@ -489,7 +489,8 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
  * outputs may not overlap any array. With 16-bit types dg, du and h are
  * rounded to type between the products.
  *
- * Calls that overlap in time need a workspace each.
+ * Calls that overlap in time need a workspace each. One of less than the bytes
+ * that are named is refused where these arrays need more of it.
  * ---------------------------------------------------------------------- */
 enum { W2V_SILU = 0, W2V_GELU = 1 };
 

@@ -933,6 +933,21 @@ class AdamW:
 
 
 # ------------------------------------------------- a learned block of such a step, and its matrices' optimizer
+def _with_workspace(workspace: torch.Tensor | None, size, dev: torch.device, call) -> None:
+    """call(pointer, bytes) with the caller's workspace, or with a new one of size() bytes where there is none or it is too
+    small (which the call says before it launches anything)."""
+    with _On(dev):
+        if workspace is not None:
+            ptr = _dev_ptr(workspace, torch.uint8, "workspace")
+            if workspace.device != dev:
+                raise ValueError(f"workspace must be on {dev}")
+            rc = call(ptr, workspace.numel())
+            if rc != W2V_E_WORKSPACE:
+                return _check(rc)
+        ws = _workspace(size(), dev)
+        _check(call(ws.data_ptr(), ws.numel()))
+
+
 _ACTS = {"silu": 0, "gelu": 1}
 
 
@@ -986,10 +1001,8 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     elif gate is not None or up is not None:
         raise ValueError("gate and up are written with save only")
     outs = _matrix(y, (n, d), x, "out"), _matrix(gate, (n, h), x, "gate"), _matrix(up, (n, h), x, "up")
-    with _On(x.device):
-        ws = _kept(workspace, lib().w2v_gated_ffn_workspace_bytes(*sizes[:4]), x.device)
-        _check(lib().w2v_gated_ffn(*arrays, *sizes, *outs, None if ws is None else ws.data_ptr(),
-                                   0 if ws is None else ws.numel(), _stream(x.device)))
+    _with_workspace(workspace, lambda: lib().w2v_gated_ffn_workspace_bytes(*sizes[:4]), x.device,
+                    lambda ws, size: lib().w2v_gated_ffn(*arrays, *sizes, *outs, ws, size, _stream(x.device)))
     return y, gate, up
 
 
@@ -1007,10 +1020,8 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     grads = [torch.empty(s, dtype=x.dtype, device=x.device) if t is None else t
              for t, s in zip((dx, dw_gate, dw_up, dw_down), shapes)]
     outs = [_matrix(t, s, x, name) for t, s, name in zip(grads, shapes, ("dx", "dw_gate", "dw_up", "dw_down"))]
-    with _On(x.device):
-        ws = _kept(workspace, lib().w2v_gated_ffn_backward_workspace_bytes(*sizes[:4]), x.device)
-        _check(lib().w2v_gated_ffn_backward(*ins, *sizes, *outs, None if ws is None else ws.data_ptr(),
-                                            0 if ws is None else ws.numel(), _stream(x.device)))
+    _with_workspace(workspace, lambda: lib().w2v_gated_ffn_backward_workspace_bytes(*sizes[:4]), x.device,
+                    lambda ws, size: lib().w2v_gated_ffn_backward(*ins, *sizes, *outs, ws, size, _stream(x.device)))
     return tuple(grads)
 
 
@@ -1042,10 +1053,8 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: torch
     out = torch.empty_like(g, memory_format=torch.contiguous_format) if out is None else out
     op = _stack_of(out, "out", g)
     sizes = g.shape[0] if g.dim() == 3 else 1, *g.shape[-2:], kind
-    with _On(g.device):
-        ws = _kept(workspace, lib().w2v_orthogonalize_workspace_bytes(*sizes), g.device)
-        _check(lib().w2v_orthogonalize(*gp, *sizes, steps, eps, *op, None if ws is None else ws.data_ptr(),
-                                       0 if ws is None else ws.numel(), _stream(g.device)))
+    _with_workspace(workspace, lambda: lib().w2v_orthogonalize_workspace_bytes(*sizes), g.device,
+                    lambda ws, size: lib().w2v_orthogonalize(*gp, *sizes, steps, eps, *op, ws, size, _stream(g.device)))
     return out
 
 

@@ -75,34 +75,34 @@ struct Place {
 // Up to three products of one kind and k, or two whose results are added.
 struct Product {
     Side a, b;
-    int64_t m, n, gm, gn, first;   // sizes, tiles, number of its first tile
+    int64_t m, n;
+    int32_t gm, gn, first;   // tiles, and the number of the first one
     void *out;
     int64_t out_stride;
 };
 template <class T>
 struct ProductJob {
     Product p[3];
-    int32_t count, splits;
+    int32_t count;
     const char *a2, *b2;           // what p[0]'s k goes on with, or null
-    int64_t k, tiles;
-    float *part;
+    int64_t k;
+    Tiling t;
 
     template <class Q>
-    __device__ __forceinline__ Place at(int64_t tile) const {
+    __device__ __forceinline__ Place at(int tile) const {
         Place w;
         w.which = count > 2 && tile >= p[2].first ? 2 : count > 1 && tile >= p[1].first ? 1 : 0;
-        int64_t tm, tn;
+        int tm, tn;
         tile_at(tile - p[w.which].first, p[w.which].gm, p[w.which].gn, tm, tn);
-        w.m0 = tm * Q::BM;
-        w.n0 = tn * Q::BN;
+        w.m0 = int64_t(tm) * Q::BM;
+        w.n0 = int64_t(tn) * Q::BN;
         return w;
     }
     template <class Q>
-    __device__ __forceinline__ void multiply(const Place &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+    __device__ __forceinline__ void multiply(const Place &w, int step, int end, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         const Product &x = p[w.which];
         const int64_t all = Q::TWO ? ceil_div(k, Q::BK) * Q::BK + k : k;
-        const int64_t step = split_steps(all, Q::BK, splits), k0 = split * step, k1 = std::min(all, k0 + step);
-        if (k0 < k1) Q::run(x.a, x.b, a2, b2, 0, w.m0, x.m, w.n0, x.n, k, k0, k1, lds, acc);
+        Q::run(x.a, x.b, a2, b2, 0, w.m0, x.m, w.n0, x.n, k, int64_t(step) * Q::BK, std::min(all, int64_t(end) * Q::BK), lds, acc);
     }
     template <class Q>
     __device__ __forceinline__ void take(const Place &w, int row, int col, char *region, Lanes lanes) const {
@@ -119,24 +119,24 @@ template <class T, class E, int P>
 struct UpJob {
     Side x, w;
     int64_t other;   // from Wg to Wu, bytes
-    int64_t m, n, gm, gn, k, tiles;
-    int32_t splits, act;
-    float *part;
+    int64_t m, n, k;
+    int32_t gm, gn;
+    int32_t act;
+    Tiling t;
     E *h;
     int64_t h_stride, h_plane;
     T *gate, *up;
     int64_t gate_stride, up_stride;
 
     template <class Q>
-    __device__ __forceinline__ Place at(int64_t tile) const {
-        int64_t tm, tn;
+    __device__ __forceinline__ Place at(int tile) const {
+        int tm, tn;
         tile_at(tile, gm, gn, tm, tn);
-        return Place{tm * Q::BM, tn * (Q::BN / 2), 0};
+        return Place{int64_t(tm) * Q::BM, int64_t(tn) * (Q::BN / 2), 0};
     }
     template <class Q>
-    __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
-        const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
-        if (k0 < k1) Q::run(x, w, nullptr, nullptr, other, w0.m0, m, w0.n0, n, k, k0, k1, lds, acc);
+    __device__ __forceinline__ void multiply(const Place &w0, int step, int end, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        Q::run(x, w, nullptr, nullptr, other, w0.m0, m, w0.n0, n, k, int64_t(step) * Q::BK, std::min(k, int64_t(end) * Q::BK), lds, acc);
     }
     template <class Q>
     __device__ __forceinline__ void take(const Place &w0, int row, int col, char *region, Lanes lanes) const {
@@ -157,24 +157,24 @@ struct UpJob {
 template <class T, class E, int P>
 struct BackJob {
     Side dy, w;
-    int64_t m, n, gm, gn, k, tiles;
-    int32_t splits, act;
-    float *part;
+    int64_t m, n, k;
+    int32_t gm, gn;
+    int32_t act;
+    Tiling t;
     E *dg, *du, *h;
     int64_t h_stride, h_plane;
     const T *gate, *up;
     int64_t gate_stride, up_stride;
 
     template <class Q>
-    __device__ __forceinline__ Place at(int64_t tile) const {
-        int64_t tm, tn;
+    __device__ __forceinline__ Place at(int tile) const {
+        int tm, tn;
         tile_at(tile, gm, gn, tm, tn);
-        return Place{tm * Q::BM, tn * Q::BN, 0};
+        return Place{int64_t(tm) * Q::BM, int64_t(tn) * Q::BN, 0};
     }
     template <class Q>
-    __device__ __forceinline__ void multiply(const Place &w0, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
-        const int64_t step = split_steps(k, Q::BK, splits), k0 = split * step, k1 = std::min(k, k0 + step);
-        if (k0 < k1) Q::run(dy, w, nullptr, nullptr, 0, w0.m0, m, w0.n0, n, k, k0, k1, lds, acc);
+    __device__ __forceinline__ void multiply(const Place &w0, int step, int end, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
+        Q::run(dy, w, nullptr, nullptr, 0, w0.m0, m, w0.n0, n, k, int64_t(step) * Q::BK, std::min(k, int64_t(end) * Q::BK), lds, acc);
     }
     template <class Q>
     __device__ __forceinline__ void take(const Place &w0, int row, int col, char *region, Lanes lanes) const {
@@ -212,7 +212,7 @@ template <class E, bool A, bool B, bool PAIR, bool TWO>
 struct Tiles3 {
     using Large = Tile<E, 3, 256, 128, 4, 2, 32, A, B, PAIR, TWO>;
     using Small = Tile<E, 3, 128, 64, 2, 2, 32, A, B, PAIR, TWO>;
-    using Deep = Tile<E, 3, 128, 128, 2, 2, 32, A, B, PAIR, TWO, 3>;
+    using Deep = Tile<E, 3, 128, 128, 4, 2, 32, A, B, PAIR, TWO, 3>;
     using Tiny = Tile<E, 3, 64, 64, 2, 2, 32, A, B, PAIR, TWO, 3>;
 };
 template <class T>
@@ -405,6 +405,7 @@ int forward_few(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     const int64_t hs = ceil_div(a.hidden, 64) * 64;
     float *h = c.take<float>(static_cast<size_t>(a.rows * hs));
     if (!launch) return W2V_OK;
+    if (int rc = check_workspace(c.base, c.cap, c.used())) return rc;
     FewArgs u{};
     u.x = a.x.p;
     u.w = a.w_gate.p;
@@ -451,10 +452,12 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     pack.operands(a.w_gate, a.w_up, f, d, wg, wu);
     const Side wd = pack.operand(a.w_down, d, f);
     E *h = c.take<E>(static_cast<size_t>(K::P * n * hs));
-    const Cut up = choose_cut_of<Up>(n, 2 * f, d),
-              down = choose_cut_of<Down>(n, d, f);
+    // bytes that an element of a product's result stands for: g or u, and half of h's parts; y
+    const Cut up = choose_cut_of<Up>(n, 2 * f, d, sizeof(T) + K::P),
+              down = choose_cut_of<Down>(n, d, f, sizeof(T));
     float *part = c.take<float>(std::max(up.floats, down.floats));
     if (!launch) return W2V_OK;
+    if (int rc = check_workspace(c.base, c.cap, c.used())) return rc;
     if (up.tiles > kMaxTiles || down.tiles > kMaxTiles) return fail(W2V_E_RANGE, "too many rows for one call");
     if (int rc = launch_parts<T>(pack, s)) return rc;
     UpJob<T, E, K::P> u{};
@@ -463,11 +466,10 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     u.other = wu.p - wg.p;
     u.m = n;
     u.n = f;
-    u.gm = ceil_div(n, tile_m<Up>(up));
-    u.gn = ceil_div(2 * f, tile_n<Up>(up));
+    u.gm = tiles_along(n, tile_m<Up>(up));
+    u.gn = tiles_along(2 * f, tile_n<Up>(up));
     u.k = d;
     u.act = a.act;
-    u.part = part;
     u.h = h;
     u.h_stride = hs;
     u.h_plane = n * hs;
@@ -475,14 +477,13 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     u.up = static_cast<T *>(const_cast<void *>(a.up.p));
     u.gate_stride = a.gate.stride;
     u.up_stride = a.up.stride;
-    if (int rc = launch_cut<Up>(up, u, s)) return rc;
+    if (int rc = launch_cut<Up>(up, part, u, s)) return rc;
     ProductJob<T> y{};
-    y.p[0] = Product{Side{reinterpret_cast<char *>(h), n * hs * 2, hs * 2}, wd, n, d, ceil_div(n, tile_m<Down>(down)),
-                     ceil_div(d, tile_n<Down>(down)), 0, const_cast<void *>(a.y.p), a.y.stride};
+    y.p[0] = Product{Side{reinterpret_cast<char *>(h), n * hs * 2, hs * 2}, wd, n, d, tiles_along(n, tile_m<Down>(down)),
+                     tiles_along(d, tile_n<Down>(down)), 0, const_cast<void *>(a.y.p), a.y.stride};
     y.count = 1;
     y.k = f;
-    y.part = part;
-    return launch_cut<Down>(down, y, s);
+    return launch_cut<Down>(down, part, y, s);
 }
 
 template <class T>
@@ -504,26 +505,35 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
         h[i] = c.take<E>(static_cast<size_t>(K::P * n * hs));
         hid[i] = Side{reinterpret_cast<char *>(h[i]), n * hs * 2, hs * 2};
     }
-    const Cut back = choose_cut_of<Hidden>(n, f, d), in = choose_cut_of<Input>(n, d, 2 * f);
-    const Cut weights = choose_cut<Weights>(n, [&](auto tile) {
-        using Q = typename decltype(tile)::type;
-        return 2 * count_tiles<Q>(f, d) + count_tiles<Q>(d, f);
-    });
+    const Cut back = choose_cut_of<Hidden>(n, f, d, 2 * sizeof(T) + 6 * K::P),
+              in = choose_cut_of<Input>(n, d, f, sizeof(T), true);
+    const auto cut_weights = [&](int inputs, int outputs) {
+        return choose_cut<Weights>(n, sizeof(T), [&](auto tile) {
+            using Q = typename decltype(tile)::type;
+            return inputs * count_tiles<Q>(f, d) + outputs * count_tiles<Q>(d, f);
+        });
+    };
+    Cut weights = cut_weights(2, 1);
     float *part = c.take<float>(std::max({back.floats, in.floats, weights.floats}));
     if (!launch) return W2V_OK;
+    if (int rc = check_workspace(c.base, c.cap, c.used())) return rc;
     if (back.tiles > kMaxTiles || in.tiles > kMaxTiles || weights.tiles > kMaxTiles)
         return fail(W2V_E_RANGE, "too many rows for one call");
+    if (!a.dw_gate.p || !a.dw_up.p || !a.dw_down.p) {   // fewer gradients: whole tiles where their pieces have no room
+        const size_t room = std::max({back.floats, in.floats, weights.floats});
+        weights = cut_weights((a.dw_gate.p ? 1 : 0) + (a.dw_up.p ? 1 : 0), a.dw_down.p ? 1 : 0);
+        if (weights.floats > room) weights.whole = weights.tiles;
+    }
     if (int rc = launch_parts<T>(pack, s)) return rc;
     BackJob<T, E, K::P> b{};
     b.dy = dy;
     b.w = wd;
     b.m = n;
     b.n = f;
-    b.gm = ceil_div(n, tile_m<Hidden>(back));
-    b.gn = ceil_div(f, tile_n<Hidden>(back));
+    b.gm = tiles_along(n, tile_m<Hidden>(back));
+    b.gn = tiles_along(f, tile_n<Hidden>(back));
     b.k = d;
     b.act = a.act;
-    b.part = part;
     b.dg = h[0];
     b.du = h[1];
     b.h = h[2];
@@ -533,36 +543,31 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     b.up = static_cast<const T *>(a.up.p);
     b.gate_stride = a.gate.stride;
     b.up_stride = a.up.stride;
-    if (int rc = launch_cut<Hidden>(back, b, s)) return rc;
+    if (int rc = launch_cut<Hidden>(back, part, b, s)) return rc;
     ProductJob<T> j{};
     const Rows outs[3] = {a.dw_gate, a.dw_up, a.dw_down};
-    int64_t first = 0;
+    int32_t first = 0;
     for (int i = 0; i < 3; ++i) {
         if (!outs[i].p) continue;
         const int64_t m = i < 2 ? f : d, cols = i < 2 ? d : f;
-        const int64_t gm = ceil_div(m, tile_m<Weights>(weights)), gn = ceil_div(cols, tile_n<Weights>(weights));
+        const int32_t gm = tiles_along(m, tile_m<Weights>(weights)), gn = tiles_along(cols, tile_n<Weights>(weights));
         j.p[j.count++] = Product{i < 2 ? hid[i] : dy, i < 2 ? x : hid[2], m, cols, gm, gn, first, const_cast<void *>(outs[i].p),
                                  outs[i].stride};
         first += gm * gn;
     }
-    if (first > 0) {
-        j.k = n;
-        j.part = part;
-        Cut w = weights;
-        w.tiles = first;   // of the gradients that are wanted
-        if (int rc = launch_cut<Weights>(w, j, s)) return rc;
-    }
+    j.k = n;
+    if (j.count > 0)
+        if (int rc = launch_cut<Weights>(weights, part, j, s)) return rc;
     // dx last: it may lie where dy or x did
     if (!a.dx.p) return W2V_OK;
     ProductJob<T> i{};
-    i.p[0] = Product{hid[0], wg, n, d, ceil_div(n, tile_m<Input>(in)), ceil_div(d, tile_n<Input>(in)), 0,
+    i.p[0] = Product{hid[0], wg, n, d, tiles_along(n, tile_m<Input>(in)), tiles_along(d, tile_n<Input>(in)), 0,
                      const_cast<void *>(a.dx.p), a.dx.stride};
     i.a2 = hid[1].p;
     i.b2 = wu.p;
     i.count = 1;
     i.k = f;
-    i.part = part;
-    return launch_cut<Input>(in, i, s);
+    return launch_cut<Input>(in, part, i, s);
 }
 
 // Gradients of no rows: zeros, by a kernel (a captured graph takes no memset).
@@ -592,14 +597,14 @@ size_t ffn_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type, bool b
     return c.used();
 }
 
-int run_ffn(const FfnArgs &a, void *workspace, hipStream_t s) {
+int run_ffn(const FfnArgs &a, void *workspace, size_t bytes, hipStream_t s) {
     if (a.rows == 0) return W2V_OK;
-    Carve c(workspace);
+    Carve c(workspace, bytes);
     return with_type(a.type, [&](auto zero) { return forward<decltype(zero)>(a, c, true, s); });
 }
 
-int run_ffn_backward(const FfnArgs &a, void *workspace, hipStream_t s) {
-    Carve c(workspace);
+int run_ffn_backward(const FfnArgs &a, void *workspace, size_t bytes, hipStream_t s) {
+    Carve c(workspace, bytes);
     if (a.rows > 0) return with_type(a.type, [&](auto zero) { return backward<decltype(zero)>(a, c, true, s); });
     const Rows outs[3] = {a.dw_gate, a.dw_up, a.dw_down};
     for (int i = 0; i < 3; ++i) {

@@ -127,26 +127,25 @@ template <int P>
 struct SquareJob {
     Side x;
     int64_t step;        // bytes from a matrix to the next
-    int64_t r, k, g, tiles;
-    int32_t splits, poly;
-    float *part;
+    int64_t r, k;
+    int32_t g, poly;
+    Tiling t;
     const E *old;        // A, where poly
     E *out;
     int64_t stride, plane;
 
     template <class Q>
-    __device__ __forceinline__ Spot at(int64_t tile) const {
-        const int64_t each = g * (g + 1) / 2;
-        int64_t t = tile % each, tm = 0;
-        while (t >= g - tm) t -= g - tm++;
-        return Spot{tm * Q::BM, (tm + t) * Q::BN, tile / each};
+    __device__ __forceinline__ Spot at(int tile) const {
+        const int each = g * (g + 1) / 2, z = tile / each;
+        int in = tile - z * each, tm = 0;
+        while (in >= g - tm) in -= g - tm++;
+        return Spot{int64_t(tm) * Q::BM, int64_t(tm + in) * Q::BN, z};
     }
     template <class Q>
-    __device__ __forceinline__ void multiply(const Spot &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
-        const int64_t each = split_steps(k, Q::BK, splits), k0 = split * each, k1 = std::min(k, k0 + each);
+    __device__ __forceinline__ void multiply(const Spot &w, int from, int end, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         Side s = x;
         s.p += w.z * step;
-        if (k0 < k1) Q::run(s, s, nullptr, nullptr, 0, w.m0, r, w.n0, r, k, k0, k1, lds, acc);
+        Q::run(s, s, nullptr, nullptr, 0, w.m0, r, w.n0, r, k, int64_t(from) * Q::BK, std::min(k, int64_t(end) * Q::BK), lds, acc);
     }
     template <class Q>
     __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
@@ -191,26 +190,26 @@ template <class T, int P, bool LAST>
 struct StepJob {
     Side a, b;
     int64_t a_step, b_step;   // bytes from a matrix to the next
-    int64_t k, gm, gn, tiles;
-    int32_t splits;
-    float *part;
+    int64_t k;
+    int32_t gm, gn;
+    Tiling t;
     E *out;
     int64_t stride, plane;
     Batch batch;
 
     template <class Q>
-    __device__ __forceinline__ Spot at(int64_t tile) const {
-        int64_t tm, tn;
-        tile_at(tile % (gm * gn), gm, gn, tm, tn);
-        return Spot{tm * Q::BM, tn * Q::BN, tile / (gm * gn)};
+    __device__ __forceinline__ Spot at(int tile) const {
+        const int z = tile / (gm * gn);
+        int tm, tn;
+        tile_at(tile - z * gm * gn, gm, gn, tm, tn);
+        return Spot{int64_t(tm) * Q::BM, int64_t(tn) * Q::BN, z};
     }
     template <class Q>
-    __device__ __forceinline__ void multiply(const Spot &w, int split, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
-        const int64_t each = split_steps(k, Q::BK, splits), k0 = split * each, k1 = std::min(k, k0 + each);
+    __device__ __forceinline__ void multiply(const Spot &w, int from, int end, char *lds, f4 (&acc)[Q::FM][Q::FN]) const {
         Side l = a, r = b;
         l.p += w.z * a_step;
         r.p += w.z * b_step;
-        if (k0 < k1) Q::run(l, r, nullptr, nullptr, 0, w.m0, batch.rows, w.n0, batch.cols, k, k0, k1, lds, acc);
+        Q::run(l, r, nullptr, nullptr, 0, w.m0, batch.rows, w.n0, batch.cols, k, int64_t(from) * Q::BK, std::min(k, int64_t(end) * Q::BK), lds, acc);
     }
     template <class Q>
     __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
@@ -279,10 +278,10 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.x_plane = count * rows * w.x_stride;
     w.a_plane = count * w.r * w.a_stride;
     const auto square = [&](auto tile) { return count * triangle(ceil_div(w.r, decltype(tile)::type::BM)); };
-    w.gram = choose_cut<Tiles<P, true, true>>(w.c, square);
-    w.poly = choose_cut<Tiles<P, true, true>>(w.r, square);
+    w.gram = choose_cut<Tiles<P, true, true>>(w.c, 4 * P, square);
+    w.poly = choose_cut<Tiles<P, true, true>>(w.r, 6 * P, square);
     w.step = choose_cut<Tiles<P, true, true>>(
-        w.r, [&](auto tile) { return count * count_tiles<typename decltype(tile)::type>(rows, cols); });
+        w.r, 2 * P, [&](auto tile) { return count * count_tiles<typename decltype(tile)::type>(rows, cols); });
     Carve k(workspace);
     w.part = k.take<double>(static_cast<size_t>(count * kParts));
     for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
@@ -306,20 +305,19 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.step = b.rows * w.x_stride * 2;
         q.r = w.r;
         q.k = w.c;
-        q.g = ceil_div(w.r, tile_m<Gram>(w.gram));
-        q.part = w.sums;
+        q.g = tiles_along(w.r, tile_m<Gram>(w.gram));
         q.out = w.a;
         q.stride = w.a_stride;
         q.plane = w.a_plane;
-        if (int rc = launch_cut<Gram>(w.gram, q, s)) return rc;
+        if (int rc = launch_cut<Gram>(w.gram, w.sums, q, s)) return rc;
         q.x = Side{reinterpret_cast<const char *>(w.a), w.a_plane * 2, w.a_stride * 2};
         q.step = w.r * w.a_stride * 2;
         q.k = w.r;
-        q.g = ceil_div(w.r, tile_m<Poly>(w.poly));
+        q.g = tiles_along(w.r, tile_m<Poly>(w.poly));
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;
-        if (int rc = launch_cut<Poly>(w.poly, q, s)) return rc;
+        if (int rc = launch_cut<Poly>(w.poly, w.sums, q, s)) return rc;
         const Side poly{reinterpret_cast<const char *>(w.b), w.a_plane * 2, w.a_stride * 2};
         auto step = [&](auto job) {
             job.a = WIDE ? poly : x;
@@ -327,14 +325,13 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
             job.a_step = WIDE ? w.r * w.a_stride * 2 : b.rows * w.x_stride * 2;
             job.b_step = WIDE ? b.rows * w.x_stride * 2 : w.r * w.a_stride * 2;
             job.k = w.r;
-            job.gm = ceil_div(b.rows, tile_m<Step>(w.step));
-            job.gn = ceil_div(b.cols, tile_n<Step>(w.step));
-            job.part = w.sums;
+            job.gm = tiles_along(b.rows, tile_m<Step>(w.step));
+            job.gn = tiles_along(b.cols, tile_n<Step>(w.step));
             job.out = w.x[1 - i % 2];
             job.stride = w.x_stride;
             job.plane = w.x_plane;
             job.batch = b;
-            return launch_cut<Step>(w.step, job, s);
+            return launch_cut<Step>(w.step, w.sums, job, s);
         };
         if (int rc = i + 1 < steps ? step(StepJob<T, P, false>{}) : step(StepJob<T, P, true>{})) return rc;
     }
@@ -343,8 +340,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
 
 // All matrices of one shape and type.
 template <class T, class G, int P>
-int run_batch(const Batch &b, double eps, int32_t steps, void *workspace, hipStream_t s) {
-    const Arrays w = arrays_of<P>(b.rows, b.cols, b.count, workspace);
+int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStream_t s) {
     if (std::max({w.gram.tiles, w.poly.tiles, w.step.tiles}) > kMaxTiles) return fail(W2V_E_RANGE, "a matrix is too large");
     k_muon_momentum<G><<<static_cast<unsigned>(b.count * kParts), 256, 0, s>>>(b, w.part);
     W2V_LAUNCH_CHECK("k_muon_momentum");
@@ -365,10 +361,16 @@ int64_t together(int64_t rows, int64_t cols, int64_t count) {
     return std::max<int64_t>(1, std::min({count, int64_t(4096), (int64_t(1) << 26) / (rows * ceil_div(cols, 64) * 64)}));
 }
 
+Arrays arrays_for(int64_t rows, int64_t cols, int64_t count, int32_t type, void *workspace) {
+    return one_part(type) ? arrays_of<1>(rows, cols, count, workspace) : arrays_of<2>(rows, cols, count, workspace);
+}
+
+// The largest of the launches' needs: all but the last have `together` matrices.
 size_t batch_workspace(int64_t rows, int64_t cols, int64_t count, int32_t type) {
     if (rows == 0 || cols == 0 || count == 0) return 0;
-    const int64_t n = together(rows, cols, count);
-    return one_part(type) ? arrays_of<1>(rows, cols, n, nullptr).bytes : arrays_of<2>(rows, cols, n, nullptr).bytes;
+    const int64_t n = together(rows, cols, count), rest = count % n;
+    const size_t most = arrays_for(rows, cols, n, type, nullptr).bytes;
+    return rest == 0 ? most : std::max(most, arrays_for(rows, cols, rest, type, nullptr).bytes);
 }
 
 }  // namespace
@@ -377,9 +379,12 @@ size_t orthogonalize_bytes(int64_t batch, int64_t rows, int64_t cols, int32_t ty
     return batch_workspace(rows, cols, batch, type);
 }
 
-int run_orthogonalize(const OrthArgs &a, void *workspace, hipStream_t s) {
+int run_orthogonalize(const OrthArgs &a, void *workspace, size_t bytes, hipStream_t s) {
     if (a.batch == 0 || a.rows == 0 || a.cols == 0) return W2V_OK;
-    const int64_t most = together(a.rows, a.cols, a.batch), size = type_bytes(a.type);
+    const int64_t most = together(a.rows, a.cols, a.batch), size = type_bytes(a.type), rest = a.batch % most;
+    const Arrays many = arrays_for(a.rows, a.cols, most, a.type, workspace);
+    const Arrays last = rest == 0 ? many : arrays_for(a.rows, a.cols, rest, a.type, workspace);
+    if (int rc = check_workspace(workspace, bytes, std::max(many.bytes, last.bytes))) return rc;
     for (int64_t z = 0; z < a.batch; z += most) {
         Batch b{};
         b.first.out = static_cast<char *>(a.out) + z * a.out_step * size;
@@ -391,9 +396,10 @@ int run_orthogonalize(const OrthArgs &a, void *workspace, hipStream_t s) {
         b.rows = a.rows;
         b.cols = a.cols;
         b.count = std::min(most, a.batch - z);
+        const Arrays &w = b.count == most ? many : last;
         const int rc = with_type(a.type, [&](auto zero) {
             using T = decltype(zero);
-            return run_batch<T, T, std::is_same<T, __bf16>::value ? 1 : 2>(b, a.eps, a.steps, workspace, s);
+            return run_batch<T, T, std::is_same<T, __bf16>::value ? 1 : 2>(b, w, a.eps, a.steps, s);
         });
         if (rc) return rc;
     }
@@ -447,34 +453,47 @@ int run_muon_plan(const w2v_muon_matrix *t, int32_t n, void *plan, hipStream_t s
 }
 
 int run_muon_step(const w2v_muon_matrix *t, int32_t n, const void *plan, float *m, const w2v_muon_params &p, void *workspace,
-                  hipStream_t s) {
+                  size_t bytes, hipStream_t s) {
     const std::vector<int32_t> order = plan_order(t, n);
+    struct Launch {
+        int32_t first, count;
+        Arrays w;
+    };
+    std::vector<Launch> launches;
+    size_t need = 0;
     for (int32_t i = 0, j; i < n; i = j) {
         for (j = i; j < n && same_kind(t[order[i]], t[order[j]]);) ++j;
         const w2v_muon_matrix &x = t[order[i]];
         if (x.rows == 0 || x.cols == 0) continue;
         const int32_t most = static_cast<int32_t>(together(x.rows, x.cols, j - i));
         for (int32_t z = i; z < j; z += most) {
-            Batch b{};
-            b.table = static_cast<const Entry *>(plan) + z;
-            b.rows = x.rows;
-            b.cols = x.cols;
-            b.count = std::min(most, j - z);
-            b.m = m;
-            b.mu = static_cast<float>(p.momentum);
-            b.nesterov = p.nesterov;
-            b.muon = 1;
-            b.grad_scale = p.grad_scale;
-            b.lr = static_cast<float>(p.lr);
-            b.lr_device = p.lr_device;
-            const int rc = with_type(x.param_type, [&](auto pz) {
-                return with_type(x.grad_type, [&](auto gz) {
-                    using T = decltype(pz);
-                    return run_batch<T, decltype(gz), std::is_same<T, __bf16>::value ? 1 : 2>(b, p.eps, p.steps, workspace, s);
-                });
-            });
-            if (rc) return rc;
+            const int32_t count = std::min(most, j - z);
+            launches.push_back(Launch{z, count, arrays_for(x.rows, x.cols, count, x.param_type, workspace)});
+            need = std::max(need, launches.back().w.bytes);
         }
+    }
+    if (int rc = check_workspace(workspace, bytes, need)) return rc;
+    for (const Launch &l : launches) {
+        const w2v_muon_matrix &x = t[order[l.first]];
+        Batch b{};
+        b.table = static_cast<const Entry *>(plan) + l.first;
+        b.rows = x.rows;
+        b.cols = x.cols;
+        b.count = l.count;
+        b.m = m;
+        b.mu = static_cast<float>(p.momentum);
+        b.nesterov = p.nesterov;
+        b.muon = 1;
+        b.grad_scale = p.grad_scale;
+        b.lr = static_cast<float>(p.lr);
+        b.lr_device = p.lr_device;
+        const int rc = with_type(x.param_type, [&](auto pz) {
+            return with_type(x.grad_type, [&](auto gz) {
+                using T = decltype(pz);
+                return run_batch<T, decltype(gz), std::is_same<T, __bf16>::value ? 1 : 2>(b, l.w, p.eps, p.steps, s);
+            });
+        });
+        if (rc) return rc;
     }
     return W2V_OK;
 }

@@ -12,19 +12,23 @@
 
 using namespace w2v;
 
-namespace {
-
-hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
-
-bool aligned(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(bytes) == 0; }
+namespace w2v {
 
 int check_workspace(const void *ws, size_t have, size_t need) {
     if (have < need)
         return fail(W2V_E_WORKSPACE, "workspace_bytes " + std::to_string(have) + " < required " + std::to_string(need));
     if (need > 0 && !ws) return fail(W2V_E_ARG, "workspace is NULL");
-    if (need > 0 && !aligned(ws, 256)) return fail(W2V_E_ARG, "workspace must be 256-byte aligned");
+    if (need > 0 && reinterpret_cast<uintptr_t>(ws) % 256 != 0) return fail(W2V_E_ARG, "workspace must be 256-byte aligned");
     return W2V_OK;
 }
+
+}  // namespace w2v
+
+namespace {
+
+hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
+
+bool aligned(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(bytes) == 0; }
 
 // Rows of `dim` elements at p (required where there are any), `stride` apart. Offsets are 64-bit element counts.
 int check_rows(const void *p, int32_t type, int64_t rows, int64_t dim, int64_t stride, const std::string &name) {
@@ -396,7 +400,6 @@ int w2v_gated_ffn(w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, i
     if (int rc = check_in_place(y, x, rows, "y may be x")) return rc;
     for (const w2v_rows &w : {w_gate, w_up, w_down, gate, up})
         if (rows > 0 && w.p == y.p) return fail(W2V_E_ARG, "y may be no other array than x");
-    if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(rows, dim, hidden, type, false))) return rc;
     FfnArgs a{};
     a.rows = rows;
     a.dim = dim;
@@ -410,7 +413,7 @@ int w2v_gated_ffn(w2v_rows x, w2v_rows w_gate, w2v_rows w_up, w2v_rows w_down, i
     a.gate = rows_of(gate);
     a.up = rows_of(up);
     a.y = rows_of(y);
-    return run_ffn(a, workspace, as_stream(hip_stream));
+    return run_ffn(a, workspace, workspace_bytes, as_stream(hip_stream));
 }
 
 size_t w2v_gated_ffn_backward_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type) {
@@ -439,7 +442,6 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
     if (int rc = check_in_place(dx, x, rows, "dx may be x")) return rc;
     for (const w2v_rows &w : {w_gate, w_up, w_down, gate, up})
         if (dx.p && w.p == dx.p) return fail(W2V_E_ARG, "dx may be no other array than dy or x");
-    if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(rows, dim, hidden, type, true))) return rc;
     FfnArgs a{};
     a.rows = rows;
     a.dim = dim;
@@ -457,7 +459,7 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
     a.dw_gate = rows_of(dw_gate);
     a.dw_up = rows_of(dw_up);
     a.dw_down = rows_of(dw_down);
-    return run_ffn_backward(a, workspace, as_stream(hip_stream));
+    return run_ffn_backward(a, workspace, workspace_bytes, as_stream(hip_stream));
 }
 
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type) {
@@ -487,7 +489,6 @@ int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t b
         }
         if (out == g && rows > 1 && g_stride != out_stride) return fail(W2V_E_ARG, "out may be g only with the same strides");
     }
-    if (int rc = check_workspace(workspace, workspace_bytes, orthogonalize_bytes(batch, rows, cols, type))) return rc;
     OrthArgs a{};
     a.g = g;
     a.out = out;
@@ -501,7 +502,7 @@ int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t b
     a.g_step = g_step;
     a.out_step = out_step;
     a.eps = eps;
-    return run_orthogonalize(a, workspace, as_stream(hip_stream));
+    return run_orthogonalize(a, workspace, workspace_bytes, as_stream(hip_stream));
 }
 
 size_t w2v_muon_plan_bytes(const w2v_muon_matrix *matrices_host, int32_t n) {
@@ -544,8 +545,7 @@ int w2v_muon_step(const w2v_muon_matrix *matrices_host, int32_t n, const void *p
     if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return fail(W2V_E_ARG, "eps must be >= 0 and finite");
     if (p->steps < 1 || p->steps > 20) return fail(W2V_E_ARG, "steps must be in 1..20");
     try {
-        if (int rc = check_workspace(workspace, workspace_bytes, muon_bytes(matrices_host, n))) return rc;
-        return run_muon_step(matrices_host, n, plan, m, *p, workspace, as_stream(hip_stream));
+        return run_muon_step(matrices_host, n, plan, m, *p, workspace, workspace_bytes, as_stream(hip_stream));
     } catch (const std::exception &e) {
         return fail(W2V_E_ARG, std::string("the step's tables: ") + e.what());
     }

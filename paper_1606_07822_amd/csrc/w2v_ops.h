@@ -83,6 +83,9 @@ __device__ __forceinline__ float rows_sum(float v) {
     return a + b;
 }
 
+// Whether a workspace of `have` bytes is there where `need` are wanted.
+int check_workspace(const void *ws, size_t have, size_t need);   // ops_api.hip
+
 // Calls f with a value of the element type that t names.
 template <class F>
 int with_type(int32_t t, F f) {
@@ -164,8 +167,8 @@ struct FfnArgs {
 };
 constexpr int32_t kFfnMaxDim = 1 << 20;
 size_t ffn_bytes(int64_t rows, int32_t dim, int32_t hidden, int32_t type, bool backward);
-int run_ffn(const FfnArgs &a, void *workspace, hipStream_t s);
-int run_ffn_backward(const FfnArgs &a, void *workspace, hipStream_t s);
+int run_ffn(const FfnArgs &a, void *workspace, size_t bytes, hipStream_t s);
+int run_ffn_backward(const FfnArgs &a, void *workspace, size_t bytes, hipStream_t s);
 
 // ------------------------------------------------------------------ orthogonalised updates (muon.hip)
 struct OrthArgs {
@@ -178,12 +181,12 @@ struct OrthArgs {
 };
 constexpr int32_t kMuonMaxSide = 1 << 20;
 size_t orthogonalize_bytes(int64_t batch, int64_t rows, int64_t cols, int32_t type);
-int run_orthogonalize(const OrthArgs &a, void *workspace, hipStream_t s);
+int run_orthogonalize(const OrthArgs &a, void *workspace, size_t bytes, hipStream_t s);
 size_t muon_plan_bytes(int32_t n);
 size_t muon_bytes(const w2v_muon_matrix *t, int32_t n);
 int run_muon_plan(const w2v_muon_matrix *t, int32_t n, void *plan, hipStream_t s);
 int run_muon_step(const w2v_muon_matrix *t, int32_t n, const void *plan, float *m, const w2v_muon_params &p, void *workspace,
-                  hipStream_t s);
+                  size_t bytes, hipStream_t s);
 
 // ------------------------------------------------------------------ training in mini-batches (batch.hip)
 int check_training_args(const w2v_model *m, const w2v_params *p);   // api.hip

@@ -33,6 +33,14 @@ __device__ __forceinline__ f4 mfma32(Frag<_Float16> a, Frag<_Float16> b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// The lane, as a number that the compiler does not know anything of: what a loop's body computes from it stays in there, and
+// out of the registers that the body's products need.
+__device__ __forceinline__ int lane_here() {
+    int lane = lane_id();
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // 64 lanes' 16 bytes each from global memory into LDS, lane after lane from `lds` (the same in all lanes) on. In assembly,
 // because the compiler lets a transposing read of LDS wait for every such load before it, also of the other buffer; the
 // kernels wait for them themselves. M0 holds nothing else here: no other instruction of these kernels reads it.
@@ -104,7 +112,7 @@ template <class E_, int P_, int BM_, int BN_, int WM_, int WN_, int BK_, bool AL
 struct Tile {
     using E = E_;
     static constexpr int P = P_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
-    static constexpr bool PAIR = PAIR_, TWO = TWO_;
+    static constexpr bool PAIR = PAIR_, TWO = TWO_, kAlong = ALONG_A || ALONG_B;
     static constexpr int STAGES = STAGES_;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int kA = P * BM * BK * 2, kB = P * BN * BK * 2, kStage = kA + kB, kLds = STAGES * kStage;
@@ -121,9 +129,11 @@ struct Tile {
         static constexpr int kRowsPerLoad = kWave / kChunks;
         static_assert(kLoads >= 1 && kRowsPerLoad >= 1, "every wavefront loads");
 
-        // ALONG: 16 lanes read one chunk of 16 rows: all places of 256 bytes differ. Down: 32 lanes read two chunks of the
-        // rows 0..3 and 8..11 of a group of 16: pairs of chunks change places.
+        // ALONG: the 16 lanes that LDS serves at a time read one chunk of rows 0..3 and 12..15 of 16 and the next chunk of
+        // the others, or the other way round: all places of 256 bytes differ. Down: 32 lanes read two chunks of the rows 0..3
+        // and 8..11 of a group of 16: pairs of chunks change places.
         static __device__ __forceinline__ int place(int row, int chunk) {
+            if constexpr (ALONG && kChunks == 4) return chunk ^ (0x78 >> (row / 4 % 4 * 2) & 3);   // 0, 2, 3, 1
             if constexpr (ALONG) return chunk ^ (row / (256 / kRow)) % kChunks;
             if constexpr (kRow == 128) return chunk ^ ((row >> 1 & 1) | (row >> 2 & 2)) << 1;
             return chunk ^ ((row & 3) | (row >> 1 & 4)) << 1;
@@ -217,7 +227,7 @@ struct Tile {
     static __device__ __forceinline__ void run(const Side &a, const Side &b, const char *a2, const char *b2, int64_t other,
                                                int64_t m0, int64_t m, int64_t n0, int64_t n, int64_t k, int64_t k0,
                                                int64_t k1, char *lds, f4 (&acc)[FM][FN]) {
-        const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+        const int lane = lane_here(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
         const int wm = wave / WN, wn = wave % WN;
         HalfA ha;
         HalfB hb;
@@ -323,7 +333,7 @@ struct Tile {
         return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + to * 16);
     }
     static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], int phase, char *region) {
-        const int lane = lane_id();
+        const int lane = lane_here();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
             if (i / (FM / kPhases) == phase)
@@ -378,30 +388,81 @@ struct Tile {
 };
 
 // The workgroups of an XCD (every eighth) take neighbouring numbers, so that its L2 holds what they share.
-__device__ __forceinline__ int64_t by_xcd(int64_t id, int64_t count) {
-    const int64_t each = count / 8, more = count % 8, x = id % 8;
-    return x * each + std::min(x, more) + id / 8;
+__device__ __forceinline__ int by_xcd(int id, int count) {
+    const int each = count / 8, more = count % 8, x = id % 8;
+    return x * each + min(x, more) + id / 8;
 }
 
 // Tile number id of a gm x gn grid, column by column in bands of four rows.
-__device__ __forceinline__ void tile_at(int64_t id, int64_t gm, int64_t gn, int64_t &tm, int64_t &tn) {
-    constexpr int64_t kBand = 4;
-    const int64_t band = id / (kBand * gn), rows = std::min(gm - band * kBand, kBand), in = id % (kBand * gn);
+__device__ __forceinline__ void tile_at(int id, int gm, int gn, int &tm, int &tn) {
+    constexpr int kBand = 4;
+    const int band = id / (kBand * gn), rows = min(gm - band * kBand, kBand), in = id - band * (kBand * gn);
     tm = band * kBand + in % rows;
     tn = in / rows;
 }
 
 // ------------------------------------------------------------------ kernels over a job's tiles
-// A job says which tiles it has, multiplies one and puts its elements where they belong:
-//   int64_t tiles; int32_t splits; float *part       tiles, and the parts that each one's k is cut into
-//   Place at<T>(tile)                                 where the tile lies
-//   multiply<T>(place, split, lds, acc)               its product over one part of k
-//   take<T>(place, row, column, region, lanes)        what a region holds, from that row and column of the tile on
-// Parts of k are summed in their order by k_join, so that results do not depend on the order in which they end.
-inline __host__ __device__ int64_t split_steps(int64_t k, int bk, int32_t splits) {
-    return ceil_div(ceil_div(k, bk), splits) * bk;
+// How a launch's tiles are taken. `whole` workgroups make a tile each; the steps along k of the `tiles - whole` others are
+// shared out to `parts` workgroups: each tile's in the same number of pieces, the same piece of all tiles side by side (they
+// read the same k at a time), or all tiles' steps, one tile's after the other's, evenly, so that a workgroup has pieces of
+// one or two tiles. Sums of pieces wait in memory and are joined in k's order by k_join: results do not depend on what ends
+// first.
+template <class T>
+struct Which {
+    using type = T;
+};
+enum { kLarge, kSmall, kDeep, kTiny };
+struct Cut {
+    int32_t kind, parts;
+    int64_t tiles, whole, steps;   // steps: of one tile
+    bool evenly;                   // parts of all shared tiles' steps, not the same pieces of each
+    size_t floats;                 // of the pieces' sums
+};
+struct Tiling {
+    int32_t tiles, whole, steps, parts;
+    int32_t each, more;            // steps of a part; the first `more` parts have one more (evenly), or pieces of a tile: -more
+    float *part;
+
+    // Part j's first tile, and its steps from that tile's first one on.
+    __device__ __forceinline__ void part_of(int j, int &tile, int &step, int &end) const {
+        if (more < 0) {
+            const int shared = tiles - whole, piece = j / shared;
+            tile = whole + j - piece * shared;
+            step = piece * each;
+            end = min(step + each, steps);
+        } else {
+            const int in = begin(j) / steps;
+            tile = whole + in;
+            step = begin(j) - in * steps;
+            end = begin(j + 1) - in * steps;
+        }
+    }
+    __device__ __forceinline__ int begin(int j) const { return j * each + min(j, more); }
+    // Of the shared tiles' number `shared` (evenly): the part that has a step.
+    __device__ __forceinline__ int owner(int step) const {
+        const int with = more * (each + 1);
+        return step < with ? step / (each + 1) : more + (step - with) / each;
+    }
+};
+inline Tiling tiling_of(const Cut &c, float *part) {
+    const int64_t rest = c.tiles - c.whole, shared = rest * c.steps;
+    Tiling t{static_cast<int32_t>(c.tiles), static_cast<int32_t>(c.whole), static_cast<int32_t>(c.steps), c.parts, 0, 0, part};
+    if (rest > 0 && c.evenly) {
+        t.each = static_cast<int32_t>(shared / c.parts);
+        t.more = static_cast<int32_t>(shared % c.parts);
+    } else if (rest > 0) {
+        const int64_t pieces = c.parts / rest;
+        t.each = static_cast<int32_t>(ceil_div(c.steps, pieces));
+        t.more = static_cast<int32_t>(-pieces);
+    }
+    return t;
 }
 
+// A job says which tiles it has, multiplies one and puts its elements where they belong:
+//   Tiling t
+//   Place at<T>(tile)                                 where the tile lies
+//   multiply<T>(place, step, end, lds, acc)           its product over some of k's steps
+//   take<T>(place, row, column, region, lanes)        what a region holds, from that row and column of the tile on
 template <class T, class J>
 __device__ __forceinline__ void take_region(const J &job, const decltype(job.template at<T>(0)) &place, int wave, int phase,
                                             char *region, Lanes lanes) {
@@ -412,27 +473,41 @@ __device__ __forceinline__ void take_region(const J &job, const decltype(job.tem
 template <class T, class J>
 __global__ __launch_bounds__(T::kThreads, T::kPerSimd) void k_tiles(const J job) {
     __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
-    const int64_t id = by_xcd(blockIdx.x, gridDim.x);
-    const int64_t tile = id % job.tiles;
-    const int split = static_cast<int>(id / job.tiles);
-    const auto place = job.template at<T>(tile);
-    f4 acc[T::FM][T::FN] = {};
-    job.template multiply<T>(place, split, lds, acc);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody's reads of the last step
+    const Tiling &t = job.t;
     const int wave = static_cast<int>(threadIdx.x) / kWave;
     char *region = lds + wave * T::kRegion;
+    const int id = static_cast<int>(blockIdx.x);
+    int j = 0, tile, step = 0, end = t.steps;
+    if (id < t.whole) {
+        tile = by_xcd(id, t.whole);
+    } else {
+        j = by_xcd(id - t.whole, t.parts);
+        t.part_of(j, tile, step, end);
+    }
+#pragma unroll 1
+    for (int piece = 0; step < end; ++piece) {   // steps from `step` to `end` of this tile, and on to the next one's
+        const auto place = job.template at<T>(tile);
+        const int last = min(end, t.steps);
+        f4 acc[T::FM][T::FN] = {};
+        if (piece > 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody has left the regions
+        job.template multiply<T>(place, step, last, lds, acc);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody's reads of the last step
 #pragma unroll
-    for (int phase = 0; phase < T::kPhases; ++phase) {
-        if (phase > 0) lds_order();
-        T::fill(acc, phase, region);
-        lds_order();
-        if (job.splits == 1) {
-            take_region<T>(job, place, wave, phase, region, Lanes{lane_id(), kWave});
-            continue;
+        for (int phase = 0; phase < T::kPhases; ++phase) {
+            if (phase > 0) lds_order();
+            T::fill(acc, phase, region);
+            lds_order();
+            if (step == 0 && last == t.steps) {
+                take_region<T>(job, place, wave, phase, region, Lanes{lane_here(), kWave});
+                continue;
+            }
+            float *to = t.part + (((static_cast<int64_t>(j) * 2 + piece) * T::kWaves + wave) * T::kPhases + phase) * (T::kRegion / 4);
+            for (int c = lane_here(); c < T::kRegion / 16; c += kWave)
+                reinterpret_cast<f4 *>(to)[c] = T::cell(region, c / (T::kCols / 4), c % (T::kCols / 4));
         }
-        float *to = job.part + ((id * T::kWaves + wave) * T::kPhases + phase) * (T::kRegion / 4);
-        for (int c = lane_id(); c < T::kRegion / 16; c += kWave)
-            reinterpret_cast<f4 *>(to)[c] = T::cell(region, c / (T::kCols / 4), c % (T::kCols / 4));
+        ++tile;
+        end -= t.steps;
+        step = 0;
     }
 }
 
@@ -441,81 +516,102 @@ constexpr int kJoinThreads = 256;   // of a region
 template <class T, class J>
 __global__ __launch_bounds__(kJoinThreads) void k_join(const J job) {
     __shared__ __attribute__((aligned(1024))) char region[T::kRegion];
-    const int64_t size = T::kRegion / 16, per = T::kWaves * T::kPhases, tile = blockIdx.x / per;
-    const auto place = job.template at<T>(tile);
-    const f4 *from = reinterpret_cast<const f4 *>(job.part) + blockIdx.x * size;
-    const int64_t next = job.tiles * per * size;
+    const Tiling &t = job.t;
+    constexpr int size = T::kRegion / 16, per = T::kWaves * T::kPhases;
+    const int shared = static_cast<int>(blockIdx.x) / per, at = static_cast<int>(blockIdx.x) % per;
+    const int step = shared * t.steps, rest = t.tiles - t.whole;
+    const int first = t.more < 0 ? 0 : t.owner(step), last = t.more < 0 ? -t.more - 1 : t.owner(step + t.steps - 1);
+    if (t.more >= 0 && first == last) return;   // one workgroup had it whole
+    const f4 *part = reinterpret_cast<const f4 *>(t.part) + at * size + threadIdx.x;
     constexpr int kMine = T::kRegion / 16 / kJoinThreads;
     f4 v[kMine] = {};
 #pragma unroll 2
-    for (int s = 0; s < job.splits; ++s)
+    for (int j = first; j <= last; ++j) {
+        if (t.more < 0 && j * t.each >= t.steps) break;
+        // evenly: the piece is its workgroup's second where that began with the tile before
+        const int slot = t.more < 0 ? (j * rest + shared) * 2 : j * 2 + (j == first && t.begin(j) / t.steps != shared);
+        const f4 *from = part + static_cast<int64_t>(slot) * per * size;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) v[i] += from[s * next + i * kJoinThreads + threadIdx.x];
+        for (int i = 0; i < kMine; ++i) v[i] += from[i * kJoinThreads];
+    }
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int c = i * kJoinThreads + static_cast<int>(threadIdx.x);
         T::cell(region, c / (T::kCols / 4), c % (T::kCols / 4)) = v[i];
     }
     __syncthreads();
-    const int at = static_cast<int>(blockIdx.x % per);
-    take_region<T>(job, place, at / T::kPhases, at % T::kPhases, region, Lanes{static_cast<int>(threadIdx.x), kJoinThreads});
+    take_region<T>(job, job.template at<T>(t.whole + shared), at / T::kPhases, at % T::kPhases, region,
+                   Lanes{static_cast<int>(threadIdx.x), kJoinThreads});
 }
-
-// How a product's tiles are taken: large or small ones, and the parts of k.
-template <class T>
-struct Which {
-    using type = T;
-};
-enum { kLarge, kSmall, kDeep, kTiny };
-struct Cut {
-    int32_t kind;
-    int32_t splits;
-    int64_t tiles;
-    size_t floats;   // of the parts' sums
-};
 
 // A launch numbers its threads in 32 bits.
 constexpr int64_t kMaxTiles = int64_t(1) << 22;
 
 template <class T, class J>
-int launch_tiles(J &job, hipStream_t s) {
-    k_tiles<T, J><<<static_cast<unsigned>(job.tiles * job.splits), T::kThreads, 0, s>>>(job);
+int launch_tiles(const J &job, hipStream_t s) {
+    const int rest = job.t.tiles - job.t.whole;
+    k_tiles<T, J><<<static_cast<unsigned>(job.t.whole + (rest > 0 ? job.t.parts : 0)), T::kThreads, 0, s>>>(job);
     W2V_LAUNCH_CHECK("k_tiles");
-    if (job.splits > 1) {
-        k_join<T, J><<<static_cast<unsigned>(job.tiles * T::kWaves * T::kPhases), kJoinThreads, 0, s>>>(job);
+    if (rest > 0) {
+        k_join<T, J><<<static_cast<unsigned>(rest * T::kWaves * T::kPhases), kJoinThreads, 0, s>>>(job);
         W2V_LAUNCH_CHECK("k_join");
     }
     return W2V_OK;
 }
 
-// The cut with the least time by this model: each CU takes its share of the tiles one after the other, at the matrix
-// cores' measured rate (4.7 TFLOP/s a CU, less with smaller tiles, which read LDS more often) but a step in no less than
-// 0.2 us, with two steps until the first product; sums of parts go through memory at 4 TB/s, and joining them is another
-// launch. count(tile): the tiles of all products of a launch that have k in common. S: the tiles, Large, Small, Tiny, and
-// Deep, which are small ones with more steps on their way where a CU has but one.
+// Microseconds of a step (all of a tile's products over BK of k), measured: by whether k runs along a row of either operand,
+// by parts, and by kind, where a CU has one tile at a time, and where there are more. Large tiles do 1.4 to 1.5 PFLOP/s; small
+// ones read LDS more often.
+constexpr double kStepUs[2][3][4][2] = {{{{1.48, 1.55}, {0.66, 0.43}, {0.64, 0.59}, {0.29, 0.19}},
+                                         {{2.05, 2.07}, {0.70, 0.53}, {0.74, 0.70}, {0.31, 0.19}},
+                                         {{2.04, 2.13}, {0.70, 0.56}, {1.15, 1.18}, {0.45, 0.31}}},
+                                        {{{1.45, 1.55}, {0.65, 0.43}, {0.64, 0.59}, {0.29, 0.19}},
+                                         {{2.07, 2.14}, {0.83, 0.72}, {0.82, 0.77}, {0.32, 0.26}},
+                                         {{2.12, 2.21}, {0.90, 0.80}, {1.22, 1.25}, {0.47, 0.48}}}};
+
+// The cut with the least time by this model: the CUs take tiles in turns of their steps and two more until the first product,
+// 1 us and what an element of the result moves behind them (`bytes` of it; a CU's share of memory is 20 KB a us). Sums of
+// pieces go through memory twice, and joining them is another launch. count(tile): the tiles of all products of a launch that
+// have k in common. S: the tiles, Large, Small, Tiny, and Deep, which are small ones with more steps on their way where a CU
+// has but one.
 template <class S, class F>
-Cut choose_cut(int64_t k, F count) {
-    Cut best{kLarge, 1, 0, 0};
+Cut choose_cut(int64_t k, double bytes, F count, bool two = false) {
+    Cut best{};
     double least = 1e300;
     const int64_t cus = device_cu_count();
-    auto weigh = [&](int32_t kind, auto tile, double slow) {
+    auto weigh = [&](int32_t kind, auto tile) {
         using T = typename decltype(tile)::type;
-        const int64_t tiles = count(tile), steps = ceil_div(k, T::BK), area = T::BM * T::BN;
-        const double step_us = std::max(0.2, area * T::BK * (T::P * (T::P + 1)) / 4.7e6 * slow);
-        for (int32_t n = 1; n <= 64 && (n == 1 || n * 2 <= steps); ++n) {
-            const double turns = static_cast<double>(ceil_div(tiles * n, cus));
-            const double join = n == 1 ? 0.0 : 5.0 + 8.0 * tiles * n * area / 4e6;
-            const double us = turns * (ceil_div(steps, n) + 2) * step_us + join;
-            if (us >= least * 0.999) continue;
+        const int64_t tiles = count(tile), steps = ceil_div(k, T::BK) * (two ? 2 : 1), area = T::BM * T::BN;
+        const double *step_us = kStepUs[T::kAlong][T::P - 1][kind], out_us = 1.0 + area * (0.03 + 0.05 * bytes) * 1e-3;
+        auto offer = [&](int64_t whole, int64_t parts, bool evenly) {
+            const int64_t rest = tiles - whole, turns = ceil_div(whole, cus) + (rest > 0 ? ceil_div(parts, cus) : 0);
+            const double step = step_us[turns > 1];
+            double us = static_cast<double>(ceil_div(whole, cus)) * ((steps + 2) * step + out_us);
+            size_t floats = 0;
+            if (rest > 0) {
+                // sharing steps out evenly has the workgroups read different k at a time: 15 % more
+                const double piece = evenly ? 1.15 * (rest * steps) / parts + 2 : static_cast<double>(ceil_div(steps, parts / rest));
+                us += ceil_div(parts, cus) * ((piece + 2) * step + (evenly ? 2 : 1) * (1.0 + area * 0.23e-3)) + 6.0 +
+                      4.0 * parts * area / 4e6 + rest * area * bytes / 4e6;
+                floats = static_cast<size_t>(2 * parts * area);
+            }
+            if (us >= least * 0.999) return;
             least = us;
-            best = Cut{kind, n, tiles, n == 1 ? 0 : static_cast<size_t>(tiles * n * area)};
+            best = Cut{kind, static_cast<int32_t>(parts), tiles, whole, steps, evenly, floats};
+        };
+        offer(tiles, 1, false);
+        // the last turn's tiles, or with the turn before it
+        const int64_t left = tiles % cus;
+        for (int64_t rest : {left, left + cus}) {
+            if (rest == 0 || rest > tiles || rest * steps >= INT32_MAX) continue;
+            for (int64_t n = 2; n <= 64 && n * 2 <= steps && n * rest <= 2 * cus; ++n) offer(tiles - rest, n * rest, false);
+            if (rest * steps >= 4 * cus) offer(tiles - rest, rest > cus ? 2 * cus : cus, true);
         }
     };
-    constexpr int P = S::Large::P;
-    weigh(kLarge, Which<typename S::Large>{}, 1.0);
-    weigh(kSmall, Which<typename S::Small>{}, 1.15);
-    weigh(kDeep, Which<typename S::Deep>{}, 1.15);
-    weigh(kTiny, Which<typename S::Tiny>{}, P == 1 ? 2.2 : P == 2 ? 1.6 : 1.3);
+    weigh(kLarge, Which<typename S::Large>{});
+    weigh(kSmall, Which<typename S::Small>{});
+    weigh(kDeep, Which<typename S::Deep>{});
+    weigh(kTiny, Which<typename S::Tiny>{});
     return best;
 }
 
@@ -525,9 +621,11 @@ int64_t count_tiles(int64_t m, int64_t n) {
     return ceil_div(m, T::BM) * ceil_div(n, T::BN);
 }
 template <class S>
-Cut choose_cut_of(int64_t m, int64_t n, int64_t k) {
-    return choose_cut<S>(k, [&](auto tile) { return count_tiles<typename decltype(tile)::type>(m, n); });
+Cut choose_cut_of(int64_t m, int64_t n, int64_t k, double bytes, bool two = false) {
+    return choose_cut<S>(k, bytes, [&](auto tile) { return count_tiles<typename decltype(tile)::type>(m, n); }, two);
 }
+
+inline int32_t tiles_along(int64_t size, int64_t tile) { return static_cast<int32_t>(ceil_div(size, tile)); }
 
 // A cut's tile sizes.
 template <class S>
@@ -540,9 +638,8 @@ int64_t tile_n(const Cut &c) {
 }
 
 template <class S, class J>
-int launch_cut(const Cut &c, J &job, hipStream_t s) {
-    job.splits = c.splits;
-    job.tiles = c.tiles;
+int launch_cut(const Cut &c, float *part, J &job, hipStream_t s) {
+    job.t = tiling_of(c, part);
     switch (c.kind) {
         case kLarge: return launch_tiles<typename S::Large, J>(job, s);
         case kSmall: return launch_tiles<typename S::Small, J>(job, s);
