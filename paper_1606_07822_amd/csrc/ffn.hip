@@ -38,12 +38,12 @@ __device__ __forceinline__ void act_both(int act, float g, float &value, float &
 }
 
 // ------------------------------------------------------------------ operands as parts
-// An array as the matrix products read it: P planes of 16-bit parts in rows of whole chunks, zeros behind the last column.
+// An array as the matrix products read it: P 16-bit parts an element in rows of whole chunks, zeros behind the last column.
 struct Source {
     const void *from;
     int64_t from_stride;   // elements
     void *to;
-    int64_t rows, cols, to_stride;   // to_stride in elements, a multiple of 8
+    int64_t rows, cols, to_stride;   // to_stride in elements, a multiple of 8 (of 32 with parts)
     int64_t first;         // number of its first chunk in the launch
 };
 struct Sources {
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void k_parts(const Sources all) {
         float v[8];
         const int64_t left = s.cols - chunk * 8;
         load8<T>(static_cast<const T *>(s.from) + row * s.from_stride + chunk * 8, left, v);
-        store_parts8<E, P>(static_cast<E *>(s.to) + row * s.to_stride + chunk * 8, s.rows * s.to_stride, left, v);
+        store_parts8<E, P>(static_cast<E *>(s.to) + part_at<P>(row, chunk * 8, s.to_stride), left, v);
     }
 }
 
@@ -124,7 +124,7 @@ struct UpJob {
     int32_t act;
     Tiling t;
     E *h;
-    int64_t h_stride, h_plane;
+    int64_t h_stride;
     T *gate, *up;
     int64_t gate_stride, up_stride;
 
@@ -148,7 +148,7 @@ struct UpJob {
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = act_value(act, g[e]) * u[e];
-            store_parts8<E, P>(h + r * h_stride + c, h_plane, valid, v);
+            store_parts8<E, P>(h + part_at<P>(r, c, h_stride), valid, v);
         });
     }
 };
@@ -162,7 +162,7 @@ struct BackJob {
     int32_t act;
     Tiling t;
     E *dg, *du, *h;
-    int64_t h_stride, h_plane;
+    int64_t h_stride;
     const T *gate, *up;
     int64_t gate_stride, up_stride;
 
@@ -192,10 +192,10 @@ struct BackJob {
                 vu[e] = dh[e] * value;
                 vg[e] = dh[e] * u[e] * slope;
             }
-            const int64_t at = r * h_stride + c;
-            store_parts8<E, P>(dg + at, h_plane, valid, vg);
-            store_parts8<E, P>(du + at, h_plane, valid, vu);
-            store_parts8<E, P>(h + at, h_plane, valid, vh);
+            const int64_t at = part_at<P>(r, c, h_stride);
+            store_parts8<E, P>(dg + at, valid, vg);
+            store_parts8<E, P>(du + at, valid, vu);
+            store_parts8<E, P>(h + at, valid, vh);
         });
     }
 };
@@ -257,14 +257,14 @@ struct Packing {
         b = both ? as_is(q, rows, cols) : packed(q, rows, cols);
     }
     static Side as_is(const Rows &r, int64_t rows, int64_t cols) {
-        return Side{static_cast<const char *>(r.p), 0, (rows <= 1 ? cols : r.stride) * 2};
+        return Side{static_cast<const char *>(r.p), (rows <= 1 ? cols : r.stride) * 2};
     }
     Side packed(const Rows &r, int64_t rows, int64_t cols) {
-        const int64_t stride = ceil_div(cols, 8) * 8;
+        const int64_t unit = parts > 1 ? 32 : 8, stride = ceil_div(cols, unit) * unit;
         char *to = carve->take<char>(static_cast<size_t>(parts * rows * stride * 2));
         all.s[all.count++] = Source{r.p, r.stride, to, rows, cols, stride, all.chunks};
         all.chunks += rows * (stride / 8);
-        return Side{to, rows * stride * 2, stride * 2};
+        return Side{to, parts * stride * 2};
     }
 };
 
@@ -472,14 +472,13 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     u.act = a.act;
     u.h = h;
     u.h_stride = hs;
-    u.h_plane = n * hs;
     u.gate = static_cast<T *>(const_cast<void *>(a.gate.p));
     u.up = static_cast<T *>(const_cast<void *>(a.up.p));
     u.gate_stride = a.gate.stride;
     u.up_stride = a.up.stride;
     if (int rc = launch_cut<Up>(up, part, u, s)) return rc;
     ProductJob<T> y{};
-    y.p[0] = Product{Side{reinterpret_cast<char *>(h), n * hs * 2, hs * 2}, wd, n, d, tiles_along(n, tile_m<Down>(down)),
+    y.p[0] = Product{Side{reinterpret_cast<char *>(h), K::P * hs * 2}, wd, n, d, tiles_along(n, tile_m<Down>(down)),
                      tiles_along(d, tile_n<Down>(down)), 0, const_cast<void *>(a.y.p), a.y.stride};
     y.count = 1;
     y.k = f;
@@ -503,7 +502,7 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     Side hid[3];
     for (int i = 0; i < 3; ++i) {
         h[i] = c.take<E>(static_cast<size_t>(K::P * n * hs));
-        hid[i] = Side{reinterpret_cast<char *>(h[i]), n * hs * 2, hs * 2};
+        hid[i] = Side{reinterpret_cast<char *>(h[i]), K::P * hs * 2};
     }
     const Cut back = choose_cut_of<Hidden>(n, f, d, 2 * sizeof(T) + 6 * K::P),
               in = choose_cut_of<Input>(n, d, f, sizeof(T), true);
@@ -538,7 +537,6 @@ int backward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     b.du = h[1];
     b.h = h[2];
     b.h_stride = hs;
-    b.h_plane = n * hs;
     b.gate = static_cast<const T *>(a.gate.p);
     b.up = static_cast<const T *>(a.up.p);
     b.gate_stride = a.gate.stride;

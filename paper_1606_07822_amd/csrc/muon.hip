@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void k_muon_momentum(const Batch b, double *pa
 // X's parts, in rows of `stride` elements with zeros behind the last column.
 template <class T, int P>
 __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double *part, double eps, E *x, int64_t stride,
-                                                    int64_t plane, int64_t blocks) {
+                                                    int64_t blocks) {
     const int64_t z = blockIdx.x / blocks;
     const Entry e = b.entry(z);
     double sum = wave_sum(part[z * kParts + threadIdx.x]);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double 
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = static_cast<float>(g[i] * inverse);
-        store_parts8<E, P>(x + (z * b.rows + row) * stride + col, plane, valid, g);
+        store_parts8<E, P>(x + part_at<P>(z * b.rows + row, col, stride), valid, g);
     }
 }
 
@@ -132,7 +132,7 @@ struct SquareJob {
     Tiling t;
     const E *old;        // A, where poly
     E *out;
-    int64_t stride, plane;
+    int64_t stride;
 
     template <class Q>
     __device__ __forceinline__ Spot at(int tile) const {
@@ -149,21 +149,21 @@ struct SquareJob {
     }
     template <class Q>
     __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
-        E *to = out + w.z * r * stride;
-        const E *a = old + w.z * r * stride;
+        E *to = out + w.z * r * stride * P;
+        const E *a = old + w.z * r * stride * P;
         Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
             const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
             if (m >= r || n >= stride) return;
-            finish(a + m * stride + n, m, n, v);
-            store_parts8<E, P>(to + m * stride + n, plane, r - n, v);
+            finish(a + part_at<P>(m, n, stride), m, n, v);
+            store_parts8<E, P>(to + part_at<P>(m, n, stride), r - n, v);
         });
         if (w.m0 == w.n0) return;
         // the tile below the diagonal: A is symmetric, so that row n has from column m on what column n had from row m on
         Q::columns8(region, lanes, [&](int i, int j, float (&v)[8]) {
             const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
             if (n >= r || m >= r) return;
-            finish(a + n * stride + m, n, m, v);
-            store_parts8<E, P>(to + n * stride + m, plane, r - m, v);
+            finish(a + part_at<P>(n, m, stride), n, m, v);
+            store_parts8<E, P>(to + part_at<P>(n, m, stride), r - m, v);
         });
     }
     // `from`: A's 8 elements from (row, col) on.
@@ -172,7 +172,7 @@ struct SquareJob {
         if (poly) {
 #pragma unroll
             for (int p = P - 1; p >= 0; --p) {
-                const Frag<E> o = *reinterpret_cast<const Frag<E> *>(from + p * plane);
+                const Frag<E> o = *reinterpret_cast<const Frag<E> *>(from + p * 32);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a[e] += static_cast<float>(o[e]);
             }
@@ -194,7 +194,7 @@ struct StepJob {
     int32_t gm, gn;
     Tiling t;
     E *out;
-    int64_t stride, plane;
+    int64_t stride;
     Batch batch;
 
     template <class Q>
@@ -219,7 +219,7 @@ struct StepJob {
                 if (m >= batch.rows || n >= stride) return;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= kDown;
-                store_parts8<E, P>(out + (w.z * batch.rows + m) * stride + n, plane, batch.cols - n, v);
+                store_parts8<E, P>(out + part_at<P>(w.z * batch.rows + m, n, stride), batch.cols - n, v);
             });
         } else {
             const Entry en = batch.entry(w.z);
@@ -263,7 +263,7 @@ struct Arrays {
     double *part;
     E *x[2], *a, *b;
     float *sums;
-    int64_t r, c, x_stride, a_stride, x_plane, a_plane;
+    int64_t r, c, x_stride, a_stride;
     Cut gram, poly, step;
     size_t bytes;
 };
@@ -275,8 +275,6 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.c = std::max(rows, cols);
     w.x_stride = ceil_div(cols, 64) * 64;
     w.a_stride = ceil_div(w.r, 64) * 64;
-    w.x_plane = count * rows * w.x_stride;
-    w.a_plane = count * w.r * w.a_stride;
     const auto square = [&](auto tile) { return count * triangle(ceil_div(w.r, decltype(tile)::type::BM)); };
     w.gram = choose_cut<Tiles<P, true, true>>(w.c, 4 * P, square);
     w.poly = choose_cut<Tiles<P, true, true>>(w.r, 6 * P, square);
@@ -284,9 +282,9 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
         w.r, 2 * P, [&](auto tile) { return count * count_tiles<typename decltype(tile)::type>(rows, cols); });
     Carve k(workspace);
     w.part = k.take<double>(static_cast<size_t>(count * kParts));
-    for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * w.x_plane));
-    w.a = k.take<E>(static_cast<size_t>(P * w.a_plane));
-    w.b = k.take<E>(static_cast<size_t>(P * w.a_plane));
+    for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * count * rows * w.x_stride));
+    w.a = k.take<E>(static_cast<size_t>(P * count * w.r * w.a_stride));
+    w.b = k.take<E>(static_cast<size_t>(P * count * w.r * w.a_stride));
     w.sums = k.take<float>(std::max({w.gram.floats, w.poly.floats, w.step.floats}));
     w.bytes = k.used();
     return w;
@@ -299,37 +297,36 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
     using Step = Tiles<P, true, !WIDE>;
     for (int32_t i = 0; i < steps; ++i) {
         const E *from = w.x[i % 2];
-        const Side x{reinterpret_cast<const char *>(from), w.x_plane * 2, w.x_stride * 2};
+        const int64_t x_row = P * w.x_stride * 2, a_row = P * w.a_stride * 2;   // bytes
+        const Side x{reinterpret_cast<const char *>(from), x_row};
         SquareJob<P> q{};
         q.x = x;
-        q.step = b.rows * w.x_stride * 2;
+        q.step = b.rows * x_row;
         q.r = w.r;
         q.k = w.c;
         q.g = tiles_along(w.r, tile_m<Gram>(w.gram));
         q.out = w.a;
         q.stride = w.a_stride;
-        q.plane = w.a_plane;
         if (int rc = launch_cut<Gram>(w.gram, w.sums, q, s)) return rc;
-        q.x = Side{reinterpret_cast<const char *>(w.a), w.a_plane * 2, w.a_stride * 2};
-        q.step = w.r * w.a_stride * 2;
+        q.x = Side{reinterpret_cast<const char *>(w.a), a_row};
+        q.step = w.r * a_row;
         q.k = w.r;
         q.g = tiles_along(w.r, tile_m<Poly>(w.poly));
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;
         if (int rc = launch_cut<Poly>(w.poly, w.sums, q, s)) return rc;
-        const Side poly{reinterpret_cast<const char *>(w.b), w.a_plane * 2, w.a_stride * 2};
+        const Side poly{reinterpret_cast<const char *>(w.b), a_row};
         auto step = [&](auto job) {
             job.a = WIDE ? poly : x;
             job.b = WIDE ? x : poly;
-            job.a_step = WIDE ? w.r * w.a_stride * 2 : b.rows * w.x_stride * 2;
-            job.b_step = WIDE ? b.rows * w.x_stride * 2 : w.r * w.a_stride * 2;
+            job.a_step = WIDE ? w.r * a_row : b.rows * x_row;
+            job.b_step = WIDE ? b.rows * x_row : w.r * a_row;
             job.k = w.r;
             job.gm = tiles_along(b.rows, tile_m<Step>(w.step));
             job.gn = tiles_along(b.cols, tile_n<Step>(w.step));
             job.out = w.x[1 - i % 2];
             job.stride = w.x_stride;
-            job.plane = w.x_plane;
             job.batch = b;
             return launch_cut<Step>(w.step, w.sums, job, s);
         };
@@ -345,8 +342,7 @@ int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStr
     k_muon_momentum<G><<<static_cast<unsigned>(b.count * kParts), 256, 0, s>>>(b, w.part);
     W2V_LAUNCH_CHECK("k_muon_momentum");
     const int64_t blocks = std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 256), 4096);
-    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], w.x_stride, w.x_plane,
-                                                                               blocks);
+    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], w.x_stride, blocks);
     W2V_LAUNCH_CHECK("k_muon_start");
     return b.rows <= b.cols ? run_steps<T, P, true>(b, w, steps, s) : run_steps<T, P, false>(b, w, steps, s);
 }
@@ -355,10 +351,11 @@ int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStr
 // rounding; all others from two.
 bool one_part(int32_t type) { return type == W2V_BF16; }
 
-// Matrices that go through the steps together: as many as keep a launch's X within 2^26 elements, and 4,096 (a launch
-// numbers its threads in 32 bits).
+// Matrices that go through the steps together: launches of equal shares with X within 2^27 elements, and 4,096 matrices (a
+// launch numbers its threads in 32 bits).
 int64_t together(int64_t rows, int64_t cols, int64_t count) {
-    return std::max<int64_t>(1, std::min({count, int64_t(4096), (int64_t(1) << 26) / (rows * ceil_div(cols, 64) * 64)}));
+    const int64_t most = std::max<int64_t>(1, std::min(int64_t(4096), (int64_t(1) << 27) / (rows * ceil_div(cols, 64) * 64)));
+    return ceil_div(count, ceil_div(count, most));
 }
 
 Arrays arrays_for(int64_t rows, int64_t cols, int64_t count, int32_t type, void *workspace) {

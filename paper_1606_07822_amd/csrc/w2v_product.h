@@ -2,9 +2,11 @@
 // last step (an activation, a gradient, a weight's update) on a tile while it is in registers.
 //
 // An operand is 16-bit elements in rows of whole 16-byte chunks, with k along the rows (ALONG) or down them: the second
-// kind is read from LDS by a transposing load, so that no array is needed in two layouts. It is one plane, or P planes
+// kind is read from LDS by a transposing load, so that no array is needed in two layouts. An element is one number, or P
 // whose sum is the value (parts of 8 bits in bf16, of 11 in fp16): products p, q with p + q < P are taken, smallest
-// first, which leaves out what lies below the last part. The sums are fp32.
+// first, which leaves out what lies below the last part. The sums are fp32. A row holds the first parts of 32 elements,
+// then their second parts, and so on, so that a step's 64 bytes of each part lie in common 128-byte lines (rows of one part
+// after the other's took 40 % longer with 128 x 64 tiles of three parts: half of every line came for nothing).
 //
 // A workgroup of WM x WN wavefronts makes BM x BN of C. Each step, BK of k, goes from global memory straight into one
 // of two LDS buffers while the matrix cores work on the other; a wavefront waits for its own loads and a barrier makes
@@ -75,8 +77,15 @@ struct Lanes {
 
 struct Side {
     const char *p;
-    int64_t plane, row;   // bytes from a plane to the next, from a row to the next
+    int64_t row;   // bytes from a row to the next
 };
+
+// Where element (row, col) of an array of P parts has its first one; the others follow 32 elements apart. stride: elements
+// of a row, a multiple of 32 where there are several parts.
+template <int P>
+__device__ __forceinline__ int64_t part_at(int64_t row, int64_t col, int64_t stride) {
+    return P == 1 ? row * stride + col : row * stride * P + col / 32 * (32 * P) + col % 32;
+}
 
 // The values of 1, 2 or 3 parts. The last part takes what is left, to nearest.
 template <class E, int P>
@@ -90,9 +99,9 @@ __device__ __forceinline__ void to_parts(float v, E (&part)[P]) {
     }
 }
 
-// Parts of 8 neighbouring elements, zeros from number `valid` on, `plane` elements from a part to the next.
+// Parts of 8 neighbouring elements of an array (the first a multiple of 8), zeros from number `valid` on.
 template <class E, int P>
-__device__ __forceinline__ void store_parts8(E *to, int64_t plane, int64_t valid, const float (&v)[8]) {
+__device__ __forceinline__ void store_parts8(E *to, int64_t valid, const float (&v)[8]) {
     Frag<E> part[P];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -102,7 +111,7 @@ __device__ __forceinline__ void store_parts8(E *to, int64_t plane, int64_t valid
         for (int p = 0; p < P; ++p) part[p][e] = one[p];
     }
 #pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * plane) = part[p];
+    for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * 32) = part[p];
 }
 
 // PAIR: B's rows come in groups of 16 from two arrays in turn. TWO: k runs through a second pair of operands after the
@@ -140,17 +149,21 @@ struct Tile {
         }
 
         const char *p;
-        int64_t plane, step, corner;   // corner: bytes from an operand's start to the tile's first row or column
+        int64_t step, corner;          // corner: bytes from an operand's start to the tile's first row or column
         uint32_t off[kLoads];
         int32_t left;                  // of k, from the step that is loaded next on
+
+        // A chunk's first part in a row that starts with 32 elements'.
+        static __device__ __forceinline__ uint32_t at_chunk(int chunk) {
+            return static_cast<uint32_t>(P == 1 ? chunk * 16 : chunk / 4 * (64 * P) + chunk % 4 * 16);
+        }
 
         // valid: rows (ALONG) or columns from the tile's first one on that the operand has; what lies past them is read
         // from the last one and dropped with its results.
         __device__ __forceinline__ void start(const Side &s, int64_t first, int64_t valid, int64_t k0, int64_t k1, int wave, int lane) {
-            corner = ALONG ? first * s.row : first * 2;
-            p = s.p + corner + k0 * (ALONG ? 2 : s.row);
-            plane = s.plane;
-            step = ALONG ? kRow : BK * s.row;
+            corner = ALONG ? first * s.row : first * (2 * P);
+            p = s.p + corner + k0 * (ALONG ? 2 * P : s.row);
+            step = ALONG ? kRow * P : BK * s.row;
             left = static_cast<int32_t>(k1 - k0);
             const int last = static_cast<int>(std::min<int64_t>(valid, R)) - 1;
 #pragma unroll
@@ -158,9 +171,9 @@ struct Tile {
                 const int row = (wave * kLoads + i) * kRowsPerLoad + lane / kChunks;
                 const int chunk = place(row, lane % kChunks);
                 if constexpr (ALONG)
-                    off[i] = static_cast<uint32_t>(min(row, last)) * static_cast<uint32_t>(s.row) + static_cast<uint32_t>(chunk) * 16u;
+                    off[i] = static_cast<uint32_t>(min(row, last)) * static_cast<uint32_t>(s.row) + at_chunk(chunk);
                 else
-                    off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(s.row) + static_cast<uint32_t>(min(chunk, last / 8)) * 16u;
+                    off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(s.row) + at_chunk(min(chunk, last / 8));
             }
         }
 
@@ -186,12 +199,12 @@ struct Tile {
         template <class F>
         __device__ __forceinline__ void each_load(uint32_t lds, int wave, int64_t other, F f) {
 #pragma unroll
-            for (int q = 0; q < P; ++q)
+            for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
+                for (int q = 0; q < P; ++q) {
                     const int first = (wave * kLoads + i) * kRowsPerLoad;
                     f(lds + static_cast<uint32_t>(q * kPlane + first * kRow),
-                      p + q * plane + (PAIR && first / 16 % 2 ? other : 0), i, first);
+                      p + q * 64 + (PAIR && first / 16 % 2 ? other : 0), i, first);
                 }
         }
 
@@ -234,8 +247,8 @@ struct Tile {
         int turn_at = -1;   // the step with which the second operands begin
         const int64_t whole = (k + BK - 1) / BK * BK;
         if (TWO && k0 >= whole) {
-            ha.start(Side{a2, a.plane, a.row}, m0, m - m0, k0 - whole, k1 - whole, wave, lane);
-            hb.start(Side{b2, b.plane, b.row}, n0, n - n0, k0 - whole, k1 - whole, wave, lane);
+            ha.start(Side{a2, a.row}, m0, m - m0, k0 - whole, k1 - whole, wave, lane);
+            hb.start(Side{b2, b.row}, n0, n - n0, k0 - whole, k1 - whole, wave, lane);
         } else {
             if (TWO && k1 > whole) turn_at = static_cast<int>((whole - k0) / BK);
             ha.start(a, m0, m - m0, k0, std::min(k1, k), wave, lane);
@@ -247,7 +260,7 @@ struct Tile {
             for (int i = 0; i < HalfB::kLoads; ++i) {
                 const int row = (wave * HalfB::kLoads + i) * HalfB::kRowsPerLoad + lane / HalfB::kChunks;
                 hb.off[i] = static_cast<uint32_t>(min(row / 32 * 16 + row % 16, last)) * static_cast<uint32_t>(b.row) +
-                            static_cast<uint32_t>(HalfB::place(row, lane % HalfB::kChunks)) * 16u;
+                            HalfB::at_chunk(HalfB::place(row, lane % HalfB::kChunks));
             }
         }
         const auto base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds));
@@ -520,14 +533,14 @@ __global__ __launch_bounds__(kJoinThreads) void k_join(const J job) {
     constexpr int size = T::kRegion / 16, per = T::kWaves * T::kPhases;
     const int shared = static_cast<int>(blockIdx.x) / per, at = static_cast<int>(blockIdx.x) % per;
     const int step = shared * t.steps, rest = t.tiles - t.whole;
-    const int first = t.more < 0 ? 0 : t.owner(step), last = t.more < 0 ? -t.more - 1 : t.owner(step + t.steps - 1);
+    const int first = t.more < 0 ? 0 : t.owner(step), last = t.more < 0 ? (t.steps - 1) / t.each : t.owner(step + t.steps - 1);
     if (t.more >= 0 && first == last) return;   // one workgroup had it whole
     const f4 *part = reinterpret_cast<const f4 *>(t.part) + at * size + threadIdx.x;
     constexpr int kMine = T::kRegion / 16 / kJoinThreads;
     f4 v[kMine] = {};
-#pragma unroll 2
+    constexpr int kAhead = kMine == 1 ? 8 : 4;
+#pragma unroll kAhead
     for (int j = first; j <= last; ++j) {
-        if (t.more < 0 && j * t.each >= t.steps) break;
         // evenly: the piece is its workgroup's second where that began with the tile before
         const int slot = t.more < 0 ? (j * rest + shared) * 2 : j * 2 + (j == first && t.begin(j) / t.steps != shared);
         const f4 *from = part + static_cast<int64_t>(slot) * per * size;
@@ -562,16 +575,16 @@ int launch_tiles(const J &job, hipStream_t s) {
 // Microseconds of a step (all of a tile's products over BK of k), measured: by whether k runs along a row of either operand,
 // by parts, and by kind, where a CU has one tile at a time, and where there are more. Large tiles do 1.4 to 1.5 PFLOP/s; small
 // ones read LDS more often.
-constexpr double kStepUs[2][3][4][2] = {{{{1.48, 1.55}, {0.66, 0.43}, {0.64, 0.59}, {0.29, 0.19}},
-                                         {{2.05, 2.07}, {0.70, 0.53}, {0.74, 0.70}, {0.31, 0.19}},
-                                         {{2.04, 2.13}, {0.70, 0.56}, {1.15, 1.18}, {0.45, 0.31}}},
-                                        {{{1.45, 1.55}, {0.65, 0.43}, {0.64, 0.59}, {0.29, 0.19}},
-                                         {{2.07, 2.14}, {0.83, 0.72}, {0.82, 0.77}, {0.32, 0.26}},
-                                         {{2.12, 2.21}, {0.90, 0.80}, {1.22, 1.25}, {0.47, 0.48}}}};
+constexpr double kStepUs[2][3][4][2] = {{{{1.50, 1.56}, {0.67, 0.44}, {0.65, 0.59}, {0.28, 0.19}},
+                                         {{2.07, 2.12}, {0.71, 0.56}, {0.74, 0.72}, {0.32, 0.21}},
+                                         {{2.16, 2.20}, {0.73, 0.56}, {1.20, 1.22}, {0.45, 0.32}}},
+                                        {{{1.46, 1.57}, {0.65, 0.43}, {0.64, 0.59}, {0.30, 0.20}},
+                                         {{2.10, 2.10}, {0.73, 0.59}, {0.78, 0.73}, {0.31, 0.22}},
+                                         {{2.20, 2.20}, {0.80, 0.68}, {1.17, 1.22}, {0.43, 0.36}}}};
 
 // The cut with the least time by this model: the CUs take tiles in turns of their steps and two more until the first product,
 // 1 us and what an element of the result moves behind them (`bytes` of it; a CU's share of memory is 20 KB a us). Sums of
-// pieces go through memory twice, and joining them is another launch. count(tile): the tiles of all products of a launch that
+// pieces go through memory twice, and joining them is another launch, 0.2 us a piece of a tile. count(tile): the tiles of all products of a launch that
 // have k in common. S: the tiles, Large, Small, Tiny, and Deep, which are small ones with more steps on their way where a CU
 // has but one.
 template <class S, class F>
@@ -592,7 +605,7 @@ Cut choose_cut(int64_t k, double bytes, F count, bool two = false) {
                 // sharing steps out evenly has the workgroups read different k at a time: 15 % more
                 const double piece = evenly ? 1.15 * (rest * steps) / parts + 2 : static_cast<double>(ceil_div(steps, parts / rest));
                 us += ceil_div(parts, cus) * ((piece + 2) * step + (evenly ? 2 : 1) * (1.0 + area * 0.23e-3)) + 6.0 +
-                      4.0 * parts * area / 4e6 + rest * area * bytes / 4e6;
+                      0.2 * parts / rest + 4.0 * parts * area / 4e6 + rest * area * bytes / 4e6;
                 floats = static_cast<size_t>(2 * parts * area);
             }
             if (us >= least * 0.999) return;
