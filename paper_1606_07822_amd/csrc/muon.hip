@@ -121,14 +121,15 @@ struct Spot {
     int64_t m0, n0, z;
 };
 
-// A symmetric r x r product of each matrix with itself, of which the tiles on and above the diagonal are made: A = X X' (or
-// X' X), or with `poly` aI + bA + cAA.
+// A symmetric r x r product of each matrix with itself: A = X X' (or X' X), or with `poly` aI + bA + cAA. Of it the tiles on
+// and above the diagonal are made, and the others are their mirror images; of few tiles all are made
+// (orthogonalize 100 x 400: a mirror image takes a second pass over LDS and A, 1.5 us of a launch's 7.5).
 template <int P>
 struct SquareJob {
     Side x;
     int64_t step;        // bytes from a matrix to the next
     int64_t r, k;
-    int32_t g, poly;
+    int32_t g, poly, all;   // tiles along a side; all: none is a mirror image
     Tiling t;
     const E *old;        // A, where poly
     E *out;
@@ -136,8 +137,9 @@ struct SquareJob {
 
     template <class Q>
     __device__ __forceinline__ Spot at(int tile) const {
-        const int each = g * (g + 1) / 2, z = tile / each;
+        const int each = all ? g * g : g * (g + 1) / 2, z = tile / each;
         int in = tile - z * each, tm = 0;
+        if (all) return Spot{int64_t(in / g) * Q::BM, int64_t(in % g) * Q::BN, z};
         while (in >= g - tm) in -= g - tm++;
         return Spot{int64_t(tm) * Q::BM, int64_t(tm + in) * Q::BN, z};
     }
@@ -157,7 +159,7 @@ struct SquareJob {
             finish(a + part_at<P>(m, n, stride), m, n, v);
             store_parts8<E, P>(to + part_at<P>(m, n, stride), r - n, v);
         });
-        if (w.m0 == w.n0) return;
+        if (all || w.m0 == w.n0) return;
         // the tile below the diagonal: A is symmetric, so that row n has from column m on what column n had from row m on
         Q::columns8(region, lanes, [&](int i, int j, float (&v)[8]) {
             const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
@@ -256,7 +258,10 @@ struct Tiles<2, A, B> {
     using Tiny = Tile<E, 2, 64, 64, 2, 2, 32, A, B, false, false, 4>;
 };
 
-int64_t triangle(int64_t g) { return g * (g + 1) / 2; }
+// Whether a launch of `count` symmetric products of g x g tiles makes them all (up to a quarter of the CUs: with all of them
+// 2,731 x 1,023 takes 396 us, by halves 348).
+bool makes_all(int64_t g, int64_t count) { return count * g * g * 4 <= device_cu_count(); }
+int64_t square_tiles(int64_t g, int64_t count) { return count * (makes_all(g, count) ? g * g : g * (g + 1) / 2); }
 
 // Where the arrays of a launch of `count` matrices lie.
 struct Arrays {
@@ -275,7 +280,7 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.c = std::max(rows, cols);
     w.x_stride = ceil_div(cols, 64) * 64;
     w.a_stride = ceil_div(w.r, 64) * 64;
-    const auto square = [&](auto tile) { return count * triangle(ceil_div(w.r, decltype(tile)::type::BM)); };
+    const auto square = [&](auto tile) { return square_tiles(ceil_div(w.r, decltype(tile)::type::BM), count); };
     w.gram = choose_cut<Tiles<P, true, true>>(w.c, 4 * P, square);
     w.poly = choose_cut<Tiles<P, true, true>>(w.r, 6 * P, square);
     w.step = choose_cut<Tiles<P, true, true>>(
@@ -305,6 +310,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.r = w.r;
         q.k = w.c;
         q.g = tiles_along(w.r, tile_m<Gram>(w.gram));
+        q.all = makes_all(q.g, b.count);
         q.out = w.a;
         q.stride = w.a_stride;
         if (int rc = launch_cut<Gram>(w.gram, w.sums, q, s)) return rc;
@@ -312,6 +318,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.step = w.r * a_row;
         q.k = w.r;
         q.g = tiles_along(w.r, tile_m<Poly>(w.poly));
+        q.all = makes_all(q.g, b.count);
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;

@@ -340,9 +340,11 @@ struct Tile {
     static constexpr int kRegion = kRows * kCols * 4;
     static_assert(kRegion * kWaves <= kLds && (kCols == 32 || kCols % 64 == 0), "regions fit");
 
-    // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks.
+    // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks, and the same
+    // two columns of rows 8 apart do, too (columns8).
     static __device__ __forceinline__ f4 &cell(char *region, int row, int chunk) {
-        const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ (row & 15) ^ (chunk >> 4) * 4);
+        const int turn = (row & 15) ^ (row >> 2 & 4) ^ (row >> 4 & 2);
+        const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ turn ^ (chunk >> 4) * 4);
         return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + to * 16);
     }
     static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], int phase, char *region) {
