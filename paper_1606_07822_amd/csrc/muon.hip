@@ -51,34 +51,42 @@ struct Batch {
 };
 
 // ------------------------------------------------------------------ momentum and norms
-// Block b of matrix z: its share of the rows' chunks of four elements, and their sum of squares.
+// Both passes are bound by memory (momentum 5.6 TB/s). Block b of `blocks` of a matrix takes every `blocks`-th group of rows;
+// its threads have a place in a row and go along it: f(row, column) for the first of each N columns up to `width`.
+template <int N, class F>
+__device__ __forceinline__ void each_chunk(int64_t rows, int64_t width, int64_t block, int64_t blocks, F f) {
+    const int per = static_cast<int>(ceil_div(width, N)), wide = min(per, 256), tall = 256 / wide;
+    const int tid = static_cast<int>(threadIdx.x), in = tid / wide, at = tid - in * wide;
+    if (in >= tall) return;
+    for (int64_t row = block * tall + in; row < rows; row += blocks * tall)
+        for (int c = at; c < per; c += wide) f(row, c * N);
+}
+
+// Block b of matrix z: its share of the momentum and of U's sum of squares.
 template <class T>
 __global__ __launch_bounds__(256) void k_muon_momentum(const Batch b, double *part) {
     const int64_t z = blockIdx.x / kParts;
-    const int chunk0 = static_cast<int>(blockIdx.x % kParts);
     const Entry e = b.entry(z);
-    const int64_t per = ceil_div(b.cols, 4), chunks = b.rows * per;
     double sum = 0.0;
-    for (int64_t c = chunk0 * int64_t(256) + threadIdx.x; c < chunks; c += kParts * 256) {
-        const int64_t row = c / per, col = c % per * 4;
-        const int valid = static_cast<int>(std::min<int64_t>(4, b.cols - col));
-        float g[4];
-        load_cols<T, 4>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, 0, valid, g);
+    each_chunk<8>(b.rows, b.cols, blockIdx.x % kParts, kParts, [&](int64_t row, int col) {
+        const int64_t valid = b.cols - col;
+        float g[8];
+        load8<T>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, valid, g);
         if (b.m) {
             float *at = b.m + e.moment + row * b.cols + col;
-            float m[4];
-            load_cols<float, 4>(at, 0, valid, m);
+            float m[8];
+            load8<float>(at, valid, m);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 g[i] *= b.grad_scale;
                 m[i] = b.mu * m[i] + g[i];
                 g[i] = b.nesterov ? g[i] + b.mu * m[i] : m[i];
             }
-            store_cols<float, 4>(at, 0, valid, m);
+            store8<float>(at, valid, m);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += static_cast<double>(g[i]) * g[i];
-    }
+        for (int i = 0; i < 8; ++i) sum += static_cast<double>(g[i]) * g[i];   // squares of fp32 leave its range
+    });
     sum = wave_sum(sum);
     __shared__ double waves[4];
     if (lane_id() == 0) waves[threadIdx.x / kWave] = sum;
@@ -97,23 +105,23 @@ __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double 
     if (lane_id() == 0) waves[threadIdx.x / kWave] = sum;
     __syncthreads();
     sum = waves[0] + waves[1] + waves[2] + waves[3];
-    const double inverse = kUp / (sqrt(sum) + eps);
-    const int64_t per = stride / 8, chunks = b.rows * per;
-    for (int64_t c = blockIdx.x % blocks * 256 + threadIdx.x; c < chunks; c += blocks * 256) {
-        const int64_t row = c / per, col = c % per * 8;
-        const int valid = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(8, b.cols - col)));
+    // one over the norm as a factor below one and a power of two: either may be out of fp32's range, X is not
+    int power = 0;
+    const float factor = static_cast<float>(frexp(kUp / (sqrt(sum) + eps), &power));
+    each_chunk<8>(b.rows, stride, blockIdx.x % blocks, blocks, [&](int64_t row, int col) {
+        const int64_t valid = b.cols - col;
         float g[8];
-        load_cols<T, 8>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, 0, valid, g);
+        load8<T>(static_cast<const T *>(e.grad) + row * e.grad_stride + col, valid, g);
         if (b.m) {
             float m[8];
-            load_cols<float, 8>(b.m + e.moment + row * b.cols + col, 0, valid, m);
+            load8<float>(b.m + e.moment + row * b.cols + col, valid, m);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = b.nesterov ? g[i] * b.grad_scale + b.mu * m[i] : m[i];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = static_cast<float>(g[i] * inverse);
+        for (int i = 0; i < 8; ++i) g[i] = ldexpf(g[i] * factor, power);
         store_parts8<E, P>(x + part_at<P>(z * b.rows + row, col, stride), valid, g);
-    }
+    });
 }
 
 // ------------------------------------------------------------------ the products of a step
@@ -348,7 +356,8 @@ int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStr
     if (std::max({w.gram.tiles, w.poly.tiles, w.step.tiles}) > kMaxTiles) return fail(W2V_E_RANGE, "a matrix is too large");
     k_muon_momentum<G><<<static_cast<unsigned>(b.count * kParts), 256, 0, s>>>(b, w.part);
     W2V_LAUNCH_CHECK("k_muon_momentum");
-    const int64_t blocks = std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 256), 4096);
+    // some four chunks of eight a thread, and no more than 4,096 workgroups a matrix
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 1024), 4096));
     k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], w.x_stride, blocks);
     W2V_LAUNCH_CHECK("k_muon_start");
     return b.rows <= b.cols ? run_steps<T, P, true>(b, w, steps, s) : run_steps<T, P, false>(b, w, steps, s);

@@ -396,7 +396,7 @@ struct Tile {
             const int row = c % kPer * 8, col = c / kPer;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = cell(region, row + e, col / 4)[col % 4];
+            for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const float *>(&cell(region, row + e, col / 4))[col % 4];
             f(row, col, v);
         }
     }
