@@ -284,12 +284,13 @@ int launch_parts(const Packing &p, hipStream_t s) {
 // their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts.
 constexpr int kFewWaves = 8;   // wavefronts a workgroup
 
-// fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles 0.46), 16-bit ones up to 16 (0.063 and 0.067)
-// and small products up to 64 (64 rows, 300 x 800: 15 us and 28; 48 rows, 1,024 x 2,816: 30 and 30; 32 rows, 4,096 x 10,240:
-// 91 and 67): what they read of x again and again grows with the rows.
+// fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles, whose parts are 1.5 times as many bytes, 0.46),
+// 16-bit ones where the products are small (1 row, 4,096 x 10,240: 48 us, in tiles 50; 16 rows: 63 and 50; 16 rows, 1,024 x
+// 2,816: 15 and 19) or tiles would need copies of the weights. What they read of x again and again grows with the rows.
 template <class T>
-bool few_rows(const FfnArgs &a) {
-    return a.rows <= 16 || (a.rows <= 64 && (sizeof(T) == 4 || a.rows * a.dim * a.hidden <= int64_t(1) << 27));
+bool few_rows(const FfnArgs &a, bool copies) {
+    return a.rows <= 64 && (sizeof(T) == 4 || a.rows == 1 || (copies && a.rows <= 16) ||
+                            a.rows * a.dim * a.hidden <= int64_t(1) << 26);
 }
 
 struct FewArgs {
@@ -440,7 +441,8 @@ int forward_few(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
 // One plan of a pass: where its arrays lie, without a workspace only how many bytes they are.
 template <class T>
 int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
-    if (few_rows<T>(a)) return forward_few<T>(a, c, launch, s);
+    const bool copies = !in_place(a.type, a.w_gate, a.w_up, a.hidden, a.dim) || !in_place(a.type, a.w_down, a.dim, a.hidden);
+    if (launch ? few_rows<T>(a, copies) : few_rows<T>(a, false) && few_rows<T>(a, true)) return forward_few<T>(a, c, launch, s);
     using K = Kind<T>;
     using E = typename K::E;
     using Up = typename K::template Tiles<true, true, true>;
@@ -456,7 +458,12 @@ int forward(const FfnArgs &a, Carve &c, bool launch, hipStream_t s) {
     const Cut up = choose_cut_of<Up>(n, 2 * f, d, sizeof(T) + K::P),
               down = choose_cut_of<Down>(n, d, f, sizeof(T));
     float *part = c.take<float>(std::max(up.floats, down.floats));
-    if (!launch) return W2V_OK;
+    if (!launch) {   // arrays that need no copies may go the other way
+        Carve other;
+        if (few_rows<T>(a, true)) forward_few<T>(a, other, false, s);
+        c.off = std::max(c.off, other.off);
+        return W2V_OK;
+    }
     if (int rc = check_workspace(c.base, c.cap, c.used())) return rc;
     if (up.tiles > kMaxTiles || down.tiles > kMaxTiles) return fail(W2V_E_RANGE, "too many rows for one call");
     if (int rc = launch_parts<T>(pack, s)) return rc;

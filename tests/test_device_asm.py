@@ -38,3 +38,26 @@ def test_tree_merge_waits_for_its_stores_at_the_grid_barrier(tmp_path):
                 grid_barriers += 1
                 assert not pending, f"instruction {i}: a store may still be on its way"
     assert grid_barriers == 2   # after the first merge, and at the end of a generation
+
+
+def test_m0_holds_nothing_but_the_place_of_a_load_into_lds(tmp_path):
+    """The products' loads of LDS are assembly that sets M0 without the compiler's knowledge: no other instruction of their
+    sources may read or write it."""
+    if not os.path.exists(_build.HIPCC):
+        pytest.skip("hipcc not found")
+    for source in ("ffn.hip", "muon.hip"):
+        out = str(tmp_path / (source + ".s"))
+        subprocess.check_call([_build.HIPCC, *_build.FLAGS, "-S", "--cuda-device-only", os.path.join(_build.CSRC, source),
+                               "-o", out], stderr=subprocess.DEVNULL)
+        with open(out) as f:
+            ins = [line.split(";")[0].strip() for line in f]
+        ins = [line for line in ins if re.match(r"[a-z]+_\w+", line)]
+        uses = [i for i, line in enumerate(ins) if re.search(r"\bm0\b", line)]
+        assert len(uses) > 100
+        for i in uses:
+            assert re.match(r"s_mov_b32 m0, s\d+$", ins[i]), ins[i]
+            assert ins[i + 1].startswith("s_nop") and ins[i + 2].startswith("global_load_lds_dwordx4"), ins[i:i + 3]
+        loads = sum(line.startswith("global_load_lds") for line in ins)
+        assert loads == len(uses)
+        # a relative register index would go through M0 or the index mode
+        assert not any(line.startswith(("s_set_gpr_idx", "v_movrel", "s_movrel")) for line in ins)
