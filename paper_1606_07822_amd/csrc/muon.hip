@@ -249,21 +249,24 @@ struct StepJob {
     }
 };
 
-template <int P, bool A, bool B>
+// SQUARE: tiles as wide as tall only.
+template <int P, bool A, bool B, bool SQUARE>
 struct Tiles;
-template <bool A, bool B>
-struct Tiles<1, A, B> {
+template <bool A, bool B, bool SQUARE>
+struct Tiles<1, A, B, SQUARE> {
     using Large = Tile<E, 1, 256, 256, 2, 4, 64, A, B>;
     using Small = Tile<E, 1, 128, 128, 2, 2, 64, A, B>;
     using Deep = Tile<E, 1, 128, 128, 2, 2, 64, A, B, false, false, 5>;
     using Tiny = Tile<E, 1, 64, 64, 2, 2, 64, A, B, false, false, 4>;
+    using Middle = std::conditional_t<SQUARE, Deep, Tile<E, 1, 256, 128, 4, 2, 64, A, B, false, false, 3>>;
 };
-template <bool A, bool B>
-struct Tiles<2, A, B> {
+template <bool A, bool B, bool SQUARE>
+struct Tiles<2, A, B, SQUARE> {
     using Large = Tile<E, 2, 256, 256, 2, 4, 32, A, B>;
     using Small = Tile<E, 2, 128, 128, 2, 2, 32, A, B>;
-    using Deep = Tile<E, 2, 128, 128, 2, 2, 32, A, B, false, false, 5>;
+    using Deep = Tile<E, 2, 128, 128, 4, 2, 32, A, B, false, false, 5>;
     using Tiny = Tile<E, 2, 64, 64, 2, 2, 32, A, B, false, false, 4>;
+    using Middle = std::conditional_t<SQUARE, Deep, Tile<E, 2, 256, 128, 4, 2, 32, A, B, false, false, 3>>;
 };
 
 // Whether a launch of `count` symmetric products of g x g tiles makes them all (up to a quarter of the CUs: with all of them
@@ -289,9 +292,9 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     w.x_stride = ceil_div(cols, 64) * 64;
     w.a_stride = ceil_div(w.r, 64) * 64;
     const auto square = [&](auto tile) { return square_tiles(ceil_div(w.r, decltype(tile)::type::BM), count); };
-    w.gram = choose_cut<Tiles<P, true, true>>(w.c, 4 * P, square);
-    w.poly = choose_cut<Tiles<P, true, true>>(w.r, 6 * P, square);
-    w.step = choose_cut<Tiles<P, true, true>>(
+    w.gram = choose_cut<Tiles<P, true, true, true>>(w.c, 4 * P, square);
+    w.poly = choose_cut<Tiles<P, true, true, true>>(w.r, 6 * P, square);
+    w.step = choose_cut<Tiles<P, true, true, false>>(
         w.r, 2 * P, [&](auto tile) { return count * count_tiles<typename decltype(tile)::type>(rows, cols); });
     Carve k(workspace);
     w.part = k.take<double>(static_cast<size_t>(count * kParts));
@@ -305,9 +308,9 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
 
 template <class T, int P, bool WIDE>
 int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
-    using Gram = Tiles<P, WIDE, WIDE>;
-    using Poly = Tiles<P, true, true>;
-    using Step = Tiles<P, true, !WIDE>;
+    using Gram = Tiles<P, WIDE, WIDE, true>;
+    using Poly = Tiles<P, true, true, true>;
+    using Step = Tiles<P, true, !WIDE, false>;
     for (int32_t i = 0; i < steps; ++i) {
         const E *from = w.x[i % 2];
         const int64_t x_row = P * w.x_stride * 2, a_row = P * w.a_stride * 2;   // bytes

@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "w2v_ops.h"
 
@@ -367,7 +368,7 @@ struct Tile {
     template <class F>
     static __device__ __forceinline__ void rows8(char *region, Lanes lanes, F f) {
         constexpr int kPer = kCols / 8;
-#pragma unroll 2
+#pragma unroll 4
         for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
             float v[8];
             get8(region, c / kPer, c % kPer * 2, v);
@@ -378,7 +379,7 @@ struct Tile {
     template <class F>
     static __device__ __forceinline__ void pairs8(char *region, Lanes lanes, F f) {
         constexpr int kPer = kCols / 16;
-#pragma unroll 2
+#pragma unroll 4
         for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
             const int row = c / kPer, col = c % kPer * 8, chunk = col / 16 * 8 + col % 16 / 4;
             float v[8], w[8];
@@ -426,7 +427,7 @@ template <class T>
 struct Which {
     using type = T;
 };
-enum { kLarge, kSmall, kDeep, kTiny };
+enum { kLarge, kSmall, kDeep, kTiny, kMiddle };
 struct Cut {
     int32_t kind, parts;
     int64_t tiles, whole, steps;   // steps: of one tile
@@ -577,12 +578,12 @@ int launch_tiles(const J &job, hipStream_t s) {
 // Microseconds of a step (all of a tile's products over BK of k), measured: by whether k runs along a row of either operand,
 // by parts, and by kind, where a CU has one tile at a time, and where there are more. Large tiles do 1.4 to 1.5 PFLOP/s; small
 // ones read LDS more often.
-constexpr double kStepUs[2][3][4][2] = {{{{1.50, 1.56}, {0.67, 0.44}, {0.65, 0.59}, {0.28, 0.19}},
-                                         {{2.07, 2.12}, {0.71, 0.56}, {0.74, 0.72}, {0.32, 0.21}},
-                                         {{2.16, 2.20}, {0.73, 0.56}, {1.20, 1.22}, {0.45, 0.32}}},
-                                        {{{1.46, 1.57}, {0.65, 0.43}, {0.64, 0.59}, {0.30, 0.20}},
-                                         {{2.10, 2.10}, {0.73, 0.59}, {0.78, 0.73}, {0.31, 0.22}},
-                                         {{2.20, 2.20}, {0.80, 0.68}, {1.17, 1.22}, {0.43, 0.36}}}};
+constexpr double kStepUs[2][3][5][2] = {{{{1.50, 1.56}, {0.67, 0.44}, {0.65, 0.59}, {0.28, 0.19}, {0.90, 0.93}},
+                                         {{2.07, 2.12}, {0.71, 0.56}, {0.67, 0.67}, {0.32, 0.21}, {1.15, 1.15}},
+                                         {{2.16, 2.20}, {0.73, 0.56}, {1.20, 1.22}, {0.45, 0.32}, {}}},
+                                        {{{1.46, 1.57}, {0.65, 0.43}, {0.64, 0.59}, {0.30, 0.20}, {0.87, 0.97}},
+                                         {{2.10, 2.10}, {0.73, 0.59}, {0.66, 0.68}, {0.31, 0.22}, {1.12, 1.16}},
+                                         {{2.20, 2.20}, {0.80, 0.68}, {1.17, 1.22}, {0.43, 0.36}, {}}}};
 
 // The cut with the least time by this model: the CUs take tiles in turns of their steps and two more until the first product,
 // 1 us and what an element of the result moves behind them (`bytes` of it; a CU's share of memory is 20 KB a us). Sums of
@@ -627,6 +628,7 @@ Cut choose_cut(int64_t k, double bytes, F count, bool two = false) {
     weigh(kSmall, Which<typename S::Small>{});
     weigh(kDeep, Which<typename S::Deep>{});
     weigh(kTiny, Which<typename S::Tiny>{});
+    if constexpr (!std::is_same<typename S::Middle, typename S::Deep>::value) weigh(kMiddle, Which<typename S::Middle>{});
     return best;
 }
 
@@ -645,11 +647,13 @@ inline int32_t tiles_along(int64_t size, int64_t tile) { return static_cast<int3
 // A cut's tile sizes.
 template <class S>
 int64_t tile_m(const Cut &c) {
-    return c.kind == kLarge ? S::Large::BM : c.kind == kSmall ? S::Small::BM : c.kind == kDeep ? S::Deep::BM : S::Tiny::BM;
+    constexpr int size[] = {S::Large::BM, S::Small::BM, S::Deep::BM, S::Tiny::BM, S::Middle::BM};
+    return size[c.kind];
 }
 template <class S>
 int64_t tile_n(const Cut &c) {
-    return c.kind == kLarge ? S::Large::BN : c.kind == kSmall ? S::Small::BN : c.kind == kDeep ? S::Deep::BN : S::Tiny::BN;
+    constexpr int size[] = {S::Large::BN, S::Small::BN, S::Deep::BN, S::Tiny::BN, S::Middle::BN};
+    return size[c.kind];
 }
 
 template <class S, class J>
@@ -659,6 +663,7 @@ int launch_cut(const Cut &c, float *part, J &job, hipStream_t s) {
         case kLarge: return launch_tiles<typename S::Large, J>(job, s);
         case kSmall: return launch_tiles<typename S::Small, J>(job, s);
         case kDeep: return launch_tiles<typename S::Deep, J>(job, s);
+        case kMiddle: return launch_tiles<typename S::Middle, J>(job, s);
         default: return launch_tiles<typename S::Tiny, J>(job, s);
     }
 }
