@@ -348,7 +348,8 @@ struct Tile {
         const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ turn ^ (chunk >> 4) * 4);
         return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + to * 16);
     }
-    static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], int phase, char *region) {
+    template <int phase>
+    static __device__ __forceinline__ void fill(const f4 (&acc)[FM][FN], char *region) {
         const int lane = lane_here();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -368,7 +369,7 @@ struct Tile {
     template <class F>
     static __device__ __forceinline__ void rows8(char *region, Lanes lanes, F f) {
         constexpr int kPer = kCols / 8;
-#pragma unroll 4
+#pragma unroll 2
         for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
             float v[8];
             get8(region, c / kPer, c % kPer * 2, v);
@@ -379,7 +380,7 @@ struct Tile {
     template <class F>
     static __device__ __forceinline__ void pairs8(char *region, Lanes lanes, F f) {
         constexpr int kPer = kCols / 16;
-#pragma unroll 4
+#pragma unroll 2
         for (int c = lanes.at; c < kRows * kPer; c += lanes.step) {
             const int row = c / kPer, col = c % kPer * 8, chunk = col / 16 * 8 + col % 16 / 4;
             float v[8], w[8];
@@ -392,7 +393,7 @@ struct Tile {
     template <class F>
     static __device__ __forceinline__ void columns8(char *region, Lanes lanes, F f) {
         constexpr int kPer = kRows / 8;
-#pragma unroll 2
+#pragma unroll 1
         for (int c = lanes.at; c < kCols * kPer; c += lanes.step) {
             const int row = c % kPer * 8, col = c / kPer;
             float v[8];
@@ -508,10 +509,14 @@ __global__ __launch_bounds__(T::kThreads, T::kPerSimd) void k_tiles(const J job)
         if (piece > 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody has left the regions
         job.template multiply<T>(place, step, last, lds, acc);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // everybody's reads of the last step
-#pragma unroll
+        // one copy of what follows for both phases: half the code, in the same time
+#pragma unroll 1
         for (int phase = 0; phase < T::kPhases; ++phase) {
-            if (phase > 0) lds_order();
-            T::fill(acc, phase, region);
+            lds_order();
+            if (phase == 0)
+                T::template fill<0>(acc, region);
+            else
+                T::template fill<T::kPhases - 1>(acc, region);
             lds_order();
             if (step == 0 && last == t.steps) {
                 take_region<T>(job, place, wave, phase, region, Lanes{lane_here(), kWave});
