@@ -131,7 +131,7 @@ struct Spot {
 
 // A symmetric r x r product of each matrix with itself: A = X X' (or X' X), or with `poly` aI + bA + cAA. Of it the tiles on
 // and above the diagonal are made, and the others are their mirror images; of few tiles all are made
-// (orthogonalize 100 x 400: a mirror image takes a second pass over LDS and A, 1.5 us of a launch's 7.5).
+// (orthogonalize 100 x 400: a mirror image takes a second pass over LDS).
 template <int P>
 struct SquareJob {
     Side x;
@@ -161,19 +161,22 @@ struct SquareJob {
     __device__ __forceinline__ void take(const Spot &w, int row, int col, char *region, Lanes lanes) const {
         E *to = out + w.z * r * stride * P;
         const E *a = old + w.z * r * stride * P;
+        const bool mirror = !all && w.m0 != w.n0;
         Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
             const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
-            if (m >= r || n >= stride) return;
-            finish(a + part_at<P>(m, n, stride), m, n, v);
-            store_parts8<E, P>(to + part_at<P>(m, n, stride), r - n, v);
+            Frag<E> part[P] = {};
+            if (m < r && n < stride) {
+                finish(a + part_at<P>(m, n, stride), m, n, v);
+                to_parts8<E, P>(r - n, v, part);
+                store_parts8<E, P>(to + part_at<P>(m, n, stride), part);
+            }
+            if (mirror) Q::leave8(region, i, j, part);
         });
-        if (all || w.m0 == w.n0) return;
-        // the tile below the diagonal: A is symmetric, so that row n has from column m on what column n had from row m on
-        Q::columns8(region, lanes, [&](int i, int j, float (&v)[8]) {
+        if (!mirror) return;
+        // the tile below the diagonal: row n has from column m on what column n had from row m on, zeros where there is none
+        Q::mirror8(region, lanes, [&](int i, int j, const Frag<E> (&part)[P]) {
             const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
-            if (n >= r || m >= r) return;
-            finish(a + part_at<P>(n, m, stride), n, m, v);
-            store_parts8<E, P>(to + part_at<P>(n, m, stride), r - m, v);
+            if (n < r && m < r) store_parts8<E, P>(to + part_at<P>(n, m, stride), part);
         });
     }
     // `from`: A's 8 elements from (row, col) on.

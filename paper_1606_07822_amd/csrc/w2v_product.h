@@ -102,8 +102,7 @@ __device__ __forceinline__ void to_parts(float v, E (&part)[P]) {
 
 // Parts of 8 neighbouring elements of an array (the first a multiple of 8), zeros from number `valid` on.
 template <class E, int P>
-__device__ __forceinline__ void store_parts8(E *to, int64_t valid, const float (&v)[8]) {
-    Frag<E> part[P];
+__device__ __forceinline__ void to_parts8(int64_t valid, const float (&v)[8], Frag<E> (&part)[P]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         E one[P];
@@ -111,8 +110,17 @@ __device__ __forceinline__ void store_parts8(E *to, int64_t valid, const float (
 #pragma unroll
         for (int p = 0; p < P; ++p) part[p][e] = one[p];
     }
+}
+template <class E, int P>
+__device__ __forceinline__ void store_parts8(E *to, const Frag<E> (&part)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(to + p * 32) = part[p];
+}
+template <class E, int P>
+__device__ __forceinline__ void store_parts8(E *to, int64_t valid, const float (&v)[8]) {
+    Frag<E> part[P];
+    to_parts8<E, P>(valid, v, part);
+    store_parts8<E, P>(to, part);
 }
 
 // PAIR: B's rows come in groups of 16 from two arrays in turn. TWO: k runs through a second pair of operands after the
@@ -341,11 +349,9 @@ struct Tile {
     static constexpr int kRegion = kRows * kCols * 4;
     static_assert(kRegion * kWaves <= kLds && (kCols == 32 || kCols % 64 == 0), "regions fit");
 
-    // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks, and the same
-    // two columns of rows 8 apart do, too (columns8).
+    // Four columns of a row; their place changes with the row, so that 16 rows' same columns fill all banks.
     static __device__ __forceinline__ f4 &cell(char *region, int row, int chunk) {
-        const int turn = (row & 15) ^ (row >> 2 & 4) ^ (row >> 4 & 2);
-        const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ turn ^ (chunk >> 4) * 4);
+        const int to = kCols == 32 ? chunk ^ (row >> 1 & 7) : (chunk & ~15) + ((chunk & 15) ^ (row & 15) ^ (chunk >> 4) * 4);
         return *reinterpret_cast<f4 *>(region + row * (kCols * 4) + to * 16);
     }
     template <int phase>
@@ -389,17 +395,45 @@ struct Tile {
             f(row, col, v, w);
         }
     }
-    // f(row, column, values of 8 rows).
-    template <class F>
-    static __device__ __forceinline__ void columns8(char *region, Lanes lanes, F f) {
-        constexpr int kPer = kRows / 8;
-#pragma unroll 1
-        for (int c = lanes.at; c < kCols * kPer; c += lanes.step) {
-            const int row = c % kPer * 8, col = c / kPer;
-            float v[8];
+    // Where a region's row keeps the 32 bytes with a part's 16 columns from `col` on, once its values have become parts: in the
+    // row's own place, pairs of chunks turned as a transposing read of 4 rows wants them.
+    static __device__ __forceinline__ char *pair(char *region, int row, int p, int col) {
+        constexpr int kPairs = kCols / 8;
+        const int at = (p * (kCols / 16) + col / 16) ^ (((row & 3) | (row >> 1 & 4)) & (kPairs - 1));
+        return region + row * (kCols * 4) + at * 32;
+    }
+    // rows8's f may leave 8 columns' parts there (all of a row's lanes have read it by then) ...
+    static __device__ __forceinline__ void leave8(char *region, int row, int col, const Frag<E> (&part)[P]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const float *>(&cell(region, row + e, col / 4))[col % 4];
-            f(row, col, v);
+        for (int p = 0; p < P; ++p) *reinterpret_cast<Frag<E> *>(pair(region, row, p, col) + col % 16 * 2) = part[p];
+    }
+    // ... for f(row, column, parts of 8 rows).
+    template <class F>
+    static __device__ __forceinline__ void mirror8(char *region, Lanes lanes, F f) {
+        static_assert(P <= 2 && kRows % 32 == 0, "a row's parts take its own place");
+        using S4 = short __attribute__((ext_vector_type(4)));
+        if (lanes.step > kWave)
+            __syncthreads();
+        else
+            lds_order();
+        const int lane = lanes.at % kWave;
+#pragma unroll 1
+        for (int u = lanes.at / kWave; u < kRows / 32 * (kCols / 16); u += lanes.step / kWave) {
+            const int row = u % (kRows / 32) * 32 + lane / 16 * 8, col = u / (kRows / 32) * 16;
+            Frag<E> part[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                union {
+                    S4 h[2];
+                    Frag<E> f;
+                } v;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    v.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)(
+                        pair(region, row + i * 4 + lane % 16 / 4, p, col) + lane % 4 * 8));
+                part[p] = v.f;
+            }
+            f(row, col + lane % 16, part);
         }
     }
 };
