@@ -2,6 +2,20 @@
 //
 //   M = mu M + G,  U = G + mu M (Nesterov) or M,  X = U / (|U| + eps),  five times X = (a I + b A + c A A) X with A = X X',
 //   W = W (1 - lr decay) - lr scale X
+//
+// A step is three products: A, of which half is made (it is symmetric), aI + bA + cAA with the sum and the unit matrix where
+// the product's tiles end, and X; the last one's tiles become the result, or update the weights. A matrix taller than wide is
+// multiplied from the other side, its long axis along k either way, and nothing is transposed: X is read along its rows by
+// one product and down them by the other. Matrices of one shape and type go through the launches together.
+//
+// Numbers: a step multiplies errors by up to 3.9, so between the products everything has 22 bits in two fp16 parts (three
+// products; 3.9e-6 of a 4,096 x 10,240 result in norm, fp32 products 6e-6) and sums are fp32. bf16 results take one part of
+// 11 bits, a third of the work: 1.2e-3, below bf16's own rounding of 1.7e-3. Norms are sums in 64 bits, so that squares
+// neither overflow nor vanish.
+//
+// What bounds it: the matrix cores for large matrices (4,096 x 10,240: 7.3 ms, 1,200 TFLOP/s of 16-bit products); launches'
+// starts and ends for stacks of middling ones (36 of 1,024 x 2,816 bf16: 2.87 ms, of which the products are half) and
+// launches alone for small ones (100 x 400: 92 us, seventeen).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

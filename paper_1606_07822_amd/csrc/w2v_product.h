@@ -11,8 +11,11 @@
 // A workgroup of WM x WN wavefronts makes BM x BN of C. Each step, BK of k, goes from global memory straight into one
 // of two LDS buffers while the matrix cores work on the other; a wavefront waits for its own loads and a barrier makes
 // them everybody's, once a step. Chunks change places within 256 bytes by their row, so that the 16 lanes of a phase
-// read all 64 banks. Measured on 8,192^3: 256 x 256 tiles of bf16 1.21 PFLOP/s, two fp16 parts 0.41 (three products:
-// 1.23), three bf16 parts 0.21 (six: 1.27); 128 x 128 tiles 1.07, 0.32 and 0.18.
+// read all 64 banks. Measured on 8,192^3 with results in bf16, TFLOP/s: 256 x 256 tiles of one part 1,280 (the library's
+// product 1,370), two fp16 parts 477 (three products: 1,430), 256 x 128 of three bf16 parts 218 (six: 1,310; the library's
+// product in fp32: 153); 128 x 128 tiles 1,130 and 420, 128 x 64 of three parts 168. Large tiles read LDS least and are
+// bound by the matrix cores; of short products and few tiles a launch's start and end are the larger part (some 10 us of 37
+// with 16 steps), which two small tiles a CU do not hide either: they stay in step with each other.
 #pragma once
 
 #include <hip/hip_runtime.h>
