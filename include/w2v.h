@@ -475,9 +475,9 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
  * which the backward pass takes. y may be x with the same stride; outputs may
  * not overlap any other array. Sums are fp32. With type fp32 the products keep
  * 24 bits of each factor; with 16-bit types h is rounded to type before the
- * second product. An infinity among the factors of a fp32 product may make it
- * NaN. Errors: W2V_E_ARG, W2V_E_WORKSPACE, W2V_E_RANGE (more rows than a
- * launch takes).
+ * second product (one beyond fp16's range becomes an infinity). An infinity
+ * among the factors of a fp32 product may make it NaN. Errors: W2V_E_ARG,
+ * W2V_E_WORKSPACE, W2V_E_RANGE (more rows than a launch takes).
  *
  * w2v_gated_ffn_backward: the gradients for an upstream gradient dy (rows x
  * dim), from x, the weights and g and u as the forward pass left them:
@@ -519,7 +519,7 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
  * The products keep 22 bits of each factor and sum in fp32; with type bf16
  * they keep 11, whose error, 1.2e-3 of the result in norm, is below bf16's
  * rounding. A matrix with an element that is not finite becomes NaN, the
- * others do not; one of zeros stays zero. Errors: W2V_E_ARG, W2V_E_WORKSPACE,
+ * others do not; one of zeros stays zero (NaN with eps 0). Errors: W2V_E_ARG, W2V_E_WORKSPACE,
  * W2V_E_RANGE. */
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type);
 int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t batch, int32_t rows, int32_t cols,

@@ -538,7 +538,8 @@ int w2v_muon_step(const w2v_muon_matrix *matrices_host, int32_t n, const void *p
     if (!muon_sizes_ok(matrices_host, n)) return fail(W2V_E_ARG, "bad matrices_host / n");
     if (n > 0 && !plan) return fail(W2V_E_ARG, "plan is NULL");
     if (!aligned(plan, 256)) return fail(W2V_E_ARG, "plan must be 256-byte aligned");
-    if (int rc = check_floats(m, "m", n > 0)) return rc;
+    const bool any = std::any_of(matrices_host, matrices_host + n, [](const w2v_muon_matrix &x) { return x.rows > 0 && x.cols > 0; });
+    if (int rc = check_floats(m, "m", any)) return rc;
     if (!p->lr_device && !std::isfinite(p->lr)) return fail(W2V_E_ARG, "lr must be finite");
     if (!aligned(p->lr_device, 4)) return fail(W2V_E_ARG, "lr_device is not aligned to its type");
     if (!(p->momentum >= 0.0 && p->momentum < 1.0)) return fail(W2V_E_ARG, "momentum must be in [0, 1)");

@@ -432,6 +432,16 @@ def test_orthogonalize_nothing(w2v):
         assert w2v.orthogonalize(x).shape == shape
 
 
+def test_orthogonalize_one_matrix_as_a_stack(w2v):
+    """A stack whose matrices lie in the same memory."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x = rows_of(g, 70, 40, torch.float32)
+    out = w2v.orthogonalize(x.expand(3, 70, 40))
+    for t in out:
+        near(t, *orth_bound(x, torch.float32))
+
+
 def test_orthogonalize_more_matrices_than_a_launch(w2v):
     """5,000 small ones go in two launches."""
     g = torch.Generator(device="cuda")
@@ -511,6 +521,15 @@ def test_muon_scale_decay_and_state(w2v):
         assert torch.equal(p, q)
         near(p, w, b)
     assert torch.equal(first.m, second.m)
+
+
+def test_muon_of_nothing(w2v):
+    """A list of empty matrices: there is no momentum, and a step does nothing."""
+    params = [torch.empty(0, 5, device="cuda"), torch.empty(7, 0, device="cuda", dtype=torch.bfloat16)]
+    opt = w2v.Muon(params, [torch.empty_like(p) for p in params])
+    assert opt.n_moments == 0
+    opt.step(0.1)
+    torch.cuda.synchronize()
 
 
 def test_muon_many_kinds_in_one_list(w2v):
