@@ -325,6 +325,63 @@ def test_more_than_four_gigabytes_of_rows(w2v):
 
 
 # ------------------------------------------------------------------ Newton-Schulz
+# tiles of every size, in each product: whole ones, cut along k into equal pieces and into pieces that start and end anywhere
+CUTS = [(1100, 66, 3041), (1946, 2431, 40), (4097, 212, 1815), (2535, 871, 1768), (510, 1544, 2384), (3619, 376, 2700),
+        (799, 2643, 631), (2293, 200, 3691), (11614, 344, 960), (7257, 323, 1670), (19978, 83, 45), (16649, 386, 72),
+        (7353, 1941, 67)]
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,d,h", CUTS)
+def test_gated_ffn_cuts(w2v, n, d, h, kind):
+    act = "silu" if n % 2 else "gelu"
+    rng, x, wg, wu, wd = inputs(n, d, h, kind, n + d + h, pad=8)
+    dy = rows_of(rng, n, d, kind, 0.3)
+    want, bounds = block64(x, wg, wu, wd, act, kind)
+    y, gate, up = w2v.gated_ffn(x, wg, wu, wd, act, save=True)
+    for name, g, w, b in zip(("y", "gate", "up"), (y, gate, up), want, bounds):
+        within(g, w, b, name)
+    assert torch.equal(w2v.gated_ffn(x, wg, wu, wd, act)[0], y)
+    want, bounds = back64(dy, x, wg, wu, wd, gate, up, act, kind)
+    got = w2v.gated_ffn_backward(dy, x, wg, wu, wd, gate, up, act)
+    for name, g, w, b in zip(("dx", "dw_gate", "dw_up", "dw_down"), got, want, bounds):
+        within(g, w, b, name)
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,d,h", [(7, 60, 130), (130, 70, 300), (1100, 66, 3041), (700, 520, 1100)])
+def test_some_outputs_only(w2v, n, d, h, kind):
+    """NULL outputs through the C interface: those that are wanted are within the bounds, g and u one at a time, every set of
+    gradients, none of them."""
+    rng, x, wg, wu, wd = inputs(n, d, h, kind, 11)
+    lib, stream, t = w2v.lib(), torch.cuda.current_stream().cuda_stream, TYPES.index(kind)
+    y, gate, up = w2v.gated_ffn(x, wg, wu, wd, save=True)
+    none = w2v.CRows(None, 0)
+
+    def rows(a):
+        return none if a is None else w2v.CRows(a.data_ptr(), a.stride(0))
+    ws = w2v.gated_ffn_workspace(x, h)
+    want, bounds = block64(x, wg, wu, wd, "silu", kind)
+    for on in range(4):
+        outs = [torch.full_like(y, float("nan"))] + [torch.full_like(gate, float("nan")) if on >> i & 1 else None
+                                                     for i in range(2)]
+        assert lib.w2v_gated_ffn(rows(x), rows(wg), rows(wu), rows(wd), n, d, h, t, 0, *map(rows, outs), ws.data_ptr(),
+                                 ws.numel(), stream) == 0
+        for name, g, w, b in zip(("y", "gate", "up"), outs, want, bounds):
+            if g is not None:
+                within(g, w, b, (on, name))
+    dy = rows_of(rng, n, d, kind, 0.3)
+    ws = w2v.gated_ffn_workspace(x, h, grads=True)
+    want, bounds = back64(dy, x, wg, wu, wd, gate, up, "silu", kind)
+    for on in range(16):
+        outs = [torch.full_like(a, float("nan")) if on >> i & 1 else None for i, a in enumerate((x, wg, wu, wd))]
+        assert lib.w2v_gated_ffn_backward(rows(dy), rows(x), rows(wg), rows(wu), rows(wd), rows(gate), rows(up), n, d, h, t, 0,
+                                          *map(rows, outs), ws.data_ptr(), ws.numel(), stream) == 0
+        for name, g, w, b in zip(("dx", "dw_gate", "dw_up", "dw_down"), outs, want, bounds):
+            if g is not None:
+                within(g, w, b, (on, name))
+
+
 def steps64(x, steps=5, eps=1e-7, keep=lambda x: x):
     """In 64 bits; keep: what becomes of each matrix that the kernels store between products."""
     a, b, c = COEFFICIENTS
@@ -375,6 +432,18 @@ def test_orthogonalize(w2v, m, n, kind):
     if min(m, n) >= 50:
         s = torch.linalg.svdvals(out.double())
         assert s.max() < 1.25 and s.median() > 0.6
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("count,m,n", [(1, 1500, 1600), (1, 2300, 2000), (1, 2300, 5000), (5, 600, 1000), (40, 300, 260)])
+def test_orthogonalize_cuts(w2v, count, m, n, kind):
+    """More tiles than one turn of the card, one matrix's and a stack's, and k cut into pieces of several lengths."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m)
+    x = torch.randn(count, m, n, generator=g, device="cuda").to(kind)
+    out = w2v.orthogonalize(x)
+    for i in range(0, count, 13):
+        near(out[i], *orth_bound(x[i], kind))
 
 
 @pytest.mark.parametrize("kind", TYPES, ids=IDS)
