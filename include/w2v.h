@@ -513,14 +513,14 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
  * Nearly orthogonal matrices by Newton-Schulz products: X = g / (|g| + eps)
  * with the Frobenius norm, then `steps` (1..20) times X = (a I + b A + c A A) X
  * with A = X X' and a, b, c = 3.4445, -4.7750, 2.0315, which brings singular
- * values between 0.7 and 1.2 in five steps. g and out: batch matrices of rows
- * x cols elements of type (sides up to 2^20), a row `stride` and a matrix
- * `step` elements behind the one before; out may be g with the same strides.
- * The products keep 22 bits of each factor and sum in fp32; with type bf16
- * they keep 11, whose error, 1.2e-3 of the result in norm, is below bf16's
- * rounding. A matrix with an element that is not finite becomes NaN, the
- * others do not; one of zeros stays zero (NaN with eps 0). Errors: W2V_E_ARG, W2V_E_WORKSPACE,
- * W2V_E_RANGE. */
+ * values between 0.7 and 1.2 in five steps. g and out: batch (up to 2^31 - 1)
+ * matrices of rows x cols elements of type (sides up to 2^20), a row `stride`
+ * and a matrix `step` elements behind the one before; out may be g with the
+ * same strides. The products keep 22 bits of each factor and sum in fp32; with
+ * type bf16 they keep 11, whose error, 1.2e-3 of the result in norm, is below
+ * bf16's rounding. A matrix with an element that is not finite becomes NaN, the
+ * others do not; one of zeros stays zero (NaN with eps 0). Errors: W2V_E_ARG,
+ * W2V_E_WORKSPACE, W2V_E_RANGE. */
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type);
 int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t batch, int32_t rows, int32_t cols,
                       int32_t type, int32_t steps, double eps, void *out, int64_t out_stride, int64_t out_step,

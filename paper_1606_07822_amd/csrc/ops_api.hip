@@ -463,7 +463,8 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
 }
 
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type) {
-    const bool ok = batch >= 0 && rows >= 0 && cols >= 0 && rows <= kMuonMaxSide && cols <= kMuonMaxSide && type_ok(type);
+    const bool ok = batch >= 0 && batch <= INT32_MAX && rows >= 0 && cols >= 0 && rows <= kMuonMaxSide && cols <= kMuonMaxSide &&
+                    type_ok(type);
     return ok ? orthogonalize_bytes(batch, rows, cols, type) : 0;
 }
 
@@ -472,8 +473,8 @@ int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t b
                       void *workspace, size_t workspace_bytes, void *hip_stream) {
     set_error("");
     if (!type_ok(type)) return fail(W2V_E_ARG, "type must be 0 (fp32), 1 (bf16) or 2 (fp16)");
-    if (batch < 0 || rows < 0 || cols < 0 || rows > kMuonMaxSide || cols > kMuonMaxSide)
-        return fail(W2V_E_ARG, "batch must be >= 0, rows and cols in 0..2^20");
+    if (batch < 0 || batch > INT32_MAX || rows < 0 || cols < 0 || rows > kMuonMaxSide || cols > kMuonMaxSide)
+        return fail(W2V_E_ARG, "batch must be in 0..2^31 - 1, rows and cols in 0..2^20");
     if (steps < 1 || steps > 20) return fail(W2V_E_ARG, "steps must be in 1..20");
     if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(W2V_E_ARG, "eps must be >= 0 and finite");
     if (batch > 0 && rows > 0 && cols > 0) {

@@ -85,7 +85,16 @@ def orth_args(**kw):
     return list(a.values())
 
 
+def test_orthogonalize_workspace_sizes(w2v):
+    """Nothing for sizes out of range, the largest counts of matrices among them (a count that wrapped divided by zero)."""
+    size = w2v.lib().w2v_orthogonalize_workspace_bytes
+    assert size(1, 6, 8, 0) > 0 and size(2**31 - 1, 1, 1, 0) > 0 and size(0, 6, 8, 0) == 0
+    for bad in ((2**31, 1, 1, 0), (2**63 - 1, 1, 1, 0), (2**63 - 4000, 6, 8, 1), (-1, 1, 1, 0), (1, 2**20 + 1, 1, 0), (1, 1, 1, 3)):
+        assert size(*bad) == 0
+
+
 @pytest.mark.parametrize("kw,code,msg", [
+    (dict(batch=2**31), -1, "batch"), (dict(batch=2**63 - 1, g_step=0, out_step=48), -1, "batch"),
     (dict(g=None), -1, "g is NULL"), (dict(out=None), -1, "out is NULL"), (dict(g_stride=7), -1, "g's"), (dict(out_stride=7), -1, "out's"),
     (dict(batch=-1), -1, "batch"), (dict(rows=-1), -1, "rows"), (dict(cols=2**20 + 1), -1, "cols"), (dict(type=3), -1, "type"),
     (dict(steps=0), -1, "steps"), (dict(steps=21), -1, "steps"), (dict(eps=-1.0), -1, "eps"), (dict(eps=NAN), -1, "eps"),
