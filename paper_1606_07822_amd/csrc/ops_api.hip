@@ -120,7 +120,7 @@ bool ffn_sizes_ok(int64_t rows, int32_t dim, int32_t hidden, int32_t type) {
     return rows >= 0 && rows <= INT32_MAX && dim >= 1 && dim <= kFfnMaxDim && hidden >= 1 && hidden <= kFfnMaxDim && type_ok(type);
 }
 
-// An array of a call, for the checks: an output may not be another array, except where `may` names one.
+// An array of a call, for the checks: an output may not be another array (of no rows it may: nothing lies there).
 struct Named {
     w2v_rows r;
     int64_t rows, cols;
@@ -135,7 +135,7 @@ int check_arrays(const Named *a, int n, int32_t type) {
     }
     for (int i = 0; i < n; ++i)
         for (int j = 0; j < n; ++j)
-            if (i != j && a[i].out && a[i].r.p && a[i].r.p == a[j].r.p)
+            if (i != j && a[i].out && a[i].r.p && a[i].r.p == a[j].r.p && a[i].rows > 0 && a[j].rows > 0)
                 return fail(W2V_E_ARG, std::string(a[i].name) + " may not be " + a[j].name);
     return W2V_OK;
 }
@@ -441,7 +441,7 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
     if (int rc = check_in_place(dx, dy, rows, "dx may be dy")) return rc;
     if (int rc = check_in_place(dx, x, rows, "dx may be x")) return rc;
     for (const w2v_rows &w : {w_gate, w_up, w_down, gate, up})
-        if (dx.p && w.p == dx.p) return fail(W2V_E_ARG, "dx may be no other array than dy or x");
+        if (rows > 0 && dx.p && w.p == dx.p) return fail(W2V_E_ARG, "dx may be no other array than dy or x");
     FfnArgs a{};
     a.rows = rows;
     a.dim = dim;

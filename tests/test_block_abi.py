@@ -65,6 +65,15 @@ def test_gated_ffn_backward_argument_errors(w2v, kw, code, msg):
     assert msg in w2v.last_error()
 
 
+def test_arrays_of_no_rows_may_lie_anywhere(w2v):
+    """Where they end at another array, too: nothing is read or written there."""
+    for kw in (dict(gate=(UP, 12)), dict(up=(WD, 12)), dict(y=(GATE, 8)), dict(y=(X, 9)), dict(gate=(X, 12), up=(X, 12), y=(X, 8))):
+        assert w2v.lib().w2v_gated_ffn(*forward_args(w2v, rows=0, **kw)) == 0, kw
+    none = (None, 0)
+    for dx in ((WG, 8), (GATE, 12), (X, 8)):
+        assert w2v.lib().w2v_gated_ffn_backward(*backward_args(w2v, rows=0, dx=dx, dw_gate=none, dw_up=none, dw_down=none)) == 0
+
+
 def test_gated_ffn_workspace_sizes(w2v):
     """Nothing for no rows or for sizes out of range; never less for more rows."""
     for name in ("w2v_gated_ffn_workspace_bytes", "w2v_gated_ffn_backward_workspace_bytes"):
