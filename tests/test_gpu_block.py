@@ -193,6 +193,22 @@ def test_in_place(w2v, n, kind):
 
 
 @pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,d,h", [(6, 40, 56), (200, 72, 104), (513, 33, 95)])
+def test_inputs_that_are_one_array(w2v, n, d, h, kind):
+    """Tied weights, an upstream gradient that is x, g and u in one place: inputs may be each other."""
+    _, x, w, _, wd = inputs(n, d, h, kind, 31)
+    want, bounds = block64(x, w, w, wd, "silu", kind)
+    y, gate, up = w2v.gated_ffn(x, w, w, wd, save=True)
+    for name, g, t, b in zip(("y", "gate", "up"), (y, gate, up), want, bounds):
+        within(g, t, b, name)
+    assert torch.equal(gate, up)
+    want, bounds = back64(x, x, w, w, wd, gate, gate, "silu", kind)
+    got = w2v.gated_ffn_backward(x, x, w, w, wd, gate, gate)
+    for name, g, t, b in zip(("dx", "dw_gate", "dw_up", "dw_down"), got, want, bounds):
+        within(g, t, b, name)
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
 def test_no_rows(w2v, kind):
     _, x, wg, wu, wd = inputs(0, 12, 20, kind, 1)
     y, gate, up = w2v.gated_ffn(x, wg, wu, wd, save=True)
@@ -349,6 +365,26 @@ def test_gated_ffn_cuts(w2v, n, d, h, kind):
 
 
 @pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,d,h", [(1, 2**20, 3), (2, 5, 2**20), (90, 2**20, 2), (70, 3, 2**20)])
+def test_gated_ffn_widest(w2v, n, d, h, kind):
+    """The widest sizes that are taken, with few rows and with tiles; one more is refused."""
+    rng, x, wg, wu, wd = inputs(n, d, h, kind, 21)
+    dy = rows_of(rng, n, d, kind, 0.3)
+    want, bounds = block64(x, wg, wu, wd, "gelu", kind)
+    y, gate, up = w2v.gated_ffn(x, wg, wu, wd, "gelu", save=True)
+    for name, g, w, b in zip(("y", "gate", "up"), (y, gate, up), want, bounds):
+        within(g, w, b, name)
+    want, bounds = back64(dy, x, wg, wu, wd, gate, up, "gelu", kind)
+    got = w2v.gated_ffn_backward(dy, x, wg, wu, wd, gate, up, "gelu")
+    for name, g, w, b in zip(("dx", "dw_gate", "dw_up", "dw_down"), got, want, bounds):
+        within(g, w, b, name)
+    sizes = (d + 1, h) if d == 2**20 else (d, h + 1)
+    a = [torch.zeros(s, dtype=kind, device="cuda") for s in ((1, sizes[0]), (sizes[1], sizes[0]), (sizes[1], sizes[0]), sizes)]
+    with pytest.raises(w2v.W2VError):
+        w2v.gated_ffn(*a)
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
 @pytest.mark.parametrize("n,d,h", [(7, 60, 130), (130, 70, 300), (1100, 66, 3041), (700, 520, 1100)])
 def test_some_outputs_only(w2v, n, d, h, kind):
     """NULL outputs through the C interface: those that are wanted are within the bounds, g and u one at a time, every set of
@@ -432,6 +468,17 @@ def test_orthogonalize(w2v, m, n, kind):
     if min(m, n) >= 50:
         s = torch.linalg.svdvals(out.double())
         assert s.max() < 1.25 and s.median() > 0.6
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("m,n", [(1, 2**20), (2**20, 3), (130, 2**18 + 5), (2**17 - 1, 200)])
+def test_orthogonalize_longest(w2v, m, n, kind):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + n)
+    x = torch.randn(m, n, generator=g, device="cuda").to(kind)
+    near(w2v.orthogonalize(x), *orth_bound(x, kind))
+    with pytest.raises(w2v.W2VError):
+        w2v.orthogonalize(torch.zeros(2**20 + 1, 1, dtype=kind, device="cuda"))
 
 
 @pytest.mark.parametrize("kind", TYPES, ids=IDS)
