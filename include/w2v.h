@@ -474,10 +474,13 @@ int w2v_adamw_moments(const void *m, const void *v, const float *m_scale, const 
  * gate and up (rows x hidden elements of type, may be NULL) receive g and u,
  * which the backward pass takes. y may be x with the same stride; outputs may
  * not overlap any other array. Sums are fp32. With type fp32 the products keep
- * 24 bits of each factor; with 16-bit types h is rounded to type before the
- * second product (one beyond fp16's range becomes an infinity). An infinity
- * among the factors of a fp32 product may make it NaN. Errors: W2V_E_ARG,
- * W2V_E_WORKSPACE, W2V_E_RANGE (more rows than a launch takes).
+ * 24 bits of each factor. With 16-bit types h is rounded to type before the
+ * second product (one beyond the type's range becomes an infinity), but for few
+ * rows it stays fp32: for one, for up to 64 where rows * dim * hidden is at most
+ * 2^26, for up to 16 where a weight's rows are not whole aligned 16 bytes or
+ * w_gate's and w_up's strides differ. An infinity among the factors of a fp32
+ * product may make it NaN. Errors: W2V_E_ARG, W2V_E_WORKSPACE, W2V_E_RANGE
+ * (more rows than a launch takes).
  *
  * w2v_gated_ffn_backward: the gradients for an upstream gradient dy (rows x
  * dim), from x, the weights and g and u as the forward pass left them:

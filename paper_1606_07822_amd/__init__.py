@@ -991,8 +991,9 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
               ) -> tuple[torch.Tensor, torch.Tensor | None, torch.Tensor | None]:
     """(y, gate, up) of y = (act(x w_gate') * (x w_up')) w_down' for rows x [rows, dim], weights [hidden, dim] twice and
     [dim, hidden], all of one type; act "silu" or "gelu". With save, gate and up [rows, hidden] hold the two products for
-    gated_ffn_backward (None otherwise). y goes into out, which may be x; gate and up into those that are given. y carries
-    no autograd graph. Does not sync."""
+    gated_ffn_backward (None otherwise). y goes into out, which may be x; gate and up into those that are given. 16-bit
+    tensors' act() * () is rounded to their type before it meets w_down, except in calls of few rows. y carries no autograd
+    graph. Does not sync."""
     sizes, arrays = _block_of(x, w_gate, w_up, w_down, act)
     n, d, h = sizes[:3]
     y = torch.empty(n, d, dtype=x.dtype, device=x.device) if out is None else out

@@ -10,8 +10,8 @@
 //
 // Numbers: g, u and all sums are fp32. With 16-bit types h, dg and du are rounded to the type (R) between two products, as
 // the matrix cores take them; that adds to a result's own rounding one of the same size, spread over its terms (bf16: 2.3e-3
-// of the result in norm, where rounding the result alone leaves 1.7e-3). fp32 is multiplied as three bf16 parts of 8 bits,
-// six products (2.4e-7 of the result; the library's fp32 product: 7e-7).
+// of the result in norm, where rounding the result alone leaves 1.7e-3). The forward pass of few rows keeps h in fp32. fp32 is
+// multiplied as three bf16 parts of 8 bits, six products (2.4e-7 of the result; the library's fp32 product: 7e-7).
 //
 // What bounds it: the matrix cores for wide rows (16,384 rows of 4,096 bf16, hidden 10,240: 3.3 ms, 1,230 TFLOP/s; backward,
 // 8,192 rows: 3.5 ms, 1,180); memory and the matrix cores in turn for narrow ones, whose tiles end after 10 steps (65,536 rows
@@ -313,8 +313,13 @@ int launch_parts(const Packing &p, hipStream_t s) {
 // Where there are few rows every weight is read for them, and the weights' bytes are the time. A workgroup takes 16 columns
 // of the result, its wavefronts take turns along k, 128 bytes of each of the 16 weight rows at a time straight from memory
 // into the matrix cores' registers (rows need no alignment but their elements'); the wavefronts' sums are joined in LDS in
-// their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts.
+// their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts, or in fp32 in rows where one h is past
+// the type's range (its two parts would be opposite infinities): the sums are made again for these, and the others keep theirs.
 constexpr int kFewWaves = 8;   // wavefronts a workgroup
+
+// The least number that a 16-bit type rounds to an infinity.
+template <class T>
+constexpr float kPast = std::is_same<T, __bf16>::value ? 0x1.ffp127f : 65520.0f;
 
 // fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles, whose parts are 1.5 times as many bytes, 0.46),
 // 16-bit ones where the products are small (1 row, 4,096 x 10,240: 48 us, in tiles 50; 16 rows: 63 and 50; 16 rows, 1,024 x
@@ -334,11 +339,12 @@ struct FewArgs {
 };
 
 // Products of 16 weight rows' chunks (V elements of each lane's row) with 16 rows' of x.
-template <class T, class X, int V>
+template <bool FP32, class T, class X, int V>
 __device__ __forceinline__ f4 few_product(const Pack<T, V> &w, const Pack<X, V> &x, f4 acc) {
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (FP32) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], acc, 0, 0, 0);
+        for (int e = 0; e < V; ++e)
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(static_cast<float>(w.v[e]), static_cast<float>(x.v[e]), acc, 0, 0, 0);
     } else {
         Frag<T> a, hi, lo;
 #pragma unroll
@@ -356,6 +362,7 @@ __device__ __forceinline__ f4 few_product(const Pack<T, V> &w, const Pack<X, V> 
 template <class T, class X, int NT, bool PAIR>
 __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const FewArgs a) {
     constexpr int V = 16 / sizeof(T), kGroup = 8 * V, kArrays = PAIR ? 2 : 1;
+    constexpr bool kParts = sizeof(T) == 2 && sizeof(X) == 4;
     const int lane = lane_id(), wave = static_cast<int>(threadIdx.x) / kWave, c0 = static_cast<int>(blockIdx.x) * 16;
     const int64_t row = min(c0 + lane % 16, a.cols - 1);
     const T *w[kArrays];
@@ -365,9 +372,10 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const FewArgs a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) x[t] = static_cast<const X *>(a.x) + min(t * 16 + lane % 16, a.n - 1) * a.x_stride;
     f4 acc[NT][kArrays] = {};
+    float most[NT] = {};   // the largest |x| that the lane has met
     const int full = a.k / kGroup, lead = lane / 16 * V;
     // a lane's chunks of a group: number lane / 16 and 4 further on
-    auto group = [&](int g, auto whole) {
+    auto group = [&](int g, auto whole, auto fp32) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int at = g * kGroup + c * 4 * V + lead;
@@ -381,12 +389,35 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const FewArgs a) {
                 const Pack<X, V> px = decltype(whole)::value ? *reinterpret_cast<const Pack<X, V> *>(x[t] + at)
                                                              : raw_cols<X, V>(x[t] + at, 0, valid);
 #pragma unroll
-                for (int i = 0; i < kArrays; ++i) acc[t][i] = few_product<T, X, V>(pw[i], px, acc[t][i]);
+                for (int i = 0; i < kArrays; ++i) acc[t][i] = few_product<decltype(fp32)::value>(pw[i], px, acc[t][i]);
+                if constexpr (kParts)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) most[t] = fmaxf(most[t], fabsf(px.v[e]));
             }
         }
     };
-    for (int g = wave; g < full; g += kFewWaves) group(g, std::true_type{});
-    if (a.k % kGroup != 0 && full % kFewWaves == wave) group(full, std::false_type{});
+    auto groups = [&](auto fp32) {
+        for (int g = wave; g < full; g += kFewWaves) group(g, std::true_type{}, fp32);
+        if (a.k % kGroup != 0 && full % kFewWaves == wave) group(full, std::false_type{}, fp32);
+    };
+    groups(std::bool_constant<sizeof(T) == 4>{});
+    if constexpr (kParts) {
+        uint64_t past[NT], any = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) any |= past[t] = __ballot(!(most[t] < kPast<T>));
+        if (any) {   // once more in fp32; rows without such a number keep their sums
+            f4 parts[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                parts[t] = acc[t][0];
+                acc[t][0] = f4{};
+            }
+            groups(std::true_type{});
+#pragma unroll
+            for (int t = 0; t < NT; ++t)   // four lanes have one row
+                if (!((past[t] | past[t] >> 16 | past[t] >> 32 | past[t] >> 48) >> lane % 16 & 1)) acc[t][0] = parts[t];
+        }
+    }
     __shared__ f4 part[kFewWaves][NT][kArrays][kWave];
 #pragma unroll
     for (int t = 0; t < NT; ++t)

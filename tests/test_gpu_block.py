@@ -232,6 +232,49 @@ def test_a_row_that_is_not_finite_stays_alone(w2v, n, kind):
         assert torch.equal(y[rest], clean[rest]) and not y[n // 2].isfinite().any()
 
 
+@pytest.mark.parametrize("kind", TYPES[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n", [1, 5, 16, 20, 33, 64, 300])
+def test_h_beyond_the_range_of_its_type(w2v, n, kind):
+    """Row n // 2's first h is finite in fp32 and past the type's largest number; it meets weights that bring it back. Few rows
+    keep h in fp32. In tiles it is rounded to the type, an infinity, which the weights' signs hand on."""
+    _, x, wg, wu, wd = inputs(n, 24, 40, kind, 9)
+    at = n // 2
+    wg[0], wu[0], x[:, :2], x[at] = 0, 0, 0, 0   # the other rows' first h is 0
+    if kind == torch.float16:                  # 300 * 300
+        x[at, 0], wg[0, 0], wu[0, 0] = 1, 300, 300
+        wd[:, 0] = torch.linspace(-0.01, 0.01, 24, device="cuda").to(kind)
+    else:                                      # 2^64 (2^64 - 2^53), between bf16's largest number and fp32's
+        x[at, :2] = 1
+        wg[0, 0], wg[0, 1], wu[0, 0] = 2.0**64, -2.0**53, 2.0**64
+        wd[:, 0] = torch.linspace(-1, 1, 24, device="cuda").to(kind) * 2.0**-120
+    h = x[at].double() @ wg[0].double() * (x[at].double() @ wu[0].double())
+    assert torch.finfo(kind).max < h < torch.finfo(torch.float32).max
+    (want, gate, up), (off, _, _) = block64(x, wg, wu, wd, "silu", kind)
+    y, g, u = w2v.gated_ffn(x, wg, wu, wd, save=True)
+    rest = torch.arange(n, device="cuda") != at
+    if n <= 64:
+        within(y, want, off, "y")
+    else:
+        within(y[rest], want[rest], off[rest], "y")
+        assert torch.equal(y[at], wd[:, 0] * float("inf"))
+
+
+@pytest.mark.parametrize("n", [1, 7, 40])
+def test_an_infinite_h_of_few_rows(w2v, n):
+    """g u past fp32's range: an infinity of the weight's sign in that row alone, as the sum over h has it."""
+    _, x, wg, wu, wd = inputs(n, 24, 40, torch.bfloat16, 9)
+    clean = w2v.gated_ffn(x, wg, wu, wd)[0]
+    at = n // 2
+    wg[0], wu[0], wg[0, 0], wu[0, 0] = 0, 0, 2.0**70, 2.0**70
+    x[:, 0] = 0
+    base = w2v.gated_ffn(x, wg, wu, wd)[0]
+    x[at, 0] = 1
+    y = w2v.gated_ffn(x, wg, wu, wd)[0]
+    rest = torch.arange(n, device="cuda") != at
+    assert clean.isfinite().all() and torch.equal(y[rest], base[rest])
+    assert torch.equal(y[at], wd[:, 0] * float("inf"))
+
+
 @pytest.mark.parametrize("scale", [1e-18, 1e15])
 def test_small_and_large_fp32_values(w2v, scale):
     """Parts of 8 bits have fp32's range."""
