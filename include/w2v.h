@@ -520,8 +520,10 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
  * matrices of rows x cols elements of type (sides up to 2^20), a row `stride`
  * and a matrix `step` elements behind the one before; out may be g with the
  * same strides. The products keep 22 bits of each factor and sum in fp32; with
- * type bf16 they keep 11, whose error, 1.2e-3 of the result in norm, is below
- * bf16's rounding. A matrix with an element that is not finite becomes NaN, the
+ * type bf16 what is added to X in a step keeps 11, and X itself 22: an error of
+ * some 1e-3 of the result in norm whatever the singular values, 3.6e-3 where all
+ * of its roundings have one sign (a unit matrix), beside the 1.7e-3 of bf16's
+ * rounding. A matrix with an element that is not finite becomes NaN, the
  * others do not; one of zeros stays zero (NaN with eps 0). Errors: W2V_E_ARG,
  * W2V_E_WORKSPACE, W2V_E_RANGE. */
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type);
@@ -532,7 +534,7 @@ int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t b
 /* Muon over many matrices: with G = grad grad_scale and a momentum M (fp32),
  *     M = momentum M + G;  U = G + momentum M if nesterov, else M
  *     param = param (1 - lr weight_decay) - lr scale orthogonalize(U)
- * where bf16 parameters take the products of 11 bits. The momenta lie in one
+ * where bf16 parameters take orthogonalize's products for bf16. The momenta lie in one
  * float array m, matrix i's (in row order, without gaps) from moment_offset
  * on, a multiple of 256; zeros before the first step. The plan, device memory
  * of w2v_muon_plan_bytes bytes that the caller keeps, is made once from a list

@@ -9,12 +9,25 @@
 // one product and down them by the other. Matrices of one shape and type go through the launches together.
 //
 // Numbers: a step multiplies errors by up to 3.9, so between the products everything has 22 bits in two fp16 parts (three
-// products; 3.9e-6 of a 4,096 x 10,240 result in norm, fp32 products 6e-6) and sums are fp32. bf16 results take one part of
-// 11 bits, a third of the work: 1.2e-3, below bf16's own rounding of 1.7e-3. Norms are sums in 64 bits, so that squares
-// neither overflow nor vanish.
+// products; 3.9e-6 of a 4,096 x 10,240 result in norm, fp32 products 6e-6) and sums are fp32. Norms are sums in 64 bits, so that
+// squares neither overflow nor vanish.
+//
+// bf16 results take products of one part, 11 bits, a third of the work. Rounding X itself to 11 bits would not do: that is noise
+// in all directions, and the steps multiply it by up to 3.4445 each where X has no singular value of note, 485 in all (0.1 of
+// the result for an X of rank 1). So X is carried in two parts, and a step is
+//
+//   X = (a + d) X + Q X1,   Q + d = bA + cA1 A1,   A = X1 X1'
+//
+// where 1 marks first parts, Q is rounded to one and the diagonal d is what that leaves of Q's. Errors of Q and A now multiply
+// X: they turn its singular vectors by a little and stay in its own rows' (columns') space, where p(s)/s is near one, so that
+// no later step makes them grow; X's noise passes through Q X1 alone, and Q is next to nothing in the directions where it would
+// grow. The last step, after which nothing grows, takes X1 for X. Error in norm: 1.1e-3 of the result for Gaussian matrices and
+// 0.4 to 1.1e-3 for low ranks and decaying singular values, 3.6e-3 at the most that was found, where all of a matrix's roundings
+// have one sign (all entries of one size, unit matrices); bf16's own rounding is 1.7e-3. The stack
+// below takes 3.4 ms for the 2.9 of one part throughout, 5.6 with products of two; 4,096 x 10,240 3.2, 3.0 and 7.3.
 //
 // What bounds it: the matrix cores for large matrices (4,096 x 10,240: 7.3 ms, 1,200 TFLOP/s of 16-bit products); launches'
-// starts and ends for stacks of middling ones (36 of 1,024 x 2,816 bf16: 2.87 ms, of which the products are half) and
+// starts and ends for stacks of middling ones (36 of 1,024 x 2,816 bf16: 3.4 ms, the products alone 1.5) and
 // launches alone for small ones (100 x 400: 92 us, seventeen).
 #include <hip/hip_runtime.h>
 
@@ -31,8 +44,8 @@ namespace {
 
 using E = _Float16;
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-// Everything that the steps hold is kept times 2^12 in fp16: entries of X are at most 1.21 in size, of A 1.45 and of
-// aI + bA + cAA 3.45, and the second part's absolute error, 2^-25, is 2^-37 of one.
+// Everything that the steps hold is kept times 2^12 in fp16: entries of X are at most 1.21 in size, of A 1.45, of
+// aI + bA + cAA 3.45 and of bA + cAA 2.81, and the second part's absolute error, 2^-25, is 2^-37 of one.
 constexpr float kUp = 4096.0f, kDown = 1.0f / 4096.0f;
 constexpr int kParts = 256;       // sums of squares of a matrix
 
@@ -65,6 +78,14 @@ struct Batch {
 };
 
 // ------------------------------------------------------------------ momentum and norms
+// Two parts of 8 neighbouring elements in arrays of their own; second may be null.
+__device__ __forceinline__ void store_apart8(E *first, E *second, int64_t at, int64_t valid, const float (&v)[8]) {
+    Frag<E> part[2];
+    to_parts8<E, 2>(valid, v, part);
+    *reinterpret_cast<Frag<E> *>(first + at) = part[0];
+    if (second) *reinterpret_cast<Frag<E> *>(second + at) = part[1];
+}
+
 // Both passes are bound by memory (momentum 5.6 TB/s). Block b of `blocks` of a matrix takes every `blocks`-th group of rows;
 // its threads have a place in a row and go along it: f(row, column) for the first of each N columns up to `width`.
 template <int N, class F>
@@ -108,9 +129,10 @@ __global__ __launch_bounds__(256) void k_muon_momentum(const Batch b, double *pa
     if (threadIdx.x == 0) part[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 
-// X's parts, in rows of `stride` elements with zeros behind the last column.
+// X's parts, in rows of `stride` elements with zeros behind the last column. P = 1: the second parts lie in an array of their
+// own (null where the first step is the last).
 template <class T, int P>
-__global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double *part, double eps, E *x, int64_t stride,
+__global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double *part, double eps, E *x, E *second, int64_t stride,
                                                     int64_t blocks) {
     const int64_t z = blockIdx.x / blocks;
     const Entry e = b.entry(z);
@@ -134,7 +156,10 @@ __global__ __launch_bounds__(256) void k_muon_start(const Batch b, const double 
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = ldexpf(g[i] * factor, power);
-        store_parts8<E, P>(x + part_at<P>(z * b.rows + row, col, stride), valid, g);
+        if constexpr (P == 1)
+            store_apart8(x, second, (z * b.rows + row) * stride + col, valid, g);
+        else
+            store_parts8<E, P>(x + part_at<P>(z * b.rows + row, col, stride), valid, g);
     });
 }
 
@@ -143,8 +168,8 @@ struct Spot {
     int64_t m0, n0, z;
 };
 
-// A symmetric r x r product of each matrix with itself: A = X X' (or X' X), or with `poly` aI + bA + cAA. Of it the tiles on
-// and above the diagonal are made, and the others are their mirror images; of few tiles all are made
+// A symmetric r x r product of each matrix with itself: A = X X' (or X' X), or with `poly` aI + bA + cAA (P = 1: Q and d). Of it
+// the tiles on and above the diagonal are made, and the others are their mirror images; of few tiles all are made
 // (orthogonalize 100 x 400: a mirror image takes a second pass over LDS).
 template <int P>
 struct SquareJob {
@@ -156,6 +181,7 @@ struct SquareJob {
     const E *old;        // A, where poly
     E *out;
     int64_t stride;
+    float *diagonal;     // d, `stride` a matrix (P = 1, poly)
 
     template <class Q>
     __device__ __forceinline__ Spot at(int tile) const {
@@ -183,6 +209,12 @@ struct SquareJob {
                 finish(a + part_at<P>(m, n, stride), m, n, v);
                 to_parts8<E, P>(r - n, v, part);
                 store_parts8<E, P>(to + part_at<P>(m, n, stride), part);
+                if constexpr (P == 1) {
+                    if (poly)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (m == n + e) diagonal[w.z * stride + m] = (v[e] - static_cast<float>(part[0][e])) * kDown;
+                }
             }
             if (mirror) Q::leave8(region, i, j, part);
         });
@@ -207,12 +239,13 @@ struct SquareJob {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e] *= kDown;
-            if (poly) v[e] = kC * v[e] + kB * a[e] + (row == col + e ? kA * kUp : 0.0f);
+            if (poly) v[e] = kC * v[e] + kB * a[e] + (P > 1 && row == col + e ? kA * kUp : 0.0f);
         }
     }
 };
 
-// X = (aI + bA + cAA) X, or X (aI + bA + cAA) where X is taller than wide; the last one goes into the result.
+// X = (aI + bA + cAA) X, or X (aI + bA + cAA) where X is taller than wide; the last one goes into the result. P = 1:
+// (a + d) X + Q X1, or X (a + d) + X1 Q.
 template <class T, int P, bool LAST>
 struct StepJob {
     Side a, b;
@@ -223,6 +256,30 @@ struct StepJob {
     E *out;
     int64_t stride;
     Batch batch;
+    // P = 1: X's first parts, and its second ones (LAST: none), which the new X's replace if `keep`
+    const E *first;
+    E *second;
+    int32_t keep, wide;
+    const float *diagonal;
+    int64_t diagonal_stride;
+
+    // The new X's 8 elements from (m, n) on, times 2^12, from the product's.
+    __device__ __forceinline__ void finish(int64_t z, int64_t m, int64_t n, float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= kDown;
+        if constexpr (P == 1) {
+            const int64_t at = (z * batch.rows + m) * stride + n;
+            const float *d = diagonal + z * diagonal_stride;
+            const f4 low = wide ? f4{} + d[m] : *reinterpret_cast<const f4 *>(d + n),
+                     high = wide ? low : *reinterpret_cast<const f4 *>(d + n + 4);
+            const Frag<E> x1 = *reinterpret_cast<const Frag<E> *>(first + at);
+            Frag<E> x2{};
+            if constexpr (!LAST) x2 = *reinterpret_cast<const Frag<E> *>(second + at);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] += (kA + (e < 4 ? low[e & 3] : high[e & 3])) * (static_cast<float>(x1[e]) + static_cast<float>(x2[e]));
+        }
+    }
 
     template <class Q>
     __device__ __forceinline__ Spot at(int tile) const {
@@ -244,17 +301,20 @@ struct StepJob {
             Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
                 const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
                 if (m >= batch.rows || n >= stride) return;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= kDown;
-                store_parts8<E, P>(out + part_at<P>(w.z * batch.rows + m, n, stride), batch.cols - n, v);
+                finish(w.z, m, n, v);
+                if constexpr (P == 1)
+                    store_apart8(out, keep ? second : nullptr, (w.z * batch.rows + m) * stride + n, batch.cols - n, v);
+                else
+                    store_parts8<E, P>(out + part_at<P>(w.z * batch.rows + m, n, stride), batch.cols - n, v);
             });
         } else {
             const Entry en = batch.entry(w.z);
             const float lr = batch.lr_device ? *batch.lr_device : batch.lr;
-            const float keep = 1.0f - lr * en.decay, by = batch.muon ? -lr * en.scale * (kDown * kDown) : kDown * kDown;
+            const float keep = 1.0f - lr * en.decay, by = batch.muon ? -lr * en.scale * kDown : kDown;
             Q::rows8(region, lanes, [&](int i, int j, float (&v)[8]) {
                 const int64_t m = w.m0 + row + i, n = w.n0 + col + j;
-                if (m >= batch.rows) return;
+                if (m >= batch.rows || n >= batch.cols) return;
+                finish(w.z, m, n, v);
                 T *to = static_cast<T *>(en.out) + m * en.out_stride + n;
                 float old[8] = {};
                 if (batch.muon) load8<T>(to, batch.cols - n, old);
@@ -295,6 +355,8 @@ int64_t square_tiles(int64_t g, int64_t count) { return count * (makes_all(g, co
 struct Arrays {
     double *part;
     E *x[2], *a, *b;
+    E *second;           // one part: X's second parts, and d
+    float *diagonal;
     float *sums;
     int64_t r, c, x_stride, a_stride;
     Cut gram, poly, step;
@@ -318,6 +380,10 @@ Arrays arrays_of(int64_t rows, int64_t cols, int64_t count, void *workspace) {
     for (E *&x : w.x) x = k.take<E>(static_cast<size_t>(P * count * rows * w.x_stride));
     w.a = k.take<E>(static_cast<size_t>(P * count * w.r * w.a_stride));
     w.b = k.take<E>(static_cast<size_t>(P * count * w.r * w.a_stride));
+    if (P == 1) {
+        w.second = k.take<E>(static_cast<size_t>(count * rows * w.x_stride));
+        w.diagonal = k.take<float>(static_cast<size_t>(count * w.a_stride));
+    }
     w.sums = k.take<float>(std::max({w.gram.floats, w.poly.floats, w.step.floats}));
     w.bytes = k.used();
     return w;
@@ -350,6 +416,7 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
         q.poly = 1;
         q.old = w.a;
         q.out = w.b;
+        q.diagonal = w.diagonal;
         if (int rc = launch_cut<Poly>(w.poly, w.sums, q, s)) return rc;
         const Side poly{reinterpret_cast<const char *>(w.b), a_row};
         auto step = [&](auto job) {
@@ -363,6 +430,12 @@ int run_steps(const Batch &b, const Arrays &w, int32_t steps, hipStream_t s) {
             job.out = w.x[1 - i % 2];
             job.stride = w.x_stride;
             job.batch = b;
+            job.first = from;
+            job.second = w.second;
+            job.keep = i + 2 < steps;
+            job.wide = WIDE;
+            job.diagonal = w.diagonal;
+            job.diagonal_stride = w.a_stride;
             return launch_cut<Step>(w.step, w.sums, job, s);
         };
         if (int rc = i + 1 < steps ? step(StepJob<T, P, false>{}) : step(StepJob<T, P, true>{})) return rc;
@@ -378,13 +451,13 @@ int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStr
     W2V_LAUNCH_CHECK("k_muon_momentum");
     // some four chunks of eight a thread, and no more than 4,096 workgroups a matrix
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 1024), 4096));
-    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], w.x_stride, blocks);
+    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], steps > 1 ? w.second : nullptr, w.x_stride,
+                                                                                blocks);
     W2V_LAUNCH_CHECK("k_muon_start");
     return b.rows <= b.cols ? run_steps<T, P, true>(b, w, steps, s) : run_steps<T, P, false>(b, w, steps, s);
 }
 
-// bf16 results are made from one part: 11 bits a value leave an error of 1.2e-3 of the result (in norm), below bf16's own
-// rounding; all others from two.
+// bf16 results are made by products of one part, all others of two.
 bool one_part(int32_t type) { return type == W2V_BF16; }
 
 // Matrices that go through the steps together: launches of equal shares with X within 2^27 elements, and 4,096 matrices (a

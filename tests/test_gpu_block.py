@@ -585,6 +585,82 @@ def test_orthogonalize_rows_of_very_different_sizes(w2v):
     near(w2v.orthogonalize(x), *orth_bound(x, torch.float32))
 
 
+def low_rank(g, m, n, rank):
+    """m x n of this rank; entries of 1 and -1 for rank 0, small integers, which 8 bits hold, for rank 1."""
+    if rank == 0:
+        return torch.sign(torch.randn(m, 1, generator=g, device="cuda")) * torch.sign(torch.randn(1, n, generator=g, device="cuda"))
+    a, b = (torch.randn(s, generator=g, device="cuda") for s in ((m, rank), (rank, n)))
+    return (3 * a).round().clamp(-11, 11) * (3 * b).round().clamp(-11, 11) if rank == 1 else a @ b
+
+
+def decaying(g, m, n, power):
+    """Singular values 1, 2^-power, 3^-power, ..."""
+    r = min(m, n)
+    a, b = (torch.linalg.qr(torch.randn(k, r, generator=g, device="cuda"))[0] for k in (m, n))
+    return a * torch.arange(1, r + 1, device="cuda") ** -float(power) @ b.T
+
+
+def steady_bound(want, kind, steps=5):
+    """Whatever the singular values. All types: X is stored within 2^-22, and in the directions that it lacks a step multiplies
+    what that leaves by 3.4445, in all by their sum over the steps (five: 686, 1.6e-4 of an X of norm 1; ten: 3.3e5, as it would
+    be in any arithmetic of that many bits), for a result of 0.68 at least; as much again for the sums' roundings. And the
+    result's own. bf16: as much as that again for products of 11 bits: what a step stores is within 2^-12 (3e-4 where all
+    roundings have one sign), and its factors of up to 3.9 belong to X's own directions, in which they do not pile up, so that
+    some ten such errors add up."""
+    own = torch.finfo(kind).eps / 2 * (2 if kind == torch.bfloat16 else 1)
+    grown = sum(3.4445**k for k in range(1, steps + 1)) * 2.0**-22 / 0.68
+    return (own + 2 * grown) * want.norm()
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("m,n,rank", [(1024, 1024, 0), (1024, 1024, 1), (512, 1024, 8), (1024, 512, 64), (300, 700, 8),
+                                      (1400, 300, 8), (1024, 1024, 256)])
+def test_orthogonalize_few_directions(w2v, m, n, rank, kind):
+    """Gradients of few rows have a low rank: the roundings of the directions that they lack may not grow into the result."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + n + rank)
+    x = low_rank(g, m, n, rank).to(kind)
+    want = steps64(x)
+    near(w2v.orthogonalize(x), want, steady_bound(want, kind))
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+@pytest.mark.parametrize("power", [1, 2, 4])
+def test_orthogonalize_decaying_directions(w2v, power, kind):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(power)
+    for m, n in ((512, 1024), (700, 200)):
+        x = decaying(g, m, n, power).to(kind)
+        want = steps64(x)
+        near(w2v.orthogonalize(x), want, steady_bound(want, kind))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 10])
+@pytest.mark.parametrize("m,n", [(300, 700), (700, 300)])
+def test_orthogonalize_few_directions_steps(w2v, m, n, steps):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(steps)
+    x = torch.stack([low_rank(g, m, n, rank) for rank in (1, 8)]).bfloat16()
+    out = w2v.orthogonalize(x, steps=steps)
+    for a, b in zip(x, out):
+        want = steps64(a, steps=steps)
+        near(b, want, steady_bound(want, torch.bfloat16, steps))
+
+
+@pytest.mark.parametrize("gkind", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_muon_gradients_of_few_directions(w2v, gkind):
+    """bf16 parameters: the update of a zero matrix is the orthogonalised momentum itself."""
+    rng = torch.Generator(device="cuda")
+    rng.manual_seed(12)
+    shapes = [(512, 1024), (1024, 512), (512, 1024), (300, 100)]
+    grads = [(low_rank(rng, *s, r) * 1e-2).to(gkind) for s, r in zip(shapes, (1, 8, 64, 3))]
+    params = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in shapes]
+    w2v.Muon(params, grads, momentum=0.9, scale=1.0).step(1.0)
+    for p, g in zip(params, grads):
+        want = -steps64(g.double() + 0.9 * g.double())
+        near(p, want, steady_bound(want, torch.bfloat16))
+
+
 def test_orthogonalize_nothing(w2v):
     for shape in ((0, 5), (5, 0), (0, 3, 4), (2, 0, 4)):
         x = torch.empty(shape, device="cuda")
