@@ -314,6 +314,37 @@ def test_activation_at_its_ends(w2v, act):
     assert torch.isfinite(dx).all()
 
 
+def gelu_share_off(g):
+    """The relative error of Phi(g) for g < 0, and of the density beside it, in fp32: one U for the polynomial; 1 + c |g| and
+    its reciprocal 4 U, a polynomial whose terms cancel to no less than a third of their sum 9, three products and the
+    hardware's power 5; the exponent g^2 log2(e) / 2 three roundings, 1.5 g^2 U of the power. For g > 0, one less it: U more."""
+    return (20 + 2 * g * g) * U
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+def test_gelu_of_negative_arguments(w2v, kind):
+    """Phi(g) to its last digits down to where a fp32 product of it is no longer normal: g Phi(g) forward, by few rows and by
+    tiles; value and slope in the backward pass."""
+    g = torch.linspace(-12.5, 4.0, 331, device="cuda").to(kind)
+    n = g.numel()
+    a, s = act64("gelu", g.double())
+    share = gelu_share_off(g.double())
+    off = (share + 2 * U) * a.abs() + rounded(a, kind)
+    one = torch.eye(2, dtype=kind, device="cuda")
+    x = torch.stack([g, torch.ones_like(g)], 1)
+    for rows in (slice(0, n), slice(10, 50), slice(30, 31), slice(150, 151)):
+        # rounded twice: h, and the product with one
+        y = w2v.gated_ffn(x[rows], one[:1], one[1:], one[:, :1], "gelu")[0]
+        within(y[:, 0], a[rows], 1.01 * (off + rounded(a, kind))[rows], "y")
+    eye = torch.eye(n, dtype=kind, device="cuda")
+    dx, _, _, dwd = w2v.gated_ffn_backward(eye, eye, eye, torch.zeros_like(eye), eye, eye * g, torch.ones_like(eye), "gelu")
+    within(torch.diag(dwd), a, 1.01 * (off + rounded(a, kind)), "dw_down")
+    g = g.double()
+    phi, density = 0.5 * torch.special.erfc(-g / math.sqrt(2)), torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    off = (share + 4 * U) * (phi + g.abs() * density) + 2 * rounded(s, kind)
+    within(torch.diag(dx), s, 1.01 * off, "dx")
+
+
 def test_gradients_against_differences(w2v):
     """The gradients along random directions against differences of the 64-bit forward pass."""
     n, d, h, kind = 40, 24, 56, torch.float32
