@@ -515,17 +515,20 @@ int w2v_gated_ffn_backward(w2v_rows dy, w2v_rows x, w2v_rows w_gate, w2v_rows w_
 /* ------------------------------------------------------------------------
  * Nearly orthogonal matrices by Newton-Schulz products: X = g / (|g| + eps)
  * with the Frobenius norm, then `steps` (1..20) times X = (a I + b A + c A A) X
- * with A = X X' and a, b, c = 3.4445, -4.7750, 2.0315, which brings singular
- * values between 0.7 and 1.2 in five steps. g and out: batch (up to 2^31 - 1)
- * matrices of rows x cols elements of type (sides up to 2^20), a row `stride`
- * and a matrix `step` elements behind the one before; out may be g with the
- * same strides. The products keep 22 bits of each factor and sum in fp32; with
- * type bf16 what is added to X in a step keeps 11, and X itself 22: an error of
- * some 1e-3 of the result in norm whatever the singular values, 3.6e-3 where all
- * of its roundings have one sign (a unit matrix), beside the 1.7e-3 of bf16's
- * rounding. A matrix with an element that is not finite becomes NaN, the
- * others do not; one of zeros stays zero (NaN with eps 0). Errors: W2V_E_ARG,
- * W2V_E_WORKSPACE, W2V_E_RANGE. */
+ * with A = X X' and a, b, c = 3.4445, -4.7750, 2.0315. Five steps bring
+ * singular values of 0.002 of the norm or more between 0.68 and 1.21. A step
+ * multiplies smaller ones by up to 3.4445 (0.0001 becomes 0.05, 0 stays 0), and
+ * so what rounding leaves in directions that g lacks: 1e-4 of the result of a
+ * matrix of rank 1 in five steps, all of it in twenty. g and out: batch (up to
+ * 2^31 - 1) matrices of rows x cols elements of type (sides up to 2^20), a row
+ * `stride` and a matrix `step` elements behind the one before, out's a whole
+ * matrix or more; out may be g with the same strides. The products keep 22 bits
+ * of each factor and sum in fp32; with type bf16 what is added to X in a step
+ * keeps 11, and X itself 22: an error of some 1e-3 of the result in norm in
+ * five steps, 3.6e-3 where all of its roundings have one sign (a unit matrix),
+ * beside the 1.7e-3 of bf16's rounding. A matrix with an element that is not
+ * finite becomes NaN, the others do not; one of zeros stays zero (NaN with eps
+ * 0). Errors: W2V_E_ARG, W2V_E_WORKSPACE, W2V_E_RANGE. */
 size_t w2v_orthogonalize_workspace_bytes(int64_t batch, int32_t rows, int32_t cols, int32_t type);
 int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t batch, int32_t rows, int32_t cols,
                       int32_t type, int32_t steps, double eps, void *out, int64_t out_stride, int64_t out_step,
@@ -534,13 +537,13 @@ int w2v_orthogonalize(const void *g, int64_t g_stride, int64_t g_step, int64_t b
 /* Muon over many matrices: with G = grad grad_scale and a momentum M (fp32),
  *     M = momentum M + G;  U = G + momentum M if nesterov, else M
  *     param = param (1 - lr weight_decay) - lr scale orthogonalize(U)
- * where bf16 parameters take orthogonalize's products for bf16. The momenta lie in one
- * float array m, matrix i's (in row order, without gaps) from moment_offset
- * on, a multiple of 256; zeros before the first step. The plan, device memory
- * of w2v_muon_plan_bytes bytes that the caller keeps, is made once from a list
- * (synchronises the stream), and a step is given the same list again.
- * Matrices of the same sizes and types go through the products together. A
- * plan, and a workspace, belong to one step at a time. Errors: W2V_E_ARG for
+ * where bf16 parameters take orthogonalize's products for bf16. The momenta lie
+ * in one float array m, matrix i's (in row order, without gaps) from
+ * moment_offset on, a multiple of 256; zeros before the first step. The plan,
+ * device memory of w2v_muon_plan_bytes bytes that the caller keeps, is made
+ * once from a list (synchronises the stream), and a step is given the same list
+ * again. Matrices of the same sizes and types go through the products together.
+ * A plan, and a workspace, belong to one step at a time. Errors: W2V_E_ARG for
  * sizes, strides, types or NULL pointers out of range, momenta that overlap or
  * reach past n_moments (a matrix's last 256 count whole), or packed parameters
  * that overlap; W2V_E_WORKSPACE; W2V_E_RANGE. */

@@ -15,8 +15,8 @@
 //
 // What bounds it: the matrix cores for wide rows (16,384 rows of 4,096 bf16, hidden 10,240: 3.3 ms, 1,230 TFLOP/s; backward,
 // 8,192 rows: 3.5 ms, 1,180); memory and the matrix cores in turn for narrow ones, whose tiles end after 10 steps (65,536 rows
-// of 300, hidden 800: 0.70 ms forward, 1.67 backward); the weights' bytes for a single row (4,096 bf16, hidden 10,240: 48 us,
-// 5.2 TB/s); launches for small ones (257 rows of 100: 32 us backward, five launches).
+// of 300, hidden 800: 0.70 ms forward, 1.67 backward); the weights' bytes for a single row (4,096 bf16, hidden 10,240: 57 us,
+// 4.4 TB/s); launches for small ones (257 rows of 100: 32 us backward, five launches).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -316,17 +316,19 @@ int launch_parts(const Packing &p, hipStream_t s) {
 // Where there are few rows every weight is read for them, and the weights' bytes are the time. A workgroup takes 16 columns
 // of the result, its wavefronts take turns along k, 128 bytes of each of the 16 weight rows at a time straight from memory
 // into the matrix cores' registers (rows need no alignment but their elements'); the wavefronts' sums are joined in LDS in
-// their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts, or in fp32 in rows where one h is past
-// the type's range (its two parts would be opposite infinities): the sums are made again for these, and the others keep theirs.
+// their order. fp32 is multiplied in fp32. h stays fp32; 16-bit weights meet it as two parts, or in fp32 in rows where one h is
+// past the type's range (its two parts would be opposite infinities): the sums are made again for these, and the others keep
+// theirs.
 constexpr int kFewWaves = 8;   // wavefronts a workgroup
 
 // The least number that a 16-bit type rounds to an infinity.
 template <class T>
 constexpr float kPast = std::is_same<T, __bf16>::value ? 0x1.ffp127f : 65520.0f;
 
-// fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles, whose parts are 1.5 times as many bytes, 0.46),
-// 16-bit ones where the products are small (1 row, 4,096 x 10,240: 48 us, in tiles 50; 16 rows: 63 and 50; 16 rows, 1,024 x
-// 2,816: 15 and 19) or tiles would need copies of the weights. What they read of x again and again grows with the rows.
+// fp32 rows go this way up to 64 (64 rows, 4,096 x 10,240: 0.28 ms, in tiles, whose parts are 1.5 times as many bytes, 0.43),
+// 16-bit ones where the products are small (weights from memory: 1 row, 4,096 x 10,240: 57 us, in tiles 61; 16 rows, 1,024 x
+// 2,816: 16 and 20; weights in cache: 48 and 51; 15 and 19; 16 rows, 4,096 x 10,240: 63 and 50) or tiles would need copies of the
+// weights. What they read of x again and again grows with the rows.
 template <class T>
 bool few_rows(const FfnArgs &a, bool copies) {
     return a.rows <= 64 && (sizeof(T) == 4 || a.rows == 1 || (copies && a.rows <= 16) ||

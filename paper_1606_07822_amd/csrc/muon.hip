@@ -451,8 +451,8 @@ int run_batch(const Batch &b, const Arrays &w, double eps, int32_t steps, hipStr
     W2V_LAUNCH_CHECK("k_muon_momentum");
     // some four chunks of eight a thread, and no more than 4,096 workgroups a matrix
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(b.rows * (w.x_stride / 8), 1024), 4096));
-    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], steps > 1 ? w.second : nullptr, w.x_stride,
-                                                                                blocks);
+    E *second = steps > 1 ? w.second : nullptr;
+    k_muon_start<G, P><<<static_cast<unsigned>(b.count * blocks), 256, 0, s>>>(b, w.part, eps, w.x[0], second, w.x_stride, blocks);
     W2V_LAUNCH_CHECK("k_muon_start");
     return b.rows <= b.cols ? run_steps<T, P, true>(b, w, steps, s) : run_steps<T, P, false>(b, w, steps, s);
 }
